@@ -5,7 +5,8 @@ asi_compress, asi_core_project, asi_weight_grad_conv2d, asi_weight_grad_linear a
 *_batch forms, which serve several layers with every kernel launch; asi_compress_cold for the first
 iteration; AsiConv2d / AsiLinear wire the calls into autograd (the layers keep (S, U), not the activation);
 rank_selection holds the front end of Sec. 3.3 (mode spectra, explained-variance ranks, perplexity rows, the
-budgeted choice).
+budgeted choice).  lm holds what a language model's fine-tuning step needs beside the compressed layers: token log
+probabilities and their gradient, embedding, norms of queries and keys with the position rotation, AdamW.
 """
 from .autograd import AsiConv2d, AsiLinear, AsiState  # noqa: F401
 from .binding import (  # noqa: F401
@@ -44,4 +45,14 @@ from .binding import (  # noqa: F401
     make_conv,
     make_desc,
 )
-from . import rank_selection  # noqa: F401,E402
+from . import lm, rank_selection  # noqa: F401,E402
+from .lm import (  # noqa: F401,E402
+    AdamW,
+    embedding,
+    embedding_grad,
+    qk_norm_rotate,
+    qk_norm_rotate_grad,
+    rotary_table,
+    token_logprobs,
+    token_logprobs_grad,
+)

@@ -26,7 +26,10 @@ EXPORTS = ["asi_workspace_bytes", "asi_compress", "asi_compress_cold", "asi_cold
            "asi_weight_grad_linear", "asi_compress_batch", "asi_core_project_batch",
            "asi_weight_grad_conv2d_batch", "asi_weight_grad_linear_batch", "asi_status_string", "asi_version",
            "asi_profile_enable", "asi_profile_report", "asi_activation_memory", "asi_mode_spectrum_workspace_bytes",
-           "asi_mode_spectrum", "asi_mode_spectra_workspace_bytes", "asi_mode_spectra", "asi_explained_variance_ranks", "asi_frobenius_diff", "asi_rank_select"]
+           "asi_mode_spectrum", "asi_mode_spectra_workspace_bytes", "asi_mode_spectra", "asi_explained_variance_ranks", "asi_frobenius_diff", "asi_rank_select",
+           "asi_token_logprobs_workspace_bytes", "asi_token_logprobs", "asi_token_logprobs_grad", "asi_embedding",
+           "asi_embedding_grad_workspace_bytes", "asi_embedding_grad", "asi_qk_norm_rotate",
+           "asi_qk_norm_rotate_grad_workspace_bytes", "asi_qk_norm_rotate_grad", "asi_adamw"]
 FROBENIUS_WS_BYTES = 8192            # ASI_FROBENIUS_WS_BYTES of include/asi.h
 MAX_BATCH = 8
 
@@ -39,6 +42,37 @@ class Conv2dDesc(C.Structure):
     _fields_ = [("cout", C.c_int64), ("kh", C.c_int32), ("kw", C.c_int32),
                 ("stride_h", C.c_int32), ("stride_w", C.c_int32), ("pad_h", C.c_int32), ("pad_w", C.c_int32),
                 ("dil_h", C.c_int32), ("dil_w", C.c_int32), ("groups", C.c_int32)]
+
+
+class LogprobDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("vocab", C.c_int64), ("row_stride", C.c_int64), ("grad_stride", C.c_int64),
+                ("ignore_index", C.c_int64), ("dtype", C.c_int32), ("top", C.c_int32), ("scale", C.c_float),
+                ("reserved", C.c_int32)]
+
+
+class EmbeddingDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("vocab", C.c_int64), ("dim", C.c_int64), ("table_stride", C.c_int64),
+                ("out_stride", C.c_int64), ("padding_index", C.c_int64), ("table_dtype", C.c_int32),
+                ("out_dtype", C.c_int32), ("scale", C.c_float), ("reserved", C.c_int32)]
+
+
+class QkDesc(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("tokens", C.c_int64), ("max_position", C.c_int64), ("position_stride", C.c_int64),
+                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("q_out_stride", C.c_int64 * 3),
+                ("k_out_stride", C.c_int64 * 3), ("dq_stride", C.c_int64 * 3), ("dk_stride", C.c_int64 * 3), ("q_heads", C.c_int32), ("k_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("dtype", C.c_int32), ("gain_dtype", C.c_int32),
+                ("eps", C.c_float)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("master", C.c_void_p), ("exp_avg", C.c_void_p),
+                ("exp_avg_sq", C.c_void_p), ("exp_avg_scale", C.c_void_p), ("exp_avg_sq_scale", C.c_void_p),
+                ("count", C.c_int64), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("lr", C.c_double),
+                ("weight_decay", C.c_double)]
+
+
+LOGPROB_MAX_TOP = 64                 # ASI_LOGPROB_MAX_TOP, ASI_ADAMW_BLOCK of include/asi_lm.h
+ADAMW_BLOCK = 256
 
 
 class AsiError(RuntimeError):
@@ -117,6 +151,21 @@ def lib() -> C.CDLL:
         L.asi_rank_select.restype = C.c_int
         L.asi_rank_select.argtypes = [C.c_int32, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_int64), C.c_int64,
                                       C.POINTER(C.c_int32), C.POINTER(C.c_double)]
+        size, i64 = C.c_size_t, C.c_int64
+        ld, ed, qd = C.POINTER(LogprobDesc), C.POINTER(EmbeddingDesc), C.POINTER(QkDesc)
+        for name, result, args in (
+                ("asi_token_logprobs_workspace_bytes", size, [ld]),
+                ("asi_token_logprobs", C.c_int, [ld, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]),
+                ("asi_token_logprobs_grad", C.c_int, [ld, vp, vp, vp, vp, vp, vp, vp, vp]),
+                ("asi_embedding", C.c_int, [ed, vp, vp, vp, vp]),
+                ("asi_embedding_grad_workspace_bytes", size, [ed]),
+                ("asi_embedding_grad", C.c_int, [ed, vp, vp, vp, C.c_int, vp, size, vp]),
+                ("asi_qk_norm_rotate", C.c_int, [qd] + [vp] * 10),
+                ("asi_qk_norm_rotate_grad_workspace_bytes", size, [qd]),
+                ("asi_qk_norm_rotate_grad", C.c_int, [qd] + [vp] * 14 + [size, vp]),
+                ("asi_adamw", C.c_int, [C.c_int32, vp, C.c_int32, C.c_double, C.c_double, C.c_double, i64, vp, vp, vp])):
+            f = getattr(L, name)
+            f.restype, f.argtypes = result, args
         _lib = L
     return _lib
 

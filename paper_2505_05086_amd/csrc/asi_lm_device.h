@@ -1,0 +1,112 @@
+// Device helpers of the language-model operators (include/asi_lm.h): typed vectors of 16 bytes, rounding to
+// bf16, reductions over a wave.  Host helpers for their argument checks.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/asi_lm.h"
+#include "asi_device.h"
+
+namespace asi {
+
+constexpr int kWave = 64;
+
+// bf16 rounding is to nearest, ties to even, NaN stays NaN (the conversion instruction of gfx950)
+__device__ __forceinline__ bf16_t to_bf16(float x) {
+    union { __bf16 b; uint16_t u; } c;
+    c.b = (__bf16)x;
+    return bf16_t{c.u};
+}
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float x) { return to_bf16(x); }
+
+// 16 bytes of a row: 4 fp32 or 8 bf16 values, kept as loaded so that many can be in flight at little cost in registers
+template <typename T> struct Vec16 {
+    static constexpr int N = 16 / sizeof(T);
+    uint4 raw;
+    __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = raw; }
+    __device__ __forceinline__ float get(int i) const;
+    __device__ __forceinline__ void set(const float* f);
+};
+template <> __device__ __forceinline__ float Vec16<float>::get(int i) const {
+    return __uint_as_float(i == 0 ? raw.x : i == 1 ? raw.y : i == 2 ? raw.z : raw.w);
+}
+template <> __device__ __forceinline__ float Vec16<bf16_t>::get(int i) const {
+    const uint32_t w = (i >> 1) == 0 ? raw.x : (i >> 1) == 1 ? raw.y : (i >> 1) == 2 ? raw.z : raw.w;
+    return __uint_as_float((i & 1) ? (w & 0xffff0000u) : (w << 16));
+}
+template <> __device__ __forceinline__ void Vec16<float>::set(const float* f) {
+    raw = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) { return (uint32_t)to_bf16(lo).bits | ((uint32_t)to_bf16(hi).bits << 16); }
+template <> __device__ __forceinline__ void Vec16<bf16_t>::set(const float* f) {
+    raw = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+
+// N values (a multiple of 4) to and from fp32, in accesses of up to 16 bytes; the address has to be a multiple of min(16, N * size)
+template <int N> __device__ __forceinline__ void load_values(const float* p, float* f) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p + i);
+        f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+    }
+}
+template <int N> __device__ __forceinline__ void load_values(const bf16_t* p, float* f) {
+    if constexpr (N % 8 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 8) {
+            Vec16<bf16_t> v;
+            v.load(p + i);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[i + k] = v.get(k);
+        }
+    } else {
+        static_assert(N == 4, "4 or a multiple of 8");
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
+        f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+    }
+}
+template <int N> __device__ __forceinline__ void store_values(float* p, const float* f) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+}
+template <int N> __device__ __forceinline__ void store_values(bf16_t* p, const float* f) {
+    if constexpr (N % 8 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 8) {
+            Vec16<bf16_t> v;
+            v.set(f + i);
+            v.store(p + i);
+        }
+    } else {
+        static_assert(N == 4, "4 or a multiple of 8");
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+    }
+}
+
+// Reductions over `width` neighbouring lanes (a power of two); every lane gets the result, always in the same order.
+template <int WIDTH = kWave> __device__ __forceinline__ float lanes_sum(float x) {
+#pragma unroll
+    for (int o = WIDTH / 2; o; o >>= 1) x += __shfl_xor(x, o);
+    return x;
+}
+template <int WIDTH = kWave> __device__ __forceinline__ float lanes_max(float x) {
+#pragma unroll
+    for (int o = WIDTH / 2; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+    return x;
+}
+
+// the larger of two, NaN if either is
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// ---- host ----
+inline bool dtype_ok(int32_t d) { return d == ASI_F32 || d == ASI_BF16; }
+inline size_t dtype_size(int32_t d) { return d == ASI_F32 ? 4 : 2; }
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
+inline asi_status launched() { return hipGetLastError() == hipSuccess ? ASI_OK : ASI_ERR_HIP; }
+
+}  // namespace asi

@@ -1,0 +1,463 @@
+// Log probabilities of given tokens with entropy and the top alternatives, and their gradient (include/asi_lm.h).
+//
+// With m the largest logit of a row, d_i = x_i - m and e_i = exp(scale d_i):
+//     s = sum e_i,  w = sum d_i e_i;   logprob = scale d_target - log s;   entropy = log s - scale w / s
+// Differences from the row's largest logit keep the digits that z - lse would lose where logits are large.
+//
+// Forward: a workgroup takes a row in one pass; every thread keeps a running largest logit and the sums relative to it.
+// Top alternatives: of the threads' largest logits each wave takes its c-th, c = ceil(top / waves); the least of those is a bound
+// that at least `top` logits reach.  Only threads whose largest reaches it look at their logits again and hand over those that
+// do, a few more than wanted; of these each finds its place by counting the ones before it.  Rows where too many reach the
+// bound (many equal logits) are searched `top` times instead.
+//
+// Gradient: a row is kept in registers between the pass that sums and the one that writes, so that it is read once and written once;
+// rows too long for that are read again.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "asi_lm_device.h"
+
+namespace asi {
+namespace {
+
+constexpr float kLowest = -3.402823466e+38f;     // stands for a thread that has seen no logit above -infinity
+// Differences are not let below this: exp(scale d) is 0 there for every scale that is taken, and its product with d is 0, not NaN.
+constexpr float kFar = -1e24f;
+constexpr float kLeastScale = 1e-20f, kMostScale = 1e20f;
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A row as 16-byte vectors from its first aligned address on, with up to N - 1 elements before them and behind.
+template <typename T> struct RowView {
+    const T* x;
+    int head, nvec, tail_at, n;
+    __device__ __forceinline__ RowView(const T* row, int vocab) {
+        constexpr int N = Vec16<T>::N;
+        x = row;
+        n = vocab;
+        head = min((int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(T), vocab);
+        nvec = (vocab - head) / N;
+        tail_at = head + nvec * N;
+    }
+    // the element of this thread that no vector holds: index, or -1
+    __device__ __forceinline__ int loose(int tid) const {
+        if (tid < head) return tid;
+        const int i = tail_at + tid - head;
+        return tid >= head && i < n ? i : -1;
+    }
+    __device__ __forceinline__ const T* vec(int v) const { return x + head + v * Vec16<T>::N; }
+    __device__ __forceinline__ int index(int v) const { return head + v * Vec16<T>::N; }
+};
+
+struct Sums {
+    float m, s, w;
+};
+// Sums of another part joined to these: both relative to the larger of the two largest logits.
+__device__ __forceinline__ Sums joined(const Sums& a, const Sums& b, float c) {
+    Sums r;
+    r.m = fmaxf(a.m, b.m);
+    const float da = max_nan(a.m - r.m, kFar), db = max_nan(b.m - r.m, kFar);
+    const float fa = exp2_fast(da * c), fb = exp2_fast(db * c);
+    r.s = a.s * fa + b.s * fb;
+    r.w = fa * (a.w + da * a.s) + fb * (b.w + db * b.s);
+    return r;
+}
+// Over the workgroup; every thread gets the result.
+template <int THREADS> __device__ __forceinline__ Sums over_workgroup(Sums a, float c, Sums* scratch) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        Sums b;
+        b.m = __shfl_xor(a.m, o); b.s = __shfl_xor(a.s, o); b.w = __shfl_xor(a.w, o);
+        a = joined(a, b, c);
+    }
+    constexpr int W = THREADS / 64;
+    if (W > 1) {
+        if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = a;
+        __syncthreads();
+        a = scratch[0];
+        for (int k = 1; k < W; ++k) a = joined(a, scratch[k], c);
+    }
+    return a;
+}
+// `cnt` more logits of a thread
+template <int CNT> __device__ __forceinline__ void take(Sums* a, const float* x, float c) {
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < CNT; ++i) top = fmaxf(top, x[i]);
+    if (top > a->m) {
+        const float d = max_nan(a->m - top, kFar), f = exp2_fast(d * c);
+        a->w = f * (a->w + d * a->s);
+        a->s *= f;
+        a->m = top;
+    }
+#pragma unroll
+    for (int i = 0; i < CNT; ++i) {
+        const float d = max_nan(x[i] - a->m, kFar), e = exp2_fast(d * c);
+        a->s += e;
+        a->w += d * e;
+    }
+}
+
+struct Values {
+    float lse, logprob, entropy;
+};
+// target < 0: none
+template <typename T> __device__ __forceinline__ Values values_of(const Sums& a, const T* row, long long target, int vocab, long long ignore, float scale) {
+    Values v;
+    const float inf = __builtin_inff(), nan = __builtin_nanf("");
+    const bool empty = a.s == 0.f;                // no logit above -infinity
+    const float ls = logf(a.s);
+    v.lse = empty ? -inf : a.m * scale + ls;
+    v.entropy = empty ? 0.f : ls - scale * (a.w / a.s);
+    if (target == ignore) v.logprob = 0.f;
+    else if (target < 0 || target >= vocab) v.logprob = nan;
+    else v.logprob = empty ? -inf : (to_f32(row[target]) - a.m) * scale - ls;
+    return v;
+}
+
+struct Args {
+    const void* x;
+    const int64_t* targets;
+    float* logprob;
+    float* entropy;
+    float* lse;
+    float* top_logprob;
+    int64_t* top_index;
+    long long stride, ignore;
+    int vocab, top;
+    float scale;
+};
+
+// ---- top alternatives -----------------------------------------------------------------------------------------
+// Logits as whole numbers in their order: NaN above everything, -0 equal to 0.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    if (x != x) return 0xffffffffu;
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+// An alternative: larger is earlier.  Equal logits: the lower index is.
+__device__ __forceinline__ unsigned long long rank_key(float x, int index) { return (unsigned long long)order_of(x) << 32 | (uint32_t)~index; }
+__device__ __forceinline__ unsigned long long lanes_max64(unsigned long long k) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        const unsigned long long other = __shfl_xor(k, o);
+        k = other > k ? other : k;
+    }
+    return k;
+}
+constexpr int kCandidates = 1024;
+template <int THREADS> struct TopScratch {
+    unsigned long long key[kCandidates];
+    unsigned long long wave[THREADS / 64];
+    uint32_t bound[THREADS / 64];
+    int count;
+};
+template <typename T, typename F> __device__ __forceinline__ void each_of_thread(const RowView<T>& r, int threads, F f) {
+    constexpr int N = Vec16<T>::N;
+    const int l = r.loose(threadIdx.x);
+    if (l >= 0) f(to_f32(r.x[l]), l);
+    for (int v = threadIdx.x; v < r.nvec; v += threads) {
+        Vec16<T> raw;
+        raw.load(r.vec(v));
+#pragma unroll
+        for (int i = 0; i < N; ++i) f(raw.get(i), r.index(v) + i);
+    }
+}
+template <typename T, int THREADS>
+__device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, const Args& a, float lse, long long row, TopScratch<THREADS>* sc) {
+    constexpr int W = THREADS / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float* out = a.top_logprob + row * a.top;
+    int64_t* out_i = a.top_index + row * a.top;
+    auto write = [&](int place, unsigned long long key) {
+        const int index = (int)~(uint32_t)key;
+        const float x = to_f32(r.x[index]);
+        out[place] = x == -__builtin_inff() && lse == lse ? x : x * a.scale - lse;     // also where lse is -infinity
+        out_i[place] = index;
+    };
+    // This wave's c-th largest of its threads' largest, equal ones counted each.  Waves whose threads do not all have a vector
+    // bound nothing; where there is no other, everything is handed over (less than kCandidates then).
+    const int full = min(W, r.nvec / 64);
+    uint32_t bound = full ? 0xffffffffu : 0u;
+    if (wave < full) {
+        uint32_t left = most;
+        const int c = (a.top + full - 1) / full;
+        for (int got = 0; got < c;) {
+            uint32_t m = left;
+#pragma unroll
+            for (int o = 32; o; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
+            bound = m;
+            got += __popcll(__ballot(left == m));
+            if (left == m) left = 0;
+        }
+    }
+    if (threadIdx.x == 0) sc->count = 0;
+    if (lane == 0) sc->bound[wave] = bound;
+    __syncthreads();
+    bound = sc->bound[0];
+    for (int k = 1; k < W; ++k) bound = min(bound, sc->bound[k]);
+    if (most >= bound) {
+        each_of_thread(r, THREADS, [&](float x, int i) {
+            if (order_of(x) >= bound) {
+                const int at = atomicAdd(&sc->count, 1);
+                if (at < kCandidates) sc->key[at] = rank_key(x, i);
+            }
+        });
+    }
+    __syncthreads();
+    const int n = sc->count;
+    if (n <= kCandidates) {
+        for (int i = threadIdx.x; i < n; i += THREADS) {
+            const unsigned long long key = sc->key[i];
+            int before = 0;
+            for (int k = 0; k < n; ++k) before += sc->key[k] > key;
+            if (before < a.top) write(before, key);
+        }
+        return;
+    }
+    unsigned long long last = ~0ull;              // no key is that: an index is not negative
+    for (int place = 0; place < a.top; ++place) {
+        unsigned long long best = 0;
+        each_of_thread(r, THREADS, [&](float x, int i) {
+            const unsigned long long key = rank_key(x, i);
+            if (key < last && key > best) best = key;
+        });
+        best = lanes_max64(best);
+        __syncthreads();
+        if (lane == 0) sc->wave[wave] = best;
+        __syncthreads();
+        best = sc->wave[0];
+        for (int k = 1; k < W; ++k) best = sc->wave[k] > best ? sc->wave[k] : best;
+        last = best;
+        if (threadIdx.x == 0) write(place, best);
+    }
+}
+
+// ---- forward ----------------------------------------------------------------------------------------------------
+template <typename T, int THREADS, bool TOP> __global__ __launch_bounds__(THREADS) void k_logprobs(const Args a) {
+    constexpr int N = Vec16<T>::N;
+    __shared__ Sums scratch[THREADS / 64];
+    const long long row = blockIdx.x;
+    const T* x = static_cast<const T*>(a.x) + row * a.stride;
+    const RowView<T> r(x, a.vocab);
+    const float c = a.scale * kLog2e;
+    Sums acc{kLowest, 0.f, 0.f};
+    uint32_t most = 0;
+    const int l = r.loose(threadIdx.x);
+    if (l >= 0) {
+        const float v = to_f32(x[l]);
+        take<1>(&acc, &v, c);
+        if (TOP) most = order_of(v);
+    }
+    for (int v = threadIdx.x; v < r.nvec; v += THREADS) {
+        Vec16<T> raw;
+        raw.load(r.vec(v));
+        float f[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = raw.get(i);
+        take<N>(&acc, f, c);
+        if (TOP) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) most = max(most, order_of(f[i]));
+        }
+    }
+    const Sums all = over_workgroup<THREADS>(acc, c, scratch);
+    const long long target = a.targets ? a.targets[row] : a.ignore;
+    const Values val = values_of(all, x, target, a.vocab, a.ignore, a.scale);
+    if (threadIdx.x == 0) {
+        if (a.logprob) a.logprob[row] = val.logprob;
+        if (a.entropy) a.entropy[row] = val.entropy;
+        if (a.lse) a.lse[row] = val.lse;
+    }
+    if constexpr (TOP) {
+        __shared__ TopScratch<THREADS> top;
+        write_top<T, THREADS>(r, most, a, val.lse, row, &top);
+    }
+}
+
+// ---- gradient ---------------------------------------------------------------------------------------------------
+struct GradArgs {
+    const void* x;
+    void* dx;
+    const int64_t* targets;
+    const float* a;
+    const float* b;
+    float* logprob;
+    float* entropy;
+    long long stride, grad_stride, ignore;
+    int vocab;
+    float scale;
+};
+// KEEP: vectors that a thread keeps in registers, 0: the row is read again
+template <typename T, int THREADS, int KEEP> __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const GradArgs g) {
+    constexpr int N = Vec16<T>::N;
+    __shared__ Sums scratch[THREADS / 64];
+    const long long row = blockIdx.x;
+    const T* x = static_cast<const T*>(g.x) + row * g.stride;
+    T* dx = static_cast<T*>(g.dx) + row * g.grad_stride;
+    const RowView<T> r(x, g.vocab);
+    const float c = g.scale * kLog2e;
+    const int l = r.loose(threadIdx.x);
+    const float loose = l >= 0 ? to_f32(x[l]) : 0.f;
+    const long long target = g.targets ? g.targets[row] : g.ignore;
+    Sums acc{kLowest, 0.f, 0.f};
+    Vec16<T> kept[KEEP ? KEEP : 1];
+    if constexpr (KEEP > 0) {
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k) {
+            const int v = threadIdx.x + k * THREADS;
+            if (v < r.nvec) kept[k].load(r.vec(v));
+        }
+    }
+    if (l >= 0) take<1>(&acc, &loose, c);
+    if constexpr (KEEP > 0) {
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k) {
+            if (threadIdx.x + k * THREADS < r.nvec) {
+                float f[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) f[i] = kept[k].get(i);
+                take<N>(&acc, f, c);
+            }
+        }
+    } else {
+        for (int v = threadIdx.x; v < r.nvec; v += THREADS) {
+            kept[0].load(r.vec(v));
+            float f[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[i] = kept[0].get(i);
+            take<N>(&acc, f, c);
+        }
+    }
+    const Sums all = over_workgroup<THREADS>(acc, c, scratch);
+    const Values val = values_of(all, x, target, g.vocab, g.ignore, g.scale);
+    __syncthreads();                              // before dx, which may be x, is written every thread has read its target
+    if (threadIdx.x == 0) {
+        if (g.logprob) g.logprob[row] = val.logprob;
+        if (g.entropy) g.entropy[row] = val.entropy;
+    }
+    const bool given = target != g.ignore, in_range = target >= 0 && target < g.vocab;
+    const float wa = given && g.a ? g.a[row] : 0.f, wb = g.b ? g.b[row] : 0.f;
+    const bool empty = all.s == 0.f;
+    // dx_i = scale (a delta_i - p_i (a + b (log p_i + entropy))),  log p_i = scale d_i - log s:  p_i (k0 + k1 d_i) with these
+    const float inv = empty ? 0.f : 1.f / all.s, ls = empty ? 0.f : logf(all.s);
+    const float bad = given && !in_range ? __builtin_nanf("") : 0.f;
+    const float k0 = -g.scale * inv * (wa + wb * (val.entropy - ls)) + bad, k1 = -g.scale * inv * wb * g.scale;
+    const float hot = empty ? 0.f : g.scale * wa;
+    const int at = given && in_range ? (int)target : -1;
+    auto grad = [&](float v, int i) {
+        const float d = max_nan(v - all.m, kFar), e = exp2_fast(d * c);
+        const float p = e * (k0 + k1 * d);
+        return i == at ? p + hot : p;
+    };
+    if (l >= 0) dx[l] = from_f32<T>(grad(loose, l));
+    // dx's rows need not lie as x's do
+    const bool vec = ((reinterpret_cast<uintptr_t>(dx + r.head)) & 15) == 0;
+    auto write = [&](const Vec16<T>& raw, int v) {
+        float f[N];
+        const int i0 = r.index(v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = grad(raw.get(i), i0 + i);
+        if (vec) {
+            store_values<N>(dx + i0, f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) dx[i0 + i] = from_f32<T>(f[i]);
+        }
+    };
+    if constexpr (KEEP > 0) {
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k) {
+            const int v = threadIdx.x + k * THREADS;
+            if (v < r.nvec) write(kept[k], v);
+        }
+    } else {
+        for (int v = threadIdx.x; v < r.nvec; v += THREADS) {
+            kept[0].load(r.vec(v));
+            write(kept[0], v);
+        }
+    }
+}
+
+// ---- host ----
+asi_status check(const asi_logprob_desc* d) {
+    if (!d) return ASI_ERR_INVALID_ARG;
+    if (!dtype_ok(d->dtype)) return ASI_ERR_UNSUPPORTED;
+    if (d->rows < 0 || d->vocab < 1 || d->row_stride < d->vocab || d->reserved) return ASI_ERR_INVALID_ARG;
+    if (!(d->scale > 0.f) || !std::isfinite(d->scale)) return ASI_ERR_INVALID_ARG;
+    if (d->scale < kLeastScale || d->scale > kMostScale) return ASI_ERR_UNSUPPORTED;
+    if (d->rows > 0x7fffffffLL || d->vocab > (1LL << 28)) return ASI_ERR_UNSUPPORTED;
+    return ASI_OK;
+}
+template <typename T, int THREADS> void forward(const Args& a, unsigned rows, hipStream_t st) {
+    if (a.top) hipLaunchKernelGGL((k_logprobs<T, THREADS, true>), dim3(rows), THREADS, 0, st, a);
+    else hipLaunchKernelGGL((k_logprobs<T, THREADS, false>), dim3(rows), THREADS, 0, st, a);
+}
+template <typename T> void forward(const Args& a, unsigned rows, hipStream_t st) {
+    const int nvec = a.vocab / Vec16<T>::N;
+    if (nvec <= 512) forward<T, 256>(a, rows, st);
+    else forward<T, 1024>(a, rows, st);
+}
+template <typename T> void backward(const GradArgs& g, unsigned rows, hipStream_t st) {
+    const int nvec = g.vocab / Vec16<T>::N;
+#define ASI_GRAD(THREADS, KEEP) hipLaunchKernelGGL((k_logprobs_grad<T, THREADS, KEEP>), dim3(rows), THREADS, 0, st, g)
+    if (nvec <= 256) ASI_GRAD(256, 1);
+    else if (nvec <= 1024) ASI_GRAD(256, 4);
+    else if (nvec <= 4096) ASI_GRAD(512, 8);
+    else if (nvec <= 8192) ASI_GRAD(1024, 8);
+    else if (nvec <= 16384) ASI_GRAD(1024, 16);
+    else ASI_GRAD(1024, 0);
+#undef ASI_GRAD
+}
+
+}  // namespace
+}  // namespace asi
+
+using namespace asi;
+
+extern "C" {
+
+size_t asi_token_logprobs_workspace_bytes(const asi_logprob_desc*) { return 0; }
+
+asi_status asi_token_logprobs(const asi_logprob_desc* desc, const void* logits, const int64_t* targets, float* logprob,
+                              float* entropy, float* lse, float* top_logprob, int64_t* top_index, void* ws,
+                              size_t ws_bytes, asi_stream_t stream) {
+    (void)ws;
+    (void)ws_bytes;
+    if (asi_status why = check(desc); why != ASI_OK) return why;
+    if (desc->top < 0 || desc->top > desc->vocab || desc->top > ASI_LOGPROB_MAX_TOP) return ASI_ERR_INVALID_ARG;
+    if (desc->rows == 0) return ASI_OK;
+    const size_t es = dtype_size(desc->dtype);
+    if (!logits || !aligned(logits, es) || (logprob && !targets) || !aligned(targets, 8) || !aligned(logprob, 4) || !aligned(entropy, 4) ||
+        !aligned(lse, 4) || (desc->top && (!top_logprob || !top_index || !aligned(top_logprob, 4) || !aligned(top_index, 8))))
+        return ASI_ERR_INVALID_ARG;
+    const Args a{logits, targets, logprob, entropy, lse, top_logprob, top_index, desc->row_stride, desc->ignore_index, (int)desc->vocab,
+                 desc->top, desc->scale};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (desc->dtype == ASI_F32) forward<float>(a, (unsigned)desc->rows, st);
+    else forward<bf16_t>(a, (unsigned)desc->rows, st);
+    return launched();
+}
+
+asi_status asi_token_logprobs_grad(const asi_logprob_desc* desc, const void* logits, const int64_t* targets,
+                                   const float* grad_logprob, const float* grad_entropy, void* dlogits, float* logprob,
+                                   float* entropy, asi_stream_t stream) {
+    if (asi_status why = check(desc); why != ASI_OK) return why;
+    if (desc->grad_stride < desc->vocab || (dlogits == logits && desc->grad_stride != desc->row_stride)) return ASI_ERR_INVALID_ARG;
+    if (desc->rows == 0) return ASI_OK;
+    const size_t es = dtype_size(desc->dtype);
+    if (!logits || !dlogits || !aligned(logits, es) || !aligned(dlogits, es) || ((logprob || grad_logprob) && !targets) || !aligned(targets, 8) ||
+        !aligned(grad_logprob, 4) || !aligned(grad_entropy, 4) || !aligned(logprob, 4) || !aligned(entropy, 4))
+        return ASI_ERR_INVALID_ARG;
+    const GradArgs g{logits, dlogits, targets, grad_logprob, grad_entropy, logprob, entropy, desc->row_stride, desc->grad_stride,
+                     desc->ignore_index, (int)desc->vocab, desc->scale};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (desc->dtype == ASI_F32) backward<float>(g, (unsigned)desc->rows, st);
+    else backward<bf16_t>(g, (unsigned)desc->rows, st);
+    return launched();
+}
+
+}  // extern "C"
