@@ -67,7 +67,7 @@ asi_status asi_token_logprobs_grad(const asi_logprob_desc* desc, const void* log
  * out[t] = scale * table[token_t];     dtable[v] = scale * sum over t with token_t = v of grad_out[t],
  * the sum taken in an order that depends on the tokens alone, so that equal calls give equal bits. */
 typedef struct {
-    int64_t tokens, vocab, dim;    /* tokens < 2^30, vocab < 2^30 */
+    int64_t tokens, vocab, dim;    /* tokens < 2^30, vocab <= 2^24 */
     int64_t table_stride;      /* of table / dtable, >= dim */
     int64_t out_stride;        /* of out / grad_out, >= dim */
     int64_t padding_index;     /* a token whose row gets no gradient; -1: none */

@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "asi_lds.h"
 #include "asi_lm_device.h"
 
 namespace asi {
@@ -72,46 +73,127 @@ template <typename T, typename O> __global__ __launch_bounds__(kThreads) void k_
 }
 
 // ---- gradient: sorting ----------------------------------------------------------------------------------------
-// A token that counts for nothing sorts behind all others, as `vocab`.
+// One launch: workgroup w looks at every token and keeps those in its `span` ids, so that the number of smaller ones, which
+// is where its part of the sorted list begins, comes with the same look.  Its 16 waves take a part of the positions each, in
+// order, and sort what they found by counting: a table of counts for each (id, wave), its prefix sums, and within a wave the rank
+// among equal ids.  No atomics, and the time does not depend on the tokens.  A token that counts for nothing sorts behind all
+// others, as `vocab`.
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kSortList = 256;        // entries of a wave that are kept; a wave with more looks at its tokens again
+constexpr int kMaxSpan = kSortThreads;
 struct SortArgs {
     const int64_t* tokens;
     uint32_t* key;                    // sorted tokens
     uint32_t* pos;                    // their positions
     long long padding;
     uint32_t vocab;
-    int n;
+    int n, span;
 };
-__device__ __forceinline__ uint32_t key_of(const SortArgs& a, int i) {
-    const long long t = a.tokens[i];
+__device__ __forceinline__ uint32_t key_of(const SortArgs& a, long long t) {
     return t >= 0 && t < (long long)a.vocab && t != a.padding ? (uint32_t)t : a.vocab;
 }
-// Every entry's place is the number of entries before it: those with a smaller token and those with the same one at an earlier position.
-constexpr int kRankKeys = 16, kRankTile = 4096;
-__global__ __launch_bounds__(kThreads) void k_rank(const SortArgs a) {
-    __shared__ uint32_t tile[kRankTile];
-    __shared__ int count[kThreads / kRankKeys][kRankKeys];
-    const int which = threadIdx.x & (kRankKeys - 1), share = threadIdx.x / kRankKeys;
-    const int i = blockIdx.x * kRankKeys + which;
-    const uint32_t mine = i < a.n ? key_of(a, i) : 0;
-    int before = 0;
-    for (int base = 0; base < a.n; base += kRankTile) {
-        const int m = min(kRankTile, a.n - base);
-        __syncthreads();
-        for (int j = threadIdx.x; j < m; j += kThreads) tile[j] = key_of(a, base + j);
-        __syncthreads();
-        for (int j = share; j < m; j += kThreads / kRankKeys) {
-            const uint32_t k = tile[j];
-            before += k < mine || (k == mine && base + j < i);
+__device__ __forceinline__ int lanes_below(unsigned long long mask) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+}
+// the lanes of `members` with this lane's `low`
+__device__ __forceinline__ unsigned long long lanes_alike(unsigned long long members, uint32_t low) {
+    unsigned long long m = members;
+#pragma unroll
+    for (int bit = 0; bit < 10; ++bit) {
+        const unsigned long long set = __ballot(low >> bit & 1u);
+        m &= low >> bit & 1u ? set : ~set;
+    }
+    return m;
+}
+static_assert(kMaxSpan <= 1 << 10, "ids within a workgroup's span have 10 bits");
+__global__ __launch_bounds__(kSortThreads) void k_sort(const SortArgs a) {
+    extern __shared__ uint32_t lds[];
+    uint32_t* count = lds;                                     // [wave][span]
+    uint32_t(*list)[2] = reinterpret_cast<uint32_t(*)[2]>(lds + kSortWaves * a.span);   // [wave][kSortList]: id within the span, position
+    __shared__ int smaller[kSortWaves], totals[kSortWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t lo = blockIdx.x * (uint32_t)a.span, span = (uint32_t)a.span;
+    const int part = ((a.n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+    const int begin = min(a.n, wave * part), end = min(a.n, begin + part);
+    for (int i = threadIdx.x; i < kSortWaves * a.span; i += kSortThreads) count[i] = 0;
+    int less = 0, found = 0;
+    constexpr int U = 8;
+    for (int base = begin; base < end; base += 64 * U) {
+        long long t[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) t[u] = a.tokens[min(base + 64 * u + lane, a.n - 1)];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = base + 64 * u + lane;
+            const uint32_t k = key_of(a, t[u]);
+            less += __popcll(__ballot(i < end && k < lo));
+            const bool mine = i < end && k - lo < span;
+            const unsigned long long m = __ballot(mine);
+            const int at = found + lanes_below(m);
+            if (mine && at < kSortList) {
+                list[wave * kSortList + at][0] = k - lo;
+                list[wave * kSortList + at][1] = (uint32_t)i;
+            }
+            found += __popcll(m);
         }
     }
-    count[share][which] = before;
+    if (lane == 0) smaller[wave] = less;
     __syncthreads();
-    if (threadIdx.x < kRankKeys && i < a.n) {
-        int place = 0;
-        for (int s = 0; s < kThreads / kRankKeys; ++s) place += count[s][which];
-        a.key[place] = mine;
-        a.pos[place] = (uint32_t)i;
+    uint32_t* mine = count + wave * a.span;
+    // f(member, id within the span, position) for this wave's entries in order, 64 at a time
+    auto entries = [&](auto f) {
+        if (found <= kSortList) {
+            for (int e = lane; e - lane < found; e += 64) {
+                const bool member = e < found;
+                f(member, member ? list[wave * kSortList + e][0] : 0u, member ? list[wave * kSortList + e][1] : 0u);
+            }
+        } else {
+            for (int i = begin + lane; i - lane < end; i += 64) {
+                const uint32_t k = i < end ? key_of(a, a.tokens[i]) : 0u;
+                f(i < end && k - lo < span, k - lo < span ? k - lo : 0u, (uint32_t)i);
+            }
+        }
+    };
+    entries([&](bool member, uint32_t low, uint32_t) {
+        const unsigned long long alike = lanes_alike(__ballot(member), low);
+        if (member && lanes_below(alike) == 0) mine[low] += (uint32_t)__popcll(alike);
+        __builtin_amdgcn_wave_barrier();
+    });
+    __syncthreads();
+    // prefix sums: ids in order, of each id the waves in order
+    uint32_t total = 0;
+    if (threadIdx.x < span)
+        for (int w = 0; w < kSortWaves; ++w) total += count[w * a.span + threadIdx.x];
+    uint32_t upto = total;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t v = (uint32_t)__shfl_up((int)upto, o);
+        if (lane >= o) upto += v;
     }
+    if (lane == 63) totals[wave] = (int)upto;
+    __syncthreads();
+    uint32_t at = upto - total;
+    for (int w = 0; w < kSortWaves; ++w) at += (uint32_t)smaller[w] + (w < wave ? (uint32_t)totals[w] : 0u);
+    if (threadIdx.x < span) {
+        for (int w = 0; w < kSortWaves; ++w) {
+            const uint32_t c = count[w * a.span + threadIdx.x];
+            count[w * a.span + threadIdx.x] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
+    entries([&](bool member, uint32_t low, uint32_t position) {
+        const unsigned long long alike = lanes_alike(__ballot(member), low);
+        const int rank = lanes_below(alike);
+        if (member) {
+            const uint32_t first = mine[low];
+            a.key[first + rank] = lo + low;
+            a.pos[first + rank] = position;
+            __builtin_amdgcn_wave_barrier();       // every lane has read before the first of them writes
+            if (rank == 0) mine[low] = first + (uint32_t)__popcll(alike);
+        }
+        __builtin_amdgcn_wave_barrier();
+    });
 }
 
 // ---- gradient: sums -------------------------------------------------------------------------------------------
@@ -129,69 +211,105 @@ struct SumArgs {
     int accumulate, vec;
     float scale;
 };
-template <typename D, int N> __device__ __forceinline__ void write_row(const SumArgs& a, uint32_t token, int d, const float* acc) {
-    D* dst = static_cast<D*>(a.dtable) + (long long)token * a.table_stride + d;
-    float v[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = acc[i] * a.scale;
+// N columns of a row of the result, plus what was there
+template <typename D, int N> __device__ __forceinline__ void load_row(const SumArgs& a, uint32_t token, int d, float* old) {
+    const D* src = static_cast<const D*>(a.dtable) + (long long)token * a.table_stride + d;
     if constexpr (N > 1) {
         if (a.vec) {
-            if (a.accumulate) {
-                float old[N];
-                load_values<N>(dst, old);
+            load_values<N>(src, old);
+            return;
+        }
+    }
 #pragma unroll
-                for (int i = 0; i < N; ++i) v[i] += old[i];
-            }
+    for (int i = 0; i < N; ++i) old[i] = to_f32(src[i]);
+}
+template <typename D, int N> __device__ __forceinline__ void store_row(const SumArgs& a, uint32_t token, int d, const float* v) {
+    D* dst = static_cast<D*>(a.dtable) + (long long)token * a.table_stride + d;
+    if constexpr (N > 1) {
+        if (a.vec) {
             store_values<N>(dst, v);
             return;
         }
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) dst[i] = from_f32<D>(a.accumulate ? to_f32(dst[i]) + v[i] : v[i]);
+    for (int i = 0; i < N; ++i) dst[i] = from_f32<D>(v[i]);
 }
-// N: columns of a lane
-template <typename O, typename D, int N> __device__ __forceinline__ void sum_run(const SumArgs& a) {
-    const int groups = kThreads / a.lanes, lane = threadIdx.x & (a.lanes - 1);
+constexpr int kLeastLanes = 8, kMostRun = 64;
+constexpr int kMostEntries = kThreads / kLeastLanes * kMostRun;
+// N: columns of a lane.  ADD: the result is added to.  Rows are loaded several at a time, with the rows of the result that they
+// complete where those are added to, so that a run waits for memory a few times, not once for each entry.
+template <typename O, typename D, int N, bool ADD> __device__ __forceinline__ void sum_run(const SumArgs& a) {
+    constexpr int U = ADD ? 4 : 8;
+    __shared__ uint32_t key[kMostEntries + 2], pos[kMostEntries];       // key[0]: of the entry before this workgroup's
+    const int groups = kThreads / a.lanes, lane = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes;
     const int id = blockIdx.x / a.column_tiles, tile = blockIdx.x - id * a.column_tiles;
-    const int r = id * groups + threadIdx.x / a.lanes;
+    const int first = id * groups * a.run, entries = min(a.n - first, groups * a.run);
+    for (int i = threadIdx.x; i < entries + 2; i += kThreads) {
+        const int e = first + i - 1;
+        key[i] = e >= 0 && e < a.n ? a.key[e] : 0xffffffffu;
+        if (i < entries) pos[i] = a.pos[first + i];
+    }
+    __syncthreads();
+    const int r = id * groups + group;
     const int d = tile * a.columns + lane * N;
     if (r >= a.runs || d >= a.dim) return;
-    const int begin = r * a.run, end = min(a.n, begin + a.run);
+    const int begin = group * a.run, end = min(entries, begin + a.run);
     const O* dout = static_cast<const O*>(a.dout) + d;
-    uint32_t token = a.key[begin];
-    bool before = begin > 0 && a.key[begin - 1] == token;
+    bool before = key[begin] == key[begin + 1];
     float acc[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) acc[i] = 0.f;
-    for (int e = begin; e < end; ++e) {
-        const uint32_t next = e + 1 < a.n ? a.key[e + 1] : 0xffffffffu;
-        if (token < a.vocab) {
-            const O* row = dout + (long long)a.pos[e] * a.out_stride;
-            if constexpr (N == Vec16<O>::N) {
-                Vec16<O> v;
-                v.load(row);
+    for (int e0 = begin; e0 < end; e0 += U) {
+        Vec16<O> v[U];
+        O s[U];
+        float old[ADD ? U : 1][N];
+        bool begun = before;             // whether the token at hand began in an earlier run
 #pragma unroll
-                for (int i = 0; i < N; ++i) acc[i] += v.get(i);
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) acc[i] += to_f32(row[i]);
+        for (int u = 0; u < U; ++u) {
+            const int e = min(e0 + u, end - 1);
+            const O* row = dout + (long long)pos[e] * a.out_stride;
+            if constexpr (N == Vec16<O>::N) v[u].load(row);
+            else s[u] = *row;
+            if constexpr (ADD) {
+                const uint32_t token = key[e + 1];
+                const bool last = key[e + 2] != token;
+                if (last && !begun && token < a.vocab) load_row<D, N>(a, token, d, old[u]);
+                if (last) begun = false;
             }
         }
-        if (next != token || e + 1 == end) {
-            const bool after = next == token;
-            if (token < a.vocab) {
-                if (!before && !after) {
-                    write_row<D, N>(a, token, d, acc);
-                } else {
-                    float* p = a.part + ((long long)r * 2 + (before ? 0 : 1)) * a.dim + d;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) p[i] = acc[i];
+        for (int u = 0; u < U; ++u) {
+            const int e = e0 + u;
+            if (e < end) {
+                const uint32_t token = key[e + 1];
+                const bool after = key[e + 2] == token;
+                if constexpr (N == Vec16<O>::N) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) acc[i] += v[u].get(i);
+                } else {
+                    acc[0] += to_f32(s[u]);
+                }
+                if (!after || e + 1 == end) {
+                    if (token < a.vocab) {
+                        if (before || after) {
+                            float* p = a.part + ((long long)r * 2 + (before ? 0 : 1)) * a.dim + d;
+                            if constexpr (N > 1) store_values<N>(p, acc);      // rows of whole vectors: see the choice of N
+                            else *p = acc[0];
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < N; ++i) acc[i] = acc[i] * a.scale;
+                            if constexpr (ADD) {
+#pragma unroll
+                                for (int i = 0; i < N; ++i) acc[i] += old[u][i];
+                            }
+                            store_row<D, N>(a, token, d, acc);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < N; ++i) acc[i] = 0.f;
+                    before = false;
                 }
             }
-#pragma unroll
-            for (int i = 0; i < N; ++i) acc[i] = 0.f;
-            before = false;
-            token = next;
         }
     }
 }
@@ -236,42 +354,73 @@ template <typename D> __device__ __forceinline__ void write_zeros(const SumArgs&
         }
     }
 }
-template <typename O, typename D, int N> __global__ __launch_bounds__(kThreads) void k_sum(const SumArgs a) {
+template <typename O, typename D, int N, bool ADD> __global__ __launch_bounds__(kThreads) void k_sum(const SumArgs a) {
     if ((int)blockIdx.x >= a.run_blocks) write_zeros<D>(a);
-    else sum_run<O, D, N>(a);
+    else sum_run<O, D, N, ADD>(a);
 }
-// Adds up the partial rows of the token that run `blockIdx.x / tiles` shares with the next one and none before it.
-template <typename D> __global__ __launch_bounds__(kThreads) void k_join(const SumArgs a, int tiles) {
-    const int r = blockIdx.x / tiles, tile = blockIdx.x - r * tiles;
-    const int last = (r + 1) * a.run - 1;                         // r is not the last run
-    const uint32_t token = a.key[last];
-    if (token >= a.vocab || a.key[last + 1] != token) return;
-    if (a.key[r * a.run] == token && r > 0 && a.key[r * a.run - 1] == token) return;    // it began in an earlier run
-    // runs r + 1 .. r + more begin with it
+// Adds up the partial rows of tokens that cross the ends of runs, of every token in the order of the runs.  A workgroup has 8 runs and
+// 64 columns; a wave looks whether its run shares a token with the next one and none before it, and adds up a short list alone.
+// Long lists are shared by all waves, each a stretch of the runs.
+constexpr int kJoinThreads = 512, kJoinRuns = kJoinThreads / 64, kShort = 8;
+template <typename D> __global__ __launch_bounds__(kJoinThreads) void k_join(const SumArgs a, int tiles) {
+    __shared__ int more[kJoinRuns];               // runs that go on with the token of this one
+    __shared__ float sums[kJoinRuns][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int more = 0;
-    for (;;) {
-        const int at = r + 1 + more + lane;
-        const unsigned long long same = __ballot(at < a.runs && a.key[(long long)at * a.run] == token);
+    const int r0 = blockIdx.x / tiles * kJoinRuns, d = (blockIdx.x % tiles) * 64 + lane;
+    const int r = r0 + wave;
+    uint32_t token = a.vocab;
+    int n = 0;
+    if (r + 1 < a.runs) {
+        const int last = (r + 1) * a.run - 1;
+        const uint32_t k = a.key[last], next = a.key[last + 1], head = a.key[r * a.run], prior = r > 0 ? a.key[r * a.run - 1] : 0xffffffffu;
+        if (k == next && !(head == k && prior == k)) token = k;
+    }
+    while (token < a.vocab) {
+        const int at = r + 1 + n + lane;
+        const unsigned long long same = __ballot(at < a.runs && a.key[(long long)(at < a.runs ? at : 0) * a.run] == token);
         const int c = same == ~0ull ? 64 : __ffsll((long long)~same) - 1;
-        more += c;
+        n += c;
         if (c < 64) break;
     }
-    __shared__ float sums[kThreads / 64][64];
-    const int d = tile * 64 + lane;
-    float v = 0.f;
-    if (d < a.dim) {
-        if (wave == 0) v = a.part[((long long)r * 2 + 1) * a.dim + d];
-        const int share = (more + kThreads / 64 - 1) / (kThreads / 64);
-        const int from = wave * share, to = min(more, from + share);
-#pragma unroll 8
-        for (int k = from; k < to; ++k) v += a.part[(long long)(r + 1 + k) * 2 * a.dim + d];
+    if (lane == 0) more[wave] = n;
+    // slot 1 of its first run, slot 0 of the others
+    auto partial = [&](int run, int slot) { return a.part[((long long)run * 2 + slot) * a.dim + d]; };
+    auto finish = [&](uint32_t t, float v) {
+        v *= a.scale;
+        float old;
+        if (a.accumulate) {
+            load_row<D, 1>(a, t, d, &old);
+            v += old;
+        }
+        store_row<D, 1>(a, t, d, &v);
+    };
+    if (n > 0 && n <= kShort && d < a.dim) {
+        float v = partial(r, 1), p[kShort];
+#pragma unroll
+        for (int k = 0; k < kShort; ++k) p[k] = k < n ? partial(r + 1 + k, 0) : 0.f;
+#pragma unroll
+        for (int k = 0; k < kShort; ++k) v += p[k];
+        finish(token, v);
     }
-    sums[wave][lane] = v;
     __syncthreads();
-    if (wave == 0 && d < a.dim) {
-        for (int w = 1; w < kThreads / 64; ++w) v += sums[w][lane];
-        write_row<D, 1>(a, token, d, &v);
+    for (int w = 0; w < kJoinRuns; ++w) {
+        const int m = more[w];
+        if (m <= kShort) continue;
+        const int share = (m + kJoinRuns - 1) / kJoinRuns, from = wave * share, to = min(m, from + share);
+        float v = 0.f;
+        if (d < a.dim) {
+            if (wave == 0) v = partial(r0 + w, 1);
+#pragma unroll 8
+            for (int k = from; k < to; ++k) v += partial(r0 + w + 1 + k, 0);
+        }
+        sums[wave][lane] = v;
+        __syncthreads();
+        if (wave == w && d < a.dim) {
+            v = sums[0][lane];
+            for (int k = 1; k < kJoinRuns; ++k) v += sums[k][lane];
+            finish(token, v);
+        }
+        __syncthreads();
     }
 }
 
@@ -281,15 +430,11 @@ asi_status check(const asi_embedding_desc* d) {
     if (!dtype_ok(d->table_dtype) || !dtype_ok(d->out_dtype)) return ASI_ERR_UNSUPPORTED;
     if (d->tokens < 0 || d->vocab < 1 || d->dim < 1 || d->table_stride < d->dim || d->out_stride < d->dim || d->reserved) return ASI_ERR_INVALID_ARG;
     if (!std::isfinite(d->scale)) return ASI_ERR_INVALID_ARG;
-    if (d->tokens >= (1LL << 30) || d->vocab >= (1LL << 30) || d->dim > (1LL << 24)) return ASI_ERR_UNSUPPORTED;
+    if (d->tokens >= (1LL << 30) || d->vocab > (1LL << 24) || d->dim > (1LL << 24)) return ASI_ERR_UNSUPPORTED;
     return ASI_OK;
 }
-// Entries of a run: 32, more where the table's rows are many so that partial rows stay few
-int run_length(const asi_embedding_desc* d) {
-    int run = 32;
-    while (d->tokens / run > 1024 && run < 1024) run *= 2;
-    return run;
-}
+// Entries of a run: few where there are few, so that the runs fill the chip; more of many, so that there are fewer partial rows.
+int run_length(const asi_embedding_desc* d) { return d->tokens <= 8192 ? 16 : d->tokens <= 131072 ? 32 : kMostRun; }
 struct GradPlan {
     size_t key, pos, part, bytes;     // offsets
     int run, runs;
@@ -309,8 +454,13 @@ template <typename T, typename O> void lookup(const LookupArgs& a, bool vec, dim
     else hipLaunchKernelGGL((k_lookup_any<T, O>), grid, kThreads, 0, st, a);
 }
 template <typename O, typename D> void sum(const SumArgs& a, int n, unsigned blocks, hipStream_t st) {
-    if (n == Vec16<O>::N) hipLaunchKernelGGL((k_sum<O, D, Vec16<O>::N>), dim3(blocks), kThreads, 0, st, a);
-    else hipLaunchKernelGGL((k_sum<O, D, 1>), dim3(blocks), kThreads, 0, st, a);
+    if (n == Vec16<O>::N) {
+        if (a.accumulate) hipLaunchKernelGGL((k_sum<O, D, Vec16<O>::N, true>), dim3(blocks), kThreads, 0, st, a);
+        else hipLaunchKernelGGL((k_sum<O, D, Vec16<O>::N, false>), dim3(blocks), kThreads, 0, st, a);
+    } else {
+        if (a.accumulate) hipLaunchKernelGGL((k_sum<O, D, 1, true>), dim3(blocks), kThreads, 0, st, a);
+        else hipLaunchKernelGGL((k_sum<O, D, 1, false>), dim3(blocks), kThreads, 0, st, a);
+    }
 }
 
 }  // namespace
@@ -373,7 +523,7 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
     a.vec = aligned(dtable, 16) && desc->table_stride % (16 / ds) == 0 && desc->dim % (16 / ds) == 0;
     const int wide = (int)(16 / os);
     const int n = desc->dim % wide == 0 && desc->out_stride % wide == 0 && aligned(grad_out, 16) ? wide : 1;
-    a.lanes = 1;
+    a.lanes = kLeastLanes;
     while (a.lanes < kThreads && a.lanes * n < a.dim) a.lanes *= 2;
     a.columns = a.lanes * n;
     a.column_tiles = (a.dim + a.columns - 1) / a.columns;
@@ -384,8 +534,15 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
     if (run_blocks + fill_blocks > 0x7fffffffLL || (long long)p.runs * tiles > 0x7fffffffLL) return ASI_ERR_UNSUPPORTED;
     a.run_blocks = (int)run_blocks;
     if (desc->tokens) {
-        const SortArgs s{tokens, reinterpret_cast<uint32_t*>(w + p.key), reinterpret_cast<uint32_t*>(w + p.pos), desc->padding_index, a.vocab, a.n};
-        hipLaunchKernelGGL(k_rank, dim3((unsigned)((a.n + kRankKeys - 1) / kRankKeys)), kThreads, 0, st, s);
+        // about one workgroup a CU; the id `vocab` is one more
+        const long long ids = desc->vocab + 1;
+        const int span = (int)std::min<long long>(kMaxSpan, (ids + 255) / 256);
+        const SortArgs s{tokens, reinterpret_cast<uint32_t*>(w + p.key), reinterpret_cast<uint32_t*>(w + p.pos), desc->padding_index, a.vocab, a.n, span};
+        constexpr size_t lists = (size_t)kSortWaves * kSortList * 8;
+        static LdsAllowed allowed;
+        if (allow_lds(reinterpret_cast<const void*>(k_sort), (size_t)kSortWaves * kMaxSpan * 4 + lists, allowed) != hipSuccess) return ASI_ERR_HIP;
+        const size_t lds = (size_t)kSortWaves * span * 4 + lists;
+        hipLaunchKernelGGL(k_sort, dim3((unsigned)((ids + span - 1) / span)), kSortThreads, lds, st, s);
     }
     const unsigned blocks = (unsigned)(run_blocks + fill_blocks);
     if (desc->out_dtype == ASI_F32) {
@@ -396,9 +553,9 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
         else sum<bf16_t, bf16_t>(a, n, blocks, st);
     }
     if (p.runs > 1) {
-        const dim3 grid((unsigned)((p.runs - 1) * tiles));
-        if (desc->table_dtype == ASI_F32) hipLaunchKernelGGL(k_join<float>, grid, kThreads, 0, st, a, tiles);
-        else hipLaunchKernelGGL(k_join<bf16_t>, grid, kThreads, 0, st, a, tiles);
+        const dim3 grid((unsigned)((p.runs - 1 + kJoinRuns - 1) / kJoinRuns * tiles));
+        if (desc->table_dtype == ASI_F32) hipLaunchKernelGGL(k_join<float>, grid, kJoinThreads, 0, st, a, tiles);
+        else hipLaunchKernelGGL(k_join<bf16_t>, grid, kJoinThreads, 0, st, a, tiles);
     }
     return launched();
 }
