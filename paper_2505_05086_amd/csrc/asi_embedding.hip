@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "asi_lds.h"
 #include "asi_lm_device.h"
@@ -208,37 +209,46 @@ struct SumArgs {
     int n, run, runs, dim;
     int columns, lanes, column_tiles; // lanes: of a group (a power of two); columns: that a group covers
     int run_blocks;                   // workgroups of runs, before those that write zeros
-    int accumulate, vec;
+    int accumulate, vec;              // vec: rows of zeros can be written 16 bytes at a time
     float scale;
 };
-// N columns of a row of the result, plus what was there
-template <typename D, int N> __device__ __forceinline__ void load_row(const SumArgs& a, uint32_t token, int d, float* old) {
+// C neighbouring columns of a row as loaded: so many rows can be in flight at little cost in registers
+template <typename O, int C> struct Columns {
+    static_assert(C == 1 || (C * sizeof(O) == 8 || C * sizeof(O) == 16), "one value, 8 or 16 bytes");
+    using Raw = std::conditional_t<C == 1, O, std::conditional_t<C * sizeof(O) == 8, uint2, uint4>>;
+    Raw raw;
+    __device__ __forceinline__ void load(const O* p) { raw = *reinterpret_cast<const Raw*>(p); }
+    __device__ __forceinline__ void add_to(float* f) const {
+        if constexpr (C == 1) {
+            f[0] += to_f32(raw);
+        } else if constexpr (sizeof(O) == 4) {
+            f[0] += __uint_as_float(raw.x); f[1] += __uint_as_float(raw.y); f[2] += __uint_as_float(raw.z); f[3] += __uint_as_float(raw.w);
+        } else {
+            f[0] += __uint_as_float(raw.x << 16); f[1] += __uint_as_float(raw.x & 0xffff0000u);
+            f[2] += __uint_as_float(raw.y << 16); f[3] += __uint_as_float(raw.y & 0xffff0000u);
+            if constexpr (C == 8) {
+                f[4] += __uint_as_float(raw.z << 16); f[5] += __uint_as_float(raw.z & 0xffff0000u);
+                f[6] += __uint_as_float(raw.w << 16); f[7] += __uint_as_float(raw.w & 0xffff0000u);
+            }
+        }
+    }
+};
+template <typename D, int C> __device__ __forceinline__ void load_result(const SumArgs& a, uint32_t token, int d, float* old) {
     const D* src = static_cast<const D*>(a.dtable) + (long long)token * a.table_stride + d;
-    if constexpr (N > 1) {
-        if (a.vec) {
-            load_values<N>(src, old);
-            return;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) old[i] = to_f32(src[i]);
+    if constexpr (C > 1) load_values<C>(src, old);
+    else old[0] = to_f32(*src);
 }
-template <typename D, int N> __device__ __forceinline__ void store_row(const SumArgs& a, uint32_t token, int d, const float* v) {
+template <typename D, int C> __device__ __forceinline__ void store_result(const SumArgs& a, uint32_t token, int d, const float* v) {
     D* dst = static_cast<D*>(a.dtable) + (long long)token * a.table_stride + d;
-    if constexpr (N > 1) {
-        if (a.vec) {
-            store_values<N>(dst, v);
-            return;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) dst[i] = from_f32<D>(v[i]);
+    if constexpr (C > 1) store_values<C>(dst, v);
+    else *dst = from_f32<D>(v[0]);
 }
 constexpr int kLeastLanes = 8, kMostRun = 64;
 constexpr int kMostEntries = kThreads / kLeastLanes * kMostRun;
-// N: columns of a lane.  ADD: the result is added to.  Rows are loaded several at a time, with the rows of the result that they
+// A lane has P pieces of C neighbouring columns, the pieces of a group's lanes side by side, so that loads and stores of either
+// type are whole lines.  ADD: the result is added to.  Rows are loaded several at a time, with the rows of the result that they
 // complete where those are added to, so that a run waits for memory a few times, not once for each entry.
-template <typename O, typename D, int N, bool ADD> __device__ __forceinline__ void sum_run(const SumArgs& a) {
+template <typename O, typename D, int C, int P, bool ADD> __device__ __forceinline__ void sum_run(const SumArgs& a) {
     constexpr int U = ADD ? 4 : 8;
     __shared__ uint32_t key[kMostEntries + 2], pos[kMostEntries];       // key[0]: of the entry before this workgroup's
     const int groups = kThreads / a.lanes, lane = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes;
@@ -251,29 +261,40 @@ template <typename O, typename D, int N, bool ADD> __device__ __forceinline__ vo
     }
     __syncthreads();
     const int r = id * groups + group;
-    const int d = tile * a.columns + lane * N;
+    const int d = tile * a.columns + lane * C, apart = a.lanes * C;     // first column of the first piece; from piece to piece
     if (r >= a.runs || d >= a.dim) return;
     const int begin = group * a.run, end = min(entries, begin + a.run);
-    const O* dout = static_cast<const O*>(a.dout) + d;
-    bool before = key[begin] == key[begin + 1];
-    float acc[N];
+    const O* dout = static_cast<const O*>(a.dout);
+    int col[P];                          // a piece behind the row's end reads the first one's columns again and writes nothing
+    bool has[P];
 #pragma unroll
-    for (int i = 0; i < N; ++i) acc[i] = 0.f;
+    for (int p = 0; p < P; ++p) {
+        has[p] = d + p * apart < a.dim;
+        col[p] = has[p] ? d + p * apart : d;
+    }
+    bool before = key[begin] == key[begin + 1];
+    float acc[P][C];
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int i = 0; i < C; ++i) acc[p][i] = 0.f;
     for (int e0 = begin; e0 < end; e0 += U) {
-        Vec16<O> v[U];
-        O s[U];
-        float old[ADD ? U : 1][N];
+        Columns<O, C> v[U][P];
+        float old[ADD ? U : 1][P][C];
         bool begun = before;             // whether the token at hand began in an earlier run
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int e = min(e0 + u, end - 1);
             const O* row = dout + (long long)pos[e] * a.out_stride;
-            if constexpr (N == Vec16<O>::N) v[u].load(row);
-            else s[u] = *row;
+#pragma unroll
+            for (int p = 0; p < P; ++p) v[u][p].load(row + col[p]);
             if constexpr (ADD) {
                 const uint32_t token = key[e + 1];
                 const bool last = key[e + 2] != token;
-                if (last && !begun && token < a.vocab) load_row<D, N>(a, token, d, old[u]);
+                if (last && !begun && token < a.vocab) {
+#pragma unroll
+                    for (int p = 0; p < P; ++p) load_result<D, C>(a, token, col[p], old[u][p]);
+                }
                 if (last) begun = false;
             }
         }
@@ -283,30 +304,31 @@ template <typename O, typename D, int N, bool ADD> __device__ __forceinline__ vo
             if (e < end) {
                 const uint32_t token = key[e + 1];
                 const bool after = key[e + 2] == token;
-                if constexpr (N == Vec16<O>::N) {
 #pragma unroll
-                    for (int i = 0; i < N; ++i) acc[i] += v[u].get(i);
-                } else {
-                    acc[0] += to_f32(s[u]);
-                }
+                for (int p = 0; p < P; ++p) v[u][p].add_to(acc[p]);
                 if (!after || e + 1 == end) {
                     if (token < a.vocab) {
                         if (before || after) {
-                            float* p = a.part + ((long long)r * 2 + (before ? 0 : 1)) * a.dim + d;
-                            if constexpr (N > 1) store_values<N>(p, acc);      // rows of whole vectors: see the choice of N
-                            else *p = acc[0];
+                            float* out = a.part + ((long long)r * 2 + (before ? 0 : 1)) * a.dim;
+#pragma unroll
+                            for (int p = 0; p < P; ++p) {
+                                if (!has[p]) continue;
+                                if constexpr (C > 1) store_values<C>(out + col[p], acc[p]);      // dim is a multiple of C then
+                                else out[col[p]] = acc[p][0];
+                            }
                         } else {
 #pragma unroll
-                            for (int i = 0; i < N; ++i) acc[i] = acc[i] * a.scale;
-                            if constexpr (ADD) {
+                            for (int p = 0; p < P; ++p) {
 #pragma unroll
-                                for (int i = 0; i < N; ++i) acc[i] += old[u][i];
+                                for (int i = 0; i < C; ++i) acc[p][i] = ADD ? acc[p][i] * a.scale + old[u][p][i] : acc[p][i] * a.scale;
+                                if (has[p]) store_result<D, C>(a, token, col[p], acc[p]);
                             }
-                            store_row<D, N>(a, token, d, acc);
                         }
                     }
 #pragma unroll
-                    for (int i = 0; i < N; ++i) acc[i] = 0.f;
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int i = 0; i < C; ++i) acc[p][i] = 0.f;
                     before = false;
                 }
             }
@@ -354,9 +376,9 @@ template <typename D> __device__ __forceinline__ void write_zeros(const SumArgs&
         }
     }
 }
-template <typename O, typename D, int N, bool ADD> __global__ __launch_bounds__(kThreads) void k_sum(const SumArgs a) {
+template <typename O, typename D, int C, int P, bool ADD> __global__ __launch_bounds__(kThreads) void k_sum(const SumArgs a) {
     if ((int)blockIdx.x >= a.run_blocks) write_zeros<D>(a);
-    else sum_run<O, D, N, ADD>(a);
+    else sum_run<O, D, C, P, ADD>(a);
 }
 // Adds up the partial rows of tokens that cross the ends of runs, of every token in the order of the runs.  A workgroup has 8 runs and
 // 64 columns; a wave looks whether its run shares a token with the next one and none before it, and adds up a short list alone.
@@ -389,10 +411,10 @@ template <typename D> __global__ __launch_bounds__(kJoinThreads) void k_join(con
         v *= a.scale;
         float old;
         if (a.accumulate) {
-            load_row<D, 1>(a, t, d, &old);
+            load_result<D, 1>(a, t, d, &old);
             v += old;
         }
-        store_row<D, 1>(a, t, d, &v);
+        store_result<D, 1>(a, t, d, &v);
     };
     if (n > 0 && n <= kShort && d < a.dim) {
         float v = partial(r, 1), p[kShort];
@@ -433,8 +455,16 @@ asi_status check(const asi_embedding_desc* d) {
     if (d->tokens >= (1LL << 30) || d->vocab > (1LL << 24) || d->dim > (1LL << 24)) return ASI_ERR_UNSUPPORTED;
     return ASI_OK;
 }
-// Entries of a run: few where there are few, so that the runs fill the chip; more of many, so that there are fewer partial rows.
-int run_length(const asi_embedding_desc* d) { return d->tokens <= 8192 ? 16 : d->tokens <= 131072 ? 32 : kMostRun; }
+// Entries of a run: short ones of few entries, where a run is a chain that nothing overlaps (954 x 1437 with 8, 16, 32 entries 19.0, 22.0,
+// 29.2 us, 377 x 2501 16.4, 20.0, 27.2); longer ones, with fewer partial rows, where the chip is filled all the same (4096 x 2048
+// 56.6, 53.0, 56.0; 25807 x 136 30.6, 28.0, 31.7; 32767 x 1000 72.7, 63.3, 57.7, with 64 62.4).
+int run_length(const asi_embedding_desc* d) {
+    if (d->tokens <= 2048) return 8;
+    const long long row = (d->dim + 255) / 256;
+    int run = 16;
+    while (run < kMostRun && d->tokens / run * row > 4500) run *= 2;
+    return run;
+}
 struct GradPlan {
     size_t key, pos, part, bytes;     // offsets
     int run, runs;
@@ -453,13 +483,27 @@ template <typename T, typename O> void lookup(const LookupArgs& a, bool vec, dim
     if (vec) hipLaunchKernelGGL((k_lookup<T, O>), grid, kThreads, 0, st, a);
     else hipLaunchKernelGGL((k_lookup_any<T, O>), grid, kThreads, 0, st, a);
 }
-template <typename O, typename D> void sum(const SumArgs& a, int n, unsigned blocks, hipStream_t st) {
-    if (n == Vec16<O>::N) {
-        if (a.accumulate) hipLaunchKernelGGL((k_sum<O, D, Vec16<O>::N, true>), dim3(blocks), kThreads, 0, st, a);
-        else hipLaunchKernelGGL((k_sum<O, D, Vec16<O>::N, false>), dim3(blocks), kThreads, 0, st, a);
+// Columns of a piece and pieces of a lane: 16 bytes of the wider type, twice where the rows that are read are the narrower ones
+template <typename O, typename D> struct Shape {
+    static constexpr int C = sizeof(D) == 2 && sizeof(O) == 2 ? 8 : 4, P = sizeof(O) < sizeof(D) ? 2 : 1;
+};
+constexpr int kLoose = 4;             // pieces of a lane where they are single columns
+template <typename O, typename D> void sum(SumArgs a, bool vec, int fill_blocks, hipStream_t st) {
+    constexpr int C = Shape<O, D>::C, P = Shape<O, D>::P;
+    const int n = vec ? C * P : kLoose;
+    a.lanes = kLeastLanes;
+    while (a.lanes < kThreads && a.lanes * n < a.dim) a.lanes *= 2;
+    a.columns = a.lanes * n;
+    a.column_tiles = (a.dim + a.columns - 1) / a.columns;
+    const int groups = kThreads / a.lanes;
+    a.run_blocks = (a.runs + groups - 1) / groups * a.column_tiles;
+    const dim3 grid((unsigned)(a.run_blocks + fill_blocks));
+    if (vec) {
+        if (a.accumulate) hipLaunchKernelGGL((k_sum<O, D, C, P, true>), grid, kThreads, 0, st, a);
+        else hipLaunchKernelGGL((k_sum<O, D, C, P, false>), grid, kThreads, 0, st, a);
     } else {
-        if (a.accumulate) hipLaunchKernelGGL((k_sum<O, D, 1, true>), dim3(blocks), kThreads, 0, st, a);
-        else hipLaunchKernelGGL((k_sum<O, D, 1, false>), dim3(blocks), kThreads, 0, st, a);
+        if (a.accumulate) hipLaunchKernelGGL((k_sum<O, D, 1, kLoose, true>), grid, kThreads, 0, st, a);
+        else hipLaunchKernelGGL((k_sum<O, D, 1, kLoose, false>), grid, kThreads, 0, st, a);
     }
 }
 
@@ -521,18 +565,13 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
     a.accumulate = accumulate != 0;
     a.scale = desc->scale;
     a.vec = aligned(dtable, 16) && desc->table_stride % (16 / ds) == 0 && desc->dim % (16 / ds) == 0;
-    const int wide = (int)(16 / os);
-    const int n = desc->dim % wide == 0 && desc->out_stride % wide == 0 && aligned(grad_out, 16) ? wide : 1;
-    a.lanes = kLeastLanes;
-    while (a.lanes < kThreads && a.lanes * n < a.dim) a.lanes *= 2;
-    a.columns = a.lanes * n;
-    a.column_tiles = (a.dim + a.columns - 1) / a.columns;
-    const int groups = kThreads / a.lanes;
-    const long long run_blocks = (long long)((p.runs + groups - 1) / groups) * a.column_tiles;
-    const long long fill_blocks = accumulate ? 0 : (desc->vocab + kFillRows - 1) / kFillRows;
+    // whole pieces: 4 columns, 8 where both types are bf16
+    const int piece = ds == 2 && os == 2 ? 8 : 4;
+    const bool vec = desc->dim % piece == 0 && desc->out_stride % piece == 0 && desc->table_stride % piece == 0 && aligned(grad_out, piece * os) && aligned(dtable, piece * ds);
+    const int fill_blocks = accumulate ? 0 : (int)((desc->vocab + kFillRows - 1) / kFillRows);
     const int tiles = (a.dim + 63) / 64;
-    if (run_blocks + fill_blocks > 0x7fffffffLL || (long long)p.runs * tiles > 0x7fffffffLL) return ASI_ERR_UNSUPPORTED;
-    a.run_blocks = (int)run_blocks;
+    // an upper bound of the workgroups of either launch
+    if ((long long)p.runs * tiles + fill_blocks > 0x7fffffffLL) return ASI_ERR_UNSUPPORTED;
     if (desc->tokens) {
         // about one workgroup a CU; the id `vocab` is one more
         const long long ids = desc->vocab + 1;
@@ -544,13 +583,12 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
         const size_t lds = (size_t)kSortWaves * span * 4 + lists;
         hipLaunchKernelGGL(k_sort, dim3((unsigned)((ids + span - 1) / span)), kSortThreads, lds, st, s);
     }
-    const unsigned blocks = (unsigned)(run_blocks + fill_blocks);
     if (desc->out_dtype == ASI_F32) {
-        if (desc->table_dtype == ASI_F32) sum<float, float>(a, n, blocks, st);
-        else sum<float, bf16_t>(a, n, blocks, st);
+        if (desc->table_dtype == ASI_F32) sum<float, float>(a, vec, fill_blocks, st);
+        else sum<float, bf16_t>(a, vec, fill_blocks, st);
     } else {
-        if (desc->table_dtype == ASI_F32) sum<bf16_t, float>(a, n, blocks, st);
-        else sum<bf16_t, bf16_t>(a, n, blocks, st);
+        if (desc->table_dtype == ASI_F32) sum<bf16_t, float>(a, vec, fill_blocks, st);
+        else sum<bf16_t, bf16_t>(a, vec, fill_blocks, st);
     }
     if (p.runs > 1) {
         const dim3 grid((unsigned)((p.runs - 1 + kJoinRuns - 1) / kJoinRuns * tiles));
