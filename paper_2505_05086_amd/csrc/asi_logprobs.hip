@@ -4,11 +4,12 @@
 //     s = sum e_i,  w = sum d_i e_i;   logprob = scale d_target - log s;   entropy = log s - scale w / s
 // Differences from the row's largest logit keep the digits that z - lse would lose where logits are large.
 //
-// Forward: a workgroup takes a row in one pass; every thread keeps a running largest logit and the sums relative to it.
+// Forward: a workgroup takes a row in one pass, several vectors a thread at a time; every thread keeps a running largest logit
+// and the sums relative to it.
 // Top alternatives: of the threads' largest logits each wave takes its c-th, c = ceil(top / waves); the least of those is a bound
-// that at least `top` logits reach.  Only threads whose largest reaches it look at their logits again and hand over those that
-// do, a few more than wanted; of these each finds its place by counting the ones before it.  Rows where too many reach the
-// bound (many equal logits) are searched `top` times instead.
+// that at least `top` logits reach.  Only the vectors of threads whose largest reaches it are looked at again, shared by all threads,
+// and hand over the logits that reach it, a few more than wanted; of these each finds its place by counting the ones before
+// it.  Rows where too many reach the bound (many equal logits) are searched `top` times instead.
 //
 // Gradient: a row is kept in registers between the pass that sums and the one that writes, so that it is read once and written once;
 // rows too long for that are read again.
@@ -65,39 +66,65 @@ __device__ __forceinline__ Sums joined(const Sums& a, const Sums& b, float c) {
     r.w = fa * (a.w + da * a.s) + fb * (b.w + db * b.s);
     return r;
 }
-// Over the workgroup; every thread gets the result.
-template <int THREADS> __device__ __forceinline__ Sums over_workgroup(Sums a, float c, Sums* scratch) {
+template <int WIDTH> __device__ __forceinline__ Sums over_lanes(Sums a, float c) {
 #pragma unroll
-    for (int o = 32; o; o >>= 1) {
+    for (int o = WIDTH / 2; o; o >>= 1) {
         Sums b;
         b.m = __shfl_xor(a.m, o); b.s = __shfl_xor(a.s, o); b.w = __shfl_xor(a.w, o);
         a = joined(a, b, c);
     }
-    constexpr int W = THREADS / 64;
-    if (W > 1) {
-        if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = a;
-        __syncthreads();
-        a = scratch[0];
-        for (int k = 1; k < W; ++k) a = joined(a, scratch[k], c);
-    }
     return a;
 }
-// `cnt` more logits of a thread
-template <int CNT> __device__ __forceinline__ void take(Sums* a, const float* x, float c) {
-    float top = x[0];
+// Over the workgroup; every thread gets the result.
+template <int THREADS> __device__ __forceinline__ Sums over_workgroup(Sums a, float c, Sums* scratch) {
+    constexpr int W = THREADS / 64;
+    a = over_lanes<64>(a, c);
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = a;
+    __syncthreads();
+    return over_lanes<W>(scratch[threadIdx.x & (W - 1)], c);
+}
+// Keeps the instructions of one vector together: interleaving several costs more registers than it saves time.
+__device__ __forceinline__ void one_at_a_time() { __builtin_amdgcn_sched_barrier(0); }
+// One more logit of a thread
+__device__ __forceinline__ void take_one(Sums* a, float x, float c) {
+    Sums b{x > kLowest ? x : kLowest, 0.f, 0.f};
+    const float d = max_nan(x - b.m, kFar);
+    b.s = exp2_fast(d * c);
+    b.w = d * b.s;
+    *a = joined(*a, b, c);
+}
+template <typename T> __device__ __forceinline__ float largest(const Vec16<T>& v) {
+    float m = v.get(0);
 #pragma unroll
-    for (int i = 1; i < CNT; ++i) top = fmaxf(top, x[i]);
-    if (top > a->m) {
-        const float d = max_nan(a->m - top, kFar), f = exp2_fast(d * c);
-        a->w = f * (a->w + d * a->s);
-        a->s *= f;
-        a->m = top;
+    for (int i = 1; i < Vec16<T>::N; ++i) m = fmaxf(m, v.get(i));
+    return m;
+}
+// a vector of nothing but -infinity
+template <typename T> __device__ __forceinline__ void set_nothing(Vec16<T>* v) {
+    const uint32_t w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    v->raw = make_uint4(w, w, w, w);
+}
+// U more vectors
+template <typename T, int U> __device__ __forceinline__ void take(Sums* a, const Vec16<T>* v, float c) {
+    float m = a->m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        m = fmaxf(m, largest(v[u]));
+        if (U > 2) one_at_a_time();
     }
+    const float shift = max_nan(a->m - m, kFar), f = exp2_fast(shift * c);
+    a->w = f * (a->w + shift * a->s);
+    a->s *= f;
+    a->m = m;
 #pragma unroll
-    for (int i = 0; i < CNT; ++i) {
-        const float d = max_nan(x[i] - a->m, kFar), e = exp2_fast(d * c);
-        a->s += e;
-        a->w += d * e;
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int i = 0; i < Vec16<T>::N; ++i) {
+            const float d = max_nan(v[u].get(i) - m, kFar), e = exp2_fast(d * c);
+            a->s += e;
+            a->w += d * e;
+        }
+        if (U > 2) one_at_a_time();
     }
 }
 
@@ -148,35 +175,29 @@ __device__ __forceinline__ unsigned long long lanes_max64(unsigned long long k) 
     }
     return k;
 }
+__device__ __forceinline__ float logit_of(unsigned long long key) {
+    const uint32_t o = (uint32_t)(key >> 32);
+    return o == 0xffffffffu ? __builtin_nanf("") : __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+}
 constexpr int kCandidates = 1024;
 template <int THREADS> struct TopScratch {
     unsigned long long key[kCandidates];
     unsigned long long wave[THREADS / 64];
     uint32_t bound[THREADS / 64];
-    int count;
+    int who[THREADS];                 // threads whose vectors are looked at again
+    int count, many;
 };
-template <typename T, typename F> __device__ __forceinline__ void each_of_thread(const RowView<T>& r, int threads, F f) {
-    constexpr int N = Vec16<T>::N;
-    const int l = r.loose(threadIdx.x);
-    if (l >= 0) f(to_f32(r.x[l]), l);
-    for (int v = threadIdx.x; v < r.nvec; v += threads) {
-        Vec16<T> raw;
-        raw.load(r.vec(v));
-#pragma unroll
-        for (int i = 0; i < N; ++i) f(raw.get(i), r.index(v) + i);
-    }
-}
+// `most`: the order of this thread's largest logit in its vectors (NaN counts as the largest), 0 without any
 template <typename T, int THREADS>
 __device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, const Args& a, float lse, long long row, TopScratch<THREADS>* sc) {
-    constexpr int W = THREADS / 64;
+    constexpr int W = THREADS / 64, N = Vec16<T>::N;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float* out = a.top_logprob + row * a.top;
     int64_t* out_i = a.top_index + row * a.top;
     auto write = [&](int place, unsigned long long key) {
-        const int index = (int)~(uint32_t)key;
-        const float x = to_f32(r.x[index]);
+        const float x = logit_of(key);
         out[place] = x == -__builtin_inff() && lse == lse ? x : x * a.scale - lse;     // also where lse is -infinity
-        out_i[place] = index;
+        out_i[place] = (int)~(uint32_t)key;
     };
     // This wave's c-th largest of its threads' largest, equal ones counted each.  Waves whose threads do not all have a vector
     // bound nothing; where there is no other, everything is handed over (less than kCandidates then).
@@ -194,18 +215,32 @@ __device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, co
             if (left == m) left = 0;
         }
     }
-    if (threadIdx.x == 0) sc->count = 0;
+    if (threadIdx.x == 0) sc->count = sc->many = 0;
     if (lane == 0) sc->bound[wave] = bound;
     __syncthreads();
     bound = sc->bound[0];
     for (int k = 1; k < W; ++k) bound = min(bound, sc->bound[k]);
-    if (most >= bound) {
-        each_of_thread(r, THREADS, [&](float x, int i) {
-            if (order_of(x) >= bound) {
-                const int at = atomicAdd(&sc->count, 1);
-                if (at < kCandidates) sc->key[at] = rank_key(x, i);
+    auto hand_over = [&](float x, int i) {
+        if (order_of(x) >= bound) {
+            const int at = atomicAdd(&sc->count, 1);
+            if (at < kCandidates) sc->key[at] = rank_key(x, i);
+        }
+    };
+    if (most >= bound && most) sc->who[atomicAdd(&sc->many, 1)] = threadIdx.x;
+    if (const int l = r.loose(threadIdx.x); l >= 0) hand_over(to_f32(r.x[l]), l);
+    __syncthreads();
+    {
+        const int each = (r.nvec + THREADS - 1) / THREADS, all = sc->many * each;
+#pragma unroll 4
+        for (int item = threadIdx.x; item < all; item += THREADS) {
+            const int k = item / each, v = sc->who[k] + (item - k * each) * THREADS;
+            if (v < r.nvec) {
+                Vec16<T> raw;
+                raw.load(r.vec(v));
+#pragma unroll
+                for (int i = 0; i < N; ++i) hand_over(raw.get(i), r.index(v) + i);
             }
-        });
+        }
     }
     __syncthreads();
     const int n = sc->count;
@@ -221,10 +256,18 @@ __device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, co
     unsigned long long last = ~0ull;              // no key is that: an index is not negative
     for (int place = 0; place < a.top; ++place) {
         unsigned long long best = 0;
-        each_of_thread(r, THREADS, [&](float x, int i) {
+        auto look = [&](float x, int i) {
             const unsigned long long key = rank_key(x, i);
             if (key < last && key > best) best = key;
-        });
+        };
+        if (const int l = r.loose(threadIdx.x); l >= 0) look(to_f32(r.x[l]), l);
+#pragma unroll 4
+        for (int v = threadIdx.x; v < r.nvec; v += THREADS) {
+            Vec16<T> raw;
+            raw.load(r.vec(v));
+#pragma unroll
+            for (int i = 0; i < N; ++i) look(raw.get(i), r.index(v) + i);
+        }
         best = lanes_max64(best);
         __syncthreads();
         if (lane == 0) sc->wave[wave] = best;
@@ -237,33 +280,33 @@ __device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, co
 }
 
 // ---- forward ----------------------------------------------------------------------------------------------------
-template <typename T, int THREADS, bool TOP> __global__ __launch_bounds__(THREADS) void k_logprobs(const Args a) {
-    constexpr int N = Vec16<T>::N;
+// U: vectors that a thread loads at a time
+template <typename T, int THREADS, int U, bool TOP> __global__ __launch_bounds__(THREADS) void k_logprobs(const Args a) {
     __shared__ Sums scratch[THREADS / 64];
     const long long row = blockIdx.x;
     const T* x = static_cast<const T*>(a.x) + row * a.stride;
     const RowView<T> r(x, a.vocab);
     const float c = a.scale * kLog2e;
     Sums acc{kLowest, 0.f, 0.f};
-    uint32_t most = 0;
-    const int l = r.loose(threadIdx.x);
-    if (l >= 0) {
-        const float v = to_f32(x[l]);
-        take<1>(&acc, &v, c);
-        if (TOP) most = order_of(v);
+    Vec16<T> v[U];
+    int at = threadIdx.x;
+    for (; at - (int)threadIdx.x + THREADS * U <= r.nvec; at += THREADS * U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u].load(r.vec(at + u * THREADS));
+        take<T, U>(&acc, v, c);
     }
-    for (int v = threadIdx.x; v < r.nvec; v += THREADS) {
-        Vec16<T> raw;
-        raw.load(r.vec(v));
-        float f[N];
+    if (at - (int)threadIdx.x < r.nvec) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = raw.get(i);
-        take<N>(&acc, f, c);
-        if (TOP) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) most = max(most, order_of(f[i]));
+        for (int u = 0; u < U; ++u) {
+            if (at + u * THREADS < r.nvec) v[u].load(r.vec(at + u * THREADS));
+            else set_nothing(&v[u]);
         }
+        take<T, U>(&acc, v, c);
     }
+    // the largest logit of the thread's vectors: not a number above -infinity where nothing was added up, NaN where the sum is
+    uint32_t most = 0;
+    if (TOP && (int)threadIdx.x < r.nvec) most = acc.s != acc.s ? 0xffffffffu : order_of(acc.s == 0.f ? -__builtin_inff() : acc.m);
+    if (const int l = r.loose(threadIdx.x); l >= 0) take_one(&acc, to_f32(x[l]), c);
     const Sums all = over_workgroup<THREADS>(acc, c, scratch);
     const long long target = a.targets ? a.targets[row] : a.ignore;
     const Values val = values_of(all, x, target, a.vocab, a.ignore, a.scale);
@@ -310,31 +353,20 @@ template <typename T, int THREADS, int KEEP> __global__ __launch_bounds__(THREAD
         for (int k = 0; k < KEEP; ++k) {
             const int v = threadIdx.x + k * THREADS;
             if (v < r.nvec) kept[k].load(r.vec(v));
+            else set_nothing(&kept[k]);
         }
     }
-    if (l >= 0) take<1>(&acc, &loose, c);
     if constexpr (KEEP > 0) {
-#pragma unroll
-        for (int k = 0; k < KEEP; ++k) {
-            if (threadIdx.x + k * THREADS < r.nvec) {
-                float f[N];
-#pragma unroll
-                for (int i = 0; i < N; ++i) f[i] = kept[k].get(i);
-                take<N>(&acc, f, c);
-            }
-        }
+        take<T, KEEP>(&acc, kept, c);
     } else {
         for (int v = threadIdx.x; v < r.nvec; v += THREADS) {
             kept[0].load(r.vec(v));
-            float f[N];
-#pragma unroll
-            for (int i = 0; i < N; ++i) f[i] = kept[0].get(i);
-            take<N>(&acc, f, c);
+            take<T, 1>(&acc, kept, c);
         }
     }
+    if (l >= 0) take_one(&acc, loose, c);
     const Sums all = over_workgroup<THREADS>(acc, c, scratch);
     const Values val = values_of(all, x, target, g.vocab, g.ignore, g.scale);
-    __syncthreads();                              // before dx, which may be x, is written every thread has read its target
     if (threadIdx.x == 0) {
         if (g.logprob) g.logprob[row] = val.logprob;
         if (g.entropy) g.entropy[row] = val.entropy;
@@ -347,20 +379,17 @@ template <typename T, int THREADS, int KEEP> __global__ __launch_bounds__(THREAD
     const float bad = given && !in_range ? __builtin_nanf("") : 0.f;
     const float k0 = -g.scale * inv * (wa + wb * (val.entropy - ls)) + bad, k1 = -g.scale * inv * wb * g.scale;
     const float hot = empty ? 0.f : g.scale * wa;
-    const int at = given && in_range ? (int)target : -1;
-    auto grad = [&](float v, int i) {
+    auto grad = [&](float v) {
         const float d = max_nan(v - all.m, kFar), e = exp2_fast(d * c);
-        const float p = e * (k0 + k1 * d);
-        return i == at ? p + hot : p;
+        return e * (k0 + k1 * d);
     };
-    if (l >= 0) dx[l] = from_f32<T>(grad(loose, l));
     // dx's rows need not lie as x's do
     const bool vec = ((reinterpret_cast<uintptr_t>(dx + r.head)) & 15) == 0;
     auto write = [&](const Vec16<T>& raw, int v) {
         float f[N];
         const int i0 = r.index(v);
 #pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = grad(raw.get(i), i0 + i);
+        for (int i = 0; i < N; ++i) f[i] = grad(raw.get(i));
         if (vec) {
             store_values<N>(dx + i0, f);
         } else {
@@ -368,11 +397,17 @@ template <typename T, int THREADS, int KEEP> __global__ __launch_bounds__(THREAD
             for (int i = 0; i < N; ++i) dx[i0 + i] = from_f32<T>(f[i]);
         }
     };
+    // Of the target there is more to say: its thread writes it once more, behind its vector.
+    const int at = given && in_range ? (int)target : -1;
+    const float of_target = at >= 0 ? to_f32(x[at]) : 0.f;
+    __syncthreads();                              // before dx, which may be x, is written every thread has read its target
+    if (l >= 0) dx[l] = from_f32<T>(grad(loose));
     if constexpr (KEEP > 0) {
 #pragma unroll
         for (int k = 0; k < KEEP; ++k) {
             const int v = threadIdx.x + k * THREADS;
             if (v < r.nvec) write(kept[k], v);
+            one_at_a_time();
         }
     } else {
         for (int v = threadIdx.x; v < r.nvec; v += THREADS) {
@@ -380,6 +415,8 @@ template <typename T, int THREADS, int KEEP> __global__ __launch_bounds__(THREAD
             write(kept[0], v);
         }
     }
+    const bool in_vector = at >= r.head && at < r.tail_at;
+    if (at >= 0 && (in_vector ? (at - r.head) / N % THREADS == (int)threadIdx.x : at == l)) dx[at] = from_f32<T>(grad(of_target) + hot);
 }
 
 // ---- host ----
@@ -392,14 +429,14 @@ asi_status check(const asi_logprob_desc* d) {
     if (d->rows > 0x7fffffffLL || d->vocab > (1LL << 28)) return ASI_ERR_UNSUPPORTED;
     return ASI_OK;
 }
-template <typename T, int THREADS> void forward(const Args& a, unsigned rows, hipStream_t st) {
-    if (a.top) hipLaunchKernelGGL((k_logprobs<T, THREADS, true>), dim3(rows), THREADS, 0, st, a);
-    else hipLaunchKernelGGL((k_logprobs<T, THREADS, false>), dim3(rows), THREADS, 0, st, a);
+template <typename T, int THREADS, int U> void forward(const Args& a, unsigned rows, hipStream_t st) {
+    if (a.top) hipLaunchKernelGGL((k_logprobs<T, THREADS, U, true>), dim3(rows), THREADS, 0, st, a);
+    else hipLaunchKernelGGL((k_logprobs<T, THREADS, U, false>), dim3(rows), THREADS, 0, st, a);
 }
 template <typename T> void forward(const Args& a, unsigned rows, hipStream_t st) {
     const int nvec = a.vocab / Vec16<T>::N;
-    if (nvec <= 512) forward<T, 256>(a, rows, st);
-    else forward<T, 1024>(a, rows, st);
+    if (nvec <= 1024 || rows > 512) forward<T, 256, 8>(a, rows, st);
+    else forward<T, 1024, 4>(a, rows, st);
 }
 template <typename T> void backward(const GradArgs& g, unsigned rows, hipStream_t st) {
     const int nvec = g.vocab / Vec16<T>::N;
