@@ -6,8 +6,8 @@
 //
 // Forward: a workgroup takes a row in one pass, several vectors a thread at a time; every thread keeps a running largest logit
 // and the sums relative to it.
-// Top alternatives: of the threads' largest logits each wave takes its c-th, c = ceil(top / waves); the least of those is a bound
-// that at least `top` logits reach.  Only the vectors of threads whose largest reaches it are looked at again, shared by all threads,
+// Top alternatives: each wave takes the c largest of its threads' largest logits, c = ceil(top / waves) + 1; the `top`-th of all of
+// those is a bound that at least `top` logits reach.  Only the vectors of threads whose largest reaches it are looked at again, shared by all threads,
 // and hand over the logits that reach it, a few more than wanted; of these each finds its place by counting the ones before
 // it.  Rows where too many reach the bound (many equal logits) are searched `top` times instead.
 //
@@ -85,6 +85,11 @@ template <int THREADS> __device__ __forceinline__ Sums over_workgroup(Sums a, fl
 }
 // Keeps the instructions of one vector together: interleaving several costs more registers than it saves time.
 __device__ __forceinline__ void one_at_a_time() { __builtin_amdgcn_sched_barrier(0); }
+// Has the bf16 values of a vector taken apart anew from here on, rather than kept as twice the registers
+__device__ __forceinline__ void taken_apart_anew(Vec16<float>*) {}
+__device__ __forceinline__ void taken_apart_anew(Vec16<bf16_t>* v) {
+    asm volatile("" : "+v"(v->raw.x), "+v"(v->raw.y), "+v"(v->raw.z), "+v"(v->raw.w));
+}
 // One more logit of a thread
 __device__ __forceinline__ void take_one(Sums* a, float x, float c) {
     Sums b{x > kLowest ? x : kLowest, 0.f, 0.f};
@@ -104,12 +109,12 @@ template <typename T> __device__ __forceinline__ void set_nothing(Vec16<T>* v) {
     const uint32_t w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
     v->raw = make_uint4(w, w, w, w);
 }
-// U more vectors
-template <typename T, int U> __device__ __forceinline__ void take(Sums* a, const Vec16<T>* v, float c) {
+// Vectors v[0 .. U) of which the first `have` are the thread's own or nothing; `have` is the same in all threads
+template <typename T, int U> __device__ __forceinline__ void take(Sums* a, Vec16<T>* v, int have, float c) {
     float m = a->m;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        m = fmaxf(m, largest(v[u]));
+        if (u < have) m = fmaxf(m, largest(v[u]));
         if (U > 2) one_at_a_time();
     }
     const float shift = max_nan(a->m - m, kFar), f = exp2_fast(shift * c);
@@ -118,14 +123,32 @@ template <typename T, int U> __device__ __forceinline__ void take(Sums* a, const
     a->m = m;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+        if (u < have) {
+            if (U > 4) taken_apart_anew(&v[u]);       // up to 4 vectors leave room for their values
 #pragma unroll
-        for (int i = 0; i < Vec16<T>::N; ++i) {
-            const float d = max_nan(v[u].get(i) - m, kFar), e = exp2_fast(d * c);
-            a->s += e;
-            a->w += d * e;
+            for (int i = 0; i < Vec16<T>::N; ++i) {
+                const float d = max_nan(v[u].get(i) - m, kFar), e = exp2_fast(d * c);
+                a->s += e;
+                a->w += d * e;
+            }
         }
         if (U > 2) one_at_a_time();
     }
+}
+// Vectors first, first + threads, ... of the thread, U of them; behind the row's end nothing.  Returns how many some thread has.
+template <typename T, int U> __device__ __forceinline__ int load(const RowView<T>& r, int first, int threads, Vec16<T>* v) {
+    const int base = first - (int)threadIdx.x;
+    if (base + threads * U <= r.nvec) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u].load(r.vec(first + u * threads));
+        return U;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (first + u * threads < r.nvec) v[u].load(r.vec(first + u * threads));
+        else set_nothing(&v[u]);
+    }
+    return (max(0, r.nvec - base) + threads - 1) / threads;
 }
 
 struct Values {
@@ -180,10 +203,11 @@ __device__ __forceinline__ float logit_of(unsigned long long key) {
     return o == 0xffffffffu ? __builtin_nanf("") : __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
 constexpr int kCandidates = 1024;
+constexpr int kBounds = 128;          // at least waves * (ceil(ASI_LOGPROB_MAX_TOP / waves) + 1)
 template <int THREADS> struct TopScratch {
     unsigned long long key[kCandidates];
     unsigned long long wave[THREADS / 64];
-    uint32_t bound[THREADS / 64];
+    uint32_t largest[kBounds];        // of the threads of each wave
     int who[THREADS];                 // threads whose vectors are looked at again
     int count, many;
 };
@@ -199,27 +223,44 @@ __device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, co
         out[place] = x == -__builtin_inff() && lse == lse ? x : x * a.scale - lse;     // also where lse is -infinity
         out_i[place] = (int)~(uint32_t)key;
     };
-    // This wave's c-th largest of its threads' largest, equal ones counted each.  Waves whose threads do not all have a vector
-    // bound nothing; where there is no other, everything is handed over (less than kCandidates then).
+    // Waves whose threads do not all have a vector bound nothing; where there is no other, everything is handed over (less than
+    // kCandidates then).
     const int full = min(W, r.nvec / 64);
-    uint32_t bound = full ? 0xffffffffu : 0u;
+    const int c = full ? min(64, (a.top + full - 1) / full + 1) : 0;
+    static_assert(W <= 16 && W * (ASI_LOGPROB_MAX_TOP / W + 2) <= kBounds, "room for the waves' largest");
     if (wave < full) {
         uint32_t left = most;
-        const int c = (a.top + full - 1) / full;
         for (int got = 0; got < c;) {
-            uint32_t m = left;
-#pragma unroll
-            for (int o = 32; o; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
-            bound = m;
-            got += __popcll(__ballot(left == m));
-            if (left == m) left = 0;
+            const uint32_t m = wave_max(left);
+            const unsigned long long with = __ballot(left == m);
+            if (left == m) {
+                const int at = got + __builtin_amdgcn_mbcnt_hi((uint32_t)(with >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)with, 0u));
+                if (at < c) sc->largest[wave * c + at] = m;
+                left = 0;
+            }
+            got += __popcll(with);
         }
     }
     if (threadIdx.x == 0) sc->count = sc->many = 0;
-    if (lane == 0) sc->bound[wave] = bound;
     __syncthreads();
-    bound = sc->bound[0];
-    for (int k = 1; k < W; ++k) bound = min(bound, sc->bound[k]);
+    uint32_t bound = 0;
+    if (full) {
+        // every wave finds the `top`-th of them: the one that fewer than `top` are above and at least `top` reach
+        const int n = full * c;                   // at least `top`
+        uint32_t found = 0;
+        for (int half = 0; half < n; half += 64) {
+            const uint32_t mine = half + lane < n ? sc->largest[half + lane] : 0u;
+            int above = 0, reach = 0;
+#pragma unroll 8
+            for (int k = 0; k < n; ++k) {
+                const uint32_t o = sc->largest[k];
+                above += o > mine;
+                reach += o >= mine;
+            }
+            if (half + lane < n && above < a.top && reach >= a.top) found = mine;
+        }
+        bound = wave_max(found);
+    }
     auto hand_over = [&](float x, int i) {
         if (order_of(x) >= bound) {
             const int at = atomicAdd(&sc->count, 1);
@@ -231,7 +272,7 @@ __device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, co
     __syncthreads();
     {
         const int each = (r.nvec + THREADS - 1) / THREADS, all = sc->many * each;
-#pragma unroll 4
+#pragma unroll 1
         for (int item = threadIdx.x; item < all; item += THREADS) {
             const int k = item / each, v = sc->who[k] + (item - k * each) * THREADS;
             if (v < r.nvec) {
@@ -248,6 +289,7 @@ __device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, co
         for (int i = threadIdx.x; i < n; i += THREADS) {
             const unsigned long long key = sc->key[i];
             int before = 0;
+#pragma unroll 8
             for (int k = 0; k < n; ++k) before += sc->key[k] > key;
             if (before < a.top) write(before, key);
         }
@@ -261,7 +303,7 @@ __device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, co
             if (key < last && key > best) best = key;
         };
         if (const int l = r.loose(threadIdx.x); l >= 0) look(to_f32(r.x[l]), l);
-#pragma unroll 4
+#pragma unroll 1
         for (int v = threadIdx.x; v < r.nvec; v += THREADS) {
             Vec16<T> raw;
             raw.load(r.vec(v));
@@ -289,19 +331,9 @@ template <typename T, int THREADS, int U, bool TOP> __global__ __launch_bounds__
     const float c = a.scale * kLog2e;
     Sums acc{kLowest, 0.f, 0.f};
     Vec16<T> v[U];
-    int at = threadIdx.x;
-    for (; at - (int)threadIdx.x + THREADS * U <= r.nvec; at += THREADS * U) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) v[u].load(r.vec(at + u * THREADS));
-        take<T, U>(&acc, v, c);
-    }
-    if (at - (int)threadIdx.x < r.nvec) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (at + u * THREADS < r.nvec) v[u].load(r.vec(at + u * THREADS));
-            else set_nothing(&v[u]);
-        }
-        take<T, U>(&acc, v, c);
+    for (int base = 0; base < r.nvec; base += THREADS * U) {
+        const int have = load<T, U>(r, base + threadIdx.x, THREADS, v);
+        take<T, U>(&acc, v, have, c);
     }
     // the largest logit of the thread's vectors: not a number above -infinity where nothing was added up, NaN where the sum is
     uint32_t most = 0;
@@ -334,8 +366,8 @@ struct GradArgs {
     int vocab;
     float scale;
 };
-// KEEP: vectors that a thread keeps in registers, 0: the row is read again
-template <typename T, int THREADS, int KEEP> __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const GradArgs g) {
+// KEEP: vectors that a thread keeps in registers.  REST: the row is longer, its rest is read again.
+template <typename T, int THREADS, int KEEP, bool REST> __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const GradArgs g) {
     constexpr int N = Vec16<T>::N;
     __shared__ Sums scratch[THREADS / 64];
     const long long row = blockIdx.x;
@@ -347,21 +379,13 @@ template <typename T, int THREADS, int KEEP> __global__ __launch_bounds__(THREAD
     const float loose = l >= 0 ? to_f32(x[l]) : 0.f;
     const long long target = g.targets ? g.targets[row] : g.ignore;
     Sums acc{kLowest, 0.f, 0.f};
-    Vec16<T> kept[KEEP ? KEEP : 1];
-    if constexpr (KEEP > 0) {
-#pragma unroll
-        for (int k = 0; k < KEEP; ++k) {
-            const int v = threadIdx.x + k * THREADS;
-            if (v < r.nvec) kept[k].load(r.vec(v));
-            else set_nothing(&kept[k]);
-        }
-    }
-    if constexpr (KEEP > 0) {
-        take<T, KEEP>(&acc, kept, c);
-    } else {
-        for (int v = threadIdx.x; v < r.nvec; v += THREADS) {
-            kept[0].load(r.vec(v));
-            take<T, 1>(&acc, kept, c);
+    Vec16<T> kept[KEEP], again[2];
+    const int have = load<T, KEEP>(r, threadIdx.x, THREADS, kept);
+    take<T, KEEP>(&acc, kept, have, c);
+    if constexpr (REST) {
+        for (int base = KEEP * THREADS; base < r.nvec; base += 2 * THREADS) {
+            const int more = load<T, 2>(r, base + threadIdx.x, THREADS, again);
+            take<T, 2>(&acc, again, more, c);
         }
     }
     if (l >= 0) take_one(&acc, loose, c);
@@ -402,17 +426,18 @@ template <typename T, int THREADS, int KEEP> __global__ __launch_bounds__(THREAD
     const float of_target = at >= 0 ? to_f32(x[at]) : 0.f;
     __syncthreads();                              // before dx, which may be x, is written every thread has read its target
     if (l >= 0) dx[l] = from_f32<T>(grad(loose));
-    if constexpr (KEEP > 0) {
 #pragma unroll
-        for (int k = 0; k < KEEP; ++k) {
-            const int v = threadIdx.x + k * THREADS;
-            if (v < r.nvec) write(kept[k], v);
-            one_at_a_time();
-        }
-    } else {
-        for (int v = threadIdx.x; v < r.nvec; v += THREADS) {
-            kept[0].load(r.vec(v));
-            write(kept[0], v);
+    for (int k = 0; k < KEEP; ++k) {
+        const int v = threadIdx.x + k * THREADS;
+        if (v < r.nvec) write(kept[k], v);
+        one_at_a_time();
+    }
+    if constexpr (REST) {
+        for (int base = KEEP * THREADS; base < r.nvec; base += 2 * THREADS) {
+            load<T, 2>(r, base + threadIdx.x, THREADS, again);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (const int v = base + k * THREADS + (int)threadIdx.x; v < r.nvec) write(again[k], v);
         }
     }
     const bool in_vector = at >= r.head && at < r.tail_at;
@@ -435,18 +460,19 @@ template <typename T, int THREADS, int U> void forward(const Args& a, unsigned r
 }
 template <typename T> void forward(const Args& a, unsigned rows, hipStream_t st) {
     const int nvec = a.vocab / Vec16<T>::N;
-    if (nvec <= 1024 || rows > 512) forward<T, 256, 8>(a, rows, st);
+    if (nvec <= 2048) forward<T, 256, 4>(a, rows, st);
+    else if (rows > 256) forward<T, 512, 4>(a, rows, st);
     else forward<T, 1024, 4>(a, rows, st);
 }
 template <typename T> void backward(const GradArgs& g, unsigned rows, hipStream_t st) {
     const int nvec = g.vocab / Vec16<T>::N;
-#define ASI_GRAD(THREADS, KEEP) hipLaunchKernelGGL((k_logprobs_grad<T, THREADS, KEEP>), dim3(rows), THREADS, 0, st, g)
-    if (nvec <= 256) ASI_GRAD(256, 1);
-    else if (nvec <= 1024) ASI_GRAD(256, 4);
-    else if (nvec <= 4096) ASI_GRAD(512, 8);
-    else if (nvec <= 8192) ASI_GRAD(1024, 8);
-    else if (nvec <= 16384) ASI_GRAD(1024, 16);
-    else ASI_GRAD(1024, 0);
+#define ASI_GRAD(THREADS, KEEP, REST) hipLaunchKernelGGL((k_logprobs_grad<T, THREADS, KEEP, REST>), dim3(rows), THREADS, 0, st, g)
+    if (nvec <= 256) ASI_GRAD(256, 1, false);
+    else if (nvec <= 1024) ASI_GRAD(256, 4, false);
+    else if (nvec <= 4096) ASI_GRAD(512, 8, false);
+    else if (nvec <= 8192) ASI_GRAD(512, 16, false);
+    else if (nvec <= 12288) ASI_GRAD(512, 24, false);
+    else ASI_GRAD(1024, 24, true);
 #undef ASI_GRAD
 }
 
