@@ -460,14 +460,15 @@ template <typename T, int THREADS, int U> void forward(const Args& a, unsigned r
 }
 template <typename T> void forward(const Args& a, unsigned rows, hipStream_t st) {
     const int nvec = a.vocab / Vec16<T>::N;
-    if (nvec <= 2048) forward<T, 256, 4>(a, rows, st);
+    if (nvec <= 256) forward<T, 64, 4>(a, rows, st);
+    else if (nvec <= 2048) forward<T, 256, 4>(a, rows, st);
     else if (rows > 256) forward<T, 512, 4>(a, rows, st);
     else forward<T, 1024, 4>(a, rows, st);
 }
 template <typename T> void backward(const GradArgs& g, unsigned rows, hipStream_t st) {
     const int nvec = g.vocab / Vec16<T>::N;
 #define ASI_GRAD(THREADS, KEEP, REST) hipLaunchKernelGGL((k_logprobs_grad<T, THREADS, KEEP, REST>), dim3(rows), THREADS, 0, st, g)
-    if (nvec <= 256) ASI_GRAD(256, 1, false);
+    if (nvec <= 256) ASI_GRAD(64, 4, false);
     else if (nvec <= 1024) ASI_GRAD(256, 4, false);
     else if (nvec <= 4096) ASI_GRAD(512, 8, false);
     else if (nvec <= 8192) ASI_GRAD(512, 16, false);

@@ -1,11 +1,12 @@
 // Norms of queries and keys for each head with the position rotation in the same pass, and the backward pass
 // (include/asi_lm.h).
 //
-// A head is read once, into registers, as pairs of 16-byte vectors that are turned into each other: vector i of the first half
-// of the rotated part with vector i of its second half, or, where neighbours are turned into each other (and behind the
-// rotated part), two vectors in a row.  A lane holds one such pair, a group of 2^k neighbouring lanes a head, so that the
-// partners of a rotation are in one lane and only the sum of squares crosses lanes.  Heads whose length or addresses do not
-// allow vectors take the kernel that goes element by element, a wave a head.
+// A head is read once, into registers, as pairs of 16-byte vectors: vector i of the first half of the rotated part with vector i of
+// its second half, which are turned into each other; of what is not turned, and where neighbours are turned into each other, the
+// vectors of one half with those of the other.  A lane holds one such pair, a group of 2^k neighbouring lanes a head, so
+// that the partners of a rotation are in one lane, neighbouring lanes load and store neighbouring vectors, and only the sum of
+// squares crosses lanes.  Heads whose length or addresses do not allow vectors take the kernel that goes element by element, a
+// wave a head.
 //
 // Backward: with u = x r, n = u gain, w = gain dn:  dn = rotation of dy by the negative angle,
 //     dx = r (w - u mean(w u)),   dgain = sum dn u.
@@ -23,6 +24,20 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// n / d of 0 <= n < 2^31 by a product: m = floor(2^(31 + l) / d) + 1 with 2^l >= d is off by less than n can show
+struct Divider {
+    uint64_t m;
+    int shift, d;
+    void set(int divisor) {
+        d = divisor;
+        int l = 0;
+        while ((1LL << l) < d) ++l;
+        shift = 31 + l;
+        m = (1ull << shift) / (uint64_t)d + 1;
+    }
+    __device__ __forceinline__ int quotient(int n) const { return (int)((uint64_t)(uint32_t)n * m >> shift); }
+};
+
 struct Side {                      // queries or keys
     const void* x;
     const void* gain;
@@ -30,6 +45,7 @@ struct Side {                      // queries or keys
     const void* dy;                // backward: gradient of the output
     long long xs[3], ys[3], ds[3]; // strides of x, of the output (or dy), of dx
     int heads;
+    Divider by_heads;              // backward
 };
 struct Args {
     Side side[2];
@@ -39,6 +55,8 @@ struct Args {
     float* part;                   // backward: [side][workgroup][head_dim]
     long long rows;                // batch * tokens
     long long position_stride, max_position;
+    Divider by_tokens, by_parts;   // parts: what the heads of a token are taken in, forward
+    int q_parts, parts;
     int tokens, head_dim, rot_dim, interleaved;
     float eps, inv_dim;
 };
@@ -50,18 +68,23 @@ __device__ __forceinline__ long long position_of(const Args& a, int b, int t) {
     return p >= 0 && p < a.max_position ? p : -1;
 }
 
-// The two vectors of a lane's pair `slot`: their first elements, and where their angles are.
+// The two vectors of a lane's pair `slot`: their first elements, and whether they are turned.
 struct Pair {
     int ia, ib;
-    int angle;                     // index of the first angle, -1: not turned
+    bool ta, tb;
 };
-template <typename T> __device__ __forceinline__ Pair pair_of(int slot, int rot, bool inter) {
+template <typename T, bool INTER> __device__ __forceinline__ Pair pair_of(int slot, int dim, int rot) {
     constexpr int N = Vec16<T>::N;
-    const int turned = rot / (2 * N);          // pairs of vectors in the rotated part
-    if (slot >= turned || inter) return {2 * slot * N, (2 * slot + 1) * N, slot < turned ? slot * N : -1};
-    return {slot * N, rot / 2 + slot * N, slot * N};
+    if (INTER) {
+        const int ia = slot * N, ib = dim / 2 + slot * N;
+        return {ia, ib, ia < rot, ib < rot};
+    }
+    const int behind = slot * N - rot / 2;        // elements behind the rotated part's first half
+    if (behind < 0) return {slot * N, rot / 2 + slot * N, true, true};
+    return {rot + behind, rot + (dim - rot) / 2 + behind, false, false};
 }
-// (f, g) turned by the lane's angles; `sign` -1 turns back.  INTER: neighbours within the vectors are partners.
+// (f, g) turned by the lane's angles; `sign` -1 turns back.  INTER: neighbours within the vectors are partners, the first half of the
+// angles belongs to f.
 template <typename T, bool INTER> __device__ __forceinline__ void turn(float* f, float* g, const float* c, const float* s, float sign) {
     constexpr int N = Vec16<T>::N;
     if (INTER) {
@@ -81,77 +104,100 @@ template <typename T, bool INTER> __device__ __forceinline__ void turn(float* f,
         }
     }
 }
-template <typename T> __device__ __forceinline__ void load_angles(const Args& a, const Pair& p, long long pos, float* c, float* s) {
-    constexpr int N = Vec16<T>::N;
-    const int half = a.rot_dim / 2;
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-        float4 vc = make_float4(1.f, 1.f, 1.f, 1.f), vs = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (p.angle >= 0) {
-            if (pos < 0) {
-                const float q = __builtin_nanf("");
-                vc = make_float4(q, q, q, q);
-            } else {
-                vc = *reinterpret_cast<const float4*>(a.cos + pos * half + p.angle + i);
-                vs = *reinterpret_cast<const float4*>(a.sin + pos * half + p.angle + i);
-            }
+template <int M> __device__ __forceinline__ void load_angles(const Args& a, long long at, bool in_range, bool turned, float* c, float* s) {
+    if (turned && in_range) {
+        if constexpr (M % 4 == 0) {
+            load_values<M>(a.cos + at, c);
+            load_values<M>(a.sin + at, s);
+        } else {
+            const float2 vc = *reinterpret_cast<const float2*>(a.cos + at), vs = *reinterpret_cast<const float2*>(a.sin + at);
+            c[0] = vc.x; c[1] = vc.y; s[0] = vs.x; s[1] = vs.y;
         }
-        c[i] = vc.x; c[i + 1] = vc.y; c[i + 2] = vc.z; c[i + 3] = vc.w;
-        s[i] = vs.x; s[i + 1] = vs.y; s[i + 2] = vs.z; s[i + 3] = vs.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            c[i] = turned ? __builtin_nanf("") : 1.f;
+            s[i] = 0.f;
+        }
     }
 }
+// cos and sin of a lane's pair, 1 and 0 where it is not turned, NaN where there is no such position
+template <typename T, bool INTER> __device__ __forceinline__ void load_angles(const Args& a, const Pair& p, long long pos, float* c, float* s) {
+    constexpr int N = Vec16<T>::N;
+    const long long row = pos * (a.rot_dim / 2);
+    if (INTER) {
+        load_angles<N / 2>(a, row + p.ia / 2, pos >= 0, p.ta, c, s);
+        load_angles<N / 2>(a, row + p.ib / 2, pos >= 0, p.tb, c + N / 2, s + N / 2);
+    } else {
+        load_angles<N>(a, row + p.ia, pos >= 0, p.ta, c, s);
+    }
+}
+// gains: N values, their address a multiple of 16 bytes or of the N values' size
 template <typename T, typename G> __device__ __forceinline__ void load_gain(const void* gain, int at, float* w) {
     constexpr int N = Vec16<T>::N;
+    if (gain) {
+        load_values<N>(static_cast<const G*>(gain) + at, w);
+    } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = gain ? to_f32(static_cast<const G*>(gain)[at + i]) : 1.f;
+        for (int i = 0; i < N; ++i) w[i] = 1.f;
+    }
 }
 
-// One head a group of GROUP lanes, all heads of all tokens in a row of groups.
-template <typename T, typename G, int GROUP, bool INTER> __global__ __launch_bounds__(kThreads) void k_rotate(const Args a) {
+// Forward: a group of GROUP lanes takes HEADS neighbouring heads of a token, which share its angles and the gains.
+template <typename T, typename G, int GROUP, int HEADS, bool INTER> __global__ __launch_bounds__(kThreads) void k_rotate(const Args a) {
     constexpr int N = Vec16<T>::N;
     const int lane = threadIdx.x & (GROUP - 1);
     const long long id = (long long)blockIdx.x * (kThreads / GROUP) + threadIdx.x / GROUP;
-    const int heads = a.side[0].heads + a.side[1].heads;
-    const bool have = id < a.rows * heads;
-    const unsigned row = have ? (unsigned)id / (unsigned)heads : 0u;
-    int h = have ? (int)((unsigned)id - row * (unsigned)heads) : 0;
-    const int b = (int)(row / (unsigned)a.tokens), t = (int)(row - (unsigned)b * (unsigned)a.tokens);
-    const bool is_k = h >= a.side[0].heads;
-    if (is_k) h -= a.side[0].heads;
+    const bool have = id < a.rows * a.parts;
+    const int row = have ? a.by_parts.quotient((int)id) : 0;
+    int part = have ? (int)id - row * a.parts : 0;
+    const int b = a.by_tokens.quotient(row), t = row - b * a.tokens;
+    const bool is_k = part >= a.q_parts;
+    if (is_k) part -= a.q_parts;
     const Side& s = a.side[is_k];
-    const Pair p = pair_of<T>(lane, a.rot_dim, INTER);
-    const bool mine = have && p.ib < a.head_dim;
-    const T* x = static_cast<const T*>(s.x) + b * s.xs[0] + t * s.xs[1] + h * s.xs[2];
-    Vec16<T> va{}, vb{};
-    if (mine) { va.load(x + p.ia); vb.load(x + p.ib); }
-    float f[N], g[N], sum = 0.f;
+    const Pair p = pair_of<T, INTER>(lane, a.head_dim, a.rot_dim);
+    const bool mine = have && lane * 2 * N < a.head_dim;
+    const int h0 = part * HEADS;
+    const T* x = static_cast<const T*>(s.x) + b * s.xs[0] + t * s.xs[1] + h0 * s.xs[2];
+    Vec16<T> va[HEADS], vb[HEADS];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        f[i] = va.get(i); g[i] = vb.get(i);
-        sum += f[i] * f[i] + g[i] * g[i];
+    for (int h = 0; h < HEADS; ++h) {
+        va[h].raw = vb[h].raw = make_uint4(0, 0, 0, 0);
+        if (mine && h0 + h < s.heads) { va[h].load(x + h * s.xs[2] + p.ia); vb[h].load(x + h * s.xs[2] + p.ib); }
     }
-    sum = lanes_sum<GROUP>(sum);
-    if (!mine) return;
-    const float r = 1.f / sqrtf(sum * a.inv_dim + a.eps);
     float wa[N], wb[N], c[N], sn[N];
-    load_gain<T, G>(s.gain, p.ia, wa);
-    load_gain<T, G>(s.gain, p.ib, wb);
-    load_angles<T>(a, p, position_of(a, b, t), c, sn);
+    if (mine) {
+        load_gain<T, G>(s.gain, p.ia, wa);
+        load_gain<T, G>(s.gain, p.ib, wb);
+        load_angles<T, INTER>(a, p, position_of(a, b, t), c, sn);
+    }
+    T* y = static_cast<T*>(s.y) + b * s.ys[0] + t * s.ys[1] + h0 * s.ys[2];
 #pragma unroll
-    for (int i = 0; i < N; ++i) { f[i] *= r * wa[i]; g[i] *= r * wb[i]; }
-    if (p.angle >= 0) turn<T, INTER>(f, g, c, sn, 1.f);
-    T* y = static_cast<T*>(s.y) + b * s.ys[0] + t * s.ys[1] + h * s.ys[2];
-    va.set(f); va.store(y + p.ia);
-    vb.set(g); vb.store(y + p.ib);
+    for (int h = 0; h < HEADS; ++h) {
+        float f[N], g[N], sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            f[i] = va[h].get(i); g[i] = vb[h].get(i);
+            sum += f[i] * f[i] + g[i] * g[i];
+        }
+        sum = lanes_sum<GROUP>(sum);
+        if (!mine || h0 + h >= s.heads) continue;
+        const float r = 1.f / sqrtf(sum * a.inv_dim + a.eps);
+#pragma unroll
+        for (int i = 0; i < N; ++i) { f[i] *= r * wa[i]; g[i] *= r * wb[i]; }
+        turn<T, INTER>(f, g, c, sn, 1.f);
+        store_values<N>(y + h * s.ys[2] + p.ia, f);
+        store_values<N>(y + h * s.ys[2] + p.ib, g);
+    }
 }
 
 // Backward: the groups of the grid take the heads of one side after another, a grid apart.
-template <typename T, typename G, int GROUP, bool INTER> __global__ __launch_bounds__(kThreads) void k_rotate_grad(const Args a) {
+template <typename T, typename G, int GROUP, bool INTER> __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 3) void k_rotate_grad(const Args a) {
     constexpr int N = Vec16<T>::N;
     constexpr int GROUPS = kThreads / GROUP;
     const int lane = threadIdx.x & (GROUP - 1), group = threadIdx.x / GROUP;
-    const Pair p = pair_of<T>(lane, a.rot_dim, INTER);
-    const bool column = p.ib < a.head_dim;
+    const Pair p = pair_of<T, INTER>(lane, a.head_dim, a.rot_dim);
+    const bool column = lane * 2 * N < a.head_dim;
     __shared__ float sums[kThreads / 64][2 * N * GROUP];
     for (int side = 0; side < 2; ++side) {
         const Side& s = a.side[side];
@@ -165,19 +211,17 @@ template <typename T, typename G, int GROUP, bool INTER> __global__ __launch_bou
         for (long long id0 = (long long)blockIdx.x * GROUPS; id0 < n; id0 += (long long)gridDim.x * GROUPS) {
             const long long id = id0 + group;
             const bool have = id < n, mine = have && column;
-            const unsigned row = have ? (unsigned)id / (unsigned)s.heads : 0u;
-            const int h = have ? (int)((unsigned)id - row * (unsigned)s.heads) : 0;
-            const int b = (int)(row / (unsigned)a.tokens), t = (int)(row - (unsigned)b * (unsigned)a.tokens);
-            const long long xo = b * s.xs[0] + t * s.xs[1] + h * s.xs[2], yo = b * s.ys[0] + t * s.ys[1] + h * s.ys[2];
-            const long long po = b * s.ds[0] + t * s.ds[1] + h * s.ds[2];
+            const int row = have ? s.by_heads.quotient((int)id) : 0;
+            const int h = have ? (int)id - row * s.heads : 0;
+            const int b = a.by_tokens.quotient(row), t = row - b * a.tokens;
             Vec16<T> va{}, vb{}, da{}, db{};
             float c[N], sn[N];
             if (mine) {
-                const T* x = static_cast<const T*>(s.x) + xo;
-                const T* dy = static_cast<const T*>(s.dy) + yo;
+                const T* x = static_cast<const T*>(s.x) + b * s.xs[0] + t * s.xs[1] + h * s.xs[2];
+                const T* dy = static_cast<const T*>(s.dy) + b * s.ys[0] + t * s.ys[1] + h * s.ys[2];
                 va.load(x + p.ia); vb.load(x + p.ib);
                 da.load(dy + p.ia); db.load(dy + p.ib);
-                load_angles<T>(a, p, position_of(a, b, t), c, sn);
+                load_angles<T, INTER>(a, p, position_of(a, b, t), c, sn);
             }
             float f[N], g[N], df[N], dg[N], sq = 0.f, dot = 0.f;
 #pragma unroll
@@ -186,7 +230,7 @@ template <typename T, typename G, int GROUP, bool INTER> __global__ __launch_bou
                 df[i] = da.get(i); dg[i] = db.get(i);
                 sq += f[i] * f[i] + g[i] * g[i];
             }
-            if (mine && p.angle >= 0) turn<T, INTER>(df, dg, c, sn, -1.f);
+            if (mine) turn<T, INTER>(df, dg, c, sn, -1.f);
 #pragma unroll
             for (int i = 0; i < N; ++i) dot += wa[i] * df[i] * f[i] + wb[i] * dg[i] * g[i];
             sq = lanes_sum<GROUP>(sq);
@@ -201,9 +245,9 @@ template <typename T, typename G, int GROUP, bool INTER> __global__ __launch_bou
                     f[i] = r * (wa[i] * df[i] - f[i] * k);
                     g[i] = r * (wb[i] * dg[i] - g[i] * k);
                 }
-                T* dx = static_cast<T*>(s.y) + po;
-                va.set(f); va.store(dx + p.ia);
-                vb.set(g); vb.store(dx + p.ib);
+                T* dx = static_cast<T*>(s.y) + b * s.ds[0] + t * s.ds[1] + h * s.ds[2];
+                store_values<N>(dx + p.ia, f);
+                store_values<N>(dx + p.ib, g);
             }
         }
         if (!a.part) continue;
@@ -336,22 +380,27 @@ template <typename T, typename G> __global__ __launch_bounds__(64) void k_rotate
     }
 }
 
-// dgain[side][d] = sum over workgroups of part[side][.][d]: a workgroup takes 64 columns of a side, its 16 waves a sixteenth of
-// the parts each.  A side without heads has no parts: its gradient is zero.
-__global__ __launch_bounds__(1024) void k_gain_sum(const float* part, int parts, int q_parts, int k_parts, int dim, float* dq, float* dk) {
-    const int side = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
+// dgain[side][d] = sum over workgroups of part[side][.][d]: a workgroup takes 16 columns of a side, a sixty-fourth of the parts a
+// thread, several of them on their way at a time.  A side without heads has no parts: its gradient is zero.
+constexpr int kSumColumns = 16, kSumShares = 64;
+__global__ __launch_bounds__(kSumColumns * kSumShares) void k_gain_sum(const float* part, int parts, int q_parts, int k_parts, int dim, float* dq, float* dk) {
+    const int side = blockIdx.y, column = threadIdx.x % kSumColumns, share = threadIdx.x / kSumColumns, d = blockIdx.x * kSumColumns + column;
     float* out = side ? dk : dq;
     if (!out) return;
-    __shared__ float sums[16][64];
+    __shared__ float sums[kSumShares][kSumColumns + 1];
     float v = 0.f;
-    if (d < dim)
-        for (int w = wave; w < (side ? k_parts : q_parts); w += 16) v += part[((long long)side * parts + w) * dim + d];
-    sums[wave][lane] = v;
-    __syncthreads();
-    if (wave == 0 && d < dim) {
-        for (int w = 1; w < 16; ++w) v += sums[w][lane];
-        out[d] = v;
+    const int n = side ? k_parts : q_parts;
+    if (d < dim) {
+#pragma unroll 8
+        for (int w = share; w < n; w += kSumShares) v += part[((long long)side * parts + w) * dim + d];
     }
+    sums[share][column] = v;
+    __syncthreads();
+    for (int half = kSumShares / 2; half; half /= 2) {
+        if (share < half) sums[share][column] += sums[share + half][column];
+        __syncthreads();
+    }
+    if (share == 0 && d < dim) out[d] = sums[0][column];
 }
 
 // ---- host ----
@@ -376,7 +425,7 @@ int group_of(const asi_qk_desc* d, const Args& a, bool back) {
     if (d->rot_dim && (!aligned(a.cos, 16) || !aligned(a.sin, 16))) return 0;
     for (const Side& s : a.side) {
         if (!s.heads) continue;
-        if (!aligned(s.x, 16) || !aligned(s.y, 16) || (back && !aligned(s.dy, 16))) return 0;
+        if (!aligned(s.x, 16) || !aligned(s.y, 16) || !aligned(s.gain, 16) || (back && !aligned(s.dy, 16))) return 0;
         for (int k = 0; k < 3; ++k)
             if (s.xs[k] % n || s.ys[k] % n || (back && s.ds[k] % n)) return 0;
     }
@@ -401,6 +450,14 @@ void fill(const asi_qk_desc* d, Args* a) {
     a->max_position = d->max_position;
     a->eps = d->eps;
     a->inv_dim = 1.f / (float)d->head_dim;
+    a->by_tokens.set(std::max(1, a->tokens));
+    for (Side& s : a->side) s.by_heads.set(std::max(1, s.heads));
+}
+// Forward: how the heads of a token are taken
+void set_parts(Args* a, int heads) {
+    a->q_parts = (a->side[0].heads + heads - 1) / heads;
+    a->parts = a->q_parts + (a->side[1].heads + heads - 1) / heads;
+    a->by_parts.set(std::max(1, a->parts));
 }
 bool fits(const asi_qk_desc* d, const Args& a, bool back) {
     const size_t es = dtype_size(d->dtype);
@@ -412,23 +469,34 @@ bool fits(const asi_qk_desc* d, const Args& a, bool back) {
     if (d->rot_dim && (!a.cos || !a.sin || !aligned(a.cos, 4) || !aligned(a.sin, 4))) return false;
     return aligned(a.positions, 8);
 }
-// Workgroups of the backward pass: a function of the descriptor alone, whatever the pointers allow
-int grad_blocks(const asi_qk_desc* d) {
+// Workgroups of the backward pass: as many as are resident at once, which is what registers leave room for (bf16, 16384 tokens of
+// 18 heads of 128: 768 51 us, 1024, which the compiler has to spill for, 54; fp32, half of that: 1024 46 us, 768 48), fewer where
+// that gives every group of lanes a head.  Scratch is planned for a head a group of 64 lanes.
+int most_blocks(const asi_qk_desc* d) {
     const long long heads = d->batch * d->tokens * std::max(d->q_heads, d->k_heads);
-    return (int)std::max(1LL, std::min(1024LL, (heads + 15) / 16));
+    return (int)std::max(1LL, std::min(d->dtype == ASI_F32 ? 1024LL : 768LL, (heads + 3) / 4));
+}
+int grad_blocks(const asi_qk_desc* d, int group) {
+    if (!group) return most_blocks(d);
+    const long long heads = d->batch * d->tokens * std::max(d->q_heads, d->k_heads), groups = kThreads / group;
+    return (int)std::max(1LL, std::min<long long>(most_blocks(d), (heads + groups - 1) / groups));
 }
 
+template <typename T, typename G, int GROUP, int HEADS> void forward(Args a, hipStream_t st) {
+    set_parts(&a, HEADS);
+    const long long n = a.rows * a.parts;
+    const dim3 grid((unsigned)((n + kThreads / GROUP - 1) / (kThreads / GROUP)));
+    if (a.interleaved) hipLaunchKernelGGL((k_rotate<T, G, GROUP, HEADS, true>), grid, kThreads, 0, st, a);
+    else hipLaunchKernelGGL((k_rotate<T, G, GROUP, HEADS, false>), grid, kThreads, 0, st, a);
+}
 template <typename T, typename G, int GROUP> void go(const Args& a, bool back, int blocks, hipStream_t st) {
-    if (!back) {
-        const long long n = a.rows * (a.side[0].heads + a.side[1].heads);
-        const dim3 grid((unsigned)((n + kThreads / GROUP - 1) / (kThreads / GROUP)));
-        if (a.interleaved) hipLaunchKernelGGL((k_rotate<T, G, GROUP, true>), grid, kThreads, 0, st, a);
-        else hipLaunchKernelGGL((k_rotate<T, G, GROUP, false>), grid, kThreads, 0, st, a);
-    } else if (a.interleaved) {
-        hipLaunchKernelGGL((k_rotate_grad<T, G, GROUP, true>), dim3(blocks), kThreads, 0, st, a);
-    } else {
-        hipLaunchKernelGGL((k_rotate_grad<T, G, GROUP, false>), dim3(blocks), kThreads, 0, st, a);
-    }
+    // two heads a lane share the angles and gains (8 x 512 tokens of 36 heads of 64 9.9 us, one head 11.0, four 10.8); where one
+    // head a lane does not fill the chip the shorter chain counts (8 tokens of these heads 3.4 us, two 3.8)
+    const long long waves = a.rows * (a.side[0].heads + a.side[1].heads) * GROUP / 64;
+    if (!back && waves > 4096) forward<T, G, GROUP, 2>(a, st);
+    else if (!back) forward<T, G, GROUP, 1>(a, st);
+    else if (a.interleaved) hipLaunchKernelGGL((k_rotate_grad<T, G, GROUP, true>), dim3(blocks), kThreads, 0, st, a);
+    else hipLaunchKernelGGL((k_rotate_grad<T, G, GROUP, false>), dim3(blocks), kThreads, 0, st, a);
 }
 template <typename T, typename G> void go(int group, const Args& a, bool back, int blocks, hipStream_t st) {
     switch (group) {
@@ -447,8 +515,7 @@ template <typename T, typename G> void go(int group, const Args& a, bool back, i
             }
     }
 }
-void go(const asi_qk_desc* d, const Args& a, bool back, int blocks, hipStream_t st) {
-    const int group = group_of(d, a, back);
+void go(const asi_qk_desc* d, const Args& a, int group, bool back, int blocks, hipStream_t st) {
     if (d->dtype == ASI_F32) {
         if (d->gain_dtype == ASI_F32) go<float, float>(group, a, back, blocks, st);
         else go<float, bf16_t>(group, a, back, blocks, st);
@@ -476,13 +543,13 @@ asi_status asi_qk_norm_rotate(const asi_qk_desc* desc, const void* q, const void
     a.side[1].x = k; a.side[1].gain = k_gain; a.side[1].y = k_out;
     a.positions = positions; a.cos = cos; a.sin = sin;
     if (!fits(desc, a, false)) return ASI_ERR_INVALID_ARG;
-    go(desc, a, false, 0, static_cast<hipStream_t>(stream));
+    go(desc, a, group_of(desc, a, false), false, 0, static_cast<hipStream_t>(stream));
     return launched();
 }
 
 size_t asi_qk_norm_rotate_grad_workspace_bytes(const asi_qk_desc* desc) {
     if (check(desc) != ASI_OK || nothing(desc)) return 0;
-    return round256((size_t)2 * grad_blocks(desc) * desc->head_dim * sizeof(float));
+    return round256((size_t)2 * most_blocks(desc) * desc->head_dim * sizeof(float));
 }
 
 asi_status asi_qk_norm_rotate_grad(const asi_qk_desc* desc, const void* q, const void* k, const void* q_gain,
@@ -499,20 +566,20 @@ asi_status asi_qk_norm_rotate_grad(const asi_qk_desc* desc, const void* q, const
     a.positions = positions; a.cos = cos; a.sin = sin;
     const bool empty = nothing(desc);
     if (!empty && !fits(desc, a, true)) return ASI_ERR_INVALID_ARG;
-    if (!dq_gain && !dk_gain) {
-        if (!empty) go(desc, a, true, grad_blocks(desc), st);
-        return launched();
-    }
-    // a side without heads, or a call without tokens, has gains whose gradient is the sum of nothing
-    const int blocks = empty ? 0 : grad_blocks(desc);
+    const int group = empty ? 0 : group_of(desc, a, true);
+    const int blocks = empty ? 0 : grad_blocks(desc, group);
+    const bool gains = dq_gain || dk_gain;
     if (!empty) {
-        const size_t need = asi_qk_norm_rotate_grad_workspace_bytes(desc);
-        if (!ws || !aligned(ws, 256) || ws_bytes < need) return ASI_ERR_WORKSPACE;
-        a.part = static_cast<float*>(ws);
-        go(desc, a, true, blocks, st);
+        if (gains) {
+            if (!ws || !aligned(ws, 256) || ws_bytes < asi_qk_norm_rotate_grad_workspace_bytes(desc)) return ASI_ERR_WORKSPACE;
+            a.part = static_cast<float*>(ws);
+        }
+        go(desc, a, group, true, blocks, st);
     }
-    const dim3 grid((unsigned)((desc->head_dim + 63) / 64), 2);
-    hipLaunchKernelGGL(k_gain_sum, grid, 1024, 0, st, a.part, blocks, desc->q_heads ? blocks : 0, desc->k_heads ? blocks : 0, desc->head_dim, dq_gain, dk_gain);
+    if (!gains) return empty ? ASI_OK : launched();
+    // also of a side without heads, or a call without tokens: the sum of nothing
+    const dim3 grid((unsigned)((desc->head_dim + kSumColumns - 1) / kSumColumns), 2);
+    hipLaunchKernelGGL(k_gain_sum, grid, kSumColumns * kSumShares, 0, st, a.part, blocks, desc->q_heads ? blocks : 0, desc->k_heads ? blocks : 0, desc->head_dim, dq_gain, dk_gain);
     return launched();
 }
 
