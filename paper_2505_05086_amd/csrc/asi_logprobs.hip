@@ -11,6 +11,9 @@
 // and hand over the logits that reach it, a few more than wanted; of these each finds its place by counting the ones before
 // it.  Rows where too many reach the bound (many equal logits) are searched `top` times instead.
 //
+// Few long rows are cut into parts, a workgroup each, which leave their sums and alternatives in scratch for a second kernel to join in
+// the order of the parts.
+//
 // Gradient: a row is kept in registers between the pass that sums and the one that writes, so that it is read once and written once;
 // rows too long for that are read again.
 #include <hip/hip_runtime.h>
@@ -179,6 +182,10 @@ struct Args {
     long long stride, ignore;
     int vocab, top;
     float scale;
+    // rows in parts of `part` logits: [row][part] sums, [row][part][top] keys of alternatives, 0 where there are fewer
+    int parts, part;
+    Sums* sums;
+    unsigned long long* keys;
 };
 
 // ---- top alternatives -----------------------------------------------------------------------------------------
@@ -211,22 +218,21 @@ template <int THREADS> struct TopScratch {
     int who[THREADS];                 // threads whose vectors are looked at again
     int count, many;
 };
-// `most`: the order of this thread's largest logit in its vectors (NaN counts as the largest), 0 without any
-template <typename T, int THREADS>
-__device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, const Args& a, float lse, long long row, TopScratch<THREADS>* sc) {
+__device__ __forceinline__ void write_alternative(const Args& a, long long row, float lse, int place, unsigned long long key) {
+    const float x = logit_of(key);
+    a.top_logprob[row * a.top + place] = x == -__builtin_inff() && lse == lse ? x : x * a.scale - lse;     // also where lse is -infinity
+    a.top_index[row * a.top + place] = (int)~(uint32_t)key;
+}
+// write(place, key) for the `top` largest of the row's logits, top <= the row's length.  `most`: the order of the largest of this
+// thread's vectors, one that is there, 0 without any; `index0`: of the row's first logit.
+template <typename T, int THREADS, typename F>
+__device__ __forceinline__ void find_top(const RowView<T>& r, uint32_t most, int top, int index0, TopScratch<THREADS>* sc, F write) {
     constexpr int W = THREADS / 64, N = Vec16<T>::N;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    float* out = a.top_logprob + row * a.top;
-    int64_t* out_i = a.top_index + row * a.top;
-    auto write = [&](int place, unsigned long long key) {
-        const float x = logit_of(key);
-        out[place] = x == -__builtin_inff() && lse == lse ? x : x * a.scale - lse;     // also where lse is -infinity
-        out_i[place] = (int)~(uint32_t)key;
-    };
     // Waves whose threads do not all have a vector bound nothing; where there is no other, everything is handed over (less than
     // kCandidates then).
     const int full = min(W, r.nvec / 64);
-    const int c = full ? min(64, (a.top + full - 1) / full + 1) : 0;
+    const int c = full ? min(64, (top + full - 1) / full + 1) : 0;
     static_assert(W <= 16 && W * (ASI_LOGPROB_MAX_TOP / W + 2) <= kBounds, "room for the waves' largest");
     if (wave < full) {
         uint32_t left = most;
@@ -257,14 +263,14 @@ __device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, co
                 above += o > mine;
                 reach += o >= mine;
             }
-            if (half + lane < n && above < a.top && reach >= a.top) found = mine;
+            if (half + lane < n && above < top && reach >= top) found = mine;
         }
         bound = wave_max(found);
     }
     auto hand_over = [&](float x, int i) {
         if (order_of(x) >= bound) {
             const int at = atomicAdd(&sc->count, 1);
-            if (at < kCandidates) sc->key[at] = rank_key(x, i);
+            if (at < kCandidates) sc->key[at] = rank_key(x, index0 + i);
         }
     };
     if (most >= bound && most) sc->who[atomicAdd(&sc->many, 1)] = threadIdx.x;
@@ -291,15 +297,15 @@ __device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, co
             int before = 0;
 #pragma unroll 8
             for (int k = 0; k < n; ++k) before += sc->key[k] > key;
-            if (before < a.top) write(before, key);
+            if (before < top) write(before, key);
         }
         return;
     }
     unsigned long long last = ~0ull;              // no key is that: an index is not negative
-    for (int place = 0; place < a.top; ++place) {
+    for (int place = 0; place < top; ++place) {
         unsigned long long best = 0;
         auto look = [&](float x, int i) {
-            const unsigned long long key = rank_key(x, i);
+            const unsigned long long key = rank_key(x, index0 + i);
             if (key < last && key > best) best = key;
         };
         if (const int l = r.loose(threadIdx.x); l >= 0) look(to_f32(r.x[l]), l);
@@ -322,12 +328,25 @@ __device__ __forceinline__ void write_top(const RowView<T>& r, uint32_t most, co
 }
 
 // ---- forward ----------------------------------------------------------------------------------------------------
-// U: vectors that a thread loads at a time
-template <typename T, int THREADS, int U, bool TOP> __global__ __launch_bounds__(THREADS) void k_logprobs(const Args a) {
+// The order of the largest of a thread's vectors, where their sums are `a`: a logit that is there, as the bound of the alternatives needs
+__device__ __forceinline__ uint32_t order_of_most(const Sums& a) {
+    const float inf = __builtin_inff();
+    if (a.s != a.s) return a.m == inf ? order_of(inf) : 0xffffffffu;      // +infinity, or else NaN, is what makes the sum NaN
+    return order_of(a.s == 0.f ? -inf : a.m);
+}
+__device__ __forceinline__ void write_values(const Args& a, long long row, const Values& v) {
+    if (a.logprob) a.logprob[row] = v.logprob;
+    if (a.entropy) a.entropy[row] = v.entropy;
+    if (a.lse) a.lse[row] = v.lse;
+}
+// U: vectors that a thread loads at a time.  SPLIT: a part of the row.
+template <typename T, int THREADS, int U, bool TOP, bool SPLIT> __global__ __launch_bounds__(THREADS) void k_logprobs(const Args a) {
     __shared__ Sums scratch[THREADS / 64];
-    const long long row = blockIdx.x;
+    const long long row = SPLIT ? blockIdx.x / a.parts : blockIdx.x;
+    const int part = SPLIT ? (int)(blockIdx.x - row * a.parts) : 0, index0 = SPLIT ? part * a.part : 0;
     const T* x = static_cast<const T*>(a.x) + row * a.stride;
-    const RowView<T> r(x, a.vocab);
+    const int n = SPLIT ? min(a.part, a.vocab - index0) : a.vocab;
+    const RowView<T> r(x + index0, n);
     const float c = a.scale * kLog2e;
     Sums acc{kLowest, 0.f, 0.f};
     Vec16<T> v[U];
@@ -335,21 +354,50 @@ template <typename T, int THREADS, int U, bool TOP> __global__ __launch_bounds__
         const int have = load<T, U>(r, base + threadIdx.x, THREADS, v);
         take<T, U>(&acc, v, have, c);
     }
-    // the largest logit of the thread's vectors: not a number above -infinity where nothing was added up, NaN where the sum is
-    uint32_t most = 0;
-    if (TOP && (int)threadIdx.x < r.nvec) most = acc.s != acc.s ? 0xffffffffu : order_of(acc.s == 0.f ? -__builtin_inff() : acc.m);
-    if (const int l = r.loose(threadIdx.x); l >= 0) take_one(&acc, to_f32(x[l]), c);
+    const uint32_t most = TOP && (int)threadIdx.x < r.nvec ? order_of_most(acc) : 0u;
+    if (const int l = r.loose(threadIdx.x); l >= 0) take_one(&acc, to_f32(r.x[l]), c);
     const Sums all = over_workgroup<THREADS>(acc, c, scratch);
-    const long long target = a.targets ? a.targets[row] : a.ignore;
-    const Values val = values_of(all, x, target, a.vocab, a.ignore, a.scale);
-    if (threadIdx.x == 0) {
-        if (a.logprob) a.logprob[row] = val.logprob;
-        if (a.entropy) a.entropy[row] = val.entropy;
-        if (a.lse) a.lse[row] = val.lse;
+    Values val{};
+    if constexpr (SPLIT) {
+        if (threadIdx.x == 0) a.sums[blockIdx.x] = all;
+    } else {
+        const long long target = a.targets ? a.targets[row] : a.ignore;
+        val = values_of(all, x, target, a.vocab, a.ignore, a.scale);
+        if (threadIdx.x == 0) write_values(a, row, val);
     }
     if constexpr (TOP) {
         __shared__ TopScratch<THREADS> top;
-        write_top<T, THREADS>(r, most, a, val.lse, row, &top);
+        if constexpr (SPLIT) {
+            unsigned long long* keys = a.keys + (long long)blockIdx.x * a.top;
+            const int want = min(a.top, n);
+            find_top<T, THREADS>(r, most, want, index0, &top, [&](int place, unsigned long long key) { keys[place] = key; });
+            for (int i = want + threadIdx.x; i < a.top; i += THREADS) keys[i] = 0;
+        } else {
+            find_top<T, THREADS>(r, most, a.top, 0, &top, [&](int place, unsigned long long key) { write_alternative(a, row, val.lse, place, key); });
+        }
+    }
+}
+// The parts of a row, a workgroup a row
+constexpr int kMaxParts = 16, kJoinThreads = 256;
+template <typename T> __global__ __launch_bounds__(kJoinThreads) void k_join_parts(const Args a) {
+    __shared__ unsigned long long key[kMaxParts * ASI_LOGPROB_MAX_TOP];
+    const long long row = blockIdx.x;
+    const int n = a.parts * a.top;
+    for (int i = threadIdx.x; i < n; i += kJoinThreads) key[i] = a.keys[row * n + i];
+    const int p = threadIdx.x & (kMaxParts - 1);
+    Sums all{kLowest, 0.f, 0.f};
+    if (p < a.parts) all = a.sums[row * a.parts + p];
+    all = over_lanes<kMaxParts>(all, a.scale * kLog2e);
+    const long long target = a.targets ? a.targets[row] : a.ignore;
+    const Values val = values_of(all, static_cast<const T*>(a.x) + row * a.stride, target, a.vocab, a.ignore, a.scale);
+    if (threadIdx.x == 0) write_values(a, row, val);
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kJoinThreads) {
+        const unsigned long long mine = key[i];
+        int before = 0;
+#pragma unroll 8
+        for (int k = 0; k < n; ++k) before += key[k] > mine;
+        if (mine && before < a.top) write_alternative(a, row, val.lse, before, mine);
     }
 }
 
@@ -454,16 +502,36 @@ asi_status check(const asi_logprob_desc* d) {
     if (d->rows > 0x7fffffffLL || d->vocab > (1LL << 28)) return ASI_ERR_UNSUPPORTED;
     return ASI_OK;
 }
-template <typename T, int THREADS, int U> void forward(const Args& a, unsigned rows, hipStream_t st) {
-    if (a.top) hipLaunchKernelGGL((k_logprobs<T, THREADS, U, true>), dim3(rows), THREADS, 0, st, a);
-    else hipLaunchKernelGGL((k_logprobs<T, THREADS, U, false>), dim3(rows), THREADS, 0, st, a);
+// Parts of a row: 1, or of long rows too few to fill the chip as many as leave each 1024 vectors, and the joining kernel no more than
+// about 160 alternatives to compare with each other.  Measured: 8 rows of 128000 in bf16 without alternatives 11.3 us in one part, 6.0
+// in 15, with 20 alternatives 16.1 in one, 18.3 in 15, 12.6 in 7; 5 rows of 195072 in fp32 17.9 and 8.3; 64 of
+// 33000 in fp32 with 20 alternatives 11.0 and 13.1, without them 66000 in bf16 8.2 and 6.0.
+int parts_of(const asi_logprob_desc* d) {
+    const long long nvec = d->vocab / (int)(16 / dtype_size(d->dtype));
+    if (nvec < (d->top ? 12288 : 8192) || d->rows > 64) return 1;
+    const long long joined = d->top ? std::max(2, 160 / d->top) : kMaxParts;
+    return (int)std::max(1LL, std::min<long long>({kMaxParts, joined, nvec / 1024, 512 / std::max<int64_t>(1, d->rows)}));
+}
+size_t sums_bytes(const asi_logprob_desc* d, int parts) { return round256((size_t)d->rows * parts * sizeof(Sums)); }
+
+template <typename T, int THREADS, int U, bool SPLIT> void forward(const Args& a, unsigned blocks, hipStream_t st) {
+    if (a.top) hipLaunchKernelGGL((k_logprobs<T, THREADS, U, true, SPLIT>), dim3(blocks), THREADS, 0, st, a);
+    else hipLaunchKernelGGL((k_logprobs<T, THREADS, U, false, SPLIT>), dim3(blocks), THREADS, 0, st, a);
 }
 template <typename T> void forward(const Args& a, unsigned rows, hipStream_t st) {
     const int nvec = a.vocab / Vec16<T>::N;
-    if (nvec <= 256) forward<T, 64, 4>(a, rows, st);
-    else if (nvec <= 2048) forward<T, 256, 4>(a, rows, st);
-    else if (rows > 256) forward<T, 512, 4>(a, rows, st);
-    else forward<T, 1024, 4>(a, rows, st);
+    if (a.parts > 1) {
+        forward<T, 512, 4, true>(a, rows * a.parts, st);
+        hipLaunchKernelGGL(k_join_parts<T>, dim3(rows), kJoinThreads, 0, st, a);
+    } else if (nvec <= 256) {
+        forward<T, 64, 4, false>(a, rows, st);
+    } else if (nvec <= 2048) {
+        forward<T, 256, 4, false>(a, rows, st);
+    } else if (rows > 256) {
+        forward<T, 512, 4, false>(a, rows, st);
+    } else {
+        forward<T, 1024, 4, false>(a, rows, st);
+    }
 }
 template <typename T> void backward(const GradArgs& g, unsigned rows, hipStream_t st) {
     const int nvec = g.vocab / Vec16<T>::N;
@@ -484,13 +552,15 @@ using namespace asi;
 
 extern "C" {
 
-size_t asi_token_logprobs_workspace_bytes(const asi_logprob_desc*) { return 0; }
+size_t asi_token_logprobs_workspace_bytes(const asi_logprob_desc* desc) {
+    if (check(desc) != ASI_OK || desc->top < 0 || desc->top > desc->vocab || desc->top > ASI_LOGPROB_MAX_TOP) return 0;
+    const int parts = parts_of(desc);
+    return parts == 1 ? 0 : sums_bytes(desc, parts) + round256((size_t)desc->rows * parts * desc->top * 8);
+}
 
 asi_status asi_token_logprobs(const asi_logprob_desc* desc, const void* logits, const int64_t* targets, float* logprob,
                               float* entropy, float* lse, float* top_logprob, int64_t* top_index, void* ws,
                               size_t ws_bytes, asi_stream_t stream) {
-    (void)ws;
-    (void)ws_bytes;
     if (asi_status why = check(desc); why != ASI_OK) return why;
     if (desc->top < 0 || desc->top > desc->vocab || desc->top > ASI_LOGPROB_MAX_TOP) return ASI_ERR_INVALID_ARG;
     if (desc->rows == 0) return ASI_OK;
@@ -498,8 +568,15 @@ asi_status asi_token_logprobs(const asi_logprob_desc* desc, const void* logits, 
     if (!logits || !aligned(logits, es) || (logprob && !targets) || !aligned(targets, 8) || !aligned(logprob, 4) || !aligned(entropy, 4) ||
         !aligned(lse, 4) || (desc->top && (!top_logprob || !top_index || !aligned(top_logprob, 4) || !aligned(top_index, 8))))
         return ASI_ERR_INVALID_ARG;
-    const Args a{logits, targets, logprob, entropy, lse, top_logprob, top_index, desc->row_stride, desc->ignore_index, (int)desc->vocab,
-                 desc->top, desc->scale};
+    Args a{logits, targets, logprob, entropy, lse, top_logprob, top_index, desc->row_stride, desc->ignore_index, (int)desc->vocab,
+           desc->top, desc->scale, parts_of(desc), 0, nullptr, nullptr};
+    if (a.parts > 1) {
+        if (!ws || !aligned(ws, 256) || ws_bytes < asi_token_logprobs_workspace_bytes(desc)) return ASI_ERR_WORKSPACE;
+        a.part = (a.vocab + a.parts - 1) / a.parts;
+        a.part = (a.part + 63) / 64 * 64;         // parts begin where 128 bytes of an aligned row do
+        a.sums = static_cast<Sums*>(ws);
+        a.keys = reinterpret_cast<unsigned long long*>(static_cast<char*>(ws) + sums_bytes(desc, a.parts));
+    }
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (desc->dtype == ASI_F32) forward<float>(a, (unsigned)desc->rows, st);
     else forward<bf16_t>(a, (unsigned)desc->rows, st);

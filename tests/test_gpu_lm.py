@@ -193,6 +193,15 @@ def test_token_logprobs_grad(size, dtype):
         assert torch.equal(asi.token_logprobs_grad(x, targets, a, b, scale=scale, out=other).grad, r.grad)
 
 
+@pytest.mark.parametrize("vocab", [700, 20000, 150000])
+def test_alternatives_beside_many_infinities(vocab):
+    x = _logits(2, vocab, torch.float32, vocab)
+    x[:, torch.randperm(vocab, generator=_gen(1), device="cuda")[:vocab // 3]] = INF
+    x[1, torch.randperm(vocab, generator=_gen(2), device="cuda")[:5]] = NAN
+    r = asi.token_logprobs(x, top=20)
+    assert torch.equal(r.top_index, _order(x, 20)) and torch.isnan(r.top_logprob).all()
+
+
 def test_targets_out_of_range_give_nan():
     x = _logits(4, 1000, torch.float32, 3)
     targets = torch.tensor([-1, 1000, 999, -100], device="cuda")
