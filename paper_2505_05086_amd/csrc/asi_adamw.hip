@@ -1,13 +1,16 @@
 // AdamW over many tensors (include/asi_lm.h).
 //
 // A launch takes the records of up to kTensors tensors by value; every workgroup finds its tensor from its block index and
-// updates 4096 consecutive elements of it, each wave in pieces of 256, which is also the block that shares a scale of the
-// 8-bit states.  The update reads and writes each element once and is bound by memory.
+// updates a chunk of it, each lane 16 bytes of fp32 (4 elements) or two of them (8, states in 8 bits: half a wave then has the 256
+// elements that share a scale).  The update reads and writes each element once and is bound by memory.  A chunk is one piece a wave:
+// many short workgroups keep the memory busier than few that loop (six blocks of 2048 in fp32, 308 million elements: chunks of 8192,
+// 4096, 1024 elements 1667, 1638, 1571 us).
 //
 // Products, sums, the quotient and the root are rounded one by one (no contraction), so that the result is that of the same
 // formula in elementary fp32 operations, bit for bit: an 8-bit code then does not depend on how a compiler fused it.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "asi_lm_device.h"
@@ -17,8 +20,7 @@ namespace {
 
 constexpr int kTensors = 40;
 constexpr int kThreads = 256;
-constexpr int kPiece = ASI_ADAMW_BLOCK;          // elements a wave takes at a time: 4 a lane
-constexpr int kChunk = 4096;                     // elements of a workgroup
+constexpr int kBlock = ASI_ADAMW_BLOCK;          // elements that share a scale
 constexpr float kCodeMax = 448.f;                // largest value of the 8-bit format
 constexpr float kLeastScale = 0x1p-126f;
 
@@ -32,7 +34,7 @@ struct Tensor {
     float* sq_scale;
     long long count;
     float decay, rate;       // 1 - lr * weight_decay; lr / (1 - beta1^step)
-    int vec, pad;            // every pointer allows loads of four elements
+    int vec, pad;            // every pointer allows vectors
 };
 struct Args {
     float b1, c1, b2, c2, root_factor, eps;      // c = 1 - beta; root_factor = 1 / sqrt(1 - beta2^step)
@@ -42,66 +44,49 @@ struct Args {
     Tensor t[kTensors];
 };
 
-// Four elements of a lane: neighbours where loads of four are allowed, 64 apart otherwise and at a tensor's end.
-struct Quad {
-    long long at;
-    long long count;
+// E elements of a lane: neighbours where vectors are allowed, otherwise and at a tensor's end as far apart as the piece has lanes, so
+// that neighbouring lanes have neighbours either way.
+template <int E> struct Part {
+    long long at, count;
+    int apart;
     bool vec;
-    __device__ __forceinline__ long long index(int i) const { return vec ? at + i : at + 64LL * i; }
+    __device__ __forceinline__ long long index(int i) const { return vec ? at + i : at + (long long)apart * i; }
     __device__ __forceinline__ bool has(int i) const { return vec || index(i) < count; }
 };
-__device__ __forceinline__ void load4(const float* p, const Quad& q, float* f) {
+template <typename T, int E> __device__ __forceinline__ void load(const T* p, const Part<E>& q, float* f) {
     if (q.vec) {
-        const float4 v = *reinterpret_cast<const float4*>(p + q.at);
-        f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+        load_values<E>(p + q.at, f);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = q.has(i) ? p[q.index(i)] : 0.f;
+        for (int i = 0; i < E; ++i) f[i] = q.has(i) ? to_f32(p[q.index(i)]) : 0.f;
     }
 }
-__device__ __forceinline__ void load4(const bf16_t* p, const Quad& q, float* f) {
+template <typename T, int E> __device__ __forceinline__ void store(T* p, const Part<E>& q, const float* f) {
     if (q.vec) {
-        const uint2 v = *reinterpret_cast<const uint2*>(p + q.at);
-        f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
-        f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+        store_values<E>(p + q.at, f);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = q.has(i) ? to_f32(p[q.index(i)]) : 0.f;
+        for (int i = 0; i < E; ++i)
+            if (q.has(i)) p[q.index(i)] = from_f32<T>(f[i]);
     }
 }
-__device__ __forceinline__ void store4(float* p, const Quad& q, const float* f) {
+// 8 codes of a lane, in two words
+using Lane8 = Part<8>;
+__device__ __forceinline__ uint2 load_codes(const uint8_t* p, const Lane8& q) {
+    if (q.vec) return *reinterpret_cast<const uint2*>(p + q.at);
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (q.has(i)) w[i / 4] |= (uint32_t)p[q.index(i)] << (8 * (i & 3));
+    return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, const Lane8& q, uint2 w) {
     if (q.vec) {
-        *reinterpret_cast<float4*>(p + q.at) = make_float4(f[0], f[1], f[2], f[3]);
+        *reinterpret_cast<uint2*>(p + q.at) = w;
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (q.has(i)) p[q.index(i)] = f[i];
-    }
-}
-__device__ __forceinline__ void store4(bf16_t* p, const Quad& q, const float* f) {
-    if (q.vec) {
-        *reinterpret_cast<uint2*>(p + q.at) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (q.has(i)) p[q.index(i)] = to_bf16(f[i]);
-    }
-}
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, const Quad& q) {
-    if (q.vec) return *reinterpret_cast<const uint32_t*>(p + q.at);
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (q.has(i)) w |= (uint32_t)p[q.index(i)] << (8 * i);
-    return w;
-}
-__device__ __forceinline__ void store_codes(uint8_t* p, const Quad& q, uint32_t w) {
-    if (q.vec) {
-        *reinterpret_cast<uint32_t*>(p + q.at) = w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (q.has(i)) p[q.index(i)] = (uint8_t)(w >> (8 * i));
+        for (int i = 0; i < 8; ++i)
+            if (q.has(i)) p[q.index(i)] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
     }
 }
 __device__ __forceinline__ void decode(uint32_t w, float scale, float* f) {
@@ -113,90 +98,96 @@ __device__ __forceinline__ float finite_magnitude(float x) {
     const float a = fabsf(x);
     return a < __builtin_inff() ? a : 0.f;
 }
-// Codes of a wave's 256 values and their scale.  POSITIVE: values are roots, of which a positive one is not held as zero.
-template <bool POSITIVE> __device__ __forceinline__ uint32_t encode(const float* f, float* scale) {
+// Codes of the 256 values of half a wave and their scale.  POSITIVE: values are roots, of which a positive one is not held as zero.
+template <bool POSITIVE> __device__ __forceinline__ uint2 encode(const float* f, float* scale) {
 #pragma clang fp contract(off)
     float most = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) most = fmaxf(most, finite_magnitude(f[i]));
-    most = lanes_max(most);
+    for (int i = 0; i < 8; ++i) most = fmaxf(most, finite_magnitude(f[i]));
+    most = __uint_as_float(half_wave_max(__float_as_uint(most)));         // magnitudes are in the order of their bits
     float s = most * (1.f / kCodeMax);
     const bool held = s >= kLeastScale;
     const float inv = held ? 1.f / s : 0.f;
     *scale = held ? s : 0.f;
-    float v[4];
+    float v[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
         v[i] = f[i] * inv;
         if (!(fabsf(f[i]) < __builtin_inff())) v[i] = __builtin_nanf("");
     }
-    uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
-    w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], (int)w, true);
-    if (POSITIVE && held) {
+    uint32_t w[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (f[i] > 0.f && (w >> (8 * i) & 0xffu) == 0) w |= 1u << (8 * i);
+    for (int k = 0; k < 2; ++k) {
+        w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * k], v[4 * k + 1], 0, false);
+        w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * k + 2], v[4 * k + 3], (int)w[k], true);
+        if (POSITIVE && held) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (f[4 * k + i] > 0.f && (w[k] >> (8 * i) & 0xffu) == 0) w[k] |= 1u << (8 * i);
+        }
     }
-    return w;
+    return make_uint2(w[0], w[1]);
 }
 
+template <bool EIGHT> struct Shape {
+    static constexpr int E = EIGHT ? 8 : 4, lanes = kBlock / E, chunk = kThreads * E;     // lanes of a piece of 256 elements
+};
 template <typename PT, typename GT, bool MASTER, bool EIGHT>
 __global__ __launch_bounds__(kThreads) void k_adamw(const Args a) {
 #pragma clang fp contract(off)
+    constexpr int E = Shape<EIGHT>::E, LANES = Shape<EIGHT>::lanes;
     if (a.skip && *a.skip != 0) return;
     int j = 0;
 #pragma unroll
     for (int k = 1; k < kTensors; ++k) j += (int)blockIdx.x >= a.first[k];
     const Tensor& t = a.t[j];
     const float gs = a.grad_scale ? *a.grad_scale : 1.f;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long begin = (long long)((int)blockIdx.x - a.first[j]) * kChunk;
-#pragma unroll 2
-    for (int k = 0; k < kChunk / kPiece / (kThreads / 64); ++k) {
-        const long long base = begin + (long long)(k * (kThreads / 64) + wave) * kPiece;
-        if (base >= t.count) break;
-        Quad q;
-        q.count = t.count;
-        q.vec = t.vec && base + kPiece <= t.count;
-        q.at = base + (q.vec ? 4 * lane : lane);
-        float p[4], g[4], m[4], v[4], root[4];
-        if (MASTER) load4(t.master, q, p);
-        else load4(static_cast<const PT*>(t.param), q, p);
-        load4(static_cast<const GT*>(t.grad), q, g);
-        if (EIGHT) {
-            const uint32_t wm = load_codes(static_cast<const uint8_t*>(t.avg), q), wv = load_codes(static_cast<const uint8_t*>(t.sq), q);
-            decode(wm, t.avg_scale[base / kPiece], m);
-            decode(wv, t.sq_scale[base / kPiece], root);
+    const int lane = threadIdx.x & (LANES - 1);
+    const long long block = (long long)((int)blockIdx.x - a.first[j]) * (kThreads / LANES) + threadIdx.x / LANES, base = block * kBlock;
+    Part<E> q;
+    q.count = t.count;
+    q.apart = LANES;
+    q.vec = t.vec && base + kBlock <= t.count;
+    q.at = base + (q.vec ? E * lane : lane);
+    float p[E], g[E], m[E], v[E], root[E];
+    if (MASTER) load(t.master, q, p);
+    else load(static_cast<const PT*>(t.param), q, p);
+    load(static_cast<const GT*>(t.grad), q, g);
+    if constexpr (EIGHT) {
+        const bool any = base < t.count;
+        const uint2 wm = load_codes(static_cast<const uint8_t*>(t.avg), q), wv = load_codes(static_cast<const uint8_t*>(t.sq), q);
+        const float sm = any ? t.avg_scale[block] : 0.f, sv = any ? t.sq_scale[block] : 0.f;
+        decode(wm.x, sm, m); decode(wm.y, sm, m + 4);
+        decode(wv.x, sv, root); decode(wv.y, sv, root + 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = root[i] * root[i];
-        } else {
-            load4(static_cast<const float*>(t.avg), q, m);
-            load4(static_cast<const float*>(t.sq), q, v);
-        }
+        for (int i = 0; i < E; ++i) v[i] = root[i] * root[i];
+    } else {
+        load(static_cast<const float*>(t.avg), q, m);
+        load(static_cast<const float*>(t.sq), q, v);
+    }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float gi = g[i] * gs;
-            m[i] = m[i] * a.b1 + gi * a.c1;
-            v[i] = v[i] * a.b2 + (gi * gi) * a.c2;
-            root[i] = sqrtf(v[i]);
-            const float u = m[i] / (root[i] * a.root_factor + a.eps);
-            p[i] = p[i] * t.decay - u * t.rate;
+    for (int i = 0; i < E; ++i) {
+        const float gi = g[i] * gs;
+        m[i] = m[i] * a.b1 + gi * a.c1;
+        v[i] = v[i] * a.b2 + (gi * gi) * a.c2;
+        root[i] = sqrtf(v[i]);
+        const float u = m[i] / (root[i] * a.root_factor + a.eps);
+        p[i] = p[i] * t.decay - u * t.rate;
+    }
+    if (MASTER) store(t.master, q, p);
+    store(static_cast<PT*>(t.param), q, p);
+    if constexpr (EIGHT) {
+        float sm, sv;
+        const uint2 wm = encode<false>(m, &sm), wv = encode<true>(root, &sv);
+        store_codes(static_cast<uint8_t*>(t.avg), q, wm);
+        store_codes(static_cast<uint8_t*>(t.sq), q, wv);
+        if (lane == 0 && base < t.count) {
+            t.avg_scale[block] = sm;
+            t.sq_scale[block] = sv;
         }
-        if (MASTER) store4(t.master, q, p);
-        store4(static_cast<PT*>(t.param), q, p);
-        if (EIGHT) {
-            float sm, sv;
-            const uint32_t wm = encode<false>(m, &sm), wv = encode<true>(root, &sv);
-            store_codes(static_cast<uint8_t*>(t.avg), q, wm);
-            store_codes(static_cast<uint8_t*>(t.sq), q, wv);
-            if (lane == 0) {
-                t.avg_scale[base / kPiece] = sm;
-                t.sq_scale[base / kPiece] = sv;
-            }
-        } else {
-            store4(static_cast<float*>(t.avg), q, m);
-            store4(static_cast<float*>(t.sq), q, v);
-        }
+    } else {
+        store(static_cast<float*>(t.avg), q, m);
+        store(static_cast<float*>(t.sq), q, v);
     }
 }
 
@@ -249,6 +240,7 @@ extern "C" asi_status asi_adamw(int32_t count, const asi_adamw_tensor* tensors, 
     a.eps = (float)eps;
     a.grad_scale = grad_scale;
     a.skip = skip;
+    const int chunk = eight ? Shape<true>::chunk : Shape<false>::chunk;
     bool any = false;
     const double correction = 1.0 - std::pow(beta1, (double)step);
     for (int kind = 0; kind < 8; ++kind) {
@@ -264,16 +256,17 @@ extern "C" asi_status asi_adamw(int32_t count, const asi_adamw_tensor* tensors, 
         for (int32_t i = 0; i < count; ++i) {
             const asi_adamw_tensor& s = tensors[i];
             if (s.count == 0 || kind_of(s) != kind) continue;
-            const long long need = (s.count + kChunk - 1) / kChunk;
+            const long long need = (s.count + chunk - 1) / chunk;
             if (n == kTensors || blocks + need > 0x7fffffffLL) flush();
             Tensor& t = a.t[n];
             t.param = s.param; t.grad = s.grad; t.master = s.master; t.avg = s.exp_avg; t.sq = s.exp_avg_sq;
             t.avg_scale = s.exp_avg_scale; t.sq_scale = s.exp_avg_sq_scale; t.count = s.count;
             t.decay = (float)(1.0 - s.lr * s.weight_decay);
             t.rate = (float)(s.lr / correction);
-            const size_t state = eight ? 4 : 16;
-            t.vec = aligned(s.param, 4 * dtype_size(s.param_dtype)) && aligned(s.grad, 4 * dtype_size(s.grad_dtype)) &&
-                    aligned(s.master, 16) && aligned(s.exp_avg, state) && aligned(s.exp_avg_sq, state);
+            // accesses of up to 16 bytes
+            const size_t state = eight ? 8 : 16, e = eight ? 8 : 4;
+            t.vec = aligned(s.param, std::min<size_t>(16, e * dtype_size(s.param_dtype))) &&
+                    aligned(s.grad, std::min<size_t>(16, e * dtype_size(s.grad_dtype))) && aligned(s.master, 16) && aligned(s.exp_avg, state) && aligned(s.exp_avg_sq, state);
             a.first[n] = (int)blocks;
             blocks += need;
             ++n;

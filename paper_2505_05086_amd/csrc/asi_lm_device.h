@@ -99,16 +99,25 @@ template <int WIDTH = kWave> __device__ __forceinline__ float lanes_max(float x)
     return x;
 }
 
-// The largest over the wave, in every lane: steps within 16 lanes, then across their rows, without a way through LDS.
+// The largest over the wave, or over each half of it, in every lane: steps within 16 lanes, then across their rows, without a way
+// through LDS.
 template <int CTRL> __device__ __forceinline__ uint32_t moved(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, CTRL, 0xf, 0xf, false); }
-__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+__device__ __forceinline__ uint32_t max_at_row_pairs(uint32_t x) {
     x = max(x, moved<0x111>(x));      // from 1, 2, 4 and 8 lanes before it in its row of 16
     x = max(x, moved<0x112>(x));
     x = max(x, moved<0x114>(x));
     x = max(x, moved<0x118>(x));
-    x = max(x, moved<0x142>(x));      // the last lane of a row to the next row, of the first half to the second
-    x = max(x, moved<0x143>(x));
+    return max(x, moved<0x142>(x));   // the last lane of a row to the next row
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    x = max_at_row_pairs(x);
+    x = max(x, moved<0x143>(x));      // the last lane of the first half to the second half
     return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+__device__ __forceinline__ uint32_t half_wave_max(uint32_t x) {
+    x = max_at_row_pairs(x);
+    const uint32_t lower = (uint32_t)__builtin_amdgcn_readlane((int)x, 31), upper = (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+    return (threadIdx.x & 32) ? upper : lower;
 }
 
 // the larger of two, NaN if either is

@@ -8,6 +8,9 @@ arithmetic runs in the HIP kernels; there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
+import itertools
+import operator
 from typing import List, NamedTuple, Optional, Sequence, Tuple
 
 import numpy as np
@@ -20,34 +23,54 @@ IGNORE_INDEX = -100
 
 
 # ---- argument checks --------------------------------------------------------------------------------------
-def _dtype(t: torch.Tensor, what: str) -> int:
-    d = _DTYPE.get(t.dtype)
+# Small calls last as long as their marshalling: what follows from shapes, strides and types alone (the checks, the descriptor, the
+# scratch) is worked out once for each of them and kept by those, never by a tensor or its address.
+_plans = functools.lru_cache(maxsize=1024)
+
+
+def _dtype(dtype: torch.dtype, what: str) -> int:
+    d = _DTYPE.get(dtype)
     if d is None:
-        raise TypeError(f"{what} is fp32 or bf16, not {t.dtype}")
+        raise TypeError(f"{what} is fp32 or bf16, not {dtype}")
     return d
 
 
-def _place(*ts: Optional[torch.Tensor]) -> int:
-    """The current device's index; every tensor has to be there."""
-    here = torch.cuda.current_device()
-    for t in ts:
-        if t is not None and (not t.is_cuda or t.device.index != here):
-            raise ValueError("every tensor has to be on the current GPU (there is no CPU fallback)")
-    return here
+def _place(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
+    """The current GPU's index; every tensor has to be there."""
+    device = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != device:
+            device = -1
+    if device < 0 or device != torch._C._cuda_getDevice():
+        raise ValueError("every tensor has to be on the current GPU (there is no CPU fallback)")
+    return device
 
 
-def _f32(t: Optional[torch.Tensor], shape, what: str) -> Optional[torch.Tensor]:
-    if t is None:
-        return None
-    if t.dtype != torch.float32 or t.shape != shape:
-        raise ValueError(f"{what} is an fp32 tensor of shape {tuple(shape)}")
-    return t.contiguous()
+def _geometry(t: Optional[torch.Tensor]):
+    return None if t is None else (t.shape, t.stride(), t.dtype)
+
+
+def _dense(shape, stride) -> bool:
+    n = 1
+    for s, d in zip(reversed(shape), reversed(stride)):
+        if s != 1 and d != n and 0 not in shape:
+            return False
+        n *= s
+    return True
 
 
 def _whole(t: torch.Tensor, what: str) -> torch.Tensor:
     if t.dtype != torch.int64:
         raise TypeError(f"{what} are int64, not {t.dtype}")
-    return t.contiguous()
+    return t if t.is_contiguous() else t.contiguous()
+
+
+def _weights(t: Optional[torch.Tensor], shape, what: str) -> Optional[torch.Tensor]:
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != shape:
+        raise ValueError(f"{what} is an fp32 tensor of shape {tuple(shape)}")
+    return t if t.is_contiguous() else t.contiguous()
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -55,11 +78,11 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream(device: int) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
-def _scratch(nbytes: int, device: int) -> Optional[torch.Tensor]:
-    return torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{device}") if nbytes else None
+def _scratch(nbytes: int, like: torch.Tensor) -> Optional[torch.Tensor]:
+    return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
 
 
 # ---- token log probabilities ------------------------------------------------------------------------------
@@ -76,49 +99,73 @@ class TokenLogprobsGrad(NamedTuple):
     grad: torch.Tensor                     # of the logits, in their type
 
 
-def _rows(logits: torch.Tensor) -> torch.Tensor:
-    if logits.dim() == 2:
-        x = logits
-    elif logits.dim() == 0:
-        raise ValueError("logits have a dimension of the vocabulary")
+def _row_layout(shape, stride, what: str):
+    """Rows, vocabulary and the rows' distance of logits of any number of dimensions."""
+    if not shape:
+        raise ValueError(f"{what} have a dimension of the vocabulary")
+    vocab, rows, apart = shape[-1], 1, None
+    if 0 in shape[:-1]:
+        return 0, vocab, vocab
+    if vocab < 1 or (stride[-1] != 1 and vocab > 1):
+        raise ValueError(f"the vocabulary is the innermost dimension of {what}, its entries next to each other")
+    for n, d in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+        if n != 1:
+            if apart is None:
+                apart = d
+            elif d != apart * rows:
+                raise ValueError(f"{what} of more than two dimensions need rows at equal distances; shift the targets rather than "
+                                 "slicing the logits")
+        rows *= n
+    return rows, vocab, vocab if apart is None else apart
+
+
+@_plans
+def _logprob_plan(geometry, top, scale, ignore_index, out):
+    """Descriptor, scratch, shape of the rows, and for the gradient the shape and strides of a new result."""
+    shape, stride, dtype = geometry
+    rows, vocab, apart = _row_layout(shape, stride, "logits")
+    lead = shape[:-1]
+    new = None
+    if out is None:
+        # rows that lie in their 16 bytes as those of the logits do, so that both are accessed in whole vectors
+        grad = vocab + (apart - vocab) % (16 // dtype.itemsize)
+        if grad != vocab:
+            strides, d = [], grad
+            for n in reversed(lead):
+                strides.insert(0, d)
+                d *= n
+            new = (shape, (*strides, 1))
     else:
-        try:
-            x = logits.view(-1, logits.shape[-1])
-        except RuntimeError as e:
-            raise ValueError("logits of more than two dimensions need rows at equal distances; shift the targets rather "
-                             "than slicing the logits") from e
-    if x.shape[1] < 1 or (x.stride(1) != 1 and x.shape[1] > 1):
-        raise ValueError("the vocabulary is the innermost dimension of the logits, its entries next to each other")
-    return x
+        if out[0] != shape or out[2] != dtype:
+            raise ValueError("out has the logits' shape and type")
+        grad = _row_layout(out[0], out[1], "out")[2]
+    desc = B.LogprobDesc(rows, vocab, apart, grad, ignore_index, _dtype(dtype, "logits"), top, scale, 0)
+    return desc, int(B.lib().asi_token_logprobs_workspace_bytes(desc)), lead, new
 
 
-def _logprob_desc(x: torch.Tensor, scale: float, ignore_index: int, top: int, grad_stride: int) -> B.LogprobDesc:
-    rows, vocab = x.shape
-    return B.LogprobDesc(rows, vocab, x.stride(0) if rows > 1 else vocab, grad_stride, ignore_index, _dtype(x, "logits"),
-                         top, scale, 0)
+def _targets(targets: Optional[torch.Tensor], shape) -> Optional[torch.Tensor]:
+    if targets is None:
+        return None
+    if targets.shape != shape:
+        raise ValueError(f"one target for each row: shape {tuple(shape)}, not {tuple(targets.shape)}")
+    return _whole(targets, "targets")
 
 
 def _token_logprobs(logits, targets, top, scale, ignore_index) -> TokenLogprobs:
-    x = _rows(logits)
-    shape = logits.shape[:-1]
-    if targets is not None:
-        if targets.shape != shape:
-            raise ValueError(f"one target for each row: shape {tuple(shape)}, not {tuple(targets.shape)}")
-        targets = _whole(targets, "targets")
-    device = _place(x, targets)
-    desc = _logprob_desc(x, scale, ignore_index, top, 0)
-    new = dict(device=x.device, dtype=torch.float32)
-    logprob = None if targets is None else torch.empty(shape, **new)
-    entropy = torch.empty(shape, **new)
+    desc, nbytes, shape, _ = _logprob_plan(_geometry(logits), top, scale, ignore_index, None)
+    targets = _targets(targets, shape)
+    device = _place(logits, targets)
+    logprob = None if targets is None else logits.new_empty(shape, dtype=torch.float32)
+    entropy = logits.new_empty(shape, dtype=torch.float32)
     top_logprob = top_index = None
     if top:
-        top_logprob = torch.empty(shape + (top,), **new)
-        top_index = torch.empty(shape + (top,), device=x.device, dtype=torch.int64)
-    L = B.lib()
-    ws = _scratch(L.asi_token_logprobs_workspace_bytes(desc), device)
-    B._check(L.asi_token_logprobs(desc, x.data_ptr(), _ptr(targets), _ptr(logprob), entropy.data_ptr(), None, _ptr(top_logprob),
-                                  _ptr(top_index), _ptr(ws), 0 if ws is None else ws.numel(), _stream(device)),
-             "asi_token_logprobs")
+        top_logprob = logits.new_empty(shape + (top,), dtype=torch.float32)
+        top_index = logits.new_empty(shape + (top,), dtype=torch.int64)
+    ws = _scratch(nbytes, logits)
+    status = B.lib().asi_token_logprobs(desc, logits.data_ptr(), _ptr(targets), _ptr(logprob), entropy.data_ptr(), None,
+                                        _ptr(top_logprob), _ptr(top_index), _ptr(ws), nbytes, _stream(device))
+    if status:
+        B._check(status, "asi_token_logprobs")
     return TokenLogprobs(logprob, entropy, top_logprob, top_index)
 
 
@@ -157,59 +204,47 @@ def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor], g
     """Gradient of sum(grad_logprob * logprob + grad_entropy * entropy) in the logits, with both values, in one pass over
     the logits.  For a loss whose weights are known beforehand this replaces forward and backward.  `out` may be `logits`
     themselves: the gradient then takes their place."""
-    x = _rows(logits)
-    shape = logits.shape[:-1]
-    if targets is not None:
-        if targets.shape != shape:
-            raise ValueError(f"one target for each row: shape {tuple(shape)}, not {tuple(targets.shape)}")
-        targets = _whole(targets, "targets")
-    grad_logprob, grad_entropy = _f32(grad_logprob, shape, "grad_logprob"), _f32(grad_entropy, shape, "grad_entropy")
-    device = _place(x, targets, grad_logprob, grad_entropy, out)
-    rows, vocab = x.shape
+    desc, _, shape, new = _logprob_plan(_geometry(logits), 0, scale, ignore_index, _geometry(out))
+    targets = _targets(targets, shape)
+    grad_logprob, grad_entropy = _weights(grad_logprob, shape, "grad_logprob"), _weights(grad_entropy, shape, "grad_entropy")
+    device = _place(logits, targets, grad_logprob, grad_entropy, out)
     if out is None:
-        # rows that lie in their 16 bytes as those of the logits do, so that both are accessed in whole vectors
-        stride = vocab + (x.stride(0) - vocab) % (16 // x.element_size()) if rows > 1 else vocab
-        if stride == vocab:
-            out = torch.empty(logits.shape, dtype=x.dtype, device=x.device)
-            dx = out.view(-1, vocab)
-        else:
-            dx = torch.empty_strided((rows, vocab), (stride, 1), dtype=x.dtype, device=x.device)
-            out = dx.view(logits.shape)
-    else:
-        if out.shape != logits.shape or out.dtype != logits.dtype:
-            raise ValueError("out has the logits' shape and type")
-        dx = _rows(out)
-        stride = dx.stride(0) if rows > 1 else vocab
-    new = dict(device=x.device, dtype=torch.float32)
-    logprob = None if targets is None else torch.empty(shape, **new)
-    entropy = torch.empty(shape, **new)
-    desc = _logprob_desc(x, scale, ignore_index, 0, stride)
-    B._check(B.lib().asi_token_logprobs_grad(desc, x.data_ptr(), _ptr(targets), _ptr(grad_logprob), _ptr(grad_entropy),
-                                             dx.data_ptr(), _ptr(logprob), entropy.data_ptr(), _stream(device)),
-             "asi_token_logprobs_grad")
+        out = logits.new_empty(logits.shape) if new is None else logits.new_empty_strided(*new)
+    logprob = None if targets is None else logits.new_empty(shape, dtype=torch.float32)
+    entropy = logits.new_empty(shape, dtype=torch.float32)
+    status = B.lib().asi_token_logprobs_grad(desc, logits.data_ptr(), _ptr(targets), _ptr(grad_logprob), _ptr(grad_entropy),
+                                             out.data_ptr(), _ptr(logprob), entropy.data_ptr(), _stream(device))
+    if status:
+        B._check(status, "asi_token_logprobs_grad")
     return TokenLogprobsGrad(logprob, entropy, out)
 
 
 # ---- embedding --------------------------------------------------------------------------------------------
-def _matrix(t: torch.Tensor, what: str) -> torch.Tensor:
-    if t.dim() != 2 or t.shape[1] < 1 or (t.stride(1) != 1 and t.shape[1] > 1):
+def _matrix(geometry, what: str) -> int:
+    """The distance of a matrix's rows."""
+    shape, stride, _ = geometry
+    if len(shape) != 2 or shape[1] < 1 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError(f"{what} is a matrix whose rows' entries are next to each other")
-    return t
+    return stride[0] if shape[0] > 1 else shape[1]
 
 
-def _row_stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+@_plans
+def _embedding_plan(shape, table, scale, dtype):
+    vocab, dim = table[0][0], table[0][-1]
+    desc = B.EmbeddingDesc(shape.numel(), vocab, dim, _matrix(table, "table"), dim, -1, _dtype(table[2], "table"),
+                           _dtype(dtype, "the result"), scale, 0)
+    return desc, shape + (dim,)
 
 
 def _embedding(tokens, table, scale, dtype) -> torch.Tensor:
     tokens = _whole(tokens, "tokens")
-    _matrix(table, "table")
+    dtype = dtype or table.dtype
+    desc, shape = _embedding_plan(tokens.shape, _geometry(table), scale, dtype)
     device = _place(tokens, table)
-    vocab, dim = table.shape
-    out = torch.empty(tokens.shape + (dim,), dtype=dtype or table.dtype, device=table.device)
-    desc = B.EmbeddingDesc(tokens.numel(), vocab, dim, _row_stride(table), dim, -1, _dtype(table, "table"), _dtype(out, "the result"),
-                           scale, 0)
-    B._check(B.lib().asi_embedding(desc, tokens.data_ptr(), table.data_ptr(), out.data_ptr(), _stream(device)), "asi_embedding")
+    out = table.new_empty(shape, dtype=dtype)
+    status = B.lib().asi_embedding(desc, tokens.data_ptr(), table.data_ptr(), out.data_ptr(), _stream(device))
+    if status:
+        B._check(status, "asi_embedding")
     return out
 
 
@@ -242,30 +277,46 @@ def embedding_grad(tokens: torch.Tensor, grad_out: torch.Tensor, vocab: int, *, 
     """Gradient of the table of embedding(): (vocab, dim) in `dtype`, or written to `out`; with `accumulate` added to it,
     which leaves rows without a token alone.  Sums are in fp32 and in the order of the tokens: equal calls, equal bits."""
     tokens = _whole(tokens, "tokens")
-    if grad_out.shape[:-1] != tokens.shape or grad_out.dim() < 1:
-        raise ValueError("grad_out has the tokens' shape and one more dimension")
-    dim = grad_out.shape[-1]
     if grad_out.dim() != 2:
-        grad_out = grad_out.reshape(-1, dim)
-    if grad_out.stride(1) != 1 or (grad_out.shape[0] > 1 and grad_out.stride(0) < dim):
-        grad_out = grad_out.contiguous()
+        if grad_out.dim() < 1 or grad_out.shape[:-1] != tokens.shape:
+            raise ValueError("grad_out has the tokens' shape and one more dimension")
+        grad_out = grad_out.reshape(tokens.numel(), grad_out.shape[-1])
     if accumulate and out is None:
         raise ValueError("accumulate adds to `out`")
-    if out is None:
-        out = torch.empty((vocab, dim), dtype=dtype, device=grad_out.device)
-    elif out.shape != (vocab, dim):
-        raise ValueError(f"out is ({vocab}, {dim})")
-    _matrix(out, "out")
+    desc, nbytes, dense, shape = _embedding_grad_plan(tokens.shape, _geometry(grad_out), vocab, scale, padding_idx, dtype, _geometry(out))
+    if not dense:
+        grad_out = grad_out.contiguous()
     device = _place(tokens, grad_out, out)
+    if out is None:
+        out = grad_out.new_empty(shape, dtype=dtype)
+    ws = _scratch(nbytes, grad_out)
+    status = B.lib().asi_embedding_grad(desc, tokens.data_ptr(), grad_out.data_ptr(), out.data_ptr(), int(accumulate), _ptr(ws), nbytes,
+                                        _stream(device))
+    if status:
+        B._check(status, "asi_embedding_grad")
+    return out
+
+
+@_plans
+def _embedding_grad_plan(tokens, grad_out, vocab, scale, padding_idx, dtype, out):
+    """Descriptor, scratch, whether grad_out can be taken as it lies, shape of a new result."""
+    n = tokens.numel()
+    shape, stride, grad_dtype = grad_out
+    if shape[0] != n:
+        raise ValueError("grad_out has the tokens' shape and one more dimension")
+    dim = shape[1]
+    taken = (stride[1] == 1 or dim == 1) and (n <= 1 or stride[0] >= dim)
+    if out is not None:
+        if out[0] != (vocab, dim):
+            raise ValueError(f"out is ({vocab}, {dim})")
+        dtype, apart = out[2], _matrix(out, "out")
+    else:
+        apart = dim
     if padding_idx is not None and not 0 <= padding_idx < vocab:
         raise ValueError("padding_idx is a token of the table")
-    desc = B.EmbeddingDesc(tokens.numel(), vocab, dim, _row_stride(out), _row_stride(grad_out), -1 if padding_idx is None else padding_idx,
-                           _dtype(out, "the gradient"), _dtype(grad_out, "grad_out"), scale, 0)
-    L = B.lib()
-    ws = _scratch(L.asi_embedding_grad_workspace_bytes(desc), device)
-    B._check(L.asi_embedding_grad(desc, tokens.data_ptr(), grad_out.data_ptr(), out.data_ptr(), int(accumulate), _ptr(ws),
-                                  0 if ws is None else ws.numel(), _stream(device)), "asi_embedding_grad")
-    return out
+    desc = B.EmbeddingDesc(n, vocab, dim, apart, stride[0] if taken and n > 1 else dim, -1 if padding_idx is None else padding_idx,
+                           _dtype(dtype, "the gradient"), _dtype(grad_dtype, "grad_out"), scale, 0)
+    return desc, int(B.lib().asi_embedding_grad_workspace_bytes(desc)), taken, (vocab, dim)
 
 
 # ---- norms of queries and keys with the position rotation -----------------------------------------------------
@@ -276,66 +327,68 @@ def rotary_table(length: int, rot_dim: int, base: float = 10000.0, device="cuda"
     return angle.cos().float(), angle.sin().float()
 
 
-def _heads(t: torch.Tensor, what: str) -> torch.Tensor:
-    if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] > 1):
-        raise ValueError(f"{what} is (batch, tokens, heads, head_dim), a head's entries next to each other")
-    return t
-
-
-def _qk_desc(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved):
-    _heads(q, "q")
-    _heads(k, "k")
-    batch, tokens, hq, dim = q.shape
-    if k.shape[0] != batch or k.shape[1] != tokens or k.shape[3] != dim or k.dtype != q.dtype:
-        raise ValueError("q and k have the same batch, tokens, head_dim and type")
-    gain = None
-    for g in (q_gain, k_gain):
-        if g is not None:
-            if g.shape != (dim,) or not g.is_contiguous() or (gain is not None and gain.dtype != g.dtype):
-                raise ValueError("the gains are contiguous tensors of head_dim entries, both of one type")
-            gain = g
-    if cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32 or \
-            not (cos.is_contiguous() and sin.is_contiguous()):
-        raise ValueError("cos and sin are contiguous fp32 tables (positions, rot_dim / 2)")
-    stride = 0
-    if positions is not None:
-        if positions.dtype != torch.int64:
-            raise TypeError("positions are int64")
-        if positions.shape == (tokens,):
-            positions = positions.contiguous()
-        elif positions.shape == (batch, tokens):
-            if positions.stride(1) != 1 or positions.stride(0) < 0:
-                positions = positions.contiguous()
-            stride = positions.stride(0) if batch > 1 else 0
-        else:
-            raise ValueError("positions are (tokens) or (batch, tokens)")
-    desc = B.QkDesc()
-    desc.batch, desc.tokens, desc.max_position, desc.position_stride = batch, tokens, cos.shape[0], stride
-    desc.q_stride[:], desc.k_stride[:] = q.stride()[:3], k.stride()[:3]
-    desc.q_heads, desc.k_heads, desc.head_dim, desc.rot_dim = hq, k.shape[2], dim, 2 * cos.shape[1]
-    desc.interleaved, desc.dtype, desc.eps = bool(interleaved), _dtype(q, "q"), eps
-    desc.gain_dtype = B.ASI_F32 if gain is None else _dtype(gain, "a gain")
-    return desc, positions
-
-
-def _out_strides(t: torch.Tensor, heads_first: bool):
-    a, b, c, _ = t.stride()
-    return (a, c, b) if heads_first else (a, b, c)
-
-
-def _head_shape(x: torch.Tensor, heads_first: bool):
-    b, t, h, d = x.shape
+def _head_shape(shape, heads_first: bool):
+    b, t, h, d = shape
     return (b, h, t, d) if heads_first else (b, t, h, d)
 
 
+def _strides(geometry, heads_first: bool, what: str):
+    """(batch, token, head) distances of a tensor of heads."""
+    shape, stride, _ = geometry
+    if len(shape) != 4 or (stride[3] != 1 and shape[3] > 1):
+        raise ValueError(f"{what} has four dimensions, a head's entries next to each other")
+    return (stride[0], stride[2], stride[1]) if heads_first else stride[:3]
+
+
+def _qk_desc(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved) -> B.QkDesc:
+    """The descriptor of these geometries, the results' strides not yet in it."""
+    desc = B.QkDesc()
+    desc.q_stride[:], desc.k_stride[:] = _strides(q, False, "q"), _strides(k, False, "k")
+    batch, tokens, heads, dim = q[0]
+    if k[0][0] != batch or k[0][1] != tokens or k[0][3] != dim or k[2] != q[2]:
+        raise ValueError("q and k have the same batch, tokens, head_dim and type")
+    gains = [g for g in (q_gain, k_gain) if g is not None]
+    if any(g[0] != (dim,) or not _dense(*g[:2]) or g[2] != gains[0][2] for g in gains):
+        raise ValueError("the gains are contiguous tensors of head_dim entries, both of one type")
+    if len(cos[0]) != 2 or cos[0] != sin[0] or any(c[2] != torch.float32 or not _dense(*c[:2]) for c in (cos, sin)):
+        raise ValueError("cos and sin are contiguous fp32 tables (positions, rot_dim / 2)")
+    if positions is not None:
+        shape, stride, dtype = positions
+        if dtype != torch.int64:
+            raise TypeError("positions are int64")
+        if shape not in ((tokens,), (batch, tokens)) or (tokens > 1 and stride[-1] != 1):
+            raise ValueError("positions are (tokens) or (batch, tokens), those of a batch entry next to each other")
+        desc.position_stride = stride[0] if len(shape) == 2 and batch > 1 else 0
+    desc.batch, desc.tokens, desc.max_position = batch, tokens, cos[0][0]
+    desc.q_heads, desc.k_heads, desc.head_dim, desc.rot_dim = heads, k[0][2], dim, 2 * cos[0][1]
+    desc.interleaved, desc.dtype, desc.eps = bool(interleaved), _dtype(q[2], "q"), eps
+    desc.gain_dtype = _dtype(gains[0][2], "a gain") if gains else B.ASI_F32
+    return desc
+
+
+def _lying(shape):
+    """Strides of a new tensor of heads."""
+    _, b, c, d = shape
+    return b * c * d, c * d, d, 1
+
+
+@_plans
+def _qk_plan(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, heads_first):
+    desc = _qk_desc(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
+    shapes = [_head_shape(x[0], heads_first) for x in (q, k)]
+    desc.q_out_stride[:], desc.k_out_stride[:] = (_strides((s, _lying(s), None), heads_first, "") for s in shapes)
+    return desc, *shapes
+
+
 def _qk_norm_rotate(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, heads_first):
-    desc, positions = _qk_desc(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
+    desc, q_shape, k_shape = _qk_plan(_geometry(q), _geometry(k), _geometry(q_gain), _geometry(k_gain), _geometry(cos), _geometry(sin),
+                                      _geometry(positions), eps, interleaved, heads_first)
     device = _place(q, k, q_gain, k_gain, cos, sin, positions)
-    q_out = torch.empty(_head_shape(q, heads_first), dtype=q.dtype, device=q.device)
-    k_out = torch.empty(_head_shape(k, heads_first), dtype=q.dtype, device=q.device)
-    desc.q_out_stride[:], desc.k_out_stride[:] = _out_strides(q_out, heads_first), _out_strides(k_out, heads_first)
-    B._check(B.lib().asi_qk_norm_rotate(desc, q.data_ptr(), k.data_ptr(), _ptr(q_gain), _ptr(k_gain), _ptr(positions), cos.data_ptr(),
-                                        sin.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), _stream(device)), "asi_qk_norm_rotate")
+    q_out, k_out = q.new_empty(q_shape), k.new_empty(k_shape)
+    status = B.lib().asi_qk_norm_rotate(desc, q.data_ptr(), k.data_ptr(), _ptr(q_gain), _ptr(k_gain), _ptr(positions), cos.data_ptr(),
+                                        sin.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), _stream(device))
+    if status:
+        B._check(status, "asi_qk_norm_rotate")
     return q_out, k_out
 
 
@@ -368,36 +421,50 @@ def qk_norm_rotate(q: torch.Tensor, k: torch.Tensor, q_gain: Optional[torch.Tens
     return _qk_norm_rotate(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, heads_first)
 
 
+@_plans
+def _qk_grad_plan(q, k, q_gain, k_gain, cos, sin, positions, grad_q, grad_k, eps, interleaved, heads_first):
+    desc = _qk_desc(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
+    for g, x, what in ((grad_q, q, "grad_q"), (grad_k, k, "grad_k")):
+        if g[0] != _head_shape(x[0], heads_first) or g[2] != x[2]:
+            raise ValueError(f"{what} has the result's shape and type")
+    desc.q_out_stride[:], desc.k_out_stride[:] = _strides(grad_q, heads_first, "grad_q"), _strides(grad_k, heads_first, "grad_k")
+    desc.dq_stride[:], desc.dk_stride[:] = _lying(q[0])[:3], _lying(k[0])[:3]
+    return desc, int(B.lib().asi_qk_norm_rotate_grad_workspace_bytes(desc))
+
+
 def qk_norm_rotate_grad(q, k, q_gain, k_gain, cos, sin, grad_q: torch.Tensor, grad_k: torch.Tensor, positions=None, *,
                         eps: float = 1e-6, interleaved: bool = False, heads_first: bool = False):
     """Gradients (dq, dk, dq_gain, dk_gain) of qk_norm_rotate from those of its results.  dq and dk are contiguous in the
     shape of q and k, the gains' gradients fp32 whether or not there are gains."""
-    desc, positions = _qk_desc(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved)
-    for g, x, what in ((grad_q, q, "grad_q"), (grad_k, k, "grad_k")):
-        if g.shape != _head_shape(x, heads_first) or g.dtype != x.dtype:
-            raise ValueError(f"{what} has the result's shape and type")
-    grad_q, grad_k = (g if g.stride(3) == 1 or g.shape[3] == 1 else g.contiguous() for g in (grad_q, grad_k))
+    if grad_q.dim() == 4 and grad_q.stride(3) != 1:
+        grad_q = grad_q.contiguous()
+    if grad_k.dim() == 4 and grad_k.stride(3) != 1:
+        grad_k = grad_k.contiguous()
+    desc, nbytes = _qk_grad_plan(_geometry(q), _geometry(k), _geometry(q_gain), _geometry(k_gain), _geometry(cos), _geometry(sin),
+                                 _geometry(positions), _geometry(grad_q), _geometry(grad_k), eps, interleaved, heads_first)
     device = _place(q, k, q_gain, k_gain, cos, sin, positions, grad_q, grad_k)
-    dq, dk = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
-    dqg, dkg = (torch.empty(q.shape[3], dtype=torch.float32, device=q.device) for _ in range(2))
-    desc.q_out_stride[:], desc.k_out_stride[:] = _out_strides(grad_q, heads_first), _out_strides(grad_k, heads_first)
-    desc.dq_stride[:], desc.dk_stride[:] = dq.stride()[:3], dk.stride()[:3]
-    L = B.lib()
-    ws = _scratch(L.asi_qk_norm_rotate_grad_workspace_bytes(desc), device)
-    B._check(L.asi_qk_norm_rotate_grad(desc, q.data_ptr(), k.data_ptr(), _ptr(q_gain), _ptr(k_gain), _ptr(positions), cos.data_ptr(),
-                                       sin.data_ptr(), grad_q.data_ptr(), grad_k.data_ptr(), dq.data_ptr(), dk.data_ptr(), dqg.data_ptr(),
-                                       dkg.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(), _stream(device)),
-             "asi_qk_norm_rotate_grad")
+    dq, dk = q.new_empty(q.shape), k.new_empty(k.shape)
+    dqg, dkg = (q.new_empty(q.shape[3], dtype=torch.float32) for _ in range(2))
+    ws = _scratch(nbytes, q)
+    status = B.lib().asi_qk_norm_rotate_grad(desc, q.data_ptr(), k.data_ptr(), _ptr(q_gain), _ptr(k_gain), _ptr(positions), cos.data_ptr(),
+                                             sin.data_ptr(), grad_q.data_ptr(), grad_k.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+                                             dqg.data_ptr(), dkg.data_ptr(), _ptr(ws), nbytes, _stream(device))
+    if status:
+        B._check(status, "asi_qk_norm_rotate_grad")
     return dq, dk, dqg, dkg
 
 
 # ---- AdamW ------------------------------------------------------------------------------------------------
+_EXP_AVG, _NBYTES = operator.itemgetter("exp_avg"), operator.attrgetter("nbytes")
+
+
 class _Plan:
     """The records of a group's tensors, kept between steps: only parameters' and gradients' addresses are read anew."""
 
     def __init__(self, params, states, grads, bits):
         self.params, self.grads = params, grads
         self.first = [s["exp_avg"] for s in states]
+        self.sizes = [p.nbytes for p in params]
         self.states = states
         self.records = (B.AdamwTensor * max(1, len(params)))()
         words = C.sizeof(B.AdamwTensor) // 8
@@ -412,9 +479,11 @@ class _Plan:
             r.count, r.param_dtype, r.grad_dtype = p.numel(), _DTYPE[p.dtype], _DTYPE[g.dtype]
 
     def serves(self, params, grads) -> bool:
-        return len(params) == len(self.params) and all(a is b for a, b in zip(params, self.params)) and \
-            all(a is b or a.dtype == b.dtype for a, b in zip(grads, self.grads)) and \
-            all(s["exp_avg"] is a for s, a in zip(self.states, self.first))
+        # a parameter's data may have been replaced, in another type or memory format
+        return len(params) == len(self.params) and all(map(operator.is_, params, self.params)) and \
+            list(map(_NBYTES, params)) == self.sizes and all(map(torch.Tensor.is_contiguous, params)) and \
+            all(map(operator.is_, map(_EXP_AVG, self.states), self.first)) and \
+            (all(map(operator.is_, grads, self.grads)) or all(a.dtype == b.dtype for a, b in zip(grads, self.grads)))
 
 
 class AdamW(torch.optim.Optimizer):
@@ -453,9 +522,9 @@ class AdamW(torch.optim.Optimizer):
 
     def _state(self, p: torch.Tensor, bits: int, master: bool) -> dict:
         s = self.state[p]
+        if p.dtype not in _DTYPE or not p.is_contiguous():
+            raise TypeError("parameters are contiguous and fp32 or bf16")
         if "exp_avg" not in s:
-            if p.dtype not in _DTYPE or not p.is_contiguous():
-                raise TypeError("parameters are contiguous and fp32 or bf16")
             held = torch.float32 if bits == 32 else torch.float8_e4m3fn
             zeros = lambda shape, dtype: torch.zeros(shape, dtype=torch.uint8 if dtype.itemsize == 1 else dtype,  # noqa: E731
                                                      device=p.device).view(dtype)
@@ -484,14 +553,12 @@ class AdamW(torch.optim.Optimizer):
                 raise ValueError("grad_scale is an fp32 and skip an int32 tensor of one entry")
         if grads is not None and len(grads) != sum(len(g["params"]) for g in self.param_groups):
             raise ValueError("one gradient (or None) for each parameter")
-        device = _place(grad_scale, skip)
-        stream = _stream(device)
         at = 0
         for n, group in enumerate(self.param_groups):
             members = group["params"]
             given = [p.grad for p in members] if grads is None else grads[at:at + len(members)]
             at += len(members)
-            if any(g is None for g in given):
+            if not all(map(operator.is_not, given, itertools.repeat(None))):
                 members = [p for p, g in zip(members, given) if g is not None]
                 given = [g for g in given if g is not None]
             if not members:
@@ -499,17 +566,18 @@ class AdamW(torch.optim.Optimizer):
             bits = group["state_bits"]
             plan = self._plans.get(n)
             if plan is None or not plan.serves(members, given):
-                _place(*members)
+                _place(*members, grad_scale, skip)
                 states = [self._state(p, bits, group["master"]) for p in members]
                 _place(*[t for s in states for t in s.values() if isinstance(t, torch.Tensor)])
                 plan = self._plans[n] = _Plan(list(members), states, list(given), bits)
                 self._check_grads(plan, given, True)
             else:
                 self._check_grads(plan, given, False)
-            plan.words[:, 0] = [p.data_ptr() for p in members]
-            plan.words[:, 1] = [g.data_ptr() for g in plan.grads]
+            plan.words[:, 0] = list(map(torch.Tensor.data_ptr, members))
+            plan.words[:, 1] = list(map(torch.Tensor.data_ptr, plan.grads))
             plan.reals[:, -2] = group["lr"]
             plan.reals[:, -1] = group["weight_decay"]
+            stream = _stream(_place(members[0], grad_scale, skip))
             group["step"] += 1
             b1, b2 = group["betas"]
             B._check(B.lib().asi_adamw(len(members), C.addressof(plan.records), bits, b1, b2, group["eps"], group["step"],
@@ -518,6 +586,8 @@ class AdamW(torch.optim.Optimizer):
 
     @staticmethod
     def _check_grads(plan: _Plan, given: List[torch.Tensor], fresh: bool) -> None:
+        if not fresh and all(map(operator.is_, given, plan.grads)):
+            return
         for i, (g, p) in enumerate(zip(given, plan.params)):
             if g is plan.grads[i] and not fresh:
                 continue

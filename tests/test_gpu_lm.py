@@ -505,7 +505,7 @@ def test_qk_norm_rotate_in_place_and_packed_gradients():
         a, b = buf[..., :6 * 64].unflatten(-1, (6, 64)), buf[..., 6 * 64:8 * 64].unflatten(-1, (2, 64))
         a.copy_(q), b.copy_(k)
         buf[..., 8 * 64:] = 5
-        desc, _ = lm._qk_desc(a, b, gq, gk, cos, sin, positions, 1e-6, False)
+        desc = lm._qk_desc(*map(lm._geometry, (a, b, gq, gk, cos, sin, positions)), 1e-6, False)
         desc.q_out_stride[:], desc.k_out_stride[:] = a.stride()[:3], b.stride()[:3]
         st = torch.cuda.current_stream().cuda_stream
         p = lambda t: t.data_ptr()  # noqa: E731
@@ -669,6 +669,30 @@ def test_adamw_skip_groups_and_missing_gradients():
     b.grad = torch.ones_like(b)
     opt.step()
     assert (b != 1).all()
+
+
+def test_adamw_follows_replaced_data():
+    """Parameters and gradients whose data is exchanged between steps, as conversions of a model do."""
+    p = torch.nn.Parameter(torch.ones(1000, device="cuda"))
+    p.grad = torch.ones_like(p)
+    opt = asi.AdamW([p], lr=0.5, weight_decay=0.0)
+    opt.step()
+    kept = p.data
+    old = kept.clone()
+    p.data = torch.full((1000,), 3.0, device="cuda")
+    p.grad = torch.ones_like(p)
+    opt.step()
+    assert torch.equal(kept, old) and (p.data < 3.0).all()
+    p.grad = None
+    p.data = p.data.to(torch.bfloat16)
+    p.grad = torch.ones_like(p)
+    before = p.data.clone()
+    opt.step()
+    assert (p.data < before).all()
+    p.data = torch.ones(10, 4, 5, 5, device="cuda").to(memory_format=torch.channels_last)
+    p.grad = torch.ones_like(p)
+    with pytest.raises(TypeError):
+        opt.step()
 
 
 @pytest.mark.parametrize("bits", [32, 8])
