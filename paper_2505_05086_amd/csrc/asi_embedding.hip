@@ -7,7 +7,8 @@
 // token changes.  A token whose entries cross the end of a run leaves partial rows in scratch, which a second kernel adds in the
 // order of the runs.  So a token that makes up most of a batch costs what any other share of it costs, no sum depends on the order
 // in which workgroups run, and every row of the result is written once: the workgroups behind those of the runs fill
-// the rows without a token with zeros.
+// the rows without a token with zeros.  Few tokens take one launch without scratch: a workgroup for each position looks for
+// the positions of its token, and adds up their rows if its own is the first.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -351,7 +352,20 @@ __device__ __forceinline__ int lower_bound(const uint32_t* key, int n, uint32_t 
     }
     return lo;
 }
-template <typename D> __device__ __forceinline__ void write_zeros(const SumArgs& a) {
+// Zeros into the rows of this workgroup's kFillRows that have no token
+template <typename D> __device__ __forceinline__ void write_zeros(const SumArgs& a, uint32_t v0, int rows, const uint32_t* present) {
+    constexpr int N = Vec16<D>::N;
+    for (int r = 0; r < rows; ++r) {
+        if (present[r]) continue;
+        D* dst = static_cast<D*>(a.dtable) + (long long)(v0 + r) * a.table_stride;
+        if (a.vec) {
+            for (int d = threadIdx.x * N; d < a.dim; d += kThreads * N) *reinterpret_cast<uint4*>(dst + d) = make_uint4(0, 0, 0, 0);
+        } else {
+            for (int d = threadIdx.x; d < a.dim; d += kThreads) dst[d] = from_f32<D>(0.f);
+        }
+    }
+}
+template <typename D> __device__ __forceinline__ void fill(const SumArgs& a) {
     __shared__ uint32_t present[kFillRows];
     __shared__ int range[2];
     const uint32_t v0 = (uint32_t)(blockIdx.x - a.run_blocks) * kFillRows;
@@ -365,19 +379,10 @@ template <typename D> __device__ __forceinline__ void write_zeros(const SumArgs&
     __syncthreads();
     for (int e = range[0] + threadIdx.x; e < range[1]; e += kThreads) present[a.key[e] - v0] = 1;   // every writer writes the same
     __syncthreads();
-    constexpr int N = Vec16<D>::N;
-    for (int r = 0; r < rows; ++r) {
-        if (present[r]) continue;
-        D* dst = static_cast<D*>(a.dtable) + (long long)(v0 + r) * a.table_stride;
-        if (a.vec) {
-            for (int d = threadIdx.x * N; d < a.dim; d += kThreads * N) *reinterpret_cast<uint4*>(dst + d) = make_uint4(0, 0, 0, 0);
-        } else {
-            for (int d = threadIdx.x; d < a.dim; d += kThreads) dst[d] = from_f32<D>(0.f);
-        }
-    }
+    write_zeros<D>(a, v0, rows, present);
 }
 template <typename O, typename D, int C, int P, bool ADD> __global__ __launch_bounds__(kThreads) void k_sum(const SumArgs a) {
-    if ((int)blockIdx.x >= a.run_blocks) write_zeros<D>(a);
+    if ((int)blockIdx.x >= a.run_blocks) fill<D>(a);
     else sum_run<O, D, C, P, ADD>(a);
 }
 // Adds up the partial rows of tokens that cross the ends of runs, of every token in the order of the runs.  A workgroup has 8 runs and
@@ -446,6 +451,92 @@ template <typename D> __global__ __launch_bounds__(kJoinThreads) void k_join(con
     }
 }
 
+// ---- gradient of few tokens ------------------------------------------------------------------------------------
+// Workgroups of positions, each with a tile of columns, before those that write zeros.  The four waves share the positions of the token.
+constexpr int kFew = 512, kFewWaves = kThreads / 64;
+template <typename O, typename D, int C, int P, bool ADD> __global__ __launch_bounds__(kThreads) void k_few(const SumArgs a, const SortArgs s) {
+    __shared__ uint32_t key[kFew];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int j = threadIdx.x; j < s.n; j += kThreads) key[j] = key_of(s, s.tokens[j]);
+    if ((int)blockIdx.x >= a.run_blocks) {
+        __shared__ uint32_t present[kFillRows];
+        const uint32_t v0 = (uint32_t)(blockIdx.x - a.run_blocks) * kFillRows;
+        const int rows = (int)min((uint32_t)kFillRows, a.vocab - v0);
+        if (threadIdx.x < kFillRows) present[threadIdx.x] = 0;
+        __syncthreads();
+        for (int j = threadIdx.x; j < s.n; j += kThreads)
+            if (const uint32_t k = key[j] - v0; k < (uint32_t)rows) present[k] = 1;
+        __syncthreads();
+        write_zeros<D>(a, v0, rows, present);
+        return;
+    }
+    __shared__ int list[kFew];
+    __shared__ float sums[kFewWaves][P * C][64];
+    const int i = blockIdx.x / a.column_tiles, tile = blockIdx.x - i * a.column_tiles;
+    __syncthreads();
+    const uint32_t token = key[i];
+    int n = 0;
+    bool first = token < a.vocab;
+    for (int base = 0; base < s.n && first; base += 64) {
+        const int j = base + lane;
+        const bool same = j < s.n && key[j] == token;
+        const unsigned long long with = __ballot(same);
+        if (__ballot(same && j < i)) first = false;
+        if (same && wave == 0) list[n + lanes_below(with)] = j;
+        n += __popcll(with);
+    }
+    if (!first) return;                  // the same in all waves
+    __syncthreads();
+    const int d = tile * a.columns + lane * C, apart = 64 * C;
+    int col[P];                          // a piece behind the row's end reads the row's first columns and writes nothing
+    bool has[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        has[p] = d + p * apart < a.dim;
+        col[p] = has[p] ? d + p * apart : 0;
+    }
+    float acc[P][C], old[P][C];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        if (ADD && wave == 0) load_result<D, C>(a, token, col[p], old[p]);
+#pragma unroll
+        for (int k = 0; k < C; ++k) acc[p][k] = 0.f;
+    }
+    const int share = (n + kFewWaves - 1) / kFewWaves, begin = wave * share, end = min(n, begin + share);
+    const O* dout = static_cast<const O*>(a.dout);
+    constexpr int U = 8;
+    for (int e0 = begin; e0 < end; e0 += U) {
+        Columns<O, C> v[U][P];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const O* row = dout + (long long)list[min(e0 + u, end - 1)] * a.out_stride;
+#pragma unroll
+            for (int p = 0; p < P; ++p) v[u][p].load(row + col[p]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (e0 + u < end) {
+#pragma unroll
+                for (int p = 0; p < P; ++p) v[u][p].add_to(acc[p]);
+            }
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int k = 0; k < C; ++k) sums[wave][p * C + k][lane] = acc[p][k];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            for (int w = 1; w < kFewWaves; ++w) acc[p][k] += sums[w][p * C + k][lane];
+            acc[p][k] = ADD ? acc[p][k] * a.scale + old[p][k] : acc[p][k] * a.scale;
+        }
+        if (has[p]) store_result<D, C>(a, token, col[p], acc[p]);
+    }
+}
+
 // ---- host ----
 asi_status check(const asi_embedding_desc* d) {
     if (!d) return ASI_ERR_INVALID_ARG;
@@ -488,23 +579,26 @@ template <typename O, typename D> struct Shape {
     static constexpr int C = sizeof(D) == 2 && sizeof(O) == 2 ? 8 : 4, P = sizeof(O) < sizeof(D) ? 2 : 1;
 };
 constexpr int kLoose = 4;             // pieces of a lane where they are single columns
-template <typename O, typename D> void sum(SumArgs a, bool vec, int fill_blocks, hipStream_t st) {
-    constexpr int C = Shape<O, D>::C, P = Shape<O, D>::P;
-    const int n = vec ? C * P : kLoose;
-    a.lanes = kLeastLanes;
-    while (a.lanes < kThreads && a.lanes * n < a.dim) a.lanes *= 2;
-    a.columns = a.lanes * n;
+template <typename O, typename D, int C, int P> void sum(SumArgs a, const SortArgs& s, int fill_blocks, hipStream_t st) {
+    const bool few = a.n <= kFew;
+    a.lanes = few ? 64 : kLeastLanes;
+    while (!few && a.lanes < kThreads && a.lanes * C * P < a.dim) a.lanes *= 2;
+    a.columns = a.lanes * C * P;
     a.column_tiles = (a.dim + a.columns - 1) / a.columns;
     const int groups = kThreads / a.lanes;
-    a.run_blocks = (a.runs + groups - 1) / groups * a.column_tiles;
+    a.run_blocks = (few ? a.n : (a.runs + groups - 1) / groups) * a.column_tiles;
     const dim3 grid((unsigned)(a.run_blocks + fill_blocks));
-    if (vec) {
+    if (few) {
+        if (a.accumulate) hipLaunchKernelGGL((k_few<O, D, C, P, true>), grid, kThreads, 0, st, a, s);
+        else hipLaunchKernelGGL((k_few<O, D, C, P, false>), grid, kThreads, 0, st, a, s);
+    } else {
         if (a.accumulate) hipLaunchKernelGGL((k_sum<O, D, C, P, true>), grid, kThreads, 0, st, a);
         else hipLaunchKernelGGL((k_sum<O, D, C, P, false>), grid, kThreads, 0, st, a);
-    } else {
-        if (a.accumulate) hipLaunchKernelGGL((k_sum<O, D, 1, kLoose, true>), grid, kThreads, 0, st, a);
-        else hipLaunchKernelGGL((k_sum<O, D, 1, kLoose, false>), grid, kThreads, 0, st, a);
     }
+}
+template <typename O, typename D> void sum(const SumArgs& a, const SortArgs& s, bool vec, int fill_blocks, hipStream_t st) {
+    if (vec) sum<O, D, Shape<O, D>::C, Shape<O, D>::P>(a, s, fill_blocks, st);
+    else sum<O, D, 1, kLoose>(a, s, fill_blocks, st);
 }
 
 }  // namespace
@@ -539,7 +633,7 @@ asi_status asi_embedding(const asi_embedding_desc* desc, const int64_t* tokens, 
 }
 
 size_t asi_embedding_grad_workspace_bytes(const asi_embedding_desc* desc) {
-    if (check(desc) != ASI_OK || desc->tokens == 0) return 0;
+    if (check(desc) != ASI_OK || desc->tokens <= kFew) return 0;
     return plan(desc).bytes;
 }
 
@@ -550,14 +644,17 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
     if (!dtable || !aligned(dtable, ds)) return ASI_ERR_INVALID_ARG;
     if (desc->tokens && (!tokens || !grad_out || !aligned(tokens, 8) || !aligned(grad_out, os))) return ASI_ERR_INVALID_ARG;
     const GradPlan p = plan(desc);
-    if (desc->tokens && (!ws || !aligned(ws, 256) || ws_bytes < p.bytes)) return ASI_ERR_WORKSPACE;
+    const bool few = desc->tokens <= kFew;
+    if (!few && (!ws || !aligned(ws, 256) || ws_bytes < p.bytes)) return ASI_ERR_WORKSPACE;
     if (desc->tokens == 0 && accumulate) return ASI_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* w = static_cast<char*>(ws);
     SumArgs a{};
-    a.key = reinterpret_cast<uint32_t*>(w + p.key);
-    a.pos = reinterpret_cast<uint32_t*>(w + p.pos);
-    a.part = reinterpret_cast<float*>(w + p.part);
+    if (!few) {
+        a.key = reinterpret_cast<uint32_t*>(w + p.key);
+        a.pos = reinterpret_cast<uint32_t*>(w + p.pos);
+        a.part = reinterpret_cast<float*>(w + p.part);
+    }
     a.dout = grad_out; a.dtable = dtable;
     a.out_stride = desc->out_stride; a.table_stride = desc->table_stride;
     a.vocab = (uint32_t)desc->vocab;
@@ -571,26 +668,27 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
     const int fill_blocks = accumulate ? 0 : (int)((desc->vocab + kFillRows - 1) / kFillRows);
     const int tiles = (a.dim + 63) / 64;
     // an upper bound of the workgroups of either launch
-    if ((long long)p.runs * tiles + fill_blocks > 0x7fffffffLL) return ASI_ERR_UNSUPPORTED;
-    if (desc->tokens) {
+    if ((long long)std::max(p.runs, kFew) * tiles + fill_blocks > 0x7fffffffLL) return ASI_ERR_UNSUPPORTED;
+    SortArgs s{tokens, nullptr, nullptr, desc->padding_index, a.vocab, a.n, 0};
+    if (!few) {
         // about one workgroup a CU; the id `vocab` is one more
         const long long ids = desc->vocab + 1;
-        const int span = (int)std::min<long long>(kMaxSpan, (ids + 255) / 256);
-        const SortArgs s{tokens, reinterpret_cast<uint32_t*>(w + p.key), reinterpret_cast<uint32_t*>(w + p.pos), desc->padding_index, a.vocab, a.n, span};
+        s.key = reinterpret_cast<uint32_t*>(w + p.key);
+        s.pos = reinterpret_cast<uint32_t*>(w + p.pos);
+        s.span = (int)std::min<long long>(kMaxSpan, (ids + 255) / 256);
         constexpr size_t lists = (size_t)kSortWaves * kSortList * 8;
         static LdsAllowed allowed;
         if (allow_lds(reinterpret_cast<const void*>(k_sort), (size_t)kSortWaves * kMaxSpan * 4 + lists, allowed) != hipSuccess) return ASI_ERR_HIP;
-        const size_t lds = (size_t)kSortWaves * span * 4 + lists;
-        hipLaunchKernelGGL(k_sort, dim3((unsigned)((ids + span - 1) / span)), kSortThreads, lds, st, s);
+        hipLaunchKernelGGL(k_sort, dim3((unsigned)((ids + s.span - 1) / s.span)), kSortThreads, (size_t)kSortWaves * s.span * 4 + lists, st, s);
     }
     if (desc->out_dtype == ASI_F32) {
-        if (desc->table_dtype == ASI_F32) sum<float, float>(a, vec, fill_blocks, st);
-        else sum<float, bf16_t>(a, vec, fill_blocks, st);
+        if (desc->table_dtype == ASI_F32) sum<float, float>(a, s, vec, fill_blocks, st);
+        else sum<float, bf16_t>(a, s, vec, fill_blocks, st);
     } else {
-        if (desc->table_dtype == ASI_F32) sum<bf16_t, float>(a, vec, fill_blocks, st);
-        else sum<bf16_t, bf16_t>(a, vec, fill_blocks, st);
+        if (desc->table_dtype == ASI_F32) sum<bf16_t, float>(a, s, vec, fill_blocks, st);
+        else sum<bf16_t, bf16_t>(a, s, vec, fill_blocks, st);
     }
-    if (p.runs > 1) {
+    if (!few && p.runs > 1) {
         const dim3 grid((unsigned)((p.runs - 1 + kJoinRuns - 1) / kJoinRuns * tiles));
         if (desc->table_dtype == ASI_F32) hipLaunchKernelGGL(k_join<float>, grid, kJoinThreads, 0, st, a, tiles);
         else hipLaunchKernelGGL(k_join<bf16_t>, grid, kJoinThreads, 0, st, a, tiles);

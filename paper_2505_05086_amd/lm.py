@@ -465,6 +465,7 @@ class _Plan:
         self.params, self.grads = params, grads
         self.first = [s["exp_avg"] for s in states]
         self.sizes = [p.nbytes for p in params]
+        self.places = None
         self.states = states
         self.records = (B.AdamwTensor * max(1, len(params)))()
         words = C.sizeof(B.AdamwTensor) // 8
@@ -479,11 +480,15 @@ class _Plan:
             r.count, r.param_dtype, r.grad_dtype = p.numel(), _DTYPE[p.dtype], _DTYPE[g.dtype]
 
     def serves(self, params, grads) -> bool:
-        # a parameter's data may have been replaced, in another type or memory format
-        return len(params) == len(self.params) and all(map(operator.is_, params, self.params)) and \
-            list(map(_NBYTES, params)) == self.sizes and all(map(torch.Tensor.is_contiguous, params)) and \
-            all(map(operator.is_, map(_EXP_AVG, self.states), self.first)) and \
-            (all(map(operator.is_, grads, self.grads)) or all(a.dtype == b.dtype for a, b in zip(grads, self.grads)))
+        if len(params) != len(self.params) or not all(map(operator.is_, params, self.params)) or \
+                not all(map(operator.is_, map(_EXP_AVG, self.states), self.first)):
+            return False
+        places = list(map(torch.Tensor.data_ptr, params))
+        if places != self.places:            # a parameter's data was replaced: in another type or memory format?
+            if list(map(_NBYTES, params)) != self.sizes or not all(map(torch.Tensor.is_contiguous, params)):
+                return False
+            self.places = self.words[:, 0] = places
+        return all(map(operator.is_, grads, self.grads)) or all(a.dtype == b.dtype for a, b in zip(grads, self.grads))
 
 
 class AdamW(torch.optim.Optimizer):
@@ -571,9 +576,9 @@ class AdamW(torch.optim.Optimizer):
                 _place(*[t for s in states for t in s.values() if isinstance(t, torch.Tensor)])
                 plan = self._plans[n] = _Plan(list(members), states, list(given), bits)
                 self._check_grads(plan, given, True)
+                plan.serves(plan.params, plan.grads)
             else:
                 self._check_grads(plan, given, False)
-            plan.words[:, 0] = list(map(torch.Tensor.data_ptr, members))
             plan.words[:, 1] = list(map(torch.Tensor.data_ptr, plan.grads))
             plan.reals[:, -2] = group["lr"]
             plan.reals[:, -1] = group["weight_decay"]

@@ -69,12 +69,14 @@ def test_embedding_arguments():
         assert L.asi_embedding(_em(), *args, None) == INVALID
     assert L.asi_embedding(None, P, P, P, None) == INVALID
     assert L.asi_embedding(_em(tokens=0), None, None, None, None) == OK
-    need = L.asi_embedding_grad_workspace_bytes(_em())
-    assert need > 0 and need % 256 == 0
+    many = _em(tokens=1000)                                       # few tokens need no scratch
+    need = L.asi_embedding_grad_workspace_bytes(many)
+    assert need > 0 and need % 256 == 0 and L.asi_embedding_grad_workspace_bytes(_em()) == 0
     for ws, size in ((None, need), (P, need - 1), (P + 128, need)):
-        assert L.asi_embedding_grad(_em(), P, P, P, 0, ws, size, None) == WORKSPACE
+        assert L.asi_embedding_grad(many, P, P, P, 0, ws, size, None) == WORKSPACE
     for args in ((None, P, P), (P, None, P), (P, P, None), (P, P + 2, P)):
         assert L.asi_embedding_grad(_em(), *args, 0, P, need, None) == INVALID
+        assert L.asi_embedding_grad(many, *args, 0, P, need, None) == INVALID
     assert L.asi_embedding_grad(_em(tokens=0), None, None, P, 1, None, 0, None) == OK
 
 
