@@ -55,7 +55,7 @@ template <int E> struct Part {
 };
 template <typename T, int E> __device__ __forceinline__ void load(const T* p, const Part<E>& q, float* f) {
     if (q.vec) {
-        load_values<E>(p + q.at, f);
+        load_values_past<E>(p + q.at, f);
     } else {
 #pragma unroll
         for (int i = 0; i < E; ++i) f[i] = q.has(i) ? to_f32(p[q.index(i)]) : 0.f;
@@ -63,7 +63,7 @@ template <typename T, int E> __device__ __forceinline__ void load(const T* p, co
 }
 template <typename T, int E> __device__ __forceinline__ void store(T* p, const Part<E>& q, const float* f) {
     if (q.vec) {
-        store_values<E>(p + q.at, f);
+        store_values_past<E>(p + q.at, f);
     } else {
 #pragma unroll
         for (int i = 0; i < E; ++i)
@@ -73,7 +73,11 @@ template <typename T, int E> __device__ __forceinline__ void store(T* p, const P
 // 8 codes of a lane, in two words
 using Lane8 = Part<8>;
 __device__ __forceinline__ uint2 load_codes(const uint8_t* p, const Lane8& q) {
-    if (q.vec) return *reinterpret_cast<const uint2*>(p + q.at);
+    if (q.vec) {
+        uint2 v;
+        load_past(p + q.at, &v);
+        return v;
+    }
     uint32_t w[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -82,7 +86,7 @@ __device__ __forceinline__ uint2 load_codes(const uint8_t* p, const Lane8& q) {
 }
 __device__ __forceinline__ void store_codes(uint8_t* p, const Lane8& q, uint2 w) {
     if (q.vec) {
-        *reinterpret_cast<uint2*>(p + q.at) = w;
+        store_past(p + q.at, w);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)

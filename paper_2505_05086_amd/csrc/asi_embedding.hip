@@ -359,7 +359,7 @@ template <typename D> __device__ __forceinline__ void write_zeros(const SumArgs&
         if (present[r]) continue;
         D* dst = static_cast<D*>(a.dtable) + (long long)(v0 + r) * a.table_stride;
         if (a.vec) {
-            for (int d = threadIdx.x * N; d < a.dim; d += kThreads * N) *reinterpret_cast<uint4*>(dst + d) = make_uint4(0, 0, 0, 0);
+            for (int d = threadIdx.x * N; d < a.dim; d += kThreads * N) store_past(dst + d, make_uint4(0, 0, 0, 0));
         } else {
             for (int d = threadIdx.x; d < a.dim; d += kThreads) dst[d] = from_f32<D>(0.f);
         }

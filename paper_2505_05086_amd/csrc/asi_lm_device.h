@@ -21,11 +21,28 @@ template <typename T> __device__ __forceinline__ T from_f32(float x);
 template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
 template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float x) { return to_bf16(x); }
 
+// Accesses past the caches, of what a kernel touches once: kept in the caches it would push out what is used again (zeros into 32000
+// rows of 2048 in fp32 67.8 -> 59.8 us; 4096 x 32000 logits and their gradient 105 -> 102 with the stores, 99 with the loads; AdamW on
+// 308 million elements 1548 -> 1415 us).
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+typedef uint32_t words2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void store_past(void* p, uint4 v) { __builtin_nontemporal_store(words4{v.x, v.y, v.z, v.w}, static_cast<words4*>(p)); }
+__device__ __forceinline__ void store_past(void* p, uint2 v) { __builtin_nontemporal_store(words2{v.x, v.y}, static_cast<words2*>(p)); }
+__device__ __forceinline__ void load_past(const void* p, uint4* v) {
+    const words4 w = __builtin_nontemporal_load(static_cast<const words4*>(p));
+    *v = make_uint4(w.x, w.y, w.z, w.w);
+}
+__device__ __forceinline__ void load_past(const void* p, uint2* v) {
+    const words2 w = __builtin_nontemporal_load(static_cast<const words2*>(p));
+    *v = make_uint2(w.x, w.y);
+}
+
 // 16 bytes of a row: 4 fp32 or 8 bf16 values, kept as loaded so that many can be in flight at little cost in registers
 template <typename T> struct Vec16 {
     static constexpr int N = 16 / sizeof(T);
     uint4 raw;
     __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void load_once(const T* p) { load_past(p, &raw); }
     __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = raw; }
     __device__ __forceinline__ float get(int i) const;
     __device__ __forceinline__ void set(const float* f);
@@ -84,6 +101,55 @@ template <int N> __device__ __forceinline__ void store_values(bf16_t* p, const f
     } else {
         static_assert(N == 4, "4 or a multiple of 8");
         *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+    }
+}
+
+// The same past the caches: for large results that are written once and not read soon, and for what is read once.
+template <int N> __device__ __forceinline__ void load_values_past(const float* p, float* f) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        Vec16<float> v;
+        v.load_once(p + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[i + k] = v.get(k);
+    }
+}
+template <int N> __device__ __forceinline__ void load_values_past(const bf16_t* p, float* f) {
+    if constexpr (N % 8 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 8) {
+            Vec16<bf16_t> v;
+            v.load_once(p + i);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[i + k] = v.get(k);
+        }
+    } else {
+        static_assert(N == 4, "4 or a multiple of 8");
+        uint2 v;
+        load_past(p, &v);
+        f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
+        f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+    }
+}
+template <int N> __device__ __forceinline__ void store_values_past(float* p, const float* f) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        Vec16<float> v;
+        v.set(f + i);
+        store_past(p + i, v.raw);
+    }
+}
+template <int N> __device__ __forceinline__ void store_values_past(bf16_t* p, const float* f) {
+    if constexpr (N % 8 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 8) {
+            Vec16<bf16_t> v;
+            v.set(f + i);
+            store_past(p + i, v.raw);
+        }
+    } else {
+        static_assert(N == 4, "4 or a multiple of 8");
+        store_past(p, make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])));
     }
 }
 

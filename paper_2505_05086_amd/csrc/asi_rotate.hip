@@ -58,6 +58,7 @@ struct Args {
     Divider by_tokens, by_parts;   // parts: what the heads of a token are taken in, forward
     int q_parts, parts;
     int tokens, head_dim, rot_dim, interleaved;
+    int past;                      // backward: heads are accessed past the caches
     float eps, inv_dim;
 };
 
@@ -219,8 +220,13 @@ template <typename T, typename G, int GROUP, bool INTER> __global__ __launch_bou
             if (mine) {
                 const T* x = static_cast<const T*>(s.x) + b * s.xs[0] + t * s.xs[1] + h * s.xs[2];
                 const T* dy = static_cast<const T*>(s.dy) + b * s.ys[0] + t * s.ys[1] + h * s.ys[2];
-                va.load(x + p.ia); vb.load(x + p.ib);
-                da.load(dy + p.ia); db.load(dy + p.ib);
+                if (a.past) {
+                    va.load_once(x + p.ia); vb.load_once(x + p.ib);
+                    da.load_once(dy + p.ia); db.load_once(dy + p.ib);
+                } else {
+                    va.load(x + p.ia); vb.load(x + p.ib);
+                    da.load(dy + p.ia); db.load(dy + p.ib);
+                }
                 load_angles<T, INTER>(a, p, position_of(a, b, t), c, sn);
             }
             float f[N], g[N], df[N], dg[N], sq = 0.f, dot = 0.f;
@@ -246,8 +252,13 @@ template <typename T, typename G, int GROUP, bool INTER> __global__ __launch_bou
                     g[i] = r * (wb[i] * dg[i] - g[i] * k);
                 }
                 T* dx = static_cast<T*>(s.y) + b * s.ds[0] + t * s.ds[1] + h * s.ds[2];
-                store_values<N>(dx + p.ia, f);
-                store_values<N>(dx + p.ib, g);
+                if (a.past) {
+                    store_values_past<N>(dx + p.ia, f);
+                    store_values_past<N>(dx + p.ib, g);
+                } else {
+                    store_values<N>(dx + p.ia, f);
+                    store_values<N>(dx + p.ib, g);
+                }
             }
         }
         if (!a.part) continue;
@@ -469,6 +480,13 @@ bool fits(const asi_qk_desc* d, const Args& a, bool back) {
     if (d->rot_dim && (!a.cos || !a.sin || !aligned(a.cos, 4) || !aligned(a.sin, 4))) return false;
     return aligned(a.positions, 8);
 }
+// Whether a group's loads and stores are whole lines of 128 bytes each.  Past the caches they are faster then (12003 tokens of 24 heads of
+// 128 in fp32 91.0 -> 80.6 us, 16384 of 20 in bf16 60.4 -> 58.3) and slower otherwise, where the other part of a line comes later (20
+// heads of 160 79.3 -> 83.0, of 64 in fp32 half turned 56.2 -> 60.4).
+bool whole_lines(const asi_qk_desc* d) {
+    const int per = 2 * 128 / (int)dtype_size(d->dtype);
+    return d->interleaved ? d->head_dim % per == 0 : d->rot_dim % per == 0 && (d->head_dim - d->rot_dim) % per == 0;
+}
 // Workgroups of the backward pass: as many as are resident at once, which is what registers leave room for (bf16, 16384 tokens of
 // 18 heads of 128: 768 51 us, 1024, which the compiler has to spill for, 54; fp32, half of that: 1024 46 us, 768 48), fewer where
 // that gives every group of lanes a head.  Scratch is planned for a head a group of 64 lanes.
@@ -564,6 +582,7 @@ asi_status asi_qk_norm_rotate_grad(const asi_qk_desc* desc, const void* q, const
     a.side[0].x = q; a.side[0].gain = q_gain; a.side[0].y = dq; a.side[0].dy = grad_q;
     a.side[1].x = k; a.side[1].gain = k_gain; a.side[1].y = dk; a.side[1].dy = grad_k;
     a.positions = positions; a.cos = cos; a.sin = sin;
+    a.past = whole_lines(desc);
     const bool empty = nothing(desc);
     if (!empty && !fits(desc, a, true)) return ASI_ERR_INVALID_ARG;
     const int group = empty ? 0 : group_of(desc, a, true);
