@@ -87,12 +87,13 @@ struct SortArgs {
     const int64_t* tokens;
     uint32_t* key;                    // sorted tokens
     uint32_t* pos;                    // their positions
-    long long padding;
+    uint32_t padding;                 // vocab where there is none
     uint32_t vocab;
     int n, span;
 };
 __device__ __forceinline__ uint32_t key_of(const SortArgs& a, long long t) {
-    return t >= 0 && t < (long long)a.vocab && t != a.padding ? (uint32_t)t : a.vocab;
+    const uint32_t lo = (uint32_t)t, k = (uint32_t)((unsigned long long)t >> 32) ? a.vocab : min(lo, a.vocab);
+    return k == a.padding ? a.vocab : k;
 }
 __device__ __forceinline__ int lanes_below(unsigned long long mask) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
@@ -119,18 +120,13 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const SortArgs a) {
     const int begin = min(a.n, wave * part), end = min(a.n, begin + part);
     for (int i = threadIdx.x; i < kSortWaves * a.span; i += kSortThreads) count[i] = 0;
     int less = 0, found = 0;
-    constexpr int U = 8;
-    for (int base = begin; base < end; base += 64 * U) {
-        long long t[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) t[u] = a.tokens[min(base + 64 * u + lane, a.n - 1)];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = base + 64 * u + lane;
-            const uint32_t k = key_of(a, t[u]);
-            less += __popcll(__ballot(i < end && k < lo));
-            const bool mine = i < end && k - lo < span;
-            const unsigned long long m = __ballot(mine);
+    // a token of each lane, where it counts
+    auto look = [&](long long t, int i, bool counts) {
+        const uint32_t k = key_of(a, t);
+        less += __popcll(__ballot(counts && k < lo));
+        const bool mine = counts && k - lo < span;
+        const unsigned long long m = __ballot(mine);
+        if (m) {                              // few looks find any
             const int at = found + lanes_below(m);
             if (mine && at < kSortList) {
                 list[wave * kSortList + at][0] = k - lo;
@@ -138,6 +134,23 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const SortArgs a) {
             }
             found += __popcll(m);
         }
+    };
+    constexpr int U = 8;
+    int base = begin;
+    for (; base + 64 * U <= end; base += 64 * U) {
+        long long t[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) t[u] = a.tokens[base + 64 * u + lane];
+#pragma unroll
+        for (int u = 0; u < U; ++u) look(t[u], base + 64 * u + lane, true);
+    }
+    if (base < end) {
+        long long t[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) t[u] = a.tokens[min(base + 64 * u + lane, a.n - 1)];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (base + 64 * u < end) look(t[u], base + 64 * u + lane, base + 64 * u + lane < end);
     }
     if (lane == 0) smaller[wave] = less;
     __syncthreads();
@@ -210,7 +223,7 @@ struct SumArgs {
     int n, run, runs, dim;
     int columns, lanes, column_tiles; // lanes: of a group (a power of two); columns: that a group covers
     int run_blocks;                   // workgroups of runs, before those that write zeros
-    int accumulate, vec;              // vec: rows of zeros can be written 16 bytes at a time
+    int accumulate;
     float scale;
 };
 // C neighbouring columns of a row as loaded: so many rows can be in flight at little cost in registers
@@ -352,17 +365,18 @@ __device__ __forceinline__ int lower_bound(const uint32_t* key, int n, uint32_t 
     }
     return lo;
 }
-// Zeros into the rows of this workgroup's kFillRows that have no token
+// Zeros into the rows of this workgroup's kFillRows that have no token, a wave a row: vectors from its first whole address on, and
+// the elements before and behind them
 template <typename D> __device__ __forceinline__ void write_zeros(const SumArgs& a, uint32_t v0, int rows, const uint32_t* present) {
     constexpr int N = Vec16<D>::N;
-    for (int r = 0; r < rows; ++r) {
+    const int lane = threadIdx.x & 63;
+    for (int r = threadIdx.x >> 6; r < rows; r += kThreads / 64) {
         if (present[r]) continue;
         D* dst = static_cast<D*>(a.dtable) + (long long)(v0 + r) * a.table_stride;
-        if (a.vec) {
-            for (int d = threadIdx.x * N; d < a.dim; d += kThreads * N) store_past(dst + d, make_uint4(0, 0, 0, 0));
-        } else {
-            for (int d = threadIdx.x; d < a.dim; d += kThreads) dst[d] = from_f32<D>(0.f);
-        }
+        const int head = min((int)((16 - (reinterpret_cast<uintptr_t>(dst) & 15)) & 15) / (int)sizeof(D), a.dim), nvec = (a.dim - head) / N;
+        for (int v = lane; v < nvec; v += 64) store_past(dst + head + v * N, make_uint4(0, 0, 0, 0));
+        const int loose = lane < head ? lane : nvec * N + lane;       // behind: lane - head from the end of the vectors
+        if (loose < a.dim) dst[loose] = from_f32<D>(0.f);
     }
 }
 template <typename D> __device__ __forceinline__ void fill(const SumArgs& a) {
@@ -386,14 +400,14 @@ template <typename O, typename D, int C, int P, bool ADD> __global__ __launch_bo
     else sum_run<O, D, C, P, ADD>(a);
 }
 // Adds up the partial rows of tokens that cross the ends of runs, of every token in the order of the runs.  A workgroup has 8 runs and
-// 64 columns; a wave looks whether its run shares a token with the next one and none before it, and adds up a short list alone.
-// Long lists are shared by all waves, each a stretch of the runs.
+// a tile of columns, C a lane; a wave looks whether its run shares a token with the next one and none before it, and adds up a short
+// list alone.  Long lists are shared by all waves, each a stretch of the runs.
 constexpr int kJoinThreads = 512, kJoinRuns = kJoinThreads / 64, kShort = 8;
-template <typename D> __global__ __launch_bounds__(kJoinThreads) void k_join(const SumArgs a, int tiles) {
+template <typename D, int C> __global__ __launch_bounds__(kJoinThreads) void k_join(const SumArgs a, int tiles) {
     __shared__ int more[kJoinRuns];               // runs that go on with the token of this one
-    __shared__ float sums[kJoinRuns][64];
+    __shared__ float sums[kJoinRuns][C][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int r0 = blockIdx.x / tiles * kJoinRuns, d = (blockIdx.x % tiles) * 64 + lane;
+    const int r0 = blockIdx.x / tiles * kJoinRuns, d = ((blockIdx.x % tiles) * 64 + lane) * C;
     const int r = r0 + wave;
     uint32_t token = a.vocab;
     int n = 0;
@@ -410,23 +424,34 @@ template <typename D> __global__ __launch_bounds__(kJoinThreads) void k_join(con
         if (c < 64) break;
     }
     if (lane == 0) more[wave] = n;
+    struct Values { float v[C]; };
     // slot 1 of its first run, slot 0 of the others
-    auto partial = [&](int run, int slot) { return a.part[((long long)run * 2 + slot) * a.dim + d]; };
-    auto finish = [&](uint32_t t, float v) {
-        v *= a.scale;
-        float old;
+    auto partial = [&](int run, int slot) {
+        Values p;
+        const float* src = a.part + ((long long)run * 2 + slot) * a.dim + d;
+        if constexpr (C > 1) load_values<C>(src, p.v);
+        else p.v[0] = *src;
+        return p;
+    };
+    auto finish = [&](uint32_t t, Values v) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) v.v[i] *= a.scale;
         if (a.accumulate) {
-            load_result<D, 1>(a, t, d, &old);
-            v += old;
+            float old[C];
+            load_result<D, C>(a, t, d, old);
+#pragma unroll
+            for (int i = 0; i < C; ++i) v.v[i] += old[i];
         }
-        store_result<D, 1>(a, t, d, &v);
+        store_result<D, C>(a, t, d, v.v);
     };
     if (n > 0 && n <= kShort && d < a.dim) {
-        float v = partial(r, 1), p[kShort];
+        Values v = partial(r, 1), p[kShort];
 #pragma unroll
-        for (int k = 0; k < kShort; ++k) p[k] = k < n ? partial(r + 1 + k, 0) : 0.f;
+        for (int k = 0; k < kShort; ++k) p[k] = k < n ? partial(r + 1 + k, 0) : Values{};
 #pragma unroll
-        for (int k = 0; k < kShort; ++k) v += p[k];
+        for (int k = 0; k < kShort; ++k)
+#pragma unroll
+            for (int i = 0; i < C; ++i) v.v[i] += p[k].v[i];
         finish(token, v);
     }
     __syncthreads();
@@ -434,17 +459,25 @@ template <typename D> __global__ __launch_bounds__(kJoinThreads) void k_join(con
         const int m = more[w];
         if (m <= kShort) continue;
         const int share = (m + kJoinRuns - 1) / kJoinRuns, from = wave * share, to = min(m, from + share);
-        float v = 0.f;
+        Values v{};
         if (d < a.dim) {
             if (wave == 0) v = partial(r0 + w, 1);
 #pragma unroll 8
-            for (int k = from; k < to; ++k) v += partial(r0 + w + 1 + k, 0);
+            for (int k = from; k < to; ++k) {
+                const Values p = partial(r0 + w + 1 + k, 0);
+#pragma unroll
+                for (int i = 0; i < C; ++i) v.v[i] += p.v[i];
+            }
         }
-        sums[wave][lane] = v;
+#pragma unroll
+        for (int i = 0; i < C; ++i) sums[wave][i][lane] = v.v[i];
         __syncthreads();
         if (wave == w && d < a.dim) {
-            v = sums[0][lane];
-            for (int k = 1; k < kJoinRuns; ++k) v += sums[k][lane];
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                v.v[i] = sums[0][i][lane];
+                for (int k = 1; k < kJoinRuns; ++k) v.v[i] += sums[k][i][lane];
+            }
             finish(token, v);
         }
         __syncthreads();
@@ -596,6 +629,12 @@ template <typename O, typename D, int C, int P> void sum(SumArgs a, const SortAr
         else hipLaunchKernelGGL((k_sum<O, D, C, P, false>), grid, kThreads, 0, st, a);
     }
 }
+template <typename D> void join(const SumArgs& a, bool vec, hipStream_t st) {
+    const int wide = vec ? 256 : 64, tiles = (a.dim + wide - 1) / wide;
+    const dim3 grid((unsigned)((a.runs - 1 + kJoinRuns - 1) / kJoinRuns * tiles));
+    if (vec) hipLaunchKernelGGL((k_join<D, 4>), grid, kJoinThreads, 0, st, a, tiles);
+    else hipLaunchKernelGGL((k_join<D, 1>), grid, kJoinThreads, 0, st, a, tiles);
+}
 template <typename O, typename D> void sum(const SumArgs& a, const SortArgs& s, bool vec, int fill_blocks, hipStream_t st) {
     if (vec) sum<O, D, Shape<O, D>::C, Shape<O, D>::P>(a, s, fill_blocks, st);
     else sum<O, D, 1, kLoose>(a, s, fill_blocks, st);
@@ -661,7 +700,6 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
     a.n = (int)desc->tokens; a.run = p.run; a.runs = p.runs; a.dim = (int)desc->dim;
     a.accumulate = accumulate != 0;
     a.scale = desc->scale;
-    a.vec = aligned(dtable, 16) && desc->table_stride % (16 / ds) == 0 && desc->dim % (16 / ds) == 0;
     // whole pieces: 4 columns, 8 where both types are bf16
     const int piece = ds == 2 && os == 2 ? 8 : 4;
     const bool vec = desc->dim % piece == 0 && desc->out_stride % piece == 0 && desc->table_stride % piece == 0 && aligned(grad_out, piece * os) && aligned(dtable, piece * ds);
@@ -669,7 +707,8 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
     const int tiles = (a.dim + 63) / 64;
     // an upper bound of the workgroups of either launch
     if ((long long)std::max(p.runs, kFew) * tiles + fill_blocks > 0x7fffffffLL) return ASI_ERR_UNSUPPORTED;
-    SortArgs s{tokens, nullptr, nullptr, desc->padding_index, a.vocab, a.n, 0};
+    const bool padded = desc->padding_index >= 0 && desc->padding_index < desc->vocab;
+    SortArgs s{tokens, nullptr, nullptr, padded ? (uint32_t)desc->padding_index : a.vocab, a.vocab, a.n, 0};
     if (!few) {
         // about one workgroup a CU; the id `vocab` is one more
         const long long ids = desc->vocab + 1;
@@ -689,9 +728,8 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
         else sum<bf16_t, bf16_t>(a, s, vec, fill_blocks, st);
     }
     if (!few && p.runs > 1) {
-        const dim3 grid((unsigned)((p.runs - 1 + kJoinRuns - 1) / kJoinRuns * tiles));
-        if (desc->table_dtype == ASI_F32) hipLaunchKernelGGL(k_join<float>, grid, kJoinThreads, 0, st, a, tiles);
-        else hipLaunchKernelGGL(k_join<bf16_t>, grid, kJoinThreads, 0, st, a, tiles);
+        if (desc->table_dtype == ASI_F32) join<float>(a, vec, st);
+        else join<bf16_t>(a, vec, st);
     }
     return launched();
 }
