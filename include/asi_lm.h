@@ -147,7 +147,7 @@ typedef struct {
     void* exp_avg_sq;          /* in/out: v in fp32, or sqrt(v) as 8-bit codes */
     float* exp_avg_scale;      /* in/out, (count + 255) / 256 entries; 8 bits only */
     float* exp_avg_sq_scale;   /* in/out, the same of sqrt(v); 8 bits only */
-    int64_t count;             /* elements, >= 0 */
+    int64_t count;             /* elements, 0 .. 2^40 */
     int32_t param_dtype, grad_dtype;
     double lr, weight_decay;
 } asi_adamw_tensor;

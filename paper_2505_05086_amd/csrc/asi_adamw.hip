@@ -215,7 +215,7 @@ void launch_kind(int kind, const Args& a, bool eight, hipStream_t st) {
     }
 }
 bool valid(const asi_adamw_tensor& t, bool eight) {
-    if (!dtype_ok(t.param_dtype) || !dtype_ok(t.grad_dtype) || t.count < 0 || t.count > (1LL << 42)) return false;
+    if (!dtype_ok(t.param_dtype) || !dtype_ok(t.grad_dtype) || t.count < 0 || t.count > (1LL << 40)) return false;
     if (!std::isfinite(t.lr) || !std::isfinite(t.weight_decay)) return false;
     if (t.count == 0) return true;
     if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq || (eight && (!t.exp_avg_scale || !t.exp_avg_sq_scale))) return false;

@@ -231,7 +231,11 @@ template <typename O, int C> struct Columns {
     static_assert(C == 1 || (C * sizeof(O) == 8 || C * sizeof(O) == 16), "one value, 8 or 16 bytes");
     using Raw = std::conditional_t<C == 1, O, std::conditional_t<C * sizeof(O) == 8, uint2, uint4>>;
     Raw raw;
-    __device__ __forceinline__ void load(const O* p) { raw = *reinterpret_cast<const Raw*>(p); }
+    __device__ __forceinline__ void load(const O* p) {
+        if constexpr (C == 1) raw = *p;
+        else if constexpr (C * sizeof(O) == 8) raw = load_words2(p);
+        else raw = load_words4(p);
+    }
     __device__ __forceinline__ void add_to(float* f) const {
         if constexpr (C == 1) {
             f[0] += to_f32(raw);

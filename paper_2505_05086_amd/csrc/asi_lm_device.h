@@ -21,11 +21,22 @@ template <typename T> __device__ __forceinline__ T from_f32(float x);
 template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
 template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float x) { return to_bf16(x); }
 
+// 16 and 8 bytes of any type
+typedef uint32_t words4 __attribute__((ext_vector_type(4), may_alias));
+typedef uint32_t words2 __attribute__((ext_vector_type(2), may_alias));
+__device__ __forceinline__ uint4 load_words4(const void* p) {
+    const words4 w = *static_cast<const words4*>(p);
+    return make_uint4(w.x, w.y, w.z, w.w);
+}
+__device__ __forceinline__ uint2 load_words2(const void* p) {
+    const words2 w = *static_cast<const words2*>(p);
+    return make_uint2(w.x, w.y);
+}
+__device__ __forceinline__ void store_words(void* p, uint4 v) { *static_cast<words4*>(p) = words4{v.x, v.y, v.z, v.w}; }
+__device__ __forceinline__ void store_words(void* p, uint2 v) { *static_cast<words2*>(p) = words2{v.x, v.y}; }
 // Accesses past the caches, of what a kernel touches once: kept in the caches it would push out what is used again (zeros into 32000
 // rows of 2048 in fp32 67.8 -> 59.8 us; 4096 x 32000 logits and their gradient 105 -> 102 with the stores, 99 with the loads; AdamW on
 // 308 million elements 1548 -> 1415 us).
-typedef uint32_t words4 __attribute__((ext_vector_type(4)));
-typedef uint32_t words2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void store_past(void* p, uint4 v) { __builtin_nontemporal_store(words4{v.x, v.y, v.z, v.w}, static_cast<words4*>(p)); }
 __device__ __forceinline__ void store_past(void* p, uint2 v) { __builtin_nontemporal_store(words2{v.x, v.y}, static_cast<words2*>(p)); }
 __device__ __forceinline__ void load_past(const void* p, uint4* v) {
@@ -41,9 +52,9 @@ __device__ __forceinline__ void load_past(const void* p, uint2* v) {
 template <typename T> struct Vec16 {
     static constexpr int N = 16 / sizeof(T);
     uint4 raw;
-    __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void load(const T* p) { raw = load_words4(p); }
     __device__ __forceinline__ void load_once(const T* p) { load_past(p, &raw); }
-    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = raw; }
+    __device__ __forceinline__ void store(T* p) const { store_words(p, raw); }
     __device__ __forceinline__ float get(int i) const;
     __device__ __forceinline__ void set(const float* f);
 };
@@ -66,8 +77,10 @@ template <> __device__ __forceinline__ void Vec16<bf16_t>::set(const float* f) {
 template <int N> __device__ __forceinline__ void load_values(const float* p, float* f) {
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
-        const float4 v = *reinterpret_cast<const float4*>(p + i);
-        f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+        Vec16<float> v;
+        v.load(p + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[i + k] = v.get(k);
     }
 }
 template <int N> __device__ __forceinline__ void load_values(const bf16_t* p, float* f) {
@@ -81,14 +94,18 @@ template <int N> __device__ __forceinline__ void load_values(const bf16_t* p, fl
         }
     } else {
         static_assert(N == 4, "4 or a multiple of 8");
-        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        const uint2 v = load_words2(p);
         f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
         f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
     }
 }
 template <int N> __device__ __forceinline__ void store_values(float* p, const float* f) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+    for (int i = 0; i < N; i += 4) {
+        Vec16<float> v;
+        v.set(f + i);
+        v.store(p + i);
+    }
 }
 template <int N> __device__ __forceinline__ void store_values(bf16_t* p, const float* f) {
     if constexpr (N % 8 == 0) {
@@ -100,7 +117,7 @@ template <int N> __device__ __forceinline__ void store_values(bf16_t* p, const f
         }
     } else {
         static_assert(N == 4, "4 or a multiple of 8");
-        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+        store_words(p, make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])));
     }
 }
 
@@ -157,11 +174,6 @@ template <int N> __device__ __forceinline__ void store_values_past(bf16_t* p, co
 template <int WIDTH = kWave> __device__ __forceinline__ float lanes_sum(float x) {
 #pragma unroll
     for (int o = WIDTH / 2; o; o >>= 1) x += __shfl_xor(x, o);
-    return x;
-}
-template <int WIDTH = kWave> __device__ __forceinline__ float lanes_max(float x) {
-#pragma unroll
-    for (int o = WIDTH / 2; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
     return x;
 }
 

@@ -58,7 +58,6 @@ struct Args {
     Divider by_tokens, by_parts;   // parts: what the heads of a token are taken in, forward
     int q_parts, parts;
     int tokens, head_dim, rot_dim, interleaved;
-    int past;                      // backward: heads are accessed past the caches
     float eps, inv_dim;
 };
 
@@ -111,8 +110,9 @@ template <int M> __device__ __forceinline__ void load_angles(const Args& a, long
             load_values<M>(a.cos + at, c);
             load_values<M>(a.sin + at, s);
         } else {
-            const float2 vc = *reinterpret_cast<const float2*>(a.cos + at), vs = *reinterpret_cast<const float2*>(a.sin + at);
-            c[0] = vc.x; c[1] = vc.y; s[0] = vs.x; s[1] = vs.y;
+            const uint2 vc = load_words2(a.cos + at), vs = load_words2(a.sin + at);
+            c[0] = __uint_as_float(vc.x); c[1] = __uint_as_float(vc.y);
+            s[0] = __uint_as_float(vs.x); s[1] = __uint_as_float(vs.y);
         }
     } else {
 #pragma unroll
@@ -192,8 +192,8 @@ template <typename T, typename G, int GROUP, int HEADS, bool INTER> __global__ _
     }
 }
 
-// Backward: the groups of the grid take the heads of one side after another, a grid apart.
-template <typename T, typename G, int GROUP, bool INTER> __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 3) void k_rotate_grad(const Args a) {
+// Backward: the groups of the grid take the heads of one side after another, a grid apart.  PAST: heads are accessed past the caches.
+template <typename T, typename G, int GROUP, bool INTER, bool PAST> __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 3) void k_rotate_grad(const Args a) {
     constexpr int N = Vec16<T>::N;
     constexpr int GROUPS = kThreads / GROUP;
     const int lane = threadIdx.x & (GROUP - 1), group = threadIdx.x / GROUP;
@@ -220,7 +220,7 @@ template <typename T, typename G, int GROUP, bool INTER> __global__ __launch_bou
             if (mine) {
                 const T* x = static_cast<const T*>(s.x) + b * s.xs[0] + t * s.xs[1] + h * s.xs[2];
                 const T* dy = static_cast<const T*>(s.dy) + b * s.ys[0] + t * s.ys[1] + h * s.ys[2];
-                if (a.past) {
+                if (PAST) {
                     va.load_once(x + p.ia); vb.load_once(x + p.ib);
                     da.load_once(dy + p.ia); db.load_once(dy + p.ib);
                 } else {
@@ -252,7 +252,7 @@ template <typename T, typename G, int GROUP, bool INTER> __global__ __launch_bou
                     g[i] = r * (wb[i] * dg[i] - g[i] * k);
                 }
                 T* dx = static_cast<T*>(s.y) + b * s.ds[0] + t * s.ds[1] + h * s.ds[2];
-                if (a.past) {
+                if (PAST) {
                     store_values_past<N>(dx + p.ia, f);
                     store_values_past<N>(dx + p.ib, g);
                 } else {
@@ -483,9 +483,9 @@ bool fits(const asi_qk_desc* d, const Args& a, bool back) {
 // Whether a group's loads and stores are whole lines of 128 bytes each.  Past the caches they are faster then (12003 tokens of 24 heads of
 // 128 in fp32 91.0 -> 80.6 us, 16384 of 20 in bf16 60.4 -> 58.3) and slower otherwise, where the other part of a line comes later (20
 // heads of 160 79.3 -> 83.0, of 64 in fp32 half turned 56.2 -> 60.4).
-bool whole_lines(const asi_qk_desc* d) {
-    const int per = 2 * 128 / (int)dtype_size(d->dtype);
-    return d->interleaved ? d->head_dim % per == 0 : d->rot_dim % per == 0 && (d->head_dim - d->rot_dim) % per == 0;
+bool whole_lines(const Args& a, size_t size) {
+    const int per = 2 * 128 / (int)size;
+    return a.interleaved ? a.head_dim % per == 0 : a.rot_dim % per == 0 && (a.head_dim - a.rot_dim) % per == 0;
 }
 // Workgroups of the backward pass: as many as are resident at once, which is what registers leave room for (bf16, 16384 tokens of
 // 18 heads of 128: 768 51 us, 1024, which the compiler has to spill for, 54; fp32, half of that: 1024 46 us, 768 48), fewer where
@@ -507,14 +507,19 @@ template <typename T, typename G, int GROUP, int HEADS> void forward(Args a, hip
     if (a.interleaved) hipLaunchKernelGGL((k_rotate<T, G, GROUP, HEADS, true>), grid, kThreads, 0, st, a);
     else hipLaunchKernelGGL((k_rotate<T, G, GROUP, HEADS, false>), grid, kThreads, 0, st, a);
 }
+template <typename T, typename G, int GROUP, bool INTER> void backward(const Args& a, int blocks, hipStream_t st) {
+    constexpr bool lines = GROUP * 16 >= 128;         // a vector of each lane of a group fills a line
+    if (lines && whole_lines(a, sizeof(T))) hipLaunchKernelGGL((k_rotate_grad<T, G, GROUP, INTER, lines>), dim3(blocks), kThreads, 0, st, a);
+    else hipLaunchKernelGGL((k_rotate_grad<T, G, GROUP, INTER, false>), dim3(blocks), kThreads, 0, st, a);
+}
 template <typename T, typename G, int GROUP> void go(const Args& a, bool back, int blocks, hipStream_t st) {
     // two heads a lane share the angles and gains (8 x 512 tokens of 36 heads of 64 9.9 us, one head 11.0, four 10.8); where one
     // head a lane does not fill the chip the shorter chain counts (8 tokens of these heads 3.4 us, two 3.8)
     const long long waves = a.rows * (a.side[0].heads + a.side[1].heads) * GROUP / 64;
     if (!back && waves > 4096) forward<T, G, GROUP, 2>(a, st);
     else if (!back) forward<T, G, GROUP, 1>(a, st);
-    else if (a.interleaved) hipLaunchKernelGGL((k_rotate_grad<T, G, GROUP, true>), dim3(blocks), kThreads, 0, st, a);
-    else hipLaunchKernelGGL((k_rotate_grad<T, G, GROUP, false>), dim3(blocks), kThreads, 0, st, a);
+    else if (a.interleaved) backward<T, G, GROUP, true>(a, blocks, st);
+    else backward<T, G, GROUP, false>(a, blocks, st);
 }
 template <typename T, typename G> void go(int group, const Args& a, bool back, int blocks, hipStream_t st) {
     switch (group) {
@@ -582,7 +587,6 @@ asi_status asi_qk_norm_rotate_grad(const asi_qk_desc* desc, const void* q, const
     a.side[0].x = q; a.side[0].gain = q_gain; a.side[0].y = dq; a.side[0].dy = grad_q;
     a.side[1].x = k; a.side[1].gain = k_gain; a.side[1].y = dk; a.side[1].dy = grad_k;
     a.positions = positions; a.cos = cos; a.sin = sin;
-    a.past = whole_lines(desc);
     const bool empty = nothing(desc);
     if (!empty && !fits(desc, a, true)) return ASI_ERR_INVALID_ARG;
     const int group = empty ? 0 : group_of(desc, a, true);

@@ -723,6 +723,68 @@ def test_adamw_saved_and_loaded_goes_on_the_same(bits):
             assert t.dtype == other.state[q][key].dtype and torch.equal(t.view(torch.uint8), other.state[q][key].view(torch.uint8))
 
 
+# ---- offsets past 32 bits ------------------------------------------------------------------------------------
+def test_logits_past_32_bits():
+    rows, vocab = 66000, 66000                                    # 4.4e9 entries
+    x = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
+    x[-3:] = _logits(3, vocab, torch.bfloat16, 1)
+    targets = torch.arange(rows, device="cuda")
+    a = torch.full((rows,), -1.0, device="cuda")
+    r = asi.token_logprobs(x, targets, top=4)
+    logprob, entropy, p, _ = _definition(x[-3:], targets[-3:], 1.0, -100)
+    bound = _value_bound(x[-3:], 1.0)
+    _close(r.logprob[-3:], logprob, bound, "logprob")
+    assert torch.equal(r.top_index[-3:], _order(x[-3:], 4))
+    assert abs(float(r.logprob[0]) + math.log(vocab)) < 300 * U and r.top_index[0].tolist() == [0, 1, 2, 3]
+    last = x[-3:].clone()
+    d = asi.token_logprobs_grad(x, targets, a, out=x)
+    assert torch.equal(d.grad[-3:], asi.token_logprobs_grad(last, targets[-3:], a[-3:]).grad)
+
+
+def test_tables_past_32_bits():
+    vocab, dim = (1 << 21) + 5, 2052                              # 4.3e9 entries
+    table = torch.empty(vocab, dim, dtype=torch.bfloat16, device="cuda")
+    table[-7:] = torch.empty(7, dim, device="cuda").normal_(generator=_gen(1)).to(torch.bfloat16)
+    table[:2] = 1.0
+    tokens = torch.cat((torch.arange(vocab - 7, vocab, device="cuda").repeat(200), torch.zeros(3, dtype=torch.int64, device="cuda")))
+    assert torch.equal(asi.embedding(tokens, table, scale=2.0), (table[tokens].float() * 2.0).to(torch.bfloat16))
+    grad_out = torch.ones(len(tokens), dim, dtype=torch.bfloat16, device="cuda")
+    for n in (len(tokens), 100):                                  # sorted, and few
+        out = asi.embedding_grad(tokens[-n:], grad_out[-n:], vocab, out=table)
+        count = torch.bincount(tokens[-n:] % 1000003, minlength=0)          # ids as they are below a million, the last ones folded
+        assert (out[-7:].float() == count[torch.arange(vocab - 7, vocab, device="cuda") % 1000003][:, None]).all()
+        assert (out[0] == 3).all() and not out[1:-7].any()
+
+
+def test_heads_past_32_bits():
+    apart = (1 << 32) + 256
+    buf = torch.empty(apart + 9 * 3 * 64, dtype=torch.bfloat16, device="cuda")
+    q = buf.as_strided((2, 9, 3, 64), (apart, 192, 64, 1))
+    q.copy_(torch.empty(2, 9, 3, 64, device="cuda").normal_(generator=_gen(1)))
+    near = q.contiguous()
+    cos, sin = asi.rotary_table(20, 64)
+    for a, b in zip(asi.qk_norm_rotate(q, q, None, None, cos, sin), asi.qk_norm_rotate(near, near, None, None, cos, sin)):
+        assert torch.equal(a, b)
+    g = torch.empty_like(near).normal_(generator=_gen(2))
+    for a, b in zip(asi.qk_norm_rotate_grad(q, q, None, None, cos, sin, g, g), asi.qk_norm_rotate_grad(near, near, None, None, cos, sin, g, g)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_parameters_past_32_bits(bits):
+    n, m = (1 << 32) + 1000, 1256
+    p = torch.nn.Parameter(torch.zeros(n, dtype=torch.bfloat16, device="cuda"))
+    p.grad = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    q = torch.nn.Parameter(torch.empty(m, device="cuda").normal_(generator=_gen(1)).to(torch.bfloat16))
+    q.grad = torch.empty(m, device="cuda").normal_(generator=_gen(2)).to(torch.bfloat16)
+    with torch.no_grad():
+        p[-m:] = q
+        p.grad[-m:] = q.grad                                      # blocks of 256 begin at the same place
+    for x in (p, q):
+        asi.AdamW([x], state_bits=bits).step()
+    assert torch.equal(p[-m:], q) and not p[:-m].any()
+
+
 # ---- streams, graphs ----------------------------------------------------------------------------------------
 def _one_of_each(x, targets, table, tokens, q, k, gain, cos, sin, out):
     r = asi.token_logprobs(x, targets, top=5)

@@ -46,6 +46,15 @@ def test_logprob_arguments():
     assert _backward(_lp(), dlogits=None) == INVALID and _backward(_lp(), targets=None) == INVALID and _backward(_lp(rows=0), logits=None, dlogits=None) == OK
 
 
+def test_logprob_scratch_of_rows_in_parts():
+    few = _lp(rows=5, vocab=200000, row_stride=200000, top=3)
+    need = B.lib().asi_token_logprobs_workspace_bytes(few)
+    assert need > 0 and need % 256 == 0 and B.lib().asi_token_logprobs_workspace_bytes(_lp()) == 0
+    assert B.lib().asi_token_logprobs_workspace_bytes(_lp(rows=5, vocab=200000, row_stride=1)) == 0
+    for ws, size in ((None, need), (P, need - 1), (P + 64, need)):
+        assert B.lib().asi_token_logprobs(few, P, P, P, P, P, P, P, ws, size, None) == WORKSPACE
+
+
 def _em(**kw):
     d = dict(tokens=10, vocab=50, dim=8, table_stride=8, out_stride=8, padding_index=-1, table_dtype=0, out_dtype=0, scale=1.0, reserved=0)
     d.update(kw)
@@ -142,7 +151,7 @@ def _tensor(**kw):
 
 def test_adamw_arguments():
     assert _adamw([]) == OK and _adamw([_tensor(count=0, param=None, grad=None, exp_avg=None, exp_avg_sq=None)]) == OK
-    for bad in (dict(param=None), dict(grad=None), dict(exp_avg=None), dict(exp_avg_sq=None), dict(count=-1), dict(param_dtype=2), dict(grad_dtype=5),
+    for bad in (dict(param=None), dict(grad=None), dict(exp_avg=None), dict(exp_avg_sq=None), dict(count=-1), dict(count=(1 << 40) + 1), dict(param_dtype=2), dict(grad_dtype=5),
                 dict(param=P + 2), dict(exp_avg=P + 1), dict(lr=float("nan")), dict(weight_decay=float("inf")), dict(master=P + 2)):
         assert _adamw([_tensor(), _tensor(**bad)]) == INVALID, bad
     assert _adamw([_tensor(exp_avg_scale=P)], bits=8) == INVALID                 # scales are needed for 8 bits
