@@ -81,8 +81,10 @@ template <typename T, typename O> __global__ __launch_bounds__(kThreads) void k_
 // among equal ids.  No atomics, and the time does not depend on the tokens.  A token that counts for nothing sorts behind all
 // others, as `vocab`.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kSortList = 256;        // entries of a wave that are kept; a wave with more looks at its tokens again
+constexpr int kSortList = 1024;       // entries of a wave that are kept; a wave with more looks at its tokens again
 constexpr int kMaxSpan = kSortThreads;
+constexpr int kPlaceBits = 22;        // of an entry: its place in the wave's part of the positions; above them its id within the span
+static_assert(kMaxSpan <= 1 << (32 - kPlaceBits), "an entry is a word");
 struct SortArgs {
     const int64_t* tokens;
     uint32_t* key;                    // sorted tokens
@@ -112,7 +114,7 @@ static_assert(kMaxSpan <= 1 << 10, "ids within a workgroup's span have 10 bits")
 __global__ __launch_bounds__(kSortThreads) void k_sort(const SortArgs a) {
     extern __shared__ uint32_t lds[];
     uint32_t* count = lds;                                     // [wave][span]
-    uint32_t(*list)[2] = reinterpret_cast<uint32_t(*)[2]>(lds + kSortWaves * a.span);   // [wave][kSortList]: id within the span, position
+    uint32_t* list = lds + kSortWaves * a.span + (threadIdx.x >> 6) * kSortList;       // the wave's entries
     __shared__ int smaller[kSortWaves], totals[kSortWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t lo = blockIdx.x * (uint32_t)a.span, span = (uint32_t)a.span;
@@ -128,10 +130,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const SortArgs a) {
         const unsigned long long m = __ballot(mine);
         if (m) {                              // few looks find any
             const int at = found + lanes_below(m);
-            if (mine && at < kSortList) {
-                list[wave * kSortList + at][0] = k - lo;
-                list[wave * kSortList + at][1] = (uint32_t)i;
-            }
+            if (mine && at < kSortList) list[at] = (k - lo) << kPlaceBits | (uint32_t)(i - begin);
             found += __popcll(m);
         }
     };
@@ -157,15 +156,24 @@ __global__ __launch_bounds__(kSortThreads) void k_sort(const SortArgs a) {
     uint32_t* mine = count + wave * a.span;
     // f(member, id within the span, position) for this wave's entries in order, 64 at a time
     auto entries = [&](auto f) {
-        if (found <= kSortList) {
+        if (found <= kSortList && part <= 1 << kPlaceBits) {
             for (int e = lane; e - lane < found; e += 64) {
                 const bool member = e < found;
-                f(member, member ? list[wave * kSortList + e][0] : 0u, member ? list[wave * kSortList + e][1] : 0u);
+                const uint32_t entry = member ? list[e] : 0u;
+                f(member, entry >> kPlaceBits, (uint32_t)begin + (entry & ((1u << kPlaceBits) - 1)));
             }
         } else {
-            for (int i = begin + lane; i - lane < end; i += 64) {
-                const uint32_t k = i < end ? key_of(a, a.tokens[i]) : 0u;
-                f(i < end && k - lo < span, k - lo < span ? k - lo : 0u, (uint32_t)i);
+            for (int i0 = begin; i0 < end; i0 += 64 * U) {
+                long long t[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) t[u] = a.tokens[min(i0 + 64 * u + lane, a.n - 1)];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int i = i0 + 64 * u + lane;
+                    const uint32_t low = key_of(a, t[u]) - lo;
+                    const bool member = i < end && low < span;
+                    if (__ballot(member)) f(member, member ? low : 0u, (uint32_t)i);
+                }
             }
         }
     };
@@ -719,7 +727,7 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
         s.key = reinterpret_cast<uint32_t*>(w + p.key);
         s.pos = reinterpret_cast<uint32_t*>(w + p.pos);
         s.span = (int)std::min<long long>(kMaxSpan, (ids + 255) / 256);
-        constexpr size_t lists = (size_t)kSortWaves * kSortList * 8;
+        constexpr size_t lists = (size_t)kSortWaves * kSortList * 4;
         static LdsAllowed allowed;
         if (allow_lds(reinterpret_cast<const void*>(k_sort), (size_t)kSortWaves * kMaxSpan * 4 + lists, allowed) != hipSuccess) return ASI_ERR_HIP;
         hipLaunchKernelGGL(k_sort, dim3((unsigned)((ids + s.span - 1) / s.span)), kSortThreads, (size_t)kSortWaves * s.span * 4 + lists, st, s);
