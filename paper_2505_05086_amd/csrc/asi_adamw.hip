@@ -4,7 +4,8 @@
 // updates a chunk of it, each lane 16 bytes of fp32 (4 elements) or two of them (8, states in 8 bits: half a wave then has the 256
 // elements that share a scale).  The update reads and writes each element once and is bound by memory.  A chunk is one piece a wave:
 // many short workgroups keep the memory busier than few that loop (six blocks of 2048 in fp32, 308 million elements: chunks of 8192,
-// 4096, 1024 elements 1667, 1638, 1571 us).
+// 4096, 1024 elements 1667, 1638, 1571 us; past the caches 1383 us, 6.2 TB/s; 103 million elements in bf16 with fp32 copies and states of
+// 8 bits 301 us, 5.5 TB/s).
 //
 // Products, sums, the quotient and the root are rounded one by one (no contraction), so that the result is that of the same
 // formula in elementary fp32 operations, bit for bit: an 8-bit code then does not depend on how a compiler fused it.
