@@ -501,9 +501,9 @@ template <typename D, int C> __global__ __launch_bounds__(kJoinThreads) void k_j
 
 // ---- gradient of few tokens ------------------------------------------------------------------------------------
 // Workgroups of positions, each with a tile of columns, before those that write zeros.  The four waves share the positions of the token.
-// Up to kFew: every workgroup looks at all tokens, and a token that all of them are is one workgroup's chain (sorted and in one launch:
-// 172 x 772 14.7 and 4.4 us, 377 x 2501 16.4 and 12.0, 512 x 100 15.4 and 7.5).
-constexpr int kFew = 512, kFewWaves = kThreads / 64;
+// Up to kFew: every workgroup looks at all tokens, and a token that most of them are is one workgroup's chain (sorted and in one launch:
+// 172 x 772 14.7 and 4.4 us, 1000 x 256 14.6 and 7.9, 1000 x 2048 15.6 and 14.6, 2000 x 256 15.3 and 14.2; 1000 of one token 15 and 34).
+constexpr int kFew = 1024, kFewWaves = kThreads / 64;
 template <typename O, typename D, int C, int P, bool ADD> __global__ __launch_bounds__(kThreads) void k_few(const SumArgs a, const SortArgs s) {
     __shared__ uint32_t key[kFew];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

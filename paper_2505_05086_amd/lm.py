@@ -15,6 +15,7 @@ from typing import List, NamedTuple, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -180,6 +181,7 @@ class _TokenLogprobsFn(torch.autograd.Function):
         return tuple(r)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_logprob, grad_entropy, *_):
         logits, targets = ctx.saved_tensors
         if grad_logprob is None and grad_entropy is None:
@@ -256,6 +258,7 @@ class _EmbeddingFn(torch.autograd.Function):
         return _embedding(tokens, table, scale, dtype)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_out):
         tokens, = ctx.saved_tensors
         return None, embedding_grad(tokens, grad_out, ctx.vocab, scale=ctx.scale, padding_idx=ctx.padding_idx, dtype=ctx.dtype), \
@@ -400,6 +403,7 @@ class _QkNormRotateFn(torch.autograd.Function):
         return _qk_norm_rotate(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, heads_first)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_q, grad_k):
         q, k, q_gain, k_gain, cos, sin, positions = ctx.saved_tensors
         eps, interleaved, heads_first = ctx.options
@@ -497,7 +501,9 @@ class AdamW(torch.optim.Optimizer):
     state_bits 32: exp_avg and exp_avg_sq in fp32.  state_bits 8: exp_avg and exp_avg_sqrt, the root of the second moment,
     as 8-bit floats with an fp32 scale for each 256 elements (include/asi_lm.h).  master: bf16 parameters get an fp32 copy
     that the step updates and rounds into them; without it their updates are rounded away where they are below a
-    parameter's last bit.  Parameters are contiguous and fp32 or bf16.  The number of steps is a group's ("step").
+    parameter's last bit.  Parameters are contiguous and fp32 or bf16.  The number of steps is a group's ("step"); it and the
+    rates are the host's, so that a captured step repeats them.  Whoever writes other values into a bf16 parameter writes them into
+    its copy (state "master") too, or removes that.
     """
 
     def __init__(self, params, lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,

@@ -306,7 +306,7 @@ def _embedding_grad(tokens, grad_out, vocab, scale, padding=None):
     return total, size, torch.bincount(t, minlength=vocab)
 
 
-GRADS = [(512, 40, 24, "falling"), (513, 40, 24, "falling"), (512, 3, 1000, "one"), (300, 300, 41, "two"), (1, 1, 1, "uniform"), (2, 5, 8, "one"), (31, 7, 16, "uniform"), (33, 40, 5, "falling"), (64, 64, 64, "uniform"), (257, 3, 24, "uniform"),
+GRADS = [(1024, 40, 24, "falling"), (1025, 40, 24, "falling"), (1024, 3, 301, "one"), (512, 40, 24, "falling"), (513, 40, 24, "falling"), (512, 3, 1000, "one"), (300, 300, 41, "two"), (1, 1, 1, "uniform"), (2, 5, 8, "one"), (31, 7, 16, "uniform"), (33, 40, 5, "falling"), (64, 64, 64, "uniform"), (257, 3, 24, "uniform"),
          (500, 1000, 72, "falling"), (1000, 50, 2056, "falling"), (4096, 777, 130, "one"), (5000, 5000, 64, "two"), (9001, 33, 33, "falling"),
          (40000, 900, 64, "one"), (70001, 70000, 8, "falling"), (140000, 12, 9, "two")]
 

@@ -78,7 +78,7 @@ def test_embedding_arguments():
         assert L.asi_embedding(_em(), *args, None) == INVALID
     assert L.asi_embedding(None, P, P, P, None) == INVALID
     assert L.asi_embedding(_em(tokens=0), None, None, None, None) == OK
-    many = _em(tokens=1000)                                       # few tokens need no scratch
+    many = _em(tokens=2000)                                       # few tokens need no scratch
     need = L.asi_embedding_grad_workspace_bytes(many)
     assert need > 0 and need % 256 == 0 and L.asi_embedding_grad_workspace_bytes(_em()) == 0
     for ws, size in ((None, need), (P, need - 1), (P + 128, need)):
