@@ -79,7 +79,7 @@ def _value_bound(x, scale):
 
 
 SIZES = [(1, 1), (3, 2), (5, 7), (2, 63), (4, 64), (3, 65), (7, 257), (2, 1000), (3, 4095), (2, 4096), (3, 8193), (2, 32000), (3, 50001), (1, 131075),
-         (1, 200000)]
+         (1, 200000), (2, 40000), (2, 80000), (2100, 3001), (300, 17001), (70, 66000)]
 
 
 @pytest.mark.parametrize("dtype", list(DTYPES))
@@ -246,6 +246,13 @@ def test_token_logprobs_through_autograd_and_against_differences(dtype):
         # base + eps v is rounded too: U of |x| up to 16 for each entry, seen through the gradient
         moved = 16 * U / eps * float(x.grad.double().abs().sum())
         assert abs(slope - along) <= eps ** 2 / 6 * weight + values / eps + sizes + moved
+
+
+def test_second_derivatives_are_refused():
+    x = _logits(2, 50, torch.float32, 1).requires_grad_(True)
+    grad, = torch.autograd.grad(asi.token_logprobs(x).entropy.sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        grad.sum().backward()
 
 
 def test_no_rows_and_no_targets():
