@@ -247,6 +247,13 @@ template <typename O, int C> struct Columns {
         else if constexpr (C * sizeof(O) == 8) raw = load_words2(p);
         else raw = load_words4(p);
     }
+    // Has arrived here: the compiler would otherwise move the load of a row that may not count to where it turns out to, behind the others'.
+    __device__ __forceinline__ void arrived() {
+        if constexpr (C > 1 && C * sizeof(O) == 8) asm volatile("" : "+v"(raw.x), "+v"(raw.y));
+        if constexpr (C > 1 && C * sizeof(O) == 16) asm volatile("" : "+v"(raw.x), "+v"(raw.y), "+v"(raw.z), "+v"(raw.w));
+        if constexpr (C == 1 && sizeof(O) == 4) asm volatile("" : "+v"(raw));
+        if constexpr (C == 1 && sizeof(O) == 2) asm volatile("" : "+v"(raw.bits));
+    }
     __device__ __forceinline__ void add_to(float* f) const {
         if constexpr (C == 1) {
             f[0] += to_f32(raw);
@@ -327,6 +334,10 @@ template <typename O, typename D, int C, int P, bool ADD> __device__ __forceinli
                 if (last) begun = false;
             }
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int p = 0; p < P; ++p) v[u][p].arrived();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int e = e0 + u;
