@@ -10,8 +10,8 @@
 // the rows without a token with zeros.  Few tokens take one launch without scratch: a workgroup for each position looks for
 // the positions of its token, and adds up their rows if its own is the first.
 //
-// Measured: lookup of 4096 x 2048 in bf16 6.5 us; gradient of them into 32000 rows in fp32, zeros written past the caches, 58.4 us (4.8 TB/s),
-// of 32767 x 1000 added to rows in fp32 53.5 us, of which the sums are 34 (4.2 TB/s), the sort 13 and the join 6.
+// Measured: lookup of 4096 x 2048 in bf16 6.5 us; gradient of them into 32000 rows in fp32, zeros written past the caches, 56.7 us (4.9 TB/s),
+// of 32767 x 1000 added to rows in fp32 51.5 us, of which the sums are 32 (4.5 TB/s), the sort 13 and the join 6.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
