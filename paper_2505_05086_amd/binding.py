@@ -7,13 +7,15 @@ is no CPU fallback: a missing library raises at import of the first call.
 from __future__ import annotations
 
 import ctypes as C
+import importlib.machinery
+import importlib.util
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence, Tuple
 
 import torch
 
-from .build import LIB_PATH
+from .build import LIB_PATH, RECORDS_PATH
 
 ASI_OK = 0
 STATUS_NAMES = {0: "ASI_OK", 1: "ASI_ERR_INVALID_ARG", 2: "ASI_ERR_UNSUPPORTED",
@@ -79,6 +81,23 @@ class AsiError(RuntimeError):
     def __init__(self, status: int, where: str):
         super().__init__(f"{where}: {STATUS_NAMES.get(status, status)}")
         self.status = status
+
+
+_records = None
+
+
+def adamw_records(*args) -> Optional[bytes]:
+    """The records (AdamwTensor) of parameters, gradients and states as they are now, None if there is a tensor that none can be made of
+    (csrc/asi_records.cpp).  Raises if the module has not been built."""
+    global _records
+    if _records is None:
+        if not os.path.exists(RECORDS_PATH):
+            raise RuntimeError(f"{RECORDS_PATH} is not built; run `python -m paper_2505_05086_amd.build`")
+        loader = importlib.machinery.ExtensionFileLoader("asi_records", RECORDS_PATH)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("asi_records", loader))
+        loader.exec_module(module)
+        _records = module.adamw_records
+    return _records(*args)
 
 
 _lib = None

@@ -7,13 +7,11 @@ arithmetic runs in the HIP kernels; there is no CPU fallback.
 """
 from __future__ import annotations
 
-import ctypes as C
 import functools
 import itertools
 import operator
 from typing import List, NamedTuple, Optional, Sequence, Tuple
 
-import numpy as np
 import torch
 from torch.autograd.function import once_differentiable
 
@@ -459,40 +457,7 @@ def qk_norm_rotate_grad(q, k, q_gain, k_gain, cos, sin, grad_q: torch.Tensor, gr
 
 
 # ---- AdamW ------------------------------------------------------------------------------------------------
-_EXP_AVG, _NBYTES = operator.itemgetter("exp_avg"), operator.attrgetter("nbytes")
-
-
-class _Plan:
-    """The records of a group's tensors, kept between steps: only parameters' and gradients' addresses are read anew."""
-
-    def __init__(self, params, states, grads, bits):
-        self.params, self.grads = params, grads
-        self.first = [s["exp_avg"] for s in states]
-        self.sizes = [p.nbytes for p in params]
-        self.places = None
-        self.states = states
-        self.records = (B.AdamwTensor * max(1, len(params)))()
-        words = C.sizeof(B.AdamwTensor) // 8
-        self.words = np.frombuffer(self.records, dtype=np.int64).reshape(-1, words)[:len(params)]
-        self.reals = np.frombuffer(self.records, dtype=np.float64).reshape(-1, words)[:len(params)]
-        for r, p, s, g in zip(self.records, params, states, grads):
-            r.master = _ptr(s.get("master"))
-            r.exp_avg = s["exp_avg"].data_ptr()
-            r.exp_avg_sq = s["exp_avg_sq" if bits == 32 else "exp_avg_sqrt"].data_ptr()
-            if bits == 8:
-                r.exp_avg_scale, r.exp_avg_sq_scale = s["exp_avg_scale"].data_ptr(), s["exp_avg_sqrt_scale"].data_ptr()
-            r.count, r.param_dtype, r.grad_dtype = p.numel(), _DTYPE[p.dtype], _DTYPE[g.dtype]
-
-    def serves(self, params, grads) -> bool:
-        if len(params) != len(self.params) or not all(map(operator.is_, params, self.params)) or \
-                not all(map(operator.is_, map(_EXP_AVG, self.states), self.first)):
-            return False
-        places = list(map(torch.Tensor.data_ptr, params))
-        if places != self.places:            # a parameter's data was replaced: in another type or memory format?
-            if list(map(_NBYTES, params)) != self.sizes or not all(map(torch.Tensor.is_contiguous, params)):
-                return False
-            self.places = self.words[:, 0] = places
-        return all(map(operator.is_, grads, self.grads)) or all(a.dtype == b.dtype for a, b in zip(grads, self.grads))
+_CODES = (torch.float8_e4m3fn, torch.uint8)
 
 
 class AdamW(torch.optim.Optimizer):
@@ -512,41 +477,56 @@ class AdamW(torch.optim.Optimizer):
             raise ValueError("states have 8 or 32 bits")
         if not (0.0 <= betas[0] < 1.0 and 0.0 <= betas[1] < 1.0 and eps >= 0.0):
             raise ValueError("betas are in [0, 1) and eps is not negative")
-        self._plans = {}
         super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay, state_bits=state_bits,
                                       master=master, step=0))
 
-    def __setstate__(self, state) -> None:
-        super().__setstate__(state)
-        self._plans = {}
-
     def load_state_dict(self, state_dict) -> None:
         super().load_state_dict(state_dict)
-        self._plans.clear()
         # torch casts floating states to their parameter's type on the way: put back what this optimiser keeps in other types
         saved = [i for g in state_dict["param_groups"] for i in g["params"]]
         mine = [p for g in self.param_groups for p in g["params"]]
         for i, p in zip(saved, mine):
             for key, value in state_dict["state"].get(i, {}).items():
                 if isinstance(value, torch.Tensor):
-                    self.state[p][key] = value.detach().clone().to(p.device)
+                    self.state[p][key] = value.detach().to(p.device).clone(memory_format=torch.contiguous_format)
 
-    def _state(self, p: torch.Tensor, bits: int, master: bool) -> dict:
+    def _state(self, p: torch.Tensor, bits: int, master: bool) -> None:
+        """Makes what a parameter lacks of its state, and refuses what a record cannot be made of."""
         s = self.state[p]
         if p.dtype not in _DTYPE or not p.is_contiguous():
             raise TypeError("parameters are contiguous and fp32 or bf16")
+        second = "exp_avg_sq" if bits == 32 else "exp_avg_sqrt"
+        blocks = -(-p.numel() // B.ADAMW_BLOCK)
         if "exp_avg" not in s:
             held = torch.float32 if bits == 32 else torch.float8_e4m3fn
             zeros = lambda shape, dtype: torch.zeros(shape, dtype=torch.uint8 if dtype.itemsize == 1 else dtype,  # noqa: E731
                                                      device=p.device).view(dtype)
             s["exp_avg"] = zeros(p.shape, held)
-            s["exp_avg_sq" if bits == 32 else "exp_avg_sqrt"] = zeros(p.shape, held)
+            s[second] = zeros(p.shape, held)
             if bits == 8:
-                blocks = -(-p.numel() // B.ADAMW_BLOCK)
                 s["exp_avg_scale"], s["exp_avg_sqrt_scale"] = zeros((blocks,), torch.float32), zeros((blocks,), torch.float32)
         if master and p.dtype == torch.bfloat16 and "master" not in s:
             s["master"] = p.detach().float().clone()
-        return s
+        moments = (torch.float32,) if bits == 32 else _CODES
+        want = {"exp_avg": (p.numel(), moments), second: (p.numel(), moments)}
+        if bits == 8:
+            want.update(exp_avg_scale=(blocks, (torch.float32,)), exp_avg_sqrt_scale=(blocks, (torch.float32,)))
+        if "master" in s:
+            want["master"] = p.numel(), (torch.float32,)
+        for name, (count, dtypes) in want.items():
+            t = s.get(name)
+            if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.numel() != count or t.device != p.device or not t.is_contiguous():
+                raise ValueError(f"the state {name!r} of a parameter with {p.numel()} entries and states of {bits} bits is a contiguous "
+                                 f"tensor of {count} entries on its GPU, {' or '.join(map(str, dtypes))}")
+
+    def _ready(self, members, given, bits: int, master: bool) -> List[torch.Tensor]:
+        """The gradients in their parameters' layout, where the records could not be made at once."""
+        _place(*members)
+        for p, g in zip(members, given):
+            self._state(p, bits, master)
+            if g.is_sparse or g.shape != p.shape or g.dtype not in _DTYPE or g.device != p.device:
+                raise ValueError("a gradient is dense, of its parameter's shape and device, in fp32 or bf16")
+        return [g.contiguous() for g in given]
 
     @torch.no_grad()
     def step(self, closure=None, *, grad_scale: Optional[torch.Tensor] = None, skip: Optional[torch.Tensor] = None,
@@ -565,43 +545,27 @@ class AdamW(torch.optim.Optimizer):
         if grads is not None and len(grads) != sum(len(g["params"]) for g in self.param_groups):
             raise ValueError("one gradient (or None) for each parameter")
         at = 0
-        for n, group in enumerate(self.param_groups):
+        for group in self.param_groups:
             members = group["params"]
-            given = [p.grad for p in members] if grads is None else grads[at:at + len(members)]
+            given = [p.grad for p in members] if grads is None else list(grads[at:at + len(members)])
             at += len(members)
             if not all(map(operator.is_not, given, itertools.repeat(None))):
                 members = [p for p, g in zip(members, given) if g is not None]
                 given = [g for g in given if g is not None]
             if not members:
                 continue
-            bits = group["state_bits"]
-            plan = self._plans.get(n)
-            if plan is None or not plan.serves(members, given):
-                _place(*members, grad_scale, skip)
-                states = [self._state(p, bits, group["master"]) for p in members]
-                _place(*[t for s in states for t in s.values() if isinstance(t, torch.Tensor)])
-                plan = self._plans[n] = _Plan(list(members), states, list(given), bits)
-                self._check_grads(plan, given, True)
-                plan.serves(plan.params, plan.grads)
-            else:
-                self._check_grads(plan, given, False)
-            plan.words[:, 1] = list(map(torch.Tensor.data_ptr, plan.grads))
-            plan.reals[:, -2] = group["lr"]
-            plan.reals[:, -1] = group["weight_decay"]
-            stream = _stream(_place(members[0], grad_scale, skip))
+            bits, master = group["state_bits"], group["master"]
+            device = _place(members[0], grad_scale, skip)
+            options = self.state, bits == 8, master, device, group["lr"], group["weight_decay"]
+            records = B.adamw_records(members, given, *options)
+            if records is None:
+                given = self._ready(members, given, bits, master)
+                records = B.adamw_records(members, given, *options)
+                if records is None:
+                    raise ValueError("parameters, states and gradients are dense tensors on one GPU")
+            stream = _stream(device)
             group["step"] += 1
             b1, b2 = group["betas"]
-            B._check(B.lib().asi_adamw(len(members), C.addressof(plan.records), bits, b1, b2, group["eps"], group["step"],
-                                       _ptr(grad_scale), _ptr(skip), stream), "asi_adamw")
+            B._check(B.lib().asi_adamw(len(members), records, bits, b1, b2, group["eps"], group["step"], _ptr(grad_scale), _ptr(skip), stream),
+                     "asi_adamw")
         return loss
-
-    @staticmethod
-    def _check_grads(plan: _Plan, given: List[torch.Tensor], fresh: bool) -> None:
-        if not fresh and all(map(operator.is_, given, plan.grads)):
-            return
-        for i, (g, p) in enumerate(zip(given, plan.params)):
-            if g is plan.grads[i] and not fresh:
-                continue
-            if g.is_sparse or g.shape != p.shape or g.dtype not in _DTYPE or g.device != p.device:
-                raise ValueError("a gradient is dense, of its parameter's shape and device, in fp32 or bf16")
-            plan.grads[i] = g.contiguous()
