@@ -62,8 +62,10 @@ template <typename T> struct RowView {
 struct Sums {
     float m, s, w;
 };
-// Sums of another part joined to these: both relative to the larger of the two largest logits.
+// Sums of another part joined to these: both relative to the larger of the two largest logits.  Products are rounded by themselves, so
+// that a and b may change places and all threads of a row get the same sums.
 __device__ __forceinline__ Sums joined(const Sums& a, const Sums& b, float c) {
+#pragma clang fp contract(off)
     Sums r;
     r.m = fmaxf(a.m, b.m);
     const float da = max_nan(a.m - r.m, kFar), db = max_nan(b.m - r.m, kFar);
@@ -163,19 +165,26 @@ template <typename T, int U, bool AGAIN = false> __device__ __forceinline__ int 
 }
 
 struct Values {
-    float lse, logprob, entropy;
+    float lse, logprob, entropy, m, ls;       // m: the largest logit; ls: log s, -infinity without a logit above -infinity
 };
+// z - lse of a logit x
+__device__ __forceinline__ float logprob_of(float x, float m, float ls, float scale) {
+    if (x == -__builtin_inff() && ls == ls) return x;         // also where ls is -infinity
+    return fmaf(x - m, scale, -ls);
+}
 // target < 0: none
 template <typename T> __device__ __forceinline__ Values values_of(const Sums& a, const T* row, long long target, int vocab, long long ignore, float scale) {
     Values v;
     const float inf = __builtin_inff(), nan = __builtin_nanf("");
     const bool empty = a.s == 0.f;                // no logit above -infinity
     const float ls = logf(a.s);
+    v.m = a.m;
+    v.ls = ls;
     v.lse = empty ? -inf : a.m * scale + ls;
     v.entropy = empty ? 0.f : ls - scale * (a.w / a.s);
     if (target == ignore) v.logprob = 0.f;
     else if (target < 0 || target >= vocab) v.logprob = nan;
-    else v.logprob = empty ? -inf : (to_f32(row[target]) - a.m) * scale - ls;
+    else v.logprob = logprob_of(to_f32(row[target]), a.m, ls, scale);
     return v;
 }
 
@@ -226,9 +235,8 @@ template <int THREADS> struct TopScratch {
     int who[THREADS];                 // threads whose vectors are looked at again
     int count, many;
 };
-__device__ __forceinline__ void write_alternative(const Args& a, long long row, float lse, int place, unsigned long long key) {
-    const float x = logit_of(key);
-    a.top_logprob[row * a.top + place] = x == -__builtin_inff() && lse == lse ? x : x * a.scale - lse;     // also where lse is -infinity
+__device__ __forceinline__ void write_alternative(const Args& a, long long row, const Values& v, int place, unsigned long long key) {
+    a.top_logprob[row * a.top + place] = logprob_of(logit_of(key), v.m, v.ls, a.scale);
     a.top_index[row * a.top + place] = (int)~(uint32_t)key;
 }
 // write(place, key) for the `top` largest of the row's logits, top <= the row's length.  `most`: the order of the largest of this
@@ -381,7 +389,7 @@ template <typename T, int THREADS, int U, bool TOP, bool SPLIT> __global__ __lau
             find_top<T, THREADS>(r, most, want, index0, &top, [&](int place, unsigned long long key) { keys[place] = key; });
             for (int i = want + threadIdx.x; i < a.top; i += THREADS) keys[i] = 0;
         } else {
-            find_top<T, THREADS>(r, most, a.top, 0, &top, [&](int place, unsigned long long key) { write_alternative(a, row, val.lse, place, key); });
+            find_top<T, THREADS>(r, most, a.top, 0, &top, [&](int place, unsigned long long key) { write_alternative(a, row, val, place, key); });
         }
     }
 }
@@ -405,7 +413,7 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void k_join_par
         int before = 0;
 #pragma unroll 8
         for (int k = 0; k < n; ++k) before += key[k] > mine;
-        if (mine && before < a.top) write_alternative(a, row, val.lse, before, mine);
+        if (mine && before < a.top) write_alternative(a, row, val, before, mine);
     }
 }
 

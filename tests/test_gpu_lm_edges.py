@@ -83,3 +83,51 @@ def test_adamw_refuses_a_tensor_that_left_its_gpu():
     with pytest.raises(ValueError):
         opt.step()
     assert torch.equal(params[0], before)
+
+
+# ---- token log probabilities: what is extreme ---------------------------------------------------------------
+def _in_order(x, top):
+    """Indices of the largest, NaN before everything, equal ones by ascending index."""
+    key = torch.where(torch.isnan(x), 1.0, 0.0).double()
+    by_value = torch.sort(x.double().nan_to_num(0.0, INF, -INF), dim=-1, descending=True, stable=True).indices
+    return by_value.gather(-1, torch.sort(key.gather(-1, by_value), dim=-1, descending=True, stable=True).indices)[..., :top]
+
+
+def _gaps(x, scale):
+    """scale * (x - the row's largest), its log softmax, and the sum of p |gap|, in 64 bits."""
+    gap = (x.double() - x.double().amax(-1, keepdim=True)) * scale
+    logp = gap - gap.exp().sum(-1, keepdim=True).log()
+    return gap, logp, (logp.exp() * gap.abs()).sum(-1, keepdim=True)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows,vocab", [(3, 50), (4, 1000), (3, 32000), (2, 50001), (3, 200000), (2100, 3001)])
+@pytest.mark.parametrize("middle,spread,scale", [(3e4, 1.0, 1.0), (-1000.0, 3.0, 1.0), (0.0, 3.0, 1024.0), (1e6, 10.0, 0.5)])
+def test_alternatives_are_as_exact_as_the_target(rows, vocab, middle, spread, scale, dtype):
+    x = (middle + spread * _randn(vocab, rows, vocab)).to(DTYPES[dtype])
+    top = min(vocab, 20)
+    index = _in_order(x, top)
+    gap, logp, mean = _gaps(x, scale)
+    # gap: the difference's, the scale's and the last difference's roundings; log s: each exponent has four (difference, factor twice,
+    # product), the sum 128 that change its last bit, its joining and the logarithm as many again, of at most 13
+    bound = U * (8 * gap.abs() + 8 * mean + 320)
+    r = asi.token_logprobs(x, index[:, -1].contiguous(), top=top, scale=scale)
+    assert torch.equal(r.top_index, index)
+    off = (r.top_logprob.double() - logp.gather(1, index)).abs() - bound.gather(1, index)
+    assert float(off.max()) <= 0
+    assert torch.equal(r.top_logprob[:, -1], r.logprob)          # the same number either way
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("vocab", [9, 2000, 33000, 200000])
+def test_alternatives_where_the_scaled_logits_overflow(vocab, dtype):
+    x = torch.zeros(2, vocab, dtype=DTYPES[dtype], device="cuda")
+    x[:, 4], x[:, 7], x[:, 2] = 2e20, 1e20, -INF
+    x[1, 5] = 2e20
+    targets = torch.tensor([4, 5], device="cuda")
+    r = asi.token_logprobs(x, targets, top=4, scale=1e20)
+    assert r.top_index.tolist() == [[4, 7, 0, 1], [4, 5, 7, 0]]
+    half = float(torch.tensor(2.0).log())
+    assert r.top_logprob[0].tolist() == [0.0, -INF, -INF, -INF] and r.top_logprob[1, 2:].tolist() == [-INF, -INF]
+    assert float((r.top_logprob[1, :2] + half).abs().max()) <= 4 * U and abs(float(r.logprob[1]) + half) <= 4 * U
+    assert float(r.logprob[0]) == 0 and float(r.entropy[0]) == 0 and abs(float(r.entropy[1]) - half) <= 4 * U
