@@ -170,7 +170,9 @@ struct Values {
 // z - lse of a logit x
 __device__ __forceinline__ float logprob_of(float x, float m, float ls, float scale) {
     if (x == -__builtin_inff() && ls == ls) return x;         // also where ls is -infinity
-    return fmaf(x - m, scale, -ls);
+    const float d = x - m;
+    // finite logits farther apart than fp32 reaches: both scaled first
+    return d == -__builtin_inff() ? fmaf(x, scale, -m * scale) - ls : fmaf(d, scale, -ls);
 }
 // target < 0: none
 template <typename T> __device__ __forceinline__ Values values_of(const Sums& a, const T* row, long long target, int vocab, long long ignore, float scale) {

@@ -131,3 +131,19 @@ def test_alternatives_where_the_scaled_logits_overflow(vocab, dtype):
     assert r.top_logprob[0].tolist() == [0.0, -INF, -INF, -INF] and r.top_logprob[1, 2:].tolist() == [-INF, -INF]
     assert float((r.top_logprob[1, :2] + half).abs().max()) <= 4 * U and abs(float(r.logprob[1]) + half) <= 4 * U
     assert float(r.logprob[0]) == 0 and float(r.entropy[0]) == 0 and abs(float(r.entropy[1]) - half) <= 4 * U
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("vocab", [9, 2000, 33000, 200000])
+def test_differences_that_overflow_before_they_are_scaled(vocab, dtype):
+    x = torch.zeros(1, vocab, dtype=DTYPES[dtype], device="cuda")
+    x[0, 3], x[0, 8] = 3e38, -3e38
+    scale = float(torch.tensor(1e-20))
+    z = x.double() * scale
+    targets = torch.tensor([8], device="cuda")
+    for r in (asi.token_logprobs(x, targets, top=9, scale=scale), asi.token_logprobs_grad(x, targets, torch.ones(1, device="cuda"), scale=scale)):
+        want = float(z[0, 8] - z[0, 3])
+        assert abs(float(r.logprob) - want) <= 4 * U * abs(want) and float(r.entropy) == 0
+    r = asi.token_logprobs(x, top=vocab if vocab < 64 else 5, scale=scale)
+    want = z[0, r.top_index[0]] - z[0, 3]
+    assert float(((r.top_logprob[0].double() - want).abs() - 4 * U * want.abs()).max()) <= 0
