@@ -30,10 +30,13 @@ namespace asi {
 namespace {
 
 constexpr float kLowest = -3.402823466e+38f;     // stands for a thread that has seen no logit above -infinity
-// Differences are not let below this: exp(scale d) is 0 there for every scale that is taken, and its product with d is 0, not NaN.
-constexpr float kFar = -1e24f;
+// The scale as the kernels use it.
+struct Scale {
+    float c;             // exp(scale d) = 2^(c d)
+    float far;           // differences are not let below this, where 2^(c d) is 0 and its products with d and c d are, not NaN
+};
 constexpr float kLeastScale = 1e-20f, kMostScale = 1e20f;
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -64,32 +67,32 @@ struct Sums {
 };
 // Sums of another part joined to these: both relative to the larger of the two largest logits.  Products are rounded by themselves, so
 // that a and b may change places and all threads of a row get the same sums.
-__device__ __forceinline__ Sums joined(const Sums& a, const Sums& b, float c) {
+__device__ __forceinline__ Sums joined(const Sums& a, const Sums& b, const Scale& k) {
 #pragma clang fp contract(off)
     Sums r;
     r.m = fmaxf(a.m, b.m);
-    const float da = max_nan(a.m - r.m, kFar), db = max_nan(b.m - r.m, kFar);
-    const float fa = exp2_fast(da * c), fb = exp2_fast(db * c);
+    const float da = max_nan(a.m - r.m, k.far), db = max_nan(b.m - r.m, k.far);
+    const float fa = exp2_fast(da * k.c), fb = exp2_fast(db * k.c);
     r.s = a.s * fa + b.s * fb;
     r.w = fa * (a.w + da * a.s) + fb * (b.w + db * b.s);
     return r;
 }
-template <int WIDTH> __device__ __forceinline__ Sums over_lanes(Sums a, float c) {
+template <int WIDTH> __device__ __forceinline__ Sums over_lanes(Sums a, const Scale& k) {
 #pragma unroll
     for (int o = WIDTH / 2; o; o >>= 1) {
         Sums b;
         b.m = __shfl_xor(a.m, o); b.s = __shfl_xor(a.s, o); b.w = __shfl_xor(a.w, o);
-        a = joined(a, b, c);
+        a = joined(a, b, k);
     }
     return a;
 }
 // Over the workgroup; every thread gets the result.
-template <int THREADS> __device__ __forceinline__ Sums over_workgroup(Sums a, float c, Sums* scratch) {
+template <int THREADS> __device__ __forceinline__ Sums over_workgroup(Sums a, const Scale& k, Sums* scratch) {
     constexpr int W = THREADS / 64;
-    a = over_lanes<64>(a, c);
+    a = over_lanes<64>(a, k);
     if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = a;
     __syncthreads();
-    return over_lanes<W>(scratch[threadIdx.x & (W - 1)], c);
+    return over_lanes<W>(scratch[threadIdx.x & (W - 1)], k);
 }
 // Keeps the instructions of one vector together: interleaving several costs more registers than it saves time.
 __device__ __forceinline__ void one_at_a_time() { __builtin_amdgcn_sched_barrier(0); }
@@ -99,12 +102,12 @@ __device__ __forceinline__ void taken_apart_anew(Vec16<bf16_t>* v) {
     asm volatile("" : "+v"(v->raw.x), "+v"(v->raw.y), "+v"(v->raw.z), "+v"(v->raw.w));
 }
 // One more logit of a thread
-__device__ __forceinline__ void take_one(Sums* a, float x, float c) {
+__device__ __forceinline__ void take_one(Sums* a, float x, const Scale& k) {
     Sums b{x > kLowest ? x : kLowest, 0.f, 0.f};
-    const float d = max_nan(x - b.m, kFar);
-    b.s = exp2_fast(d * c);
+    const float d = max_nan(x - b.m, k.far);
+    b.s = exp2_fast(d * k.c);
     b.w = d * b.s;
-    *a = joined(*a, b, c);
+    *a = joined(*a, b, k);
 }
 template <typename T> __device__ __forceinline__ float largest(const Vec16<T>& v) {
     float m = v.get(0);
@@ -118,14 +121,14 @@ template <typename T> __device__ __forceinline__ void set_nothing(Vec16<T>* v) {
     v->raw = make_uint4(w, w, w, w);
 }
 // Vectors v[0 .. U) of which the first `have` are the thread's own or nothing; `have` is the same in all threads
-template <typename T, int U> __device__ __forceinline__ void take(Sums* a, Vec16<T>* v, int have, float c) {
+template <typename T, int U> __device__ __forceinline__ void take(Sums* a, Vec16<T>* v, int have, const Scale& k) {
     float m = a->m;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (u < have) m = fmaxf(m, largest(v[u]));
         if (U > 2) one_at_a_time();
     }
-    const float shift = max_nan(a->m - m, kFar), f = exp2_fast(shift * c);
+    const float shift = max_nan(a->m - m, k.far), f = exp2_fast(shift * k.c);
     a->w = f * (a->w + shift * a->s);
     a->s *= f;
     a->m = m;
@@ -135,7 +138,7 @@ template <typename T, int U> __device__ __forceinline__ void take(Sums* a, Vec16
             if (U > 4) taken_apart_anew(&v[u]);       // up to 4 vectors leave room for their values
 #pragma unroll
             for (int i = 0; i < Vec16<T>::N; ++i) {
-                const float d = max_nan(v[u].get(i) - m, kFar), e = exp2_fast(d * c);
+                const float d = max_nan(v[u].get(i) - m, k.far), e = exp2_fast(d * k.c);
                 a->s += e;
                 a->w += d * e;
             }
@@ -201,6 +204,7 @@ struct Args {
     long long stride, ignore;
     int vocab, top;
     float scale;
+    Scale k;
     // rows in parts of `part` logits: [row][part] sums, [row][part][top] keys of alternatives, 0 where there are fewer
     int parts, part;
     Sums* sums;
@@ -365,16 +369,16 @@ template <typename T, int THREADS, int U, bool TOP, bool SPLIT> __global__ __lau
     const T* x = static_cast<const T*>(a.x) + row * a.stride;
     const int n = SPLIT ? min(a.part, a.vocab - index0) : a.vocab;
     const RowView<T> r(x + index0, n);
-    const float c = a.scale * kLog2e;
+    const Scale k = a.k;
     Sums acc{kLowest, 0.f, 0.f};
     Vec16<T> v[U];
     for (int base = 0; base < r.nvec; base += THREADS * U) {
         const int have = load<T, U>(r, base + threadIdx.x, THREADS, v);
-        take<T, U>(&acc, v, have, c);
+        take<T, U>(&acc, v, have, k);
     }
     const uint32_t most = TOP && (int)threadIdx.x < r.nvec ? order_of_most(acc) : 0u;
-    if (const int l = r.loose(threadIdx.x); l >= 0) take_one(&acc, to_f32(r.x[l]), c);
-    const Sums all = over_workgroup<THREADS>(acc, c, scratch);
+    if (const int l = r.loose(threadIdx.x); l >= 0) take_one(&acc, to_f32(r.x[l]), k);
+    const Sums all = over_workgroup<THREADS>(acc, k, scratch);
     Values val{};
     if constexpr (SPLIT) {
         if (threadIdx.x == 0) a.sums[blockIdx.x] = all;
@@ -405,7 +409,7 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void k_join_par
     const int p = threadIdx.x & (kMaxParts - 1);
     Sums all{kLowest, 0.f, 0.f};
     if (p < a.parts) all = a.sums[row * a.parts + p];
-    all = over_lanes<kMaxParts>(all, a.scale * kLog2e);
+    all = over_lanes<kMaxParts>(all, a.k);
     const long long target = a.targets ? a.targets[row] : a.ignore;
     const Values val = values_of(all, static_cast<const T*>(a.x) + row * a.stride, target, a.vocab, a.ignore, a.scale);
     if (threadIdx.x == 0) write_values(a, row, val);
@@ -431,6 +435,7 @@ struct GradArgs {
     long long stride, grad_stride, ignore;
     int vocab;
     float scale;
+    Scale k;
 };
 // KEEP: vectors that a thread keeps in registers.  REST: the row is longer, its rest is read again.
 template <typename T, int THREADS, int KEEP, bool REST> __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const GradArgs g) {
@@ -440,22 +445,22 @@ template <typename T, int THREADS, int KEEP, bool REST> __global__ __launch_boun
     const T* x = static_cast<const T*>(g.x) + row * g.stride;
     T* dx = static_cast<T*>(g.dx) + row * g.grad_stride;
     const RowView<T> r(x, g.vocab);
-    const float c = g.scale * kLog2e;
+    const Scale s = g.k;
     const int l = r.loose(threadIdx.x);
     const float loose = l >= 0 ? to_f32(x[l]) : 0.f;
     const long long target = g.targets ? g.targets[row] : g.ignore;
     Sums acc{kLowest, 0.f, 0.f};
     Vec16<T> kept[KEEP], again[2];
     const int have = load<T, KEEP>(r, threadIdx.x, THREADS, kept);
-    take<T, KEEP>(&acc, kept, have, c);
+    take<T, KEEP>(&acc, kept, have, s);
     if constexpr (REST) {
         for (int base = KEEP * THREADS; base < r.nvec; base += 2 * THREADS) {
             const int more = load<T, 2, true>(r, base + threadIdx.x, THREADS, again);
-            take<T, 2>(&acc, again, more, c);
+            take<T, 2>(&acc, again, more, s);
         }
     }
-    if (l >= 0) take_one(&acc, loose, c);
-    const Sums all = over_workgroup<THREADS>(acc, c, scratch);
+    if (l >= 0) take_one(&acc, loose, s);
+    const Sums all = over_workgroup<THREADS>(acc, s, scratch);
     const Values val = values_of(all, x, target, g.vocab, g.ignore, g.scale);
     if (threadIdx.x == 0) {
         if (g.logprob) g.logprob[row] = val.logprob;
@@ -464,14 +469,15 @@ template <typename T, int THREADS, int KEEP, bool REST> __global__ __launch_boun
     const bool given = target != g.ignore, in_range = target >= 0 && target < g.vocab;
     const float wa = given && g.a ? g.a[row] : 0.f, wb = g.b ? g.b[row] : 0.f;
     const bool empty = all.s == 0.f;
-    // dx_i = scale (a delta_i - p_i (a + b (log p_i + entropy))),  log p_i = scale d_i - log s:  p_i (k0 + k1 d_i) with these
+    // dx_i = scale (a delta_i - p_i (a + b (log p_i + entropy))),  log p_i = scale d_i - log s:  e_i (k0 + k1 c d_i) with these.  The scale
+    // times d_i is within what has a probability, the scale's square need not be within fp32.
     const float inv = empty ? 0.f : 1.f / all.s, ls = empty ? 0.f : logf(all.s);
     const float bad = given && !in_range ? __builtin_nanf("") : 0.f;
-    const float k0 = -g.scale * inv * (wa + wb * (val.entropy - ls)) + bad, k1 = -g.scale * inv * wb * g.scale;
+    const float k0 = -g.scale * inv * (wa + wb * (val.entropy - ls)) + bad, k1 = -g.scale * inv * wb * kLn2;
     const float hot = empty ? 0.f : g.scale * wa;
     auto grad = [&](float v) {
-        const float d = max_nan(v - all.m, kFar), e = exp2_fast(d * c);
-        return e * (k0 + k1 * d);
+        const float d = max_nan(v - all.m, s.far) * s.c;
+        return exp2_fast(d) * (k0 + k1 * d);
     };
     // dx's rows need not lie as x's do
     const bool vec = ((reinterpret_cast<uintptr_t>(dx + r.head)) & 15) == 0;
@@ -511,6 +517,10 @@ template <typename T, int THREADS, int KEEP, bool REST> __global__ __launch_boun
 }
 
 // ---- host ----
+Scale scale_of(const asi_logprob_desc* d) {
+    const float c = d->scale * kLog2e;
+    return {c, -300.f / c};                       // 2^-300 is below the least number of fp32
+}
 asi_status check(const asi_logprob_desc* d) {
     if (!d) return ASI_ERR_INVALID_ARG;
     if (!dtype_ok(d->dtype)) return ASI_ERR_UNSUPPORTED;
@@ -594,7 +604,7 @@ asi_status asi_token_logprobs(const asi_logprob_desc* desc, const void* logits, 
         !aligned(lse, 4) || (desc->top && (!top_logprob || !top_index || !aligned(top_logprob, 4) || !aligned(top_index, 8))))
         return ASI_ERR_INVALID_ARG;
     Args a{logits, targets, logprob, entropy, lse, top_logprob, top_index, desc->row_stride, desc->ignore_index, (int)desc->vocab,
-           desc->top, desc->scale, parts_of(desc), 0, nullptr, nullptr};
+           desc->top, desc->scale, scale_of(desc), parts_of(desc), 0, nullptr, nullptr};
     if (a.parts > 1) {
         if (!ws || !aligned(ws, 256) || ws_bytes < asi_token_logprobs_workspace_bytes(desc)) return ASI_ERR_WORKSPACE;
         a.part = (a.vocab + a.parts - 1) / a.parts;
@@ -619,7 +629,7 @@ asi_status asi_token_logprobs_grad(const asi_logprob_desc* desc, const void* log
         !aligned(grad_logprob, 4) || !aligned(grad_entropy, 4) || !aligned(logprob, 4) || !aligned(entropy, 4))
         return ASI_ERR_INVALID_ARG;
     const GradArgs g{logits, dlogits, targets, grad_logprob, grad_entropy, logprob, entropy, desc->row_stride, desc->grad_stride,
-                     desc->ignore_index, (int)desc->vocab, desc->scale};
+                     desc->ignore_index, (int)desc->vocab, desc->scale, scale_of(desc)};
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (desc->dtype == ASI_F32) backward<float>(g, (unsigned)desc->rows, st);
     else backward<bf16_t>(g, (unsigned)desc->rows, st);

@@ -147,3 +147,35 @@ def test_differences_that_overflow_before_they_are_scaled(vocab, dtype):
     r = asi.token_logprobs(x, top=vocab if vocab < 64 else 5, scale=scale)
     want = z[0, r.top_index[0]] - z[0, 3]
     assert float(((r.top_logprob[0].double() - want).abs() - 4 * U * want.abs()).max()) <= 0
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("scale", [1e-20, 1e-8, 1.0, 2e7, 1e8, 1e12, 1e20])
+@pytest.mark.parametrize("rows,vocab", [(3, 9), (2, 1000), (2, 40000), (1, 300000)])
+def test_gradients_at_every_scale_beside_masked_logits(rows, vocab, scale, dtype):
+    scale = float(torch.tensor(scale))
+    x = (_randn(vocab, rows, vocab) * (3 / scale)).to(DTYPES[dtype])
+    x[:, ::3] = -INF
+    x[:, 1::5] = torch.finfo(x.dtype).min
+    targets = torch.full((rows,), 2, device="cuda")
+    x[:, 2] = 1 / scale
+    a, b = _randn(1, rows), _randn(2, rows)
+    z = x.double() * scale
+    logp = torch.log_softmax(z, -1)
+    p, entropy = logp.exp(), torch.special.entr(logp.exp()).sum(-1, keepdim=True)
+    r = asi.token_logprobs_grad(x, targets, a, b, scale=scale)
+    finite = torch.where(z.abs() < 1e3, z.abs(), 0.0).amax(-1)
+    # as in ordinary ranges: 8 roundings of the largest |z| that has a probability, and the sums'
+    bound = U * (8 * finite + 256)
+    assert float(((r.logprob.double() - logp[:, 2]).abs() - bound).max()) <= 0
+    assert float(((r.entropy.double() - entropy[:, 0]).abs() - bound - 256 * U * entropy[:, 0].clamp_min(1.0)).max()) <= 0
+    wa, wb = a.double()[:, None], b.double()[:, None]
+    hot = torch.zeros_like(p)
+    hot[:, 2] = 1
+    logp = logp.clamp_min(-1e4)
+    want = scale * (wa * (hot - p) - wb * p * (logp + entropy))
+    size = p * (wa.abs() + wb.abs() * (logp.abs() + entropy + 1))
+    err = scale * ((2 * bound[:, None] + 16 * U) * size + U * 256 * wb.abs() * p * entropy.clamp_min(1.0) + 4 * U * hot * wa.abs())
+    off = (r.grad.double() - want).abs() - err - (2.0 ** -8 if x.dtype == torch.bfloat16 else U) * 1.01 * want.abs() - 1e-38
+    assert float(off.max()) <= 0
+    assert (r.grad[:, ::3] == 0).all()
