@@ -323,12 +323,12 @@ __device__ __forceinline__ void find_top(const RowView<T>& r, uint32_t most, int
         }
         return;
     }
-    unsigned long long last = ~0ull;              // no key is that: an index is not negative
+    unsigned long long last = 0;                  // of the place before
     for (int place = 0; place < top; ++place) {
         unsigned long long best = 0;
         auto look = [&](float x, int i) {
             const unsigned long long key = rank_key(x, index0 + i);
-            if (key < last && key > best) best = key;
+            if ((place == 0 || key < last) && key > best) best = key;      // NaN at index 0 has the largest key there is
         };
         if (const int l = r.loose(threadIdx.x); l >= 0) look(to_f32(r.x[l]), l);
 #pragma unroll 1

@@ -179,3 +179,11 @@ def test_gradients_at_every_scale_beside_masked_logits(rows, vocab, scale, dtype
     off = (r.grad.double() - want).abs() - err - (2.0 ** -8 if x.dtype == torch.bfloat16 else U) * 1.01 * want.abs() - 1e-38
     assert float(off.max()) <= 0
     assert (r.grad[:, ::3] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("vocab", [40, 1025, 1500, 8192, 32000, 200000])
+def test_rows_of_nothing_but_nan(vocab, dtype):
+    for top in (1, 5, 40):
+        r = asi.token_logprobs(torch.full((2, vocab), NAN, dtype=DTYPES[dtype], device="cuda"), top=top)
+        assert torch.equal(r.top_index, torch.arange(top, device="cuda").expand(2, top)) and torch.isnan(r.top_logprob).all()
