@@ -7,7 +7,7 @@
 // Forward: a workgroup takes a row in one pass, several vectors a thread at a time; every thread keeps a running largest logit
 // and the sums relative to it.
 // Top alternatives: each wave takes the c largest of its threads' largest logits, c = ceil(top / waves) + 1; the `top`-th of all of
-// those is a bound that at least `top` logits reach.  Only the vectors of threads whose largest reaches it are looked at again, shared by all threads,
+// those is a bound that at least `top` logits reach.  Only the vectors of threads whose largest may reach it are looked at again, shared by all threads,
 // and hand over the logits that reach it, a few more than wanted; of these each finds its place by counting the ones before
 // it.  Rows where too many reach the bound (many equal logits) are searched `top` times instead.
 //
@@ -245,10 +245,13 @@ __device__ __forceinline__ void write_alternative(const Args& a, long long row, 
     a.top_logprob[row * a.top + place] = logprob_of(logit_of(key), v.m, v.ls, a.scale);
     a.top_index[row * a.top + place] = (int)~(uint32_t)key;
 }
-// write(place, key) for the `top` largest of the row's logits, top <= the row's length.  `most`: the order of the largest of this
-// thread's vectors, one that is there, 0 without any; `index0`: of the row's first logit.
+// The order of the largest of a thread's vectors, 0 without any: `least` is one that is there, none is above `upto`.
+struct Most {
+    uint32_t least, upto;
+};
+// write(place, key) for the `top` largest of the row's logits, top <= the row's length.  `index0`: of the row's first logit.
 template <typename T, int THREADS, typename F>
-__device__ __forceinline__ void find_top(const RowView<T>& r, uint32_t most, int top, int index0, TopScratch<THREADS>* sc, F write) {
+__device__ __forceinline__ void find_top(const RowView<T>& r, const Most& most, int top, int index0, TopScratch<THREADS>* sc, F write) {
     constexpr int W = THREADS / 64, N = Vec16<T>::N;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     // Waves whose threads do not all have a vector bound nothing; where there is no other, everything is handed over (less than
@@ -257,7 +260,7 @@ __device__ __forceinline__ void find_top(const RowView<T>& r, uint32_t most, int
     const int c = full ? min(64, (top + full - 1) / full + 1) : 0;
     static_assert(W <= 16 && W * (ASI_LOGPROB_MAX_TOP / W + 2) <= kBounds, "room for the waves' largest");
     if (wave < full) {
-        uint32_t left = most;
+        uint32_t left = most.least;
         for (int got = 0; got < c;) {
             const uint32_t m = wave_max(left);
             const unsigned long long with = __ballot(left == m);
@@ -295,7 +298,7 @@ __device__ __forceinline__ void find_top(const RowView<T>& r, uint32_t most, int
             if (at < kCandidates) sc->key[at] = rank_key(x, index0 + i);
         }
     };
-    if (most >= bound && most) sc->who[atomicAdd(&sc->many, 1)] = threadIdx.x;
+    if (most.upto >= bound && most.upto) sc->who[atomicAdd(&sc->many, 1)] = threadIdx.x;
     if (const int l = r.loose(threadIdx.x); l >= 0) hand_over(to_f32(r.x[l]), l);
     __syncthreads();
     {
@@ -350,11 +353,12 @@ __device__ __forceinline__ void find_top(const RowView<T>& r, uint32_t most, int
 }
 
 // ---- forward ----------------------------------------------------------------------------------------------------
-// The order of the largest of a thread's vectors, where their sums are `a`: a logit that is there, as the bound of the alternatives needs
-__device__ __forceinline__ uint32_t order_of_most(const Sums& a) {
+// The largest of a thread's vectors where their sums are `a`
+__device__ __forceinline__ Most most_of(const Sums& a) {
     const float inf = __builtin_inff();
-    if (a.s != a.s) return a.m == inf ? order_of(inf) : 0xffffffffu;      // +infinity, or else NaN, is what makes the sum NaN
-    return order_of(a.s == 0.f ? -inf : a.m);
+    if (a.s != a.s) return {a.m == inf ? order_of(inf) : 0xffffffffu, 0xffffffffu};      // +infinity makes the sum NaN, beside NaN or without
+    const uint32_t o = order_of(a.s == 0.f ? -inf : a.m);
+    return {o, o};
 }
 __device__ __forceinline__ void write_values(const Args& a, long long row, const Values& v) {
     if (a.logprob) a.logprob[row] = v.logprob;
@@ -376,7 +380,7 @@ template <typename T, int THREADS, int U, bool TOP, bool SPLIT> __global__ __lau
         const int have = load<T, U>(r, base + threadIdx.x, THREADS, v);
         take<T, U>(&acc, v, have, k);
     }
-    const uint32_t most = TOP && (int)threadIdx.x < r.nvec ? order_of_most(acc) : 0u;
+    const Most most = TOP && (int)threadIdx.x < r.nvec ? most_of(acc) : Most{0u, 0u};
     if (const int l = r.loose(threadIdx.x); l >= 0) take_one(&acc, to_f32(r.x[l]), k);
     const Sums all = over_workgroup<THREADS>(acc, k, scratch);
     Values val{};

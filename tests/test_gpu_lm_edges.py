@@ -187,3 +187,33 @@ def test_rows_of_nothing_but_nan(vocab, dtype):
     for top in (1, 5, 40):
         r = asi.token_logprobs(torch.full((2, vocab), NAN, dtype=DTYPES[dtype], device="cuda"), top=top)
         assert torch.equal(r.top_index, torch.arange(top, device="cuda").expand(2, top)) and torch.isnan(r.top_logprob).all()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("vocab", [40, 1025, 1500, 8192, 32000, 200000])
+def test_rows_of_many_nan(vocab, dtype):
+    rows = [torch.full((vocab,), NAN, device="cuda")]                        # nothing else
+    for k, share in enumerate((0.5, 0.1)):
+        x = _randn(k, vocab)
+        x[torch.rand(vocab, device="cuda", generator=_gen(10 + k)) < share] = NAN
+        x[torch.rand(vocab, device="cuda", generator=_gen(20 + k)) < share] = INF
+        rows.append(x)
+    rows.append(torch.full((vocab,), INF, device="cuda"))
+    rows[3][vocab // 2:] = NAN
+    x = torch.stack(rows).to(DTYPES[dtype])
+    for top in (1, 5, 40):
+        r = asi.token_logprobs(x, top=top)
+        assert torch.equal(r.top_index, _in_order(x, top)) and torch.isnan(r.top_logprob).all()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("vocab,apart", [(8192, 64), (32000, 64), (200000, 64)])
+def test_nan_beside_infinity_before_other_nan(vocab, apart, dtype):
+    """The first thread's vector holds both; many other threads hold NaN alone, further on."""
+    x = _randn(vocab, 1, vocab)
+    x[0, 0], x[0, 1] = INF, NAN
+    x[0, 640:640 + 40 * apart:apart] = NAN
+    x = x.to(DTYPES[dtype])
+    for top in (1, 5, 30):
+        r = asi.token_logprobs(x, top=top)
+        assert torch.equal(r.top_index, _in_order(x, top))
