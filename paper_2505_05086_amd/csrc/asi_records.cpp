@@ -1,10 +1,12 @@
 // Python module: the records of an AdamW step (asi_adamw_tensor of include/asi_lm.h) from the tensors of that step.
 //
 // Every address, type, length and layout is read from the tensors anew at every step, whatever was exchanged in between, and
-// nothing is kept.  These are some 700 reads for 74 tensors with two states each.
+// nothing is kept.  These are some 700 reads for 74 tensors with two states each.  The versions of the tensors that the step writes go up,
+// so that a backward pass that saved one of them before raises.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
+#include <vector>
 
 #include "../../include/asi_lm.h"
 
@@ -25,16 +27,18 @@ const at::Tensor* plain(PyObject* o, long long device) {
 int32_t kind(const at::Tensor& t) {
     return t.scalar_type() == at::kFloat ? ASI_F32 : t.scalar_type() == at::kBFloat16 ? ASI_BF16 : -1;
 }
+using Written = std::vector<c10::TensorImpl*>;
 // Data of an entry of a parameter's state: `count` numbers in fp32, or codes of a byte.  False if it is not that.
-bool held(PyObject* state, PyObject* name, bool codes, int64_t count, long long device, void** data) {
+bool held(PyObject* state, PyObject* name, bool codes, int64_t count, long long device, void** data, Written* written) {
     const at::Tensor* t = plain(PyDict_GetItemWithError(state, name), device);
     if (!t || t->numel() != count) return false;
     const at::ScalarType s = t->scalar_type();
     if (codes ? s != at::kFloat8_e4m3fn && s != at::kByte : s != at::kFloat) return false;
     *data = t->data_ptr();
+    written->push_back(t->unsafeGetTensorImpl());
     return true;
 }
-bool fill(asi_adamw_tensor* r, PyObject* param, PyObject* grad, PyObject* states, bool eight, bool master, long long device) {
+bool fill(asi_adamw_tensor* r, PyObject* param, PyObject* grad, PyObject* states, bool eight, bool master, long long device, Written* written) {
     const at::Tensor *p = plain(param, device), *g = plain(grad, device);
     if (!p || !g || !p->sizes().equals(g->sizes())) return false;
     r->param_dtype = kind(*p);
@@ -42,12 +46,13 @@ bool fill(asi_adamw_tensor* r, PyObject* param, PyObject* grad, PyObject* states
     if (r->param_dtype < 0 || r->grad_dtype < 0) return false;
     r->count = p->numel();
     r->param = p->data_ptr();
+    written->push_back(p->unsafeGetTensorImpl());
     r->grad = g->const_data_ptr();
     PyObject* state = PyDict_GetItemWithError(states, param);
     if (!state || !PyDict_Check(state)) return false;
     auto get = [&](PyObject* name, bool codes, int64_t count, auto** data) {
         void* at = nullptr;
-        if (!held(state, name, codes, count, device, &at)) return false;
+        if (!held(state, name, codes, count, device, &at, written)) return false;
         *data = static_cast<std::remove_reference_t<decltype(*data)>>(at);
         return true;
     };
@@ -80,14 +85,19 @@ PyObject* adamw_records(PyObject*, PyObject* args) {
     auto* r = reinterpret_cast<asi_adamw_tensor*>(PyBytes_AS_STRING(out));
     bool made = true;
     try {
+        Written written;
+        written.reserve(n * 6);
         // a parameter's hash is Python code, which could change the lists: their lengths are looked at again
         for (Py_ssize_t i = 0; made && i < n; ++i) {
             r[i] = asi_adamw_tensor{};
             r[i].lr = lr;
             r[i].weight_decay = decay;
             made = i < PyList_GET_SIZE(params) && i < PyList_GET_SIZE(grads) &&
-                   fill(r + i, PyList_GET_ITEM(params, i), PyList_GET_ITEM(grads, i), states, eight != 0, master != 0, device);
+                   fill(r + i, PyList_GET_ITEM(params, i), PyList_GET_ITEM(grads, i), states, eight != 0, master != 0, device, &written);
         }
+        if (made && !PyErr_Occurred())
+            for (c10::TensorImpl* t : written)
+                if (!t->is_inference()) t->bump_version();
     } catch (const std::exception& e) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
     }

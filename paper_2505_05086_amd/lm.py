@@ -84,6 +84,13 @@ def _scratch(nbytes: int, like: torch.Tensor) -> Optional[torch.Tensor]:
     return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
 
 
+def _written(t: torch.Tensor) -> torch.Tensor:
+    """A caller's tensor that a kernel has written: a backward pass that saved it before has to know."""
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+    return t
+
+
 # ---- token log probabilities ------------------------------------------------------------------------------
 class TokenLogprobs(NamedTuple):
     logprob: Optional[torch.Tensor]        # fp32, of each row's target; None without targets
@@ -208,7 +215,8 @@ def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor], g
     targets = _targets(targets, shape)
     grad_logprob, grad_entropy = _weights(grad_logprob, shape, "grad_logprob"), _weights(grad_entropy, shape, "grad_entropy")
     device = _place(logits, targets, grad_logprob, grad_entropy, out)
-    if out is None:
+    given = out is not None
+    if not given:
         out = logits.new_empty(logits.shape) if new is None else logits.new_empty_strided(*new)
     logprob = None if targets is None else logits.new_empty(shape, dtype=torch.float32)
     entropy = logits.new_empty(shape, dtype=torch.float32)
@@ -216,7 +224,7 @@ def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor], g
                                              out.data_ptr(), _ptr(logprob), entropy.data_ptr(), _stream(device))
     if status:
         B._check(status, "asi_token_logprobs_grad")
-    return TokenLogprobsGrad(logprob, entropy, out)
+    return TokenLogprobsGrad(logprob, entropy, _written(out) if given else out)
 
 
 # ---- embedding --------------------------------------------------------------------------------------------
@@ -288,14 +296,15 @@ def embedding_grad(tokens: torch.Tensor, grad_out: torch.Tensor, vocab: int, *, 
     if not dense:
         grad_out = grad_out.contiguous()
     device = _place(tokens, grad_out, out)
-    if out is None:
+    given = out is not None
+    if not given:
         out = grad_out.new_empty(shape, dtype=dtype)
     ws = _scratch(nbytes, grad_out)
     status = B.lib().asi_embedding_grad(desc, tokens.data_ptr(), grad_out.data_ptr(), out.data_ptr(), int(accumulate), _ptr(ws), nbytes,
                                         _stream(device))
     if status:
         B._check(status, "asi_embedding_grad")
-    return out
+    return _written(out) if given else out
 
 
 @_plans

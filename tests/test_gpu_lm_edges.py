@@ -217,3 +217,64 @@ def test_nan_beside_infinity_before_other_nan(vocab, apart, dtype):
     for top in (1, 5, 30):
         r = asi.token_logprobs(x, top=top)
         assert torch.equal(r.top_index, _in_order(x, top))
+
+
+# ---- tensors that are written over -----------------------------------------------------------------------
+def test_gradients_in_the_place_of_saved_logits_raise():
+    targets, weights = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.ones(4, device="cuda")
+    x = _randn(1, 4, 50).requires_grad_(True)
+    y = torch.tanh(x)                                            # saves its result
+    with torch.no_grad():
+        r = asi.token_logprobs_grad(y, targets, weights, out=y)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        y.backward(r.grad)
+    y = x * 1.0                                                  # does not
+    want = asi.token_logprobs_grad(y.detach(), targets, weights).grad
+    with torch.no_grad():
+        r = asi.token_logprobs_grad(y, targets, weights, out=y)
+    y.backward(r.grad)
+    assert torch.equal(x.grad, want)
+    y = x * 1.0
+    loss = asi.token_logprobs(y, targets).logprob.sum()          # saves its logits
+    with torch.no_grad():
+        asi.token_logprobs_grad(y, targets, weights, out=y)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        loss.backward()
+
+
+def test_a_saved_table_that_is_added_to_raises():
+    held = _randn(1, 10, 8)
+    w = torch.ones(10, 8, device="cuda", requires_grad=True)
+    tokens = torch.arange(4, device="cuda")
+    for accumulate in (False, True):
+        loss = (w * held).sum()
+        asi.embedding_grad(tokens, torch.ones(4, 8, device="cuda"), 10, out=held, accumulate=accumulate)
+        with pytest.raises(RuntimeError, match="modified by an inplace"):
+            loss.backward()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_between_forward_and_backward_raises(bits):
+    p = torch.nn.Parameter(_randn(1, 300).to(torch.bfloat16))
+    opt = asi.AdamW([p], state_bits=bits, master=True)
+    p.grad = torch.ones_like(p)
+    opt.step()
+    w = torch.ones(300, device="cuda", requires_grad=True)
+    losses = (p * p).sum(), (w * opt.state[p]["master"]).sum()
+    opt.step()
+    for loss in losses:
+        with pytest.raises(RuntimeError, match="modified by an inplace"):
+            loss.backward()
+    assert all(t._version > 0 for t in opt.state[p].values())
+
+
+def test_in_inference_mode():
+    with torch.inference_mode():
+        x, targets = _randn(1, 4, 50), torch.zeros(4, dtype=torch.int64, device="cuda")
+        want = asi.token_logprobs_grad(x, targets, torch.ones(4, device="cuda")).grad
+        assert torch.equal(asi.token_logprobs_grad(x, targets, torch.ones(4, device="cuda"), out=x).grad, want)
+        held = torch.zeros(10, 50, device="cuda")
+        asi.embedding_grad(targets, want, 10, out=held)
+    asi.embedding_grad(targets, want, 10, out=held, accumulate=True)       # such tensors have no version
+    # two sums of four rows and their sum: 8 roundings of magnitudes below 4
+    assert float((held[0].double() - 2 * want.double().sum(0)).abs().max()) <= 8 * 4 * U and not held[1:].any()
