@@ -13,6 +13,7 @@ import operator
 from typing import List, NamedTuple, Optional, Sequence, Tuple
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import binding as B
@@ -35,7 +36,9 @@ def _dtype(dtype: torch.dtype, what: str) -> int:
 
 
 def _place(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
-    """The current GPU's index; every tensor has to be there."""
+    """The current GPU's index; every tensor has to be there, without a tangent of forward-mode differentiation."""
+    if forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in (first, *others)):
+        raise NotImplementedError("forward-mode derivatives are not implemented")
     device = first.get_device()
     for t in others:
         if t is not None and t.get_device() != device:

@@ -278,3 +278,21 @@ def test_in_inference_mode():
     asi.embedding_grad(targets, want, 10, out=held, accumulate=True)       # such tensors have no version
     # two sums of four rows and their sum: 8 roundings of magnitudes below 4
     assert float((held[0].double() - 2 * want.double().sum(0)).abs().max()) <= 8 * 4 * U and not held[1:].any()
+
+
+# ---- forward-mode differentiation --------------------------------------------------------------------------
+def test_tangents_are_refused():
+    from torch.autograd import forward_ad
+    x, targets, a = _randn(1, 4, 6), torch.zeros(4, dtype=torch.int64, device="cuda"), torch.ones(4, device="cuda")
+    q, gain, (cos, sin) = _randn(2, 1, 4, 2, 16), torch.ones(16, device="cuda"), asi.rotary_table(8, 16)
+    calls = [(x, lambda t: asi.token_logprobs(t, targets)), (x, lambda t: asi.token_logprobs_grad(t, targets, a)), (a, lambda t: asi.token_logprobs_grad(x, targets, t)),
+             (x, lambda t: asi.embedding(targets, t)), (x, lambda t: asi.embedding_grad(targets, t, 5)),
+             (q, lambda t: asi.qk_norm_rotate(q, t, gain, gain, cos, sin)), (gain, lambda t: asi.qk_norm_rotate(q, q, t, gain, cos, sin)),
+             (cos, lambda t: asi.qk_norm_rotate(q, q, gain, gain, t, sin)), (q, lambda t: asi.qk_norm_rotate_grad(q, q, gain, gain, cos, sin, t, q))]
+    with forward_ad.dual_level():
+        for value, call in calls:
+            for needs in (False, True):
+                dual = forward_ad.make_dual(value.clone().requires_grad_(needs), torch.ones_like(value))
+                with pytest.raises(NotImplementedError):
+                    call(dual)
+            call(value)
