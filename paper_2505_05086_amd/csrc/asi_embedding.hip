@@ -685,16 +685,21 @@ asi_status asi_embedding(const asi_embedding_desc* desc, const int64_t* tokens, 
     LookupArgs a{tokens, table, out, desc->tokens, desc->vocab, desc->table_stride, desc->out_stride, (int)desc->dim, 0, desc->scale};
     const int per_wave = vec ? 256 * n : 1024;
     a.parts = (int)((desc->dim + per_wave - 1) / per_wave);
-    const long long waves = a.n * a.parts;
-    if (waves > 0x7fffffffLL) return ASI_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((waves + 3) / 4));
+    // a launch's worth of tokens at a time
+    const long long most = most_workgroups(kThreads) * (kThreads / 64) / a.parts;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (desc->table_dtype == ASI_F32) {
-        if (desc->out_dtype == ASI_F32) lookup<float, float>(a, vec, grid, st);
-        else lookup<float, bf16_t>(a, vec, grid, st);
-    } else {
-        if (desc->out_dtype == ASI_F32) lookup<bf16_t, float>(a, vec, grid, st);
-        else lookup<bf16_t, bf16_t>(a, vec, grid, st);
+    for (long long t = 0; t < desc->tokens; t += most) {
+        a.n = std::min<long long>(most, desc->tokens - t);
+        a.tokens = tokens + t;
+        a.out = static_cast<char*>(out) + t * desc->out_stride * (long long)os;
+        const dim3 grid((unsigned)((a.n * a.parts + 3) / 4));
+        if (desc->table_dtype == ASI_F32) {
+            if (desc->out_dtype == ASI_F32) lookup<float, float>(a, vec, grid, st);
+            else lookup<float, bf16_t>(a, vec, grid, st);
+        } else {
+            if (desc->out_dtype == ASI_F32) lookup<bf16_t, float>(a, vec, grid, st);
+            else lookup<bf16_t, bf16_t>(a, vec, grid, st);
+        }
     }
     return launched();
 }

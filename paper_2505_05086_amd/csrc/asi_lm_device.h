@@ -206,6 +206,8 @@ inline bool dtype_ok(int32_t d) { return d == ASI_F32 || d == ASI_BF16; }
 inline size_t dtype_size(int32_t d) { return d == ASI_F32 ? 4 : 2; }
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
+// A launch has fewer than 2^32 threads in a dimension: workgroups that are sure to fit.
+constexpr long long most_workgroups(int threads) { return 0xffffffffLL / threads; }
 inline asi_status launched() { return hipGetLastError() == hipSuccess ? ASI_OK : ASI_ERR_HIP; }
 
 }  // namespace asi

@@ -296,3 +296,13 @@ def test_tangents_are_refused():
                 with pytest.raises(NotImplementedError):
                     call(dual)
             call(value)
+
+
+# ---- more threads than a launch has ----------------------------------------------------------------------------
+def test_lookup_of_more_tokens_than_a_launch_takes():
+    n = (1 << 26) + 1001                                         # a wave a token
+    table = _randn(1, 37, 4)
+    tokens = torch.randint(0, 37, (n,), device="cuda", generator=_gen(2))
+    for t in (table, table.to(torch.bfloat16)[:, :3]):           # in vectors, element by element
+        out = asi.embedding(tokens, t)
+        assert all(torch.equal(a, t[b]) for a, b in zip(out.split(1 << 24), tokens.split(1 << 24)))
