@@ -544,6 +544,12 @@ int parts_of(const asi_logprob_desc* d) {
     const long long joined = d->top ? std::max(2, 160 / d->top) : kMaxParts;
     return (int)std::max(1LL, std::min<long long>({kMaxParts, joined, nvec / 1024, 512 / std::max<int64_t>(1, d->rows)}));
 }
+// f(first row, rows) for as many rows at a time as a launch of 1024 threads each takes
+template <typename F> void in_launches(long long rows, F f) {
+    constexpr long long most = most_workgroups(1024);
+    for (long long first = 0; first < rows; first += most) f(first, (unsigned)std::min(most, rows - first));
+}
+template <typename P> P* behind(P* p, long long n) { return p ? p + n : nullptr; }
 size_t sums_bytes(const asi_logprob_desc* d, int parts) { return round256((size_t)d->rows * parts * sizeof(Sums)); }
 
 template <typename T, int THREADS, int U, bool SPLIT> void forward(const Args& a, unsigned blocks, hipStream_t st) {
@@ -617,8 +623,14 @@ asi_status asi_token_logprobs(const asi_logprob_desc* desc, const void* logits, 
         a.keys = reinterpret_cast<unsigned long long*>(static_cast<char*>(ws) + sums_bytes(desc, a.parts));
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (desc->dtype == ASI_F32) forward<float>(a, (unsigned)desc->rows, st);
-    else forward<bf16_t>(a, (unsigned)desc->rows, st);
+    in_launches(desc->rows, [&](long long first, unsigned rows) {
+        Args b = a;
+        b.x = static_cast<const char*>(logits) + first * desc->row_stride * (long long)es;
+        b.targets = behind(targets, first); b.logprob = behind(logprob, first); b.entropy = behind(entropy, first); b.lse = behind(lse, first);
+        b.top_logprob = behind(top_logprob, first * desc->top); b.top_index = behind(top_index, first * desc->top);
+        if (desc->dtype == ASI_F32) forward<float>(b, rows, st);
+        else forward<bf16_t>(b, rows, st);
+    });
     return launched();
 }
 
@@ -635,8 +647,15 @@ asi_status asi_token_logprobs_grad(const asi_logprob_desc* desc, const void* log
     const GradArgs g{logits, dlogits, targets, grad_logprob, grad_entropy, logprob, entropy, desc->row_stride, desc->grad_stride,
                      desc->ignore_index, (int)desc->vocab, desc->scale, scale_of(desc)};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (desc->dtype == ASI_F32) backward<float>(g, (unsigned)desc->rows, st);
-    else backward<bf16_t>(g, (unsigned)desc->rows, st);
+    in_launches(desc->rows, [&](long long first, unsigned rows) {
+        GradArgs h = g;
+        h.x = static_cast<const char*>(logits) + first * desc->row_stride * (long long)es;
+        h.dx = static_cast<char*>(dlogits) + first * desc->grad_stride * (long long)es;
+        h.targets = behind(targets, first); h.a = behind(grad_logprob, first); h.b = behind(grad_entropy, first);
+        h.logprob = behind(logprob, first); h.entropy = behind(entropy, first);
+        if (desc->dtype == ASI_F32) backward<float>(h, rows, st);
+        else backward<bf16_t>(h, rows, st);
+    });
     return launched();
 }
 

@@ -306,3 +306,26 @@ def test_lookup_of_more_tokens_than_a_launch_takes():
     for t in (table, table.to(torch.bfloat16)[:, :3]):           # in vectors, element by element
         out = asi.embedding(tokens, t)
         assert all(torch.equal(a, t[b]) for a, b in zip(out.split(1 << 24), tokens.split(1 << 24)))
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_log_probabilities_of_more_rows_than_a_launch_takes(dtype):
+    rows, vocab, some = (1 << 26) + 77, 3, 1 << 23
+    x = torch.empty(rows, vocab, dtype=DTYPES[dtype], device="cuda")
+    targets = torch.empty(rows, dtype=torch.int64, device="cuda")
+    a = torch.empty(rows, device="cuda")
+    for k, at in enumerate(range(0, rows, some)):                # torch's own launches have the same limit
+        x[at:at + some] = _randn(k, *x[at:at + some].shape)
+        targets[at:at + some] = torch.randint(0, vocab, targets[at:at + some].shape, generator=_gen(100 + k), device="cuda")
+        a[at:at + some] = _randn(200 + k, *a[at:at + some].shape)
+    r, d = asi.token_logprobs(x, targets, top=2), asi.token_logprobs_grad(x, targets, a)
+    for at in (0, (1 << 22) - 5, (1 << 26) - 1000, rows - 1100):
+        part = slice(at, at + 1100)
+        s, e = asi.token_logprobs(x[part], targets[part], top=2), asi.token_logprobs_grad(x[part], targets[part], a[part])
+        assert all(torch.equal(f[part], g) for f, g in zip((*r, *d), (*s, *e)))
+    order = [b.sort(dim=-1, descending=True, stable=True).indices[:, :2] for b in x.float().split(some)]
+    assert all(torch.equal(i, o) for i, o in zip(r.top_index.split(some), order))
+    for b, p, t in zip(x.split(some), r.logprob.split(some), targets.split(some)):
+        want = torch.log_softmax(b.double(), -1).gather(1, t[:, None])[:, 0]
+        # as for any row of three: a few roundings of differences below 16 and of the logarithm
+        assert float((p.double() - want).abs().max()) <= 512 * U
