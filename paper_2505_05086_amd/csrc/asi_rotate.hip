@@ -57,6 +57,7 @@ struct Args {
     const float* sin;
     float* part;                   // backward: [side][workgroup][head_dim]
     long long rows;                // batch * tokens
+    long long first;               // forward: what the launch begins with
     long long position_stride, max_position;
     Divider by_tokens, by_parts;   // parts: what the heads of a token are taken in, forward
     int q_parts, parts;
@@ -151,7 +152,7 @@ template <typename T, typename G> __device__ __forceinline__ void load_gain(cons
 template <typename T, typename G, int GROUP, int HEADS, bool INTER> __global__ __launch_bounds__(kThreads) void k_rotate(const Args a) {
     constexpr int N = Vec16<T>::N;
     const int lane = threadIdx.x & (GROUP - 1);
-    const long long id = (long long)blockIdx.x * (kThreads / GROUP) + threadIdx.x / GROUP;
+    const long long id = a.first + (long long)blockIdx.x * (kThreads / GROUP) + threadIdx.x / GROUP;
     const bool have = id < a.rows * a.parts;
     const int row = have ? a.by_parts.quotient((int)id) : 0;
     int part = have ? (int)id - row * a.parts : 0;
@@ -295,7 +296,7 @@ __device__ __forceinline__ void partners(const Args& a, int e, int* i, int* j) {
 }
 template <typename T, typename G> __global__ __launch_bounds__(kThreads) void k_rotate_any(const Args a) {
     const int lane = threadIdx.x & 63;
-    const long long id = (long long)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    const long long id = a.first + (long long)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
     const int heads = a.side[0].heads + a.side[1].heads;
     if (id >= a.rows * heads) return;
     const unsigned row = (unsigned)id / (unsigned)heads;
@@ -503,12 +504,17 @@ int grad_blocks(const asi_qk_desc* d, int group) {
     return (int)std::max(1LL, std::min<long long>(most_blocks(d), (heads + groups - 1) / groups));
 }
 
+// Forward: f(grid) for as many of n at a time, `each` a workgroup, as a launch takes
+template <typename F> void in_launches(long long n, int each, Args* a, F f) {
+    const long long most = most_workgroups(kThreads) * each;
+    for (a->first = 0; a->first < n; a->first += most) f(dim3((unsigned)((std::min(most, n - a->first) + each - 1) / each)));
+}
 template <typename T, typename G, int GROUP, int HEADS> void forward(Args a, hipStream_t st) {
     set_parts(&a, HEADS);
-    const long long n = a.rows * a.parts;
-    const dim3 grid((unsigned)((n + kThreads / GROUP - 1) / (kThreads / GROUP)));
-    if (a.interleaved) hipLaunchKernelGGL((k_rotate<T, G, GROUP, HEADS, true>), grid, kThreads, 0, st, a);
-    else hipLaunchKernelGGL((k_rotate<T, G, GROUP, HEADS, false>), grid, kThreads, 0, st, a);
+    in_launches(a.rows * a.parts, kThreads / GROUP, &a, [&](dim3 grid) {
+        if (a.interleaved) hipLaunchKernelGGL((k_rotate<T, G, GROUP, HEADS, true>), grid, kThreads, 0, st, a);
+        else hipLaunchKernelGGL((k_rotate<T, G, GROUP, HEADS, false>), grid, kThreads, 0, st, a);
+    });
 }
 template <typename T, typename G, int GROUP, bool INTER> void backward(const Args& a, int blocks, hipStream_t st) {
     constexpr bool lines = GROUP * 16 >= 128;         // a vector of each lane of a group fills a line
@@ -536,8 +542,9 @@ template <typename T, typename G> void go(int group, const Args& a, bool back, i
             if (back) {
                 hipLaunchKernelGGL((k_rotate_grad_any<T, G>), dim3(blocks), 64, 0, st, a);
             } else {
-                const long long n = a.rows * (a.side[0].heads + a.side[1].heads);
-                hipLaunchKernelGGL((k_rotate_any<T, G>), dim3((unsigned)((n + 3) / 4)), kThreads, 0, st, a);
+                Args b = a;
+                in_launches(a.rows * (a.side[0].heads + a.side[1].heads), kThreads / 64, &b,
+                            [&](dim3 grid) { hipLaunchKernelGGL((k_rotate_any<T, G>), grid, kThreads, 0, st, b); });
             }
     }
 }

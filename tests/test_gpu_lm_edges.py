@@ -329,3 +329,21 @@ def test_log_probabilities_of_more_rows_than_a_launch_takes(dtype):
         want = torch.log_softmax(b.double(), -1).gather(1, t[:, None])[:, 0]
         # as for any row of three: a few roundings of differences below 16 and of the logarithm
         assert float((p.double() - want).abs().max()) <= 512 * U
+
+
+def test_heads_of_more_tokens_than_a_launch_takes():
+    tokens, cut = (1 << 25) + 501, (1 << 25) - 777               # 2^26 heads, a wave each
+    q = torch.empty(1, tokens, 1, 6, dtype=torch.bfloat16, device="cuda")
+    for k, part in enumerate(q.split(1 << 22, 1)):               # torch's own launches have the same limit
+        part.normal_(generator=_gen(k))
+    k = q.flip(3)
+    cos, sin = asi.rotary_table(1000, 6)
+    positions = torch.arange(tokens, device="cuda") % 1000
+    got = asi.qk_norm_rotate(q, k, None, None, cos, sin, positions)
+    for part in (slice(0, 2000), slice(cut, tokens)):
+        want = asi.qk_norm_rotate(q[:, part], k[:, part], None, None, cos, sin, positions[part])
+        assert all(torch.equal(a[:, part], b) for a, b in zip(got, want))
+    # a turn leaves the norm as it is: sqrt(6), each entry rounded to bf16
+    for a in got:
+        norms = torch.cat([torch.linalg.vector_norm(part.float(), dim=-1).flatten() for part in a.split(1 << 22, 1)])
+        assert float(norms.max()) <= 6 ** 0.5 * (1 + 2.0 ** -7) and float(norms.median()) >= 6 ** 0.5 * (1 - 2.0 ** -7)
