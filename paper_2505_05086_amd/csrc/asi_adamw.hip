@@ -246,6 +246,7 @@ extern "C" asi_status asi_adamw(int32_t count, const asi_adamw_tensor* tensors, 
     a.grad_scale = grad_scale;
     a.skip = skip;
     const int chunk = eight ? Shape<true>::chunk : Shape<false>::chunk;
+    constexpr long long most = most_workgroups(kThreads);
     bool any = false;
     const double correction = 1.0 - std::pow(beta1, (double)step);
     for (int kind = 0; kind < 8; ++kind) {
@@ -261,20 +262,31 @@ extern "C" asi_status asi_adamw(int32_t count, const asi_adamw_tensor* tensors, 
         for (int32_t i = 0; i < count; ++i) {
             const asi_adamw_tensor& s = tensors[i];
             if (s.count == 0 || kind_of(s) != kind) continue;
-            const long long need = (s.count + chunk - 1) / chunk;
-            if (n == kTensors || blocks + need > 0x7fffffffLL) flush();
-            Tensor& t = a.t[n];
-            t.param = s.param; t.grad = s.grad; t.master = s.master; t.avg = s.exp_avg; t.sq = s.exp_avg_sq;
-            t.avg_scale = s.exp_avg_scale; t.sq_scale = s.exp_avg_sq_scale; t.count = s.count;
-            t.decay = (float)(1.0 - s.lr * s.weight_decay);
-            t.rate = (float)(s.lr / correction);
+            const size_t ps = dtype_size(s.param_dtype), gs = dtype_size(s.grad_dtype), ss = eight ? 1 : 4;
             // accesses of up to 16 bytes
             const size_t state = eight ? 8 : 16, e = eight ? 8 : 4;
-            t.vec = aligned(s.param, std::min<size_t>(16, e * dtype_size(s.param_dtype))) &&
-                    aligned(s.grad, std::min<size_t>(16, e * dtype_size(s.grad_dtype))) && aligned(s.master, 16) && aligned(s.exp_avg, state) && aligned(s.exp_avg_sq, state);
-            a.first[n] = (int)blocks;
-            blocks += need;
-            ++n;
+            const bool vec = aligned(s.param, std::min<size_t>(16, e * ps)) && aligned(s.grad, std::min<size_t>(16, e * gs)) && aligned(s.master, 16) &&
+                             aligned(s.exp_avg, state) && aligned(s.exp_avg_sq, state);
+            // a tensor that is more than a launch takes is several
+            for (long long at = 0; at < s.count; at += most * chunk) {
+                const long long n_here = std::min<long long>(s.count - at, most * chunk), need = (n_here + chunk - 1) / chunk;
+                if (n == kTensors || blocks + need > most) flush();
+                Tensor& t = a.t[n];
+                t.param = static_cast<char*>(s.param) + at * ps;
+                t.grad = static_cast<const char*>(s.grad) + at * gs;
+                t.master = s.master ? s.master + at : nullptr;
+                t.avg = static_cast<char*>(s.exp_avg) + at * ss;
+                t.sq = static_cast<char*>(s.exp_avg_sq) + at * ss;
+                t.avg_scale = eight ? s.exp_avg_scale + at / kBlock : nullptr;
+                t.sq_scale = eight ? s.exp_avg_sq_scale + at / kBlock : nullptr;
+                t.count = n_here;
+                t.decay = (float)(1.0 - s.lr * s.weight_decay);
+                t.rate = (float)(s.lr / correction);
+                t.vec = vec;
+                a.first[n] = (int)blocks;
+                blocks += need;
+                ++n;
+            }
         }
         flush();
     }

@@ -1,5 +1,6 @@
 """The language-model operators (include/asi_lm.h) where they meet what is exchanged, removed, overwritten or extreme."""
 import copy
+import gc
 
 import pytest
 import torch
@@ -347,3 +348,40 @@ def test_heads_of_more_tokens_than_a_launch_takes():
     for a in got:
         norms = torch.cat([torch.linalg.vector_norm(part.float(), dim=-1).flatten() for part in a.split(1 << 22, 1)])
         assert float(norms.max()) <= 6 ** 0.5 * (1 + 2.0 ** -7) and float(norms.median()) >= 6 ** 0.5 * (1 - 2.0 ** -7)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_parameters_of_more_entries_than_a_launch_takes(bits):
+    n, m = (1 << (34 if bits == 32 else 35)) + 1000, 1256        # 2^24 workgroups of 1024 or 2048 entries
+    need = n * (2 + 2 + (8 if bits == 32 else 2 + 8 / 256)) * 1.02
+    gc.collect()
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < need:
+        pytest.skip("needs a GPU's memory of its own")
+    try:
+        p = torch.nn.Parameter(torch.empty(n, dtype=torch.bfloat16, device="cuda"))
+        p.grad = torch.empty(n, dtype=torch.bfloat16, device="cuda")
+        some, q = 1 << 30, torch.nn.Parameter(_randn(1, m).to(torch.bfloat16))
+        q.grad = _randn(2, m).to(torch.bfloat16)
+        with torch.no_grad():
+            for t, tail in ((p, q), (p.grad, q.grad)):           # torch's own launches have the same limit
+                for part in t.split(some):
+                    part.zero_()
+                t[-m:] = tail
+        opt = asi.AdamW([p], state_bits=bits)
+        state = opt.state[p]
+        codes = torch.float32 if bits == 32 else torch.uint8
+        for name in ("exp_avg", "exp_avg_sq" if bits == 32 else "exp_avg_sqrt"):
+            state[name] = torch.empty(n, dtype=codes, device="cuda")
+            for part in state[name].split(some):
+                part.zero_()
+        if bits == 8:
+            state["exp_avg_scale"], state["exp_avg_sqrt_scale"] = (torch.zeros(-(-n // 256), device="cuda") for _ in range(2))
+        opt.step()
+        asi.AdamW([q], state_bits=bits).step()
+        assert torch.equal(p[-m:], q)                            # blocks of 256 begin at the same place
+        assert not any(bool(part.any()) for part in p.detach()[:-m].split(some))
+    finally:
+        p = q = opt = state = None
+        gc.collect()
+        torch.cuda.empty_cache()
