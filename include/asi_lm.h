@@ -85,7 +85,8 @@ size_t asi_embedding_grad_workspace_bytes(const asi_embedding_desc* desc);
 
 /*   dtable  out device (vocab, dim): overwritten, rows without a token with zeros; with accumulate != 0 the
  *               rows that have tokens are added to and no other is touched
- * Tokens outside [0, vocab) and padding_index count for nothing. */
+ * Tokens outside [0, vocab) and padding_index count for nothing.  ASI_ERR_UNSUPPORTED where one launch has not enough
+ * workgroups: above some 2^38 entries of grad_out, or 2^32 in up to 1024 rows. */
 asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tokens, const void* grad_out, void* dtable,
                               int accumulate, void* ws, size_t ws_bytes, asi_stream_t stream);
 

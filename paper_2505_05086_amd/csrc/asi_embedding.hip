@@ -638,18 +638,25 @@ template <typename T, typename O> void lookup(const LookupArgs& a, bool vec, dim
 // Columns of a piece and pieces of a lane: 16 bytes of the wider type, twice where the rows that are read are the narrower ones
 template <typename O, typename D> struct Shape {
     static constexpr int C = sizeof(D) == 2 && sizeof(O) == 2 ? 8 : 4, P = sizeof(O) < sizeof(D) ? 2 : 1;
+    static_assert(C * P == (sizeof(O) == 2 ? 8 : 4), "columns of a lane");
 };
 constexpr int kLoose = 4;             // pieces of a lane where they are single columns
-template <typename O, typename D, int C, int P> void sum(SumArgs a, const SortArgs& s, int fill_blocks, hipStream_t st) {
-    const bool few = a.n <= kFew;
-    a.lanes = few ? 64 : kLeastLanes;
-    while (!few && a.lanes < kThreads && a.lanes * C * P < a.dim) a.lanes *= 2;
-    a.columns = a.lanes * C * P;
-    a.column_tiles = (a.dim + a.columns - 1) / a.columns;
-    const int groups = kThreads / a.lanes;
-    a.run_blocks = (few ? a.n : (a.runs + groups - 1) / groups) * a.column_tiles;
+// How the lanes of a workgroup share runs and columns, each lane `each` columns; false if that takes more workgroups than a launch has.
+bool share_out(SumArgs* a, int each, int fill_blocks) {
+    const bool few = a->n <= kFew;
+    a->lanes = few ? 64 : kLeastLanes;
+    while (!few && a->lanes < kThreads && a->lanes * each < a->dim) a->lanes *= 2;
+    a->columns = a->lanes * each;
+    a->column_tiles = (a->dim + a->columns - 1) / a->columns;
+    const int groups = kThreads / a->lanes;
+    const long long blocks = (long long)(few ? a->n : (a->runs + groups - 1) / groups) * a->column_tiles;
+    if (blocks + fill_blocks > most_workgroups(kThreads)) return false;
+    a->run_blocks = (int)blocks;
+    return true;
+}
+template <typename O, typename D, int C, int P> void sum(const SumArgs& a, const SortArgs& s, int fill_blocks, hipStream_t st) {
     const dim3 grid((unsigned)(a.run_blocks + fill_blocks));
-    if (few) {
+    if (a.n <= kFew) {
         if (a.accumulate) hipLaunchKernelGGL((k_few<O, D, C, P, true>), grid, kThreads, 0, st, a, s);
         else hipLaunchKernelGGL((k_few<O, D, C, P, false>), grid, kThreads, 0, st, a, s);
     } else {
@@ -657,9 +664,11 @@ template <typename O, typename D, int C, int P> void sum(SumArgs a, const SortAr
         else hipLaunchKernelGGL((k_sum<O, D, C, P, false>), grid, kThreads, 0, st, a);
     }
 }
+int join_tiles(const SumArgs& a, bool vec) { return (a.dim + (vec ? 256 : 64) - 1) / (vec ? 256 : 64); }
+long long join_blocks(const SumArgs& a, int tiles) { return (long long)((a.runs - 1 + kJoinRuns - 1) / kJoinRuns) * tiles; }
 template <typename D> void join(const SumArgs& a, bool vec, hipStream_t st) {
-    const int wide = vec ? 256 : 64, tiles = (a.dim + wide - 1) / wide;
-    const dim3 grid((unsigned)((a.runs - 1 + kJoinRuns - 1) / kJoinRuns * tiles));
+    const int tiles = join_tiles(a, vec);
+    const dim3 grid((unsigned)join_blocks(a, tiles));
     if (vec) hipLaunchKernelGGL((k_join<D, 4>), grid, kJoinThreads, 0, st, a, tiles);
     else hipLaunchKernelGGL((k_join<D, 1>), grid, kJoinThreads, 0, st, a, tiles);
 }
@@ -737,9 +746,8 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
     const int piece = ds == 2 && os == 2 ? 8 : 4;
     const bool vec = desc->dim % piece == 0 && desc->out_stride % piece == 0 && desc->table_stride % piece == 0 && aligned(grad_out, piece * os) && aligned(dtable, piece * ds);
     const int fill_blocks = accumulate ? 0 : (int)((desc->vocab + kFillRows - 1) / kFillRows);
-    const int tiles = (a.dim + 63) / 64;
-    // an upper bound of the workgroups of either launch
-    if ((long long)std::max(p.runs, kFew) * tiles + fill_blocks > 0x7fffffffLL) return ASI_ERR_UNSUPPORTED;
+    const int each = !vec ? kLoose : os == 2 ? 8 : 4;        // C * P
+    if (!share_out(&a, each, fill_blocks) || join_blocks(a, join_tiles(a, vec)) > most_workgroups(kJoinThreads)) return ASI_ERR_UNSUPPORTED;
     const bool padded = desc->padding_index >= 0 && desc->padding_index < desc->vocab;
     SortArgs s{tokens, nullptr, nullptr, padded ? (uint32_t)desc->padding_index : a.vocab, a.vocab, a.n, 0};
     if (!few) {
