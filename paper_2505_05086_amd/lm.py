@@ -24,7 +24,7 @@ IGNORE_INDEX = -100
 
 # ---- argument checks --------------------------------------------------------------------------------------
 # Small calls last as long as their marshalling: what follows from shapes, strides and types alone (the checks, the descriptor, the
-# scratch) is worked out once for each of them and kept by those, never by a tensor or its address.
+# scratch) is worked out once for each of them and kept by those, never by a tensor or its address: numbers are made plain ones first.
 _plans = functools.lru_cache(maxsize=1024)
 
 
@@ -203,6 +203,7 @@ def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None,
     """Log probabilities of `targets` under softmax(scale * logits), the entropy of each row and its `top` alternatives
     (equal logits by ascending index).  logits (..., vocab) fp32 or bf16, targets (...) int64; logprob and entropy are
     differentiable in the logits."""
+    top, scale, ignore_index = operator.index(top), float(scale), operator.index(ignore_index)
     if torch.is_grad_enabled() and logits.requires_grad:
         return TokenLogprobs(*_TokenLogprobsFn.apply(logits, targets, top, scale, ignore_index))
     return _token_logprobs(logits, targets, top, scale, ignore_index)
@@ -214,7 +215,7 @@ def token_logprobs_grad(logits: torch.Tensor, targets: Optional[torch.Tensor], g
     """Gradient of sum(grad_logprob * logprob + grad_entropy * entropy) in the logits, with both values, in one pass over
     the logits.  For a loss whose weights are known beforehand this replaces forward and backward.  `out` may be `logits`
     themselves: the gradient then takes their place."""
-    desc, _, shape, new = _logprob_plan(_geometry(logits), 0, scale, ignore_index, _geometry(out))
+    desc, _, shape, new = _logprob_plan(_geometry(logits), 0, float(scale), operator.index(ignore_index), _geometry(out))
     targets = _targets(targets, shape)
     grad_logprob, grad_entropy = _weights(grad_logprob, shape, "grad_logprob"), _weights(grad_entropy, shape, "grad_entropy")
     device = _place(logits, targets, grad_logprob, grad_entropy, out)
@@ -278,6 +279,7 @@ def embedding(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.0, 
               dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """scale * table[tokens] in `dtype` (the table's own by default), differentiable in the table.  The row of `padding_idx`
     gets no gradient; a token outside the table gives a row of NaN and no gradient."""
+    scale, padding_idx = float(scale), None if padding_idx is None else operator.index(padding_idx)
     if torch.is_grad_enabled() and table.requires_grad:
         return _EmbeddingFn.apply(tokens, table, scale, padding_idx, dtype)
     return _embedding(tokens, table, scale, dtype)
@@ -288,6 +290,7 @@ def embedding_grad(tokens: torch.Tensor, grad_out: torch.Tensor, vocab: int, *, 
                    accumulate: bool = False) -> torch.Tensor:
     """Gradient of the table of embedding(): (vocab, dim) in `dtype`, or written to `out`; with `accumulate` added to it,
     which leaves rows without a token alone.  Sums are in fp32 and in the order of the tokens: equal calls, equal bits."""
+    scale, vocab, padding_idx = float(scale), operator.index(vocab), None if padding_idx is None else operator.index(padding_idx)
     tokens = _whole(tokens, "tokens")
     if grad_out.dim() != 2:
         if grad_out.dim() < 1 or grad_out.shape[:-1] != tokens.shape:
@@ -430,6 +433,7 @@ def qk_norm_rotate(q: torch.Tensor, k: torch.Tensor, q_gain: Optional[torch.Tens
     rot_dim / 2 columns; the first rot_dim entries of a head are turned, in halves or (interleaved) in neighbouring pairs.
     positions (batch, tokens) or (tokens) int64, 0, 1, ... by default; one behind the table's end gives NaN.  heads_first:
     the results are (batch, heads, tokens, head_dim).  Differentiable in q, k and the gains."""
+    eps, interleaved, heads_first = float(eps), bool(interleaved), bool(heads_first)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or any(g is not None and g.requires_grad for g in (q_gain, k_gain))):
         return _QkNormRotateFn.apply(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, heads_first)
     return _qk_norm_rotate(q, k, q_gain, k_gain, cos, sin, positions, eps, interleaved, heads_first)
@@ -450,6 +454,7 @@ def qk_norm_rotate_grad(q, k, q_gain, k_gain, cos, sin, grad_q: torch.Tensor, gr
                         eps: float = 1e-6, interleaved: bool = False, heads_first: bool = False):
     """Gradients (dq, dk, dq_gain, dk_gain) of qk_norm_rotate from those of its results.  dq and dk are contiguous in the
     shape of q and k, the gains' gradients fp32 whether or not there are gains."""
+    eps, interleaved, heads_first = float(eps), bool(interleaved), bool(heads_first)
     if grad_q.dim() == 4 and grad_q.stride(3) != 1:
         grad_q = grad_q.contiguous()
     if grad_k.dim() == 4 and grad_k.stride(3) != 1:

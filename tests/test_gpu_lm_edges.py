@@ -385,3 +385,30 @@ def test_parameters_of_more_entries_than_a_launch_takes(bits):
         p = q = opt = state = None
         gc.collect()
         torch.cuda.empty_cache()
+
+
+# ---- numbers that are tensors ------------------------------------------------------------------------------------
+def test_numbers_that_are_tensors_are_read_at_every_call():
+    x, targets, a = _randn(1, 4, 60), torch.tensor([3, 5, 7, 9], device="cuda"), _randn(2, 4)
+    table, q, gain, (cos, sin) = _randn(3, 20, 8), _randn(4, 1, 4, 2, 16), torch.ones(16, device="cuda"), asi.rotary_table(8, 16)
+    calls = [lambda s: asi.token_logprobs(x, targets, top=3, scale=s)[:3], lambda s: asi.token_logprobs_grad(x, targets, a, a, scale=s),
+             lambda s: [asi.embedding(targets, table, scale=s)], lambda s: [asi.embedding_grad(targets, table[:4], 20, scale=s)],
+             lambda s: asi.qk_norm_rotate(q, q, gain, gain, cos, sin, eps=s), lambda s: asi.qk_norm_rotate_grad(q, q, gain, gain, cos, sin, q, q, eps=s)]
+    for call in calls:
+        number, results = torch.tensor(1.0), []
+        for value in (0.5, 2.0, 0.25):
+            number.fill_(value)
+            results.append(call(number))
+            assert all(torch.equal(f, g) for f, g in zip(results[-1], call(value)))
+        assert not torch.equal(results[0][-1], results[1][-1])
+    # what backward takes is what forward took
+    number, y = torch.tensor(0.5), x.clone().requires_grad_(True)
+    loss = (asi.token_logprobs(y, targets, scale=number).logprob * a).sum()
+    number.fill_(3.0)
+    loss.backward()
+    assert torch.equal(y.grad, asi.token_logprobs_grad(x, targets, a, scale=0.5).grad)
+    index = torch.tensor(5)
+    for value in (5, 7):
+        index.fill_(value)
+        r = asi.token_logprobs(x, targets, ignore_index=index)
+        assert (r.logprob == 0).tolist() == (targets == value).tolist()
