@@ -1024,7 +1024,7 @@ asi_status static_scratch(void** out) {
 
 extern "C" {
 
-int32_t asi_version(void) { return 1002; }
+int32_t asi_version(void) { return 1003; }
 
 int32_t asi_profile_enable(int32_t on) {
     std::lock_guard<std::mutex> lk(g_prof_mu);

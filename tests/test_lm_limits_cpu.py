@@ -13,3 +13,7 @@ UNSUPPORTED = 2
 def test_embedding_gradients_of_more_workgroups_than_a_launch_has(tokens, dim, out_dtype):
     desc = B.EmbeddingDesc(tokens, 100, dim, dim, dim, -1, B.ASI_F32, out_dtype, 1.0, 0)
     assert B.lib().asi_embedding_grad(desc, P, P, P, 0, P, 1 << 62, None) == UNSUPPORTED
+
+
+def test_the_version_tells_libraries_with_these_entry_points_apart():
+    assert B.asi_version() >= 1003
