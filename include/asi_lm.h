@@ -95,7 +95,7 @@ asi_status asi_embedding_grad(const asi_embedding_desc* desc, const int64_t* tok
  *     r = 1 / sqrt(mean_i x_i^2 + eps);   n_i = x_i r gain_i
  *     (y_i, y_j) = (n_i cos[s, e] - n_j sin[s, e], n_j cos[s, e] + n_i sin[s, e])
  * on the pairs (i, j) = (e, e + rot_dim / 2), or (2 e, 2 e + 1) if interleaved, e < rot_dim / 2; the rest of
- * the head, y_i = n_i, is not turned. */
+ * the head, y_i = n_i, is not turned.  There is no form without the norm: without gains x_i r is turned. */
 typedef struct {
     int64_t batch, tokens;
     int64_t max_position;      /* rows of cos and sin */

@@ -8,7 +8,7 @@
 // order of the runs.  So a token that makes up most of a batch costs what any other share of it costs, no sum depends on the order
 // in which workgroups run, and every row of the result is written once: the workgroups behind those of the runs fill
 // the rows without a token with zeros.  Few tokens take one launch without scratch: a workgroup for each position looks for
-// the positions of its token, and adds up their rows if its own is the first.
+// the positions of its token, and adds up their rows if its own is the first; there a token that most of them are is one chain.
 //
 // Measured: lookup of 4096 x 2048 in bf16 6.5 us; gradient of them into 32000 rows in fp32, zeros written past the caches, 56.7 us (4.9 TB/s),
 // of 32767 x 1000 added to rows in fp32 51.5 us, of which the sums are 32 (4.5 TB/s), the sort 13 and the join 6.
@@ -512,8 +512,10 @@ template <typename D, int C> __global__ __launch_bounds__(kJoinThreads) void k_j
 
 // ---- gradient of few tokens ------------------------------------------------------------------------------------
 // Workgroups of positions, each with a tile of columns, before those that write zeros.  The four waves share the positions of the token.
-// Up to kFew: every workgroup looks at all tokens, and a token that most of them are is one workgroup's chain (sorted and in one launch:
-// 172 x 772 14.7 and 4.4 us, 1000 x 256 14.6 and 7.9, 1000 x 2048 15.6 and 14.6, 2000 x 256 15.3 and 14.2; 1000 of one token 15 and 34).
+// Up to kFew: every workgroup looks at all tokens, and a token that most of them are is one workgroup's chain.  Sorted and in one launch,
+// varied tokens: 172 x 772 14.7 and 4.4 us, 1000 x 256 14.6 and 7.9, 1000 x 2048 15.6 and 14.6, 2000 x 256 15.3 and 14.2.  The rule
+// knows sizes, not tokens, and loses where one token is the whole batch: 512, 700 and 1000 x 256 of one 18, 24 and 34 us, 1000 sorted
+// 15.  Batches vary, and padding that is named counts for nothing.
 constexpr int kFew = 1024, kFewWaves = kThreads / 64;
 template <typename O, typename D, int C, int P, bool ADD> __global__ __launch_bounds__(kThreads) void k_few(const SumArgs a, const SortArgs s) {
     __shared__ uint32_t key[kFew];

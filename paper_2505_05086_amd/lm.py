@@ -428,8 +428,8 @@ class _QkNormRotateFn(torch.autograd.Function):
 def qk_norm_rotate(q: torch.Tensor, k: torch.Tensor, q_gain: Optional[torch.Tensor], k_gain: Optional[torch.Tensor],
                    cos: torch.Tensor, sin: torch.Tensor, positions: Optional[torch.Tensor] = None, *, eps: float = 1e-6,
                    interleaved: bool = False, heads_first: bool = False) -> Tuple[torch.Tensor, torch.Tensor]:
-    """Each head of q (batch, tokens, q_heads, head_dim) and k divided by its root mean square, multiplied by the gain and
-    turned by its token's position.  q and k may be views into one projection's output.  cos and sin (rotary_table) have
+    """Each head of q (batch, tokens, q_heads, head_dim) and k divided by its root mean square (there is no form without that),
+    multiplied by the gain and turned by its token's position.  q and k may be views into one projection's output.  cos and sin (rotary_table) have
     rot_dim / 2 columns; the first rot_dim entries of a head are turned, in halves or (interleaved) in neighbouring pairs.
     positions (batch, tokens) or (tokens) int64, 0, 1, ... by default; one behind the table's end gives NaN.  heads_first:
     the results are (batch, heads, tokens, head_dim).  Differentiable in q, k and the gains."""
@@ -485,7 +485,8 @@ class AdamW(torch.optim.Optimizer):
     that the step updates and rounds into them; without it their updates are rounded away where they are below a
     parameter's last bit.  Parameters are contiguous and fp32 or bf16.  The number of steps is a group's ("step"); it and the
     rates are the host's, so that a captured step repeats them.  Whoever writes other values into a bf16 parameter writes them into
-    its copy (state "master") too, or removes that.
+    its copy (state "master") too, or removes that: it is made anew.  A step takes `state` as it is then and keeps nothing else; a
+    state that does not fit its parameter, or was made with other state_bits, is refused.
     """
 
     def __init__(self, params, lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
