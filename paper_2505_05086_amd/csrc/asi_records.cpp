@@ -38,7 +38,7 @@ bool held(PyObject* state, PyObject* name, bool codes, int64_t count, long long 
     written->push_back(t->unsafeGetTensorImpl());
     return true;
 }
-bool fill(asi_adamw_tensor* r, PyObject* param, PyObject* grad, PyObject* states, bool eight, bool master, long long device, Written* written) {
+bool fill(asi_adamw_tensor* r, PyObject* param, PyObject* grad, PyObject* state, bool eight, bool master, long long device, Written* written) {
     const at::Tensor *p = plain(param, device), *g = plain(grad, device);
     if (!p || !g || !p->sizes().equals(g->sizes())) return false;
     r->param_dtype = kind(*p);
@@ -48,8 +48,6 @@ bool fill(asi_adamw_tensor* r, PyObject* param, PyObject* grad, PyObject* states
     r->param = p->data_ptr();
     written->push_back(p->unsafeGetTensorImpl());
     r->grad = g->const_data_ptr();
-    PyObject* state = PyDict_GetItemWithError(states, param);
-    if (!state || !PyDict_Check(state)) return false;
     auto get = [&](PyObject* name, bool codes, int64_t count, auto** data) {
         void* at = nullptr;
         if (!held(state, name, codes, count, device, &at, written)) return false;
@@ -84,16 +82,27 @@ PyObject* adamw_records(PyObject*, PyObject* args) {
     if (!out) return nullptr;
     auto* r = reinterpret_cast<asi_adamw_tensor*>(PyBytes_AS_STRING(out));
     bool made = true;
+    std::vector<PyObject*> state;
     try {
+        // All states are looked up first, and held: a parameter's hash is Python code, during which others may run.  Behind it none does,
+        // and what was seen of a tensor stays so.
+        state.reserve(n);
+        for (Py_ssize_t i = 0; made && i < n; ++i) {
+            PyObject* s = i < PyList_GET_SIZE(params) ? PyDict_GetItemWithError(states, PyList_GET_ITEM(params, i)) : nullptr;
+            made = s && PyDict_Check(s);
+            if (made) {
+                Py_INCREF(s);
+                state.push_back(s);
+            }
+        }
+        made = made && PyList_GET_SIZE(params) == n && PyList_GET_SIZE(grads) == n;
         Written written;
         written.reserve(n * 6);
-        // a parameter's hash is Python code, which could change the lists: their lengths are looked at again
         for (Py_ssize_t i = 0; made && i < n; ++i) {
             r[i] = asi_adamw_tensor{};
             r[i].lr = lr;
             r[i].weight_decay = decay;
-            made = i < PyList_GET_SIZE(params) && i < PyList_GET_SIZE(grads) &&
-                   fill(r + i, PyList_GET_ITEM(params, i), PyList_GET_ITEM(grads, i), states, eight != 0, master != 0, device, &written);
+            made = fill(r + i, PyList_GET_ITEM(params, i), PyList_GET_ITEM(grads, i), state[i], eight != 0, master != 0, device, &written);
         }
         if (made && !PyErr_Occurred())
             for (c10::TensorImpl* t : written)
@@ -101,6 +110,7 @@ PyObject* adamw_records(PyObject*, PyObject* args) {
     } catch (const std::exception& e) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
     }
+    for (PyObject* s : state) Py_DECREF(s);
     if (PyErr_Occurred()) {
         Py_DECREF(out);
         return nullptr;

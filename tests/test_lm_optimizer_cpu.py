@@ -254,3 +254,32 @@ def test_gradients_given_for_the_parameters(launches):
     for bad in (torch.ones(3, 300), torch.ones(300, 3, dtype=torch.float64), torch.ones(300, 3).to_sparse(), torch.ones(2, 3)):
         with pytest.raises(ValueError):
             opt.step(grads=[bad, *grads[1:]])
+
+
+def test_lists_and_states_that_a_hash_changes():
+    """A parameter's hash is Python code: what it changes is not read any more."""
+    class Sly(torch.Tensor):
+        act = None
+
+        def __hash__(self):
+            if Sly.act:
+                Sly.act()
+            return id(self)
+
+    def inputs():
+        params = [torch.Tensor._make_subclass(Sly, torch.zeros(50)) for _ in range(3)]
+        states = {p: {"exp_avg": torch.zeros(50), "exp_avg_sq": torch.zeros(50)} for p in params}
+        return params, [torch.zeros(50) for _ in params], states
+
+    params, grads, states = inputs()
+    made = B.adamw_records(params, grads, states, False, False, -1, 0.1, 0.0)
+    records = (B.AdamwTensor * 3).from_buffer_copy(made)
+    assert [r.exp_avg for r in records] == [states[p]["exp_avg"].data_ptr() for p in params]
+    kept = list(params)
+    for act in (lambda: params.clear(), lambda: grads.clear(), lambda: params.append(kept[0]), lambda: states.clear(), lambda: states.popitem() if states else None):
+        Sly.act = None
+        params, grads, states = inputs()
+        kept = list(params)
+        Sly.act = act
+        assert B.adamw_records(params, grads, states, False, False, -1, 0.1, 0.0) is None
+        Sly.act = None
