@@ -257,7 +257,8 @@ asi_status asi_rank_select(int32_t n_layers, int32_t n_eps, const double* P, con
 /* Static, human-readable name of a status code. */
 const char* asi_status_string(asi_status s);
 
-/* Library ABI version (major*1000 + minor); the entry points of asi_lm.h are there from 1003 on. */
+/* Library ABI version (major*1000 + minor); the entry points of asi_lm.h are there from 1003 on, those without logits
+ * or a stored mask and of the edge between blocks from 1004 on. */
 int32_t asi_version(void);
 
 /* Benchmark aid, off by default, not thread-safe against concurrent launches.

@@ -2,7 +2,9 @@
  * asi_lm.h - the operators of a language model's fine-tuning step that stand beside the compressed
  * layers of asi.h: token log probabilities with entropy and top alternatives and their gradient,
  * embedding lookup and its gradient, norms of queries and keys with the position rotation and their
- * gradient, and an AdamW step over many tensors with states in 32 or in 8 bits.
+ * gradient, an AdamW step over many tensors with states in 32 or in 8 bits; and what spares a step
+ * the rest of its memory: the same log probabilities and gradients without the logits, dropout without a
+ * stored mask, the edge between two blocks in one pass.
  *
  * The conventions of asi.h hold: device pointers, no allocation, no state between calls, kernels are
  * only enqueued on `stream`, argument errors are returned and enqueue nothing, scratch is the
@@ -160,6 +162,112 @@ typedef struct {
  *   skip        device int32 (1), nullable: if it is not zero when the kernels run, nothing is changed */
 asi_status asi_adamw(int32_t count, const asi_adamw_tensor* tensors, int32_t state_bits, double beta1, double beta2,
                      double eps, int64_t step, const float* grad_scale, const int32_t* skip, asi_stream_t stream);
+
+/* ---- Token log probabilities without the logits -------------------------------------------------
+ * The values of asi_token_logprobs for the logits x = H W^T, H the hidden states (rows, dim) and W the
+ * weights of the output layer (vocab, dim), and the gradients of sum_t a_t logprob_t + b_t entropy_t:
+ *     dz = scale ( a (delta_target - p) - b p (log p + entropy) )       dH = dz W        dW = dz^T H
+ * The logits are made in tiles and used up there; for the gradients they are made a second time, in pieces of
+ * the vocabulary.  Kept between the two calls are two numbers a row: the largest logit x_max (before the scale) and
+ * log sum_i exp(scale (x_i - x_max)).
+ * A row whose target is ignore_index is left out: it is not read, has logprob, entropy and gradient 0 and adds nothing
+ * to dW.  A target out of range otherwise gives NaN, as a row does that holds NaN or +infinity among its logits.
+ * Products of fp32 inputs are exact to about the rounding of fp32 (each side as three bf16 numbers, six products of
+ * them, sums in fp32).  For bf16 inputs dz is rounded to bf16 before it is multiplied, and dH and dW once at the end. */
+typedef struct {
+    int64_t rows, dim, vocab;  /* rows < 2^24, dim < 2^18, vocab < 2^28 */
+    int64_t hidden_stride;     /* of H, >= dim */
+    int64_t weight_stride;     /* of W, >= dim; dH and dW are dense */
+    int64_t ignore_index;
+    int32_t dtype;             /* of H, W, dH and dW */
+    float scale;               /* 1e-20 .. 1e20 */
+    int32_t any_address;       /* 0: weight lies at a multiple of 16 bytes; 1: it may not (bf16 weights are then copied by pieces) */
+    int32_t reserved;          /* 0 */
+} asi_linear_logprob_desc;
+
+size_t asi_linear_logprobs_workspace_bytes(const asi_linear_logprob_desc* desc);
+
+/*   targets  in  device int64 (rows), nullable if logprob is: then no row is left out
+ *   logprob, entropy  out device fp32 (rows), nullable
+ *   stats    out device fp32 (rows, 2): x_max and the logarithm, for asi_linear_logprobs_grad; nullable */
+asi_status asi_linear_logprobs(const asi_linear_logprob_desc* desc, const void* hidden, const void* weight,
+                               const int64_t* targets, float* logprob, float* entropy, float* stats, void* ws,
+                               size_t ws_bytes, asi_stream_t stream);
+
+size_t asi_linear_logprobs_grad_workspace_bytes(const asi_linear_logprob_desc* desc);
+
+/*   given    0: the values are computed first, and written where logprob and entropy are not NULL; stats is not used
+ *            1: stats and entropy are those of asi_linear_logprobs; entropy is read only if grad_entropy is given
+ *   targets       in  nullable if grad_logprob is
+ *   grad_logprob  in  device fp32 (rows): a, nullable (all zero)
+ *   grad_entropy  in  device fp32 (rows): b, nullable (all zero)
+ *   dhidden  out device (rows, dim), dweight  out device (vocab, dim), both dense, either nullable */
+asi_status asi_linear_logprobs_grad(const asi_linear_logprob_desc* desc, int given, const void* hidden, const void* weight,
+                                    const int64_t* targets, const float* stats, float* logprob, float* entropy,
+                                    const float* grad_logprob, const float* grad_entropy, void* dhidden, void* dweight,
+                                    void* ws, size_t ws_bytes, asi_stream_t stream);
+
+/* ---- Dropout without a stored mask ----------------------------------------------------------------
+ *     y_i = x_i * 2^16 / (2^16 - t) if u_i >= t, else 0;      t = round(p * 2^16)
+ * i counts the elements of (rows, dim) in order.  u_i are 16 of the 128 bits that Philox4x32-10 (Salmon et al., SC
+ * 2011) gives with the seed as its key on the counter (i / 8 mod 2^32, i / 8 div 2^32, offset mod 2^32, offset div 2^32):
+ * of word (i mod 8) / 2 the low half for even i, the high half for odd i.  The gradient is the same call on the
+ * gradient of y.  An element that is dropped is 0 whatever it held.  Different offsets are independent. */
+typedef struct {
+    int64_t rows, dim;
+    int64_t x_stride, y_stride;    /* of rows, >= dim */
+    int64_t seed;              /* read if no pointer to a seed is given */
+    int64_t offset;            /* which layer's, say */
+    double p;                  /* 0 <= p, t < 2^16 */
+    int32_t dtype;
+    int32_t reserved;          /* 0 */
+} asi_dropout_desc;
+
+/*   seed  in  device int64 (1), nullable: read when the kernel runs, so that a captured call takes new numbers
+ *   y     out device; may be x itself, with the same stride */
+asi_status asi_dropout(const asi_dropout_desc* desc, const void* x, const int64_t* seed, void* y, asi_stream_t stream);
+
+/* ---- The edge between two blocks ------------------------------------------------------------------
+ * For every row x of the stream and y of a block's output:
+ *     u = y / sqrt(mean_i y_i^2 + eps) if post_norm, else y;     n = u post_gain
+ *     s = x + scale gate dropout(n), rounded to the stream's type;     out = s / sqrt(mean_i s_i^2 + eps) pre_gain
+ * dropout as above, over (rows, dim).  Without y the stream is taken as it is, s = x: a norm alone.
+ * gate has gate_rows rows of dim entries (0: no gate); each serves rows / gate_rows consecutive rows. */
+typedef struct {
+    int64_t rows, dim;         /* dim <= ASI_RESIDUAL_MAX_DIM */
+    int64_t x_stride;          /* of x; of s in the backward pass */
+    int64_t y_stride;
+    int64_t gate_rows;         /* 0, or a divisor of rows; gate, stream, out and the gradients are dense */
+    int64_t seed, offset;      /* as asi_dropout_desc */
+    double p;
+    int32_t stream_dtype;      /* of x, s and their gradients */
+    int32_t dtype;             /* of y, out and their gradients: ASI_BF16, or both ASI_F32 */
+    int32_t gain_dtype;        /* of the gains and the gate */
+    int32_t post_norm;         /* 0 or 1 */
+    float scale, eps;          /* eps >= 0 */
+} asi_residual_desc;
+#define ASI_RESIDUAL_MAX_DIM 16384
+
+/*   y        in  nullable
+ *   post_gain, pre_gain  in  device (dim), nullable (all one); post_gain only with post_norm
+ *   gate     in  device (gate_rows, dim), NULL if and only if gate_rows is 0
+ *   stream   out device (rows, dim): s; NULL if and only if y is; may be x itself, with x_stride = dim
+ *   out      out device (rows, dim), nullable if stream is not: no norm of the stream */
+asi_status asi_residual_norm(const asi_residual_desc* desc, const void* x, const void* y, const void* post_gain,
+                             const void* gate, const void* pre_gain, const int64_t* seed, void* stream_out, void* out,
+                             asi_stream_t stream);
+
+size_t asi_residual_norm_grad_workspace_bytes(const asi_residual_desc* desc);
+
+/*   grad_stream, grad_out  in  gradients of s and out, dense, one of them nullable (zero; without grad_out: no norm)
+ *   s        in  the forward call's stream (x where there is no y), stride x_stride; nullable if grad_out is
+ *   dx, dy   out gradients of x and y, dense; dx nullable, dy NULL if and only if y is
+ *   dpost_gain, dpre_gain  out device fp32 (dim), nullable; dgate  out device fp32 (gate_rows, dim), nullable
+ * Sums over rows are in an order that the shape alone decides. */
+asi_status asi_residual_norm_grad(const asi_residual_desc* desc, const void* grad_stream, const void* grad_out, const void* s,
+                                  const void* y, const void* post_gain, const void* gate, const void* pre_gain,
+                                  const int64_t* seed, void* dx, void* dy, float* dpost_gain, float* dgate, float* dpre_gain,
+                                  void* ws, size_t ws_bytes, asi_stream_t stream);
 
 #ifdef __cplusplus
 }

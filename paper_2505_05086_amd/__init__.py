@@ -6,7 +6,8 @@ asi_compress, asi_core_project, asi_weight_grad_conv2d, asi_weight_grad_linear a
 iteration; AsiConv2d / AsiLinear wire the calls into autograd (the layers keep (S, U), not the activation);
 rank_selection holds the front end of Sec. 3.3 (mode spectra, explained-variance ranks, perplexity rows, the
 budgeted choice).  lm holds what a language model's fine-tuning step needs beside the compressed layers: token log
-probabilities and their gradient, embedding, norms of queries and keys with the position rotation, AdamW.
+probabilities and their gradient (from logits, or from hidden states without any), embedding, norms of queries and keys with
+the position rotation, dropout without a stored mask, the edge between two blocks, AdamW.
 """
 from .autograd import AsiConv2d, AsiLinear, AsiState  # noqa: F401
 from .binding import (  # noqa: F401
@@ -48,10 +49,15 @@ from .binding import (  # noqa: F401
 from . import lm, rank_selection  # noqa: F401,E402
 from .lm import (  # noqa: F401,E402
     AdamW,
+    dropout,
     embedding,
     embedding_grad,
+    linear_logprobs,
+    linear_logprobs_grad,
     qk_norm_rotate,
     qk_norm_rotate_grad,
+    residual_norm,
+    residual_norm_grad,
     rotary_table,
     token_logprobs,
     token_logprobs_grad,

@@ -31,7 +31,9 @@ EXPORTS = ["asi_workspace_bytes", "asi_compress", "asi_compress_cold", "asi_cold
            "asi_mode_spectrum", "asi_mode_spectra_workspace_bytes", "asi_mode_spectra", "asi_explained_variance_ranks", "asi_frobenius_diff", "asi_rank_select",
            "asi_token_logprobs_workspace_bytes", "asi_token_logprobs", "asi_token_logprobs_grad", "asi_embedding",
            "asi_embedding_grad_workspace_bytes", "asi_embedding_grad", "asi_qk_norm_rotate",
-           "asi_qk_norm_rotate_grad_workspace_bytes", "asi_qk_norm_rotate_grad", "asi_adamw"]
+           "asi_qk_norm_rotate_grad_workspace_bytes", "asi_qk_norm_rotate_grad", "asi_adamw",
+           "asi_linear_logprobs_workspace_bytes", "asi_linear_logprobs", "asi_linear_logprobs_grad_workspace_bytes", "asi_linear_logprobs_grad",
+           "asi_dropout", "asi_residual_norm", "asi_residual_norm_grad_workspace_bytes", "asi_residual_norm_grad"]
 FROBENIUS_WS_BYTES = 8192            # ASI_FROBENIUS_WS_BYTES of include/asi.h
 MAX_BATCH = 8
 
@@ -64,6 +66,22 @@ class QkDesc(C.Structure):
                 ("k_out_stride", C.c_int64 * 3), ("dq_stride", C.c_int64 * 3), ("dk_stride", C.c_int64 * 3), ("q_heads", C.c_int32), ("k_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("dtype", C.c_int32), ("gain_dtype", C.c_int32),
                 ("eps", C.c_float)]
+
+
+class LinearLogprobDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int64), ("vocab", C.c_int64), ("hidden_stride", C.c_int64), ("weight_stride", C.c_int64),
+                ("ignore_index", C.c_int64), ("dtype", C.c_int32), ("scale", C.c_float), ("any_address", C.c_int32), ("reserved", C.c_int32)]
+
+
+class DropoutDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int64), ("x_stride", C.c_int64), ("y_stride", C.c_int64), ("seed", C.c_int64),
+                ("offset", C.c_int64), ("p", C.c_double), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class ResidualDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int64), ("x_stride", C.c_int64), ("y_stride", C.c_int64), ("gate_rows", C.c_int64),
+                ("seed", C.c_int64), ("offset", C.c_int64), ("p", C.c_double), ("stream_dtype", C.c_int32), ("dtype", C.c_int32),
+                ("gain_dtype", C.c_int32), ("post_norm", C.c_int32), ("scale", C.c_float), ("eps", C.c_float)]
 
 
 class AdamwTensor(C.Structure):
@@ -172,6 +190,7 @@ def lib() -> C.CDLL:
                                       C.POINTER(C.c_int32), C.POINTER(C.c_double)]
         size, i64 = C.c_size_t, C.c_int64
         ld, ed, qd = C.POINTER(LogprobDesc), C.POINTER(EmbeddingDesc), C.POINTER(QkDesc)
+        hd, rd = C.POINTER(LinearLogprobDesc), C.POINTER(ResidualDesc)
         for name, result, args in (
                 ("asi_token_logprobs_workspace_bytes", size, [ld]),
                 ("asi_token_logprobs", C.c_int, [ld, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]),
@@ -182,7 +201,15 @@ def lib() -> C.CDLL:
                 ("asi_qk_norm_rotate", C.c_int, [qd] + [vp] * 10),
                 ("asi_qk_norm_rotate_grad_workspace_bytes", size, [qd]),
                 ("asi_qk_norm_rotate_grad", C.c_int, [qd] + [vp] * 14 + [size, vp]),
-                ("asi_adamw", C.c_int, [C.c_int32, vp, C.c_int32, C.c_double, C.c_double, C.c_double, i64, vp, vp, vp])):
+                ("asi_adamw", C.c_int, [C.c_int32, vp, C.c_int32, C.c_double, C.c_double, C.c_double, i64, vp, vp, vp]),
+                ("asi_linear_logprobs_workspace_bytes", size, [hd]),
+                ("asi_linear_logprobs", C.c_int, [hd, vp, vp, vp, vp, vp, vp, vp, size, vp]),
+                ("asi_linear_logprobs_grad_workspace_bytes", size, [hd]),
+                ("asi_linear_logprobs_grad", C.c_int, [hd, C.c_int, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]),
+                ("asi_dropout", C.c_int, [C.POINTER(DropoutDesc), vp, vp, vp, vp]),
+                ("asi_residual_norm", C.c_int, [rd, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
+                ("asi_residual_norm_grad_workspace_bytes", size, [rd]),
+                ("asi_residual_norm_grad", C.c_int, [rd, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp])):
             f = getattr(L, name)
             f.restype, f.argtypes = result, args
         _lib = L

@@ -11,7 +11,8 @@ OBJ_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libasi_hip.so")
 RECORDS_PATH = os.path.join(HERE, "asi_records.so")
 SOURCES = ["asi_api.hip", "asi_kernels.hip", "asi_subspace.hip", "asi_long.hip", "asi_planes.hip", "asi_steps.hip", "asi_bf16.hip", "asi_gram.hip", "asi_digits.hip", "asi_orth.hip", "asi_ttm.hip", "asi_ttm_stream.hip", "asi_corr.hip", "asi_corr_split.hip", "asi_rank.hip",
-           "asi_logprobs.hip", "asi_embedding.hip", "asi_rotate.hip", "asi_adamw.hip"]
+           "asi_logprobs.hip", "asi_embedding.hip", "asi_rotate.hip", "asi_adamw.hip",
+           "asi_head.hip", "asi_dropout.hip", "asi_residual.hip"]
 # packed-fp32 VALU forms are switched off for every HIP translation unit
 HIPCC_FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -1,0 +1,99 @@
+// Which elements dropout keeps (asi_dropout.hip, asi_residual.hip): 16 bits of Philox4x32-10 for each, eight neighbouring elements a
+// call.  16 bits and not 32 halve what the generator costs (70 integer multiplications and additions a call); the share that is
+// dropped is then a multiple of 2^-16 and the factor of the others is one over the share that is kept, so that the mean stays exact.
+#pragma once
+#include "asi_lm_device.h"
+
+namespace asi {
+
+struct Keep {
+    uint32_t key0, key1, offset0, offset1;
+    uint32_t below;            // an element is dropped if its 16 bits are below this
+    float factor;
+    const int64_t* seed;       // the key, if given
+};
+
+__device__ __forceinline__ void read_seed(Keep* k) {
+    if (!k->seed) return;
+    const uint64_t s = (uint64_t)*k->seed;
+    k->key0 = (uint32_t)s;
+    k->key1 = (uint32_t)(s >> 32);
+}
+// the bits of elements 8 group .. 8 group + 7, two to a word
+__device__ __forceinline__ void drawn(const Keep& k, unsigned long long group, uint32_t w[4]) {
+    philox4x32_10((uint32_t)group, (uint32_t)(group >> 32), k.offset0, k.offset1, k.key0, k.key1, w);
+}
+// the bits of elements first .. first + 7 for any first
+__device__ __forceinline__ void drawn_from(const Keep& k, unsigned long long first, uint32_t w[4]) {
+    const int shift = (int)(first & 7);
+    uint32_t u[8];
+    drawn(k, first >> 3, u);
+    if (shift == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = u[i];
+        return;
+    }
+    drawn(k, (first >> 3) + 1, u + 4);
+    const int whole = shift >> 1;
+    uint32_t t[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) t[i] = whole == 0 ? u[i] : whole == 1 ? u[i + 1] : whole == 2 ? u[i + 2] : u[i + 3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (shift & 1) ? (t[i] >> 16) | (t[i + 1] << 16) : t[i];
+}
+__device__ __forceinline__ bool kept(const Keep& k, const uint32_t w[4], int e) {
+    return ((e & 1) ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu) >= k.below;
+}
+
+// Eight neighbouring values, of which the first `count` exist, at an address that is a multiple of the element's size only: the
+// hardware takes whole vectors at such addresses, and at multiples of 16 in no more time than otherwise.
+typedef uint32_t loose4 __attribute__((ext_vector_type(4), aligned(2), may_alias));
+template <typename T> __device__ __forceinline__ void load8(const T* p, int count, float* f) {
+    if (count >= 8) {
+        const loose4 a = *reinterpret_cast<const loose4*>(p);
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float((i & 1) ? a[i >> 1] & 0xffff0000u : a[i >> 1] << 16);
+        } else {
+            const loose4 b = *reinterpret_cast<const loose4*>(p + 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(i < 4 ? a[i] : b[i - 4]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = i < count ? to_f32(p[i]) : 0.f;
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, int count, const float* f) {
+    if (count >= 8) {
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<loose4*>(p) = loose4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i += 4)
+                *reinterpret_cast<loose4*>(p + i) = loose4{__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3])};
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < count) p[i] = from_f32<T>(f[i]);
+}
+
+// ---- host ----
+// Fills what the device reads from p, seed and offset; false if p is none that is taken.
+inline bool fill_keep(double p, int64_t seed, int64_t offset, const int64_t* on_device, Keep* k) {
+    if (!(p >= 0.0 && p < 1.0)) return false;
+    const double below = __builtin_rint(p * 65536.0);
+    if (below >= 65536.0) return false;
+    k->key0 = (uint32_t)(uint64_t)seed;
+    k->key1 = (uint32_t)((uint64_t)seed >> 32);
+    k->offset0 = (uint32_t)(uint64_t)offset;
+    k->offset1 = (uint32_t)((uint64_t)offset >> 32);
+    k->below = (uint32_t)below;
+    k->factor = (float)(65536.0 / (65536.0 - below));
+    k->seed = on_device;
+    return true;
+}
+
+}  // namespace asi

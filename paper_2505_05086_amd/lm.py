@@ -1,5 +1,6 @@
 """The operators of a language model's fine-tuning step that stand beside the compressed layers: token log
-probabilities and their gradient, embedding, norms of queries and keys with the position rotation, AdamW.
+probabilities and their gradient (from logits, or from hidden states without any), embedding, norms of queries and keys with the
+position rotation, dropout without a stored mask, the edge between two blocks, AdamW.
 
 Thin layer over the C ABI of include/asi_lm.h: it checks and marshals arguments, allocates results and scratch from
 torch's allocator on the current stream, and wires the calls into autograd where an input requires a gradient.  All
@@ -471,6 +472,388 @@ def qk_norm_rotate_grad(q, k, q_gain, k_gain, cos, sin, grad_q: torch.Tensor, gr
     if status:
         B._check(status, "asi_qk_norm_rotate_grad")
     return dq, dk, dqg, dkg
+
+
+# ---- token log probabilities without the logits ------------------------------------------------------------
+class LinearLogprobs(NamedTuple):
+    logprob: Optional[torch.Tensor]        # fp32, of each row's target; None without targets
+    entropy: torch.Tensor                  # fp32
+
+
+class LinearLogprobsGrad(NamedTuple):
+    logprob: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    hidden: Optional[torch.Tensor]         # gradients, in their tensors' type
+    weight: Optional[torch.Tensor]
+
+
+@_plans
+def _linear_plan(hidden, weight, any_address, scale, ignore_index, grad):
+    """Descriptor, scratch, the rows' shape, and whether hidden has to be laid out anew."""
+    shape, stride, dtype = hidden
+    if len(weight[0]) != 2 or not shape or shape[-1] != weight[0][1] or weight[2] != dtype or 0 in weight[0]:
+        raise ValueError("hidden is (..., dim) and weight (vocab, dim), both of one type, neither dimension empty")
+    dense = False
+    try:
+        rows, dim, apart = _row_layout(shape, stride, "hidden")
+    except ValueError:
+        rows, dim, apart, dense = shape[:-1].numel(), shape[-1], shape[-1], True
+    if rows and apart < dim:
+        apart, dense = dim, True
+    vocab = weight[0][0]
+    desc = B.LinearLogprobDesc(rows, dim, vocab, apart, _matrix(weight, "weight"), ignore_index, _dtype(dtype, "hidden"), scale, any_address, 0)
+    L = B.lib()
+    size = (L.asi_linear_logprobs_grad_workspace_bytes if grad else L.asi_linear_logprobs_workspace_bytes)(desc)
+    return desc, int(size), shape[:-1], dense
+
+
+def _linear_start(hidden, weight, scale, ignore_index, grad):
+    desc, nbytes, shape, dense = _linear_plan(_geometry(hidden), _geometry(weight), int(weight.data_ptr() % 16 != 0), scale, ignore_index, grad)
+    return desc, nbytes, shape, hidden.contiguous() if dense else hidden
+
+
+def _linear_logprobs(hidden, weight, targets, scale, ignore_index, want_stats):
+    desc, nbytes, shape, hidden = _linear_start(hidden, weight, scale, ignore_index, False)
+    targets = _targets(targets, shape)
+    device = _place(hidden, weight, targets)
+    logprob = None if targets is None else hidden.new_empty(shape, dtype=torch.float32)
+    entropy = hidden.new_empty(shape, dtype=torch.float32)
+    stats = hidden.new_empty(shape + (2,), dtype=torch.float32) if want_stats else None
+    ws = _scratch(nbytes, hidden)
+    status = B.lib().asi_linear_logprobs(desc, hidden.data_ptr(), weight.data_ptr(), _ptr(targets), _ptr(logprob), entropy.data_ptr(),
+                                         _ptr(stats), _ptr(ws), nbytes, _stream(device))
+    if status:
+        B._check(status, "asi_linear_logprobs")
+    return logprob, entropy, stats
+
+
+def _linear_grad(hidden, weight, targets, grad_logprob, grad_entropy, scale, ignore_index, kept, hidden_grad, weight_grad):
+    """kept: (entropy, stats) of a forward call, or None."""
+    like = hidden
+    desc, nbytes, shape, hidden = _linear_start(hidden, weight, scale, ignore_index, True)
+    targets = _targets(targets, shape)
+    if targets is None and grad_logprob is not None:
+        raise ValueError("grad_logprob weighs the targets' log probabilities: there are no targets")
+    grad_logprob, grad_entropy = _weights(grad_logprob, shape, "grad_logprob"), _weights(grad_entropy, shape, "grad_entropy")
+    device = _place(hidden, weight, targets, grad_logprob, grad_entropy)
+    if kept is None:
+        logprob = None if targets is None else hidden.new_empty(shape, dtype=torch.float32)
+        entropy, stats = hidden.new_empty(shape, dtype=torch.float32), None
+    else:
+        logprob, (entropy, stats) = None, kept
+    dhidden = like.new_empty(like.shape) if hidden_grad else None
+    dweight = weight.new_empty(weight.shape) if weight_grad else None
+    ws = _scratch(nbytes, hidden)
+    status = B.lib().asi_linear_logprobs_grad(desc, int(kept is not None), hidden.data_ptr(), weight.data_ptr(), _ptr(targets), _ptr(stats),
+                                              _ptr(logprob), _ptr(entropy), _ptr(grad_logprob), _ptr(grad_entropy), _ptr(dhidden),
+                                              _ptr(dweight), _ptr(ws), nbytes, _stream(device))
+    if status:
+        B._check(status, "asi_linear_logprobs_grad")
+    return LinearLogprobsGrad(logprob, entropy, dhidden, dweight)
+
+
+class _LinearLogprobsFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, targets, scale, ignore_index):
+        logprob, entropy, stats = _linear_logprobs(hidden, weight, targets, scale, ignore_index, True)
+        ctx.save_for_backward(hidden, weight, targets, entropy, stats)
+        ctx.options = scale, ignore_index
+        ctx.set_materialize_grads(False)
+        return logprob, entropy
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_logprob, grad_entropy):
+        if grad_logprob is None and grad_entropy is None:
+            return (None,) * 5
+        hidden, weight, targets, entropy, stats = ctx.saved_tensors
+        r = _linear_grad(hidden, weight, targets, grad_logprob, grad_entropy, *ctx.options, (entropy, stats), *ctx.needs_input_grad[:2])
+        return r.hidden, r.weight, None, None, None
+
+
+def linear_logprobs(hidden: torch.Tensor, weight: torch.Tensor, targets: Optional[torch.Tensor] = None, *, scale: float = 1.0,
+                    ignore_index: int = IGNORE_INDEX) -> LinearLogprobs:
+    """Log probabilities of `targets` under softmax(scale * hidden @ weight.T) and the entropy of each row, without the logits:
+    no more than a piece of them is ever in memory, in the forward pass not even that.  hidden (..., dim), weight (vocab, dim), fp32
+    or bf16; targets (...) int64.  A row whose target is ignore_index is left out: logprob and entropy 0, no gradient, whatever it
+    holds.  Differentiable in hidden and weight."""
+    scale, ignore_index = float(scale), operator.index(ignore_index)
+    if torch.is_grad_enabled() and (hidden.requires_grad or weight.requires_grad):
+        return LinearLogprobs(*_LinearLogprobsFn.apply(hidden, weight, targets, scale, ignore_index))
+    return LinearLogprobs(*_linear_logprobs(hidden, weight, targets, scale, ignore_index, False)[:2])
+
+
+def linear_logprobs_grad(hidden: torch.Tensor, weight: torch.Tensor, targets: Optional[torch.Tensor], grad_logprob: Optional[torch.Tensor],
+                         grad_entropy: Optional[torch.Tensor] = None, *, scale: float = 1.0, ignore_index: int = IGNORE_INDEX,
+                         hidden_grad: bool = True, weight_grad: bool = True) -> LinearLogprobsGrad:
+    """Gradients of sum(grad_logprob * logprob + grad_entropy * entropy) in hidden and weight, with both values, in one call: for a
+    loss whose weights are known beforehand it replaces forward and backward.  Either gradient may be left out."""
+    return _linear_grad(hidden, weight, targets, grad_logprob, grad_entropy, float(scale), operator.index(ignore_index), None, hidden_grad,
+                        weight_grad)
+
+
+# ---- dropout without a stored mask -------------------------------------------------------------------------
+def _seed(seed, p: float):
+    """A seed as the tensor that is read on the GPU, or as a number."""
+    if isinstance(seed, torch.Tensor):
+        if seed.dtype != torch.int64 or seed.numel() != 1:
+            raise ValueError("a seed on the GPU is an int64 tensor of one entry")
+        return seed, 0
+    if seed is None:
+        if p:
+            raise ValueError("dropout needs a seed")
+        return None, 0
+    seed = operator.index(seed)
+    if not -2 ** 63 <= seed < 2 ** 64:
+        raise ValueError("a seed has 64 bits")
+    return None, seed - 2 ** 64 if seed >= 2 ** 63 else seed
+
+
+def _dropout_options(p, offset):
+    p, offset = float(p), operator.index(offset)
+    if not 0.0 <= p < 1.0 or round(p * 65536) > 65535:
+        raise ValueError("p is at least 0 and, as a multiple of 2^-16, less than 1")
+    if not -2 ** 63 <= offset < 2 ** 63:
+        raise ValueError("offset has 64 bits")
+    return p, offset
+
+
+def _drawn(desc, number: int, offset: int):
+    """The descriptor with a call's numbers; the kept one stays as it is."""
+    desc = type(desc).from_buffer_copy(desc)
+    desc.seed, desc.offset = number, offset
+    return desc
+
+
+@_plans
+def _dropout_plan(geometry, p):
+    shape, stride, dtype = geometry
+    dense = False
+    if _dense(shape, stride) or not shape:
+        rows, dim, apart = 1 if 0 not in shape else 0, max(1, shape.numel()), max(1, shape.numel())
+    else:
+        try:
+            rows, dim, apart = _row_layout(shape, stride, "x")
+        except ValueError:
+            dense = True
+        if dense or (rows and apart < dim):
+            rows, dim, apart, dense = 1, shape.numel(), shape.numel(), True
+    return B.DropoutDesc(rows, dim, apart, dim, 0, 0, p, _dtype(dtype, "x"), 0), dense
+
+
+def _dropout(x, p, seed, number, offset) -> torch.Tensor:
+    desc, dense = _dropout_plan(_geometry(x), p)
+    desc = _drawn(desc, number, offset)
+    if dense:
+        x = x.contiguous()
+    device = _place(x, seed)
+    y = x.new_empty(x.shape)
+    status = B.lib().asi_dropout(desc, x.data_ptr(), _ptr(seed), y.data_ptr(), _stream(device))
+    if status:
+        B._check(status, "asi_dropout")
+    return y
+
+
+class _DropoutFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, seed, number, offset):
+        ctx.save_for_backward(seed)
+        ctx.options = p, number, offset
+        return _dropout(x, p, seed, number, offset)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad):
+        seed, = ctx.saved_tensors
+        p, number, offset = ctx.options
+        return _dropout(grad, p, seed, number, offset), None, None, None, None
+
+
+def dropout(x: torch.Tensor, p: float, seed=None, offset: int = 0) -> torch.Tensor:
+    """Each entry of x (fp32 or bf16) with probability p replaced by 0, the others divided by 1 - p; p is taken to the nearest multiple of
+    2^-16.  Which ones is a function of the entry's place in x, the seed and the offset (a layer's number, say) alone, so no mask is kept:
+    the gradient draws it again, and dropout(grad, p, seed, offset) is that gradient.  seed: an int, or an int64 tensor of one entry that
+    is read on the GPU when the call runs (a captured step takes other numbers as the tensor changes).  Differentiable in x."""
+    p, offset = _dropout_options(p, offset)
+    seed, number = _seed(seed, p)
+    if torch.is_grad_enabled() and x.requires_grad:
+        return _DropoutFn.apply(x, p, seed, number, offset)
+    return _dropout(x, p, seed, number, offset)
+
+
+# ---- the edge between two blocks ---------------------------------------------------------------------------
+class ResidualNorm(NamedTuple):
+    stream: torch.Tensor                   # the new stream, x's type
+    out: Optional[torch.Tensor]            # its norm, the block's type; None without
+
+
+class ResidualNormGrad(NamedTuple):
+    x: torch.Tensor
+    y: Optional[torch.Tensor]
+    post_gain: Optional[torch.Tensor]      # fp32, as those below; None where there is no such norm or gate
+    gate: Optional[torch.Tensor]
+    pre_gain: Optional[torch.Tensor]
+
+
+class _ResidualOptions(NamedTuple):
+    post_norm: bool
+    pre_norm: bool
+    scale: float
+    eps: float
+    p: float
+
+
+def _rows_apart(shape, stride, what: str):
+    """Rows and their distance, or None where they have to be laid out anew."""
+    try:
+        rows, dim, apart = _row_layout(shape, stride, what)
+    except ValueError:
+        return None
+    return apart if not rows or apart >= dim else None
+
+
+@_plans
+def _residual_plan(x, y, post_gain, gate, pre_gain, dtype, options, grad):
+    """Descriptor, scratch, and which of x and y have to be laid out anew."""
+    shape = x[0]
+    if not shape or not shape[-1]:
+        raise ValueError("x is (..., dim)")
+    dim, rows = shape[-1], shape[:-1].numel()
+    if y is not None and y[0] != shape:
+        raise ValueError("x and y have one shape")
+    if y is None and (post_gain is not None or gate is not None):
+        raise ValueError("post_gain and gate are those of a block's output y")
+    if (post_gain is not None and not options.post_norm) or (pre_gain is not None and not options.pre_norm):
+        raise ValueError("a gain is given for a norm that is not")
+    if y is None and not options.pre_norm:
+        raise ValueError("neither y nor a norm of the stream: there is nothing to do")
+    given = [g for g in (post_gain, pre_gain, gate) if g is not None]
+    for g in (post_gain, pre_gain):
+        if g is not None and (g[0] != (dim,) or not _dense(*g[:2])):
+            raise ValueError("the gains are contiguous tensors of dim entries")
+    if any(g[2] != given[0][2] for g in given):
+        raise ValueError("the gains and the gate have one type")
+    gates = 0
+    if gate is not None:
+        if not _dense(*gate[:2]):
+            raise ValueError("the gate is contiguous")
+        if gate[0] == (dim,):
+            gates = 1
+        else:
+            # leading dimensions as x's, then ones
+            lead, n = gate[0][:-1], len(gate[0])
+            k = next((i for i, s in enumerate(lead) if s == 1 and shape[i:i + 1] != (1,)), len(lead)) if n == len(shape) else -1
+            if k < 0 or gate[0][-1] != dim or lead[:k] != shape[:k] or any(s != 1 for s in lead[k:]):
+                raise ValueError("the gate is (dim), or x's shape with ones in place of the last dimensions before dim")
+            gates = shape[:k].numel()
+    out = y[2] if y is not None else dtype or x[2]
+    apart = [_rows_apart(g[0], g[1], "x") if g is not None else dim for g in (x, y)]
+    desc = B.ResidualDesc(rows, dim, apart[0] or dim, apart[1] or dim, gates if rows else 0, 0, 0, options.p,
+                          _dtype(x[2], "x"), _dtype(out, "y"), _dtype(given[0][2], "a gain") if given else B.ASI_F32,
+                          bool(options.post_norm and y is not None), options.scale, options.eps)
+    return desc, int(B.lib().asi_residual_norm_grad_workspace_bytes(desc)) if grad else 0, out, apart[0] is None, apart[1] is None
+
+
+def _residual(x, y, post_gain, gate, pre_gain, seed, draw, dtype, options):
+    desc, _, out_dtype, x_anew, y_anew = _residual_plan(_geometry(x), _geometry(y), _geometry(post_gain), _geometry(gate), _geometry(pre_gain),
+                                                        dtype, options, False)
+    if options.p:
+        desc = _drawn(desc, *draw)
+    x, y = x.contiguous() if x_anew else x, y.contiguous() if y_anew else y
+    device = _place(x, y, post_gain, gate, pre_gain, seed)
+    stream = None if y is None else x.new_empty(x.shape)
+    out = x.new_empty(x.shape, dtype=out_dtype) if options.pre_norm else None
+    status = B.lib().asi_residual_norm(desc, x.data_ptr(), _ptr(y), _ptr(post_gain), _ptr(gate) if desc.gate_rows else None, _ptr(pre_gain),
+                                       _ptr(seed), _ptr(stream), _ptr(out), _stream(device))
+    if status:
+        B._check(status, "asi_residual_norm")
+    return stream, out
+
+
+def _residual_grad(grad_stream, grad_out, stream, y, post_gain, gate, pre_gain, seed, draw, options, gains):
+    desc, nbytes, out_dtype, s_anew, y_anew = _residual_plan(_geometry(stream), _geometry(y), _geometry(post_gain), _geometry(gate),
+                                                             _geometry(pre_gain), None if grad_out is None else grad_out.dtype, options, True)
+    if options.p:
+        desc = _drawn(desc, *draw)
+    for g, dtype, what in ((grad_stream, stream.dtype, "grad_stream"), (grad_out, out_dtype, "grad_out")):
+        if g is not None and (g.shape != stream.shape or g.dtype != dtype):
+            raise ValueError(f"{what} has the result's shape and type")
+    if grad_out is not None and not options.pre_norm:
+        raise ValueError("grad_out is the gradient of a norm that is not")
+    if grad_stream is None and grad_out is None:
+        raise ValueError("one gradient at least")
+    grad_stream, grad_out = (g if g is None or g.is_contiguous() else g.contiguous() for g in (grad_stream, grad_out))
+    s, y_rows = stream.contiguous() if s_anew else stream, y.contiguous() if y_anew else y
+    device = _place(s, y_rows, post_gain, gate, pre_gain, seed, grad_stream, grad_out)
+    dx, dy = stream.new_empty(stream.shape), None if y is None else y.new_empty(y.shape)
+    dim = stream.shape[-1]
+    new = lambda shape, there: stream.new_empty(shape, dtype=torch.float32) if there and gains else None  # noqa: E731
+    dpost, dpre = new(dim, options.post_norm and y is not None), new(dim, options.pre_norm)
+    dgate = None if gate is None else new(gate.shape, True)
+    if dgate is not None and not desc.gate_rows:
+        dgate.zero_()
+    ws = _scratch(nbytes, stream)
+    status = B.lib().asi_residual_norm_grad(desc, _ptr(grad_stream), _ptr(grad_out), s.data_ptr(), _ptr(y_rows), _ptr(post_gain),
+                                            _ptr(gate) if desc.gate_rows else None, _ptr(pre_gain), _ptr(seed), dx.data_ptr(), _ptr(dy),
+                                            _ptr(dpost), _ptr(dgate) if desc.gate_rows else None, _ptr(dpre), _ptr(ws), nbytes, _stream(device))
+    if status:
+        B._check(status, "asi_residual_norm_grad")
+    return ResidualNormGrad(dx, dy, dpost, dgate, dpre)
+
+
+class _ResidualNormFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, y, post_gain, gate, pre_gain, seed, draw, dtype, options):
+        stream, out = _residual(x, y, post_gain, gate, pre_gain, seed, draw, dtype, options)
+        ctx.save_for_backward(x if stream is None else stream, y, post_gain, gate, pre_gain, seed)
+        ctx.draw, ctx.options = draw, options
+        ctx.set_materialize_grads(False)
+        return stream, out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_stream, grad_out):
+        if grad_stream is None and grad_out is None:
+            return (None,) * 9
+        stream, y, post_gain, gate, pre_gain, seed = ctx.saved_tensors
+        r = _residual_grad(grad_stream, grad_out, stream, y, post_gain, gate, pre_gain, seed, ctx.draw, ctx.options,
+                           any(ctx.needs_input_grad[2:5]))
+        of = lambda g, t: None if t is None or g is None else g.to(t.dtype)  # noqa: E731
+        return r.x, r.y, of(r.post_gain, post_gain), of(r.gate, gate), of(r.pre_gain, pre_gain), None, None, None, None
+
+
+def _residual_options(post_norm, pre_norm, scale, eps, p, seed, offset):
+    p, offset = _dropout_options(p, offset)
+    seed, number = _seed(seed, p)
+    return _ResidualOptions(bool(post_norm), bool(pre_norm), float(scale), float(eps), p), seed, (number, offset)
+
+
+def residual_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None, post_gain: Optional[torch.Tensor] = None,
+                  gate: Optional[torch.Tensor] = None, pre_gain: Optional[torch.Tensor] = None, *, post_norm: bool = True,
+                  pre_norm: bool = True, scale: float = 1.0, eps: float = 1e-6, p: float = 0.0, seed=None, offset: int = 0,
+                  dtype: Optional[torch.dtype] = None) -> ResidualNorm:
+    """The edge between two blocks: stream = x + scale * gate * dropout(norm(y) * post_gain) and out = norm(stream) * pre_gain, the norms by the
+    root of a row's mean square.  x (..., dim), the stream so far, fp32 or bf16; y, the block's output, of its shape, bf16 or x's type;
+    out has y's type.  gate (dim), or x's shape with ones in place of the last dimensions before dim (a gate for each sequence, or for
+    each token).  Without y the stream is x itself and out its norm, in `dtype` (x's by default); post_norm and pre_norm leave either norm out.
+    p, seed and offset are dropout()'s.  The norm is that of the stream as it is rounded to its type.  For the gradients the stream and y are
+    kept, nothing else.  Differentiable in x, y, the gains and the gate."""
+    options, seed, draw = _residual_options(post_norm, pre_norm, scale, eps, p, seed, offset)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, y, post_gain, gate, pre_gain)):
+        stream, out = _ResidualNormFn.apply(x, y, post_gain, gate, pre_gain, seed, draw, dtype, options)
+    else:
+        stream, out = _residual(x, y, post_gain, gate, pre_gain, seed, draw, dtype, options)
+    return ResidualNorm(x if stream is None else stream, out)
+
+
+def residual_norm_grad(grad_stream: Optional[torch.Tensor], grad_out: Optional[torch.Tensor], stream: torch.Tensor,
+                       y: Optional[torch.Tensor] = None, post_gain: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                       pre_gain: Optional[torch.Tensor] = None, *, post_norm: bool = True, pre_norm: bool = True, scale: float = 1.0,
+                       eps: float = 1e-6, p: float = 0.0, seed=None, offset: int = 0) -> ResidualNormGrad:
+    """Gradients of residual_norm from those of its results (one of them may be None) and the stream that it gave (x where there is no
+    y).  The gains' and the gate's are fp32; their sums over rows have an order that the shapes alone decide."""
+    options, seed, draw = _residual_options(post_norm, pre_norm, scale, eps, p, seed, offset)
+    return _residual_grad(grad_stream, grad_out, stream, y, post_gain, gate, pre_gain, seed, draw, options, True)
 
 
 # ---- AdamW ------------------------------------------------------------------------------------------------

@@ -1,0 +1,372 @@
+"""Token log probabilities from hidden states without the logits (asi_linear_logprobs) against their definition in 64 bits.
+
+U = 2^-24 is half an fp32 ulp.  A logit is a sum of dim products, in fp32 inputs of six times as many (three bf16 parts a side; the
+parts that are left out are below 2^-24 of a product): E = (6 dim + 16) U sum_k |h_k w_k| bounds its error whatever the order, and
+what follows is a count of roundings on top; each bound is derived where it stands.
+"""
+import math
+
+import pytest
+import torch
+from torch.autograd import forward_ad
+
+import paper_2505_05086_amd as asi
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+INF, NAN = float("inf"), float("nan")
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+IGNORE = -100
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _round(dtype):
+    return 2.0 ** -8 if dtype == torch.bfloat16 else U
+
+
+def _close(got, want, bound, what):
+    """|got - want| <= bound entry by entry; where `want` is not finite the two are equal."""
+    got, want = got.double(), want.double()
+    assert got.shape == want.shape, what
+    bound = torch.as_tensor(bound, dtype=torch.float64, device=got.device).expand_as(want)
+    odd = ~torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{what}: NaN elsewhere"
+    assert torch.equal(got[odd].nan_to_num(7.0), want[odd].nan_to_num(7.0)), f"{what}: infinities"
+    off = ((got - want).abs() - bound)[~odd]
+    assert off.numel() == 0 or float(off.max()) <= 0, f"{what}: {float(off.max()):.3g} over its bound"
+
+
+def _inputs(rows, dim, vocab, dtype, seed, pad=0, shift=0, ignored=0.3, spread=2.5):
+    g = _gen(seed)
+    rand = lambda n, m, p, s, std: (torch.empty(n * (m + p) + s, device="cuda").normal_(0, std, generator=g).to(dtype)  # noqa: E731
+                                    [s:].as_strided((n, m), (m + p, 1)))
+    weight = rand(vocab, dim, pad, shift, spread * dim ** -0.5)
+    hidden = rand(rows, dim, pad, shift, 1.0)
+    targets = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    targets[torch.rand(rows, generator=g, device="cuda") < ignored] = IGNORE
+    if rows:
+        targets[0] = vocab - 1
+    a, b = (torch.randn(rows, generator=g, device="cuda") for _ in range(2))
+    return hidden, weight, targets, a, b
+
+
+class _Definition:
+    """Values, gradients and the bounds of their errors."""
+
+    def __init__(self, hidden, weight, targets, scale, a=None, b=None):
+        h, w = hidden.double(), weight.double()
+        r = _round(hidden.dtype)
+        live = torch.ones(len(h), dtype=torch.bool, device=h.device) if targets is None else targets != IGNORE
+        h = torch.where(live[:, None], h, 0.0)                            # a row that is left out is not read
+        dim, vocab = w.shape[1], w.shape[0]
+        z = h @ w.t().contiguous() * scale
+        e = (6 * dim + 16) * U * (h.abs() @ w.abs().t().contiguous()).amax(-1) * scale      # of any logit of a row
+        logp = torch.log_softmax(z, -1)
+        p = logp.exp()
+        entropy = torch.special.entr(p).sum(-1)
+        # a logit, the difference to the largest, its product, the logarithm of a sum of up to 2^12 terms in a lane and 2^12 in parts,
+        # of which no more than 128 in a row change its last bit
+        values = 2 * e + U * (8 * z.abs().amax(-1) + 256)
+        self.entropy = torch.where(live, entropy, 0.0)
+        # -sum p log p: p off by 2 e of itself
+        self.entropy_bound = torch.where(live, values * (2 + entropy), 0.0)
+        self.logprob = None
+        if targets is not None:
+            fine = (targets >= 0) & (targets < vocab)
+            at = torch.where(fine, targets, 0)[:, None]
+            self.logprob = torch.where(fine, logp.gather(1, at)[:, 0], NAN)
+            self.logprob[~live] = 0.0
+            self.logprob_bound = torch.where(live, values, 0.0)
+        if a is None and b is None:
+            return
+        hot = torch.zeros_like(z)
+        if targets is not None:
+            hot.scatter_(1, at, 1.0)
+        a = torch.zeros(len(h), device=h.device) if a is None else a
+        a, b = (torch.where(live, x.double(), 0.0)[:, None] for x in (a, torch.zeros_like(a) if b is None else b))
+        dz = scale * (a * (hot - p) - b * p * (logp + entropy[:, None]))
+        # p is off by 2 (e + the rounding of the logarithm) of itself and so is what is multiplied by it; dz is rounded to bf16 for bf16
+        # inputs, and otherwise held to 2^-24 in three parts
+        size = scale * (a.abs() * (hot + p) + b.abs() * p * (logp.abs() + entropy[:, None] + 1))
+        off = size * (4 * values[:, None] * (1 + b.abs().sign() * (1 + entropy[:, None])) + 32 * U) + (r + U) * dz.abs()
+        self.hidden = dz @ w
+        self.weight = dz.t().contiguous() @ h
+        # sums over the vocabulary (over rows) of products of numbers of either side, six times as many for fp32
+        self.hidden_bound = off @ w.abs() + (6 * vocab + 64) * U * (dz.abs() @ w.abs()) + r * self.hidden.abs()
+        self.weight_bound = off.t().contiguous() @ h.abs() + (6 * len(h) + 16) * U * (dz.abs().t().contiguous() @ h.abs()) + r * self.weight.abs()
+        self.hidden = torch.where(live[:, None], self.hidden, 0.0)
+        self.hidden_bound = torch.where(live[:, None], self.hidden_bound, 0.0)
+
+
+def _check_values(r, want, targets):
+    if targets is None:
+        assert r.logprob is None
+    else:
+        _close(r.logprob, want.logprob, want.logprob_bound, "logprob")
+    _close(r.entropy, want.entropy, want.entropy_bound, "entropy")
+
+
+SIZES = [(1, 64, 1), (1, 1, 2), (2, 7, 5), (3, 33, 100), (8, 128, 1000), (15, 1000, 63), (16, 64, 4097), (17, 64, 127), (16, 200, 129), (33, 65, 128),
+         (100, 192, 300), (127, 64, 257), (128, 128, 128), (129, 320, 1000), (300, 1000, 501), (257, 8, 3001), (1000, 64, 640)]
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("size", SIZES)
+def test_values(size, dtype):
+    for k, (pad, shift, scale, ignored) in enumerate([(0, 0, 1.0, 0.3), (8, 0, 0.7, 0.0), (3, 1, 1.3, 0.6)]):
+        hidden, weight, targets, _, _ = _inputs(*size, DTYPES[dtype], 1000 * size[0] + k, pad, shift, ignored)
+        _check_values(asi.linear_logprobs(hidden, weight, targets, scale=scale), _Definition(hidden, weight, targets, scale), targets)
+        _check_values(asi.linear_logprobs(hidden, weight, scale=scale), _Definition(hidden, weight, None, scale), None)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("size", SIZES)
+def test_gradients(size, dtype):
+    for k, (pad, shift, scale, ignored) in enumerate([(0, 0, 1.0, 0.3), (8, 0, 0.7, 0.0), (3, 1, 1.3, 0.6)]):
+        hidden, weight, targets, a, b = _inputs(*size, DTYPES[dtype], 2000 * size[0] + k, pad, shift, ignored)
+        for wa, wb in ((a, None), (a, b), (None, b)):
+            want = _Definition(hidden, weight, targets, scale, wa, wb)
+            r = asi.linear_logprobs_grad(hidden, weight, targets, wa, wb, scale=scale)
+            _check_values(r, want, targets)
+            _close(r.hidden, want.hidden, want.hidden_bound, "hidden")
+            _close(r.weight, want.weight, want.weight_bound, "weight")
+
+
+@pytest.mark.parametrize("rows,dim,vocab,dtype", [(2100, 64, 20000, "bf16"), (2100, 65, 17000, "f32"), (20, 64, 40000, "f32"), (5000, 128, 7001, "bf16"),
+                                                  (600, 1024, 2500, "bf16"), (9, 2048, 70001, "bf16")])
+def test_several_pieces_of_the_vocabulary(rows, dim, vocab, dtype):
+    hidden, weight, targets, a, b = _inputs(rows, dim, vocab, DTYPES[dtype], rows)
+    want = _Definition(hidden, weight, targets, 1.0, a, b)
+    r = asi.linear_logprobs_grad(hidden, weight, targets, a, b)
+    _check_values(r, want, targets)
+    _close(r.hidden, want.hidden, want.hidden_bound, "hidden")
+    _close(r.weight, want.weight, want.weight_bound, "weight")
+    again = asi.linear_logprobs_grad(hidden, weight, targets, a, b)
+    assert all(torch.equal(x, y) for x, y in zip(r, again))                # equal calls, equal bits
+    _check_values(asi.linear_logprobs(hidden, weight, targets), want, targets)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_autograd(dtype):
+    hidden, weight, targets, a, b = _inputs(70, 96, 333, DTYPES[dtype], 5)
+    want = asi.linear_logprobs_grad(hidden, weight, targets, a, b, scale=0.8)
+    h, w = hidden.clone().requires_grad_(), weight.clone().requires_grad_()
+    r = asi.linear_logprobs(h.view(7, 10, 96), w, targets.view(7, 10), scale=0.8)
+    (r.logprob * a.view(7, 10) + r.entropy * b.view(7, 10)).sum().backward()
+    assert torch.equal(r.logprob.flatten(), want.logprob) and torch.equal(r.entropy.flatten(), want.entropy)
+    assert torch.equal(h.grad, want.hidden) and torch.equal(w.grad, want.weight)
+    # one side only, one value only
+    h2 = hidden.clone().requires_grad_()
+    asi.linear_logprobs(h2, weight, targets, scale=0.8).logprob.sum().backward()
+    one = asi.linear_logprobs_grad(hidden, weight, targets, torch.ones_like(a), scale=0.8, weight_grad=False)
+    assert one.weight is None and torch.equal(h2.grad, one.hidden)
+    w2 = weight.clone().requires_grad_()
+    asi.linear_logprobs(hidden, w2, scale=0.8).entropy.sum().backward()
+    one = asi.linear_logprobs_grad(hidden, weight, None, None, torch.ones_like(a), scale=0.8, hidden_grad=False)
+    assert one.hidden is None and one.logprob is None and torch.equal(w2.grad, one.weight)
+    with pytest.raises(RuntimeError):
+        g, = torch.autograd.grad(asi.linear_logprobs(h, w, targets).logprob.sum(), h, create_graph=True)
+        g.sum().backward()
+
+
+def test_gradients_against_differences():
+    rows, dim, vocab, step = 24, 40, 90, 2.0 ** -6
+    hidden, weight, targets, a, _ = _inputs(rows, dim, vocab, torch.float32, 11, ignored=0.2)
+    r = asi.linear_logprobs_grad(hidden, weight, targets, a)
+    for side in ("hidden", "weight"):
+        x = dict(hidden=hidden, weight=weight)[side]
+        d = torch.randn(x.shape, generator=_gen(12), device="cuda") * dim ** -0.5
+        at = lambda s: (dict(hidden=hidden, weight=weight) | {side: x + s * d})  # noqa: E731,B023
+        both = [asi.linear_logprobs(at(s)["hidden"], at(s)["weight"], targets).logprob.double() @ a.double() for s in (step, -step)]
+        slope = float((getattr(r, side).double() * d.double()).sum())
+        want = _Definition(hidden, weight, targets, 1.0, a)
+        # values' errors over 2 step; what x + step d is rounded by, at most U of it a side; the third derivative of a log sum along a
+        # direction in which the logits change by m is at most their range's third power, 8 m^3
+        move = (d.double() @ weight.double().t()).abs() if side == "hidden" else (hidden.double() @ d.double().t()).abs()
+        rounding = U * 2 * ((hidden.double().abs() + step) @ (weight.double().abs() + step).t()).amax(-1)
+        bound = ((want.logprob_bound * 2 + 2 * rounding) / (2 * step) + step ** 2 / 6 * 8 * move.amax(-1) ** 3) @ a.double().abs()
+        slope_bound = float((getattr(want, side + "_bound") * d.double().abs()).sum())
+        assert abs(float(both[0] - both[1]) / (2 * step) - slope) <= float(bound) + slope_bound
+
+
+@pytest.mark.parametrize("rows", [7, 200])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_rows_that_are_left_out(rows, dtype):
+    hidden, weight, targets, a, b = _inputs(rows, 64, 300, DTYPES[dtype], 3, ignored=0.0)
+    out = torch.arange(rows, device="cuda") % 3 == 1
+    targets[out] = IGNORE
+    clean = asi.linear_logprobs_grad(hidden, weight, targets, a, b)
+    hidden[out] = NAN                                                     # padding may hold anything
+    a[out], b[out] = INF, NAN
+    r = asi.linear_logprobs_grad(hidden, weight, targets, a, b)
+    assert all(torch.equal(x, y) for x, y in zip(r, clean))
+    assert not r.logprob[out].any() and not r.entropy[out].any() and not r.hidden[out].any()
+    f = asi.linear_logprobs(hidden, weight, targets)
+    assert not f.logprob[out].any() and not f.entropy[out].any() and not torch.isnan(f.logprob).any()
+    targets[:] = IGNORE
+    r = asi.linear_logprobs_grad(hidden, weight, targets, a, b)
+    assert not any(t.any() for t in r)
+    assert not any(t.any() for t in asi.linear_logprobs(hidden, weight, targets))
+
+
+@pytest.mark.parametrize("rows", [5, 150])
+def test_targets_out_of_range_and_rows_that_are_not_numbers(rows):
+    hidden, weight, targets, a, _ = _inputs(rows, 64, 200, torch.float32, 4, ignored=0.0)
+    targets[1], targets[2] = 200, -1
+    hidden[3, 5] = NAN
+    r = asi.linear_logprobs_grad(hidden, weight, targets, a)
+    want = _Definition(hidden[:1], weight, targets[:1], 1.0, a[:1])
+    assert torch.isnan(r.logprob[1:4]).all() and torch.isnan(r.hidden[1:4]).all() and torch.isnan(r.entropy[3])
+    assert not torch.isnan(r.entropy[:3]).any() and not torch.isnan(r.logprob[4:]).any()
+    _close(r.hidden[:1], want.hidden, want.hidden_bound, "hidden")
+    assert torch.isnan(r.weight).all()
+    f = asi.linear_logprobs(hidden, weight, targets)
+    assert torch.isnan(f.logprob[1:4]).all() and not torch.isnan(f.entropy[:3]).any()
+
+
+@pytest.mark.parametrize("rows", [3, 40])
+def test_logits_of_infinity(rows):
+    """A token whose weights hold -infinity in a column that every hidden state has at 1 may not come."""
+    hidden, weight, targets, a, _ = _inputs(rows, 64, 300, torch.bfloat16, 6, ignored=0.0)
+    hidden[:, 7] = 1.0
+    never = torch.arange(300, device="cuda") % 4 == 1
+    targets[never[targets]] = 0
+    weight[never, 7] = -INF
+    r = asi.linear_logprobs(hidden, weight, targets)
+    kept = weight[~never].clone()
+    place = torch.cumsum(~never, 0) - 1
+    want = _Definition(hidden, kept, place[targets], 1.0)
+    _check_values(r, want, targets)
+    weight[:, 7] = -INF
+    r = asi.linear_logprobs(hidden, weight, targets)
+    assert (r.logprob == -INF).all() and not r.entropy.any()
+    weight[5, 7] = INF
+    assert torch.isnan(asi.linear_logprobs(hidden, weight, targets).logprob).all()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_large_logits_and_scales(dtype):
+    """Logits of thousands, of which one or a few matter, and scales far from one."""
+    for spread, scale in ((1000.0, 1.0), (2.5, 100.0), (2.5e4, 1e-4), (1e-3, 1e-3)):
+        hidden, weight, targets, a, b = _inputs(50, 128, 700, DTYPES[dtype], 8, spread=spread)
+        want = _Definition(hidden, weight, targets, scale, a, b)
+        r = asi.linear_logprobs_grad(hidden, weight, targets, a, b, scale=scale)
+        _check_values(r, want, targets)
+        _close(r.hidden, want.hidden, want.hidden_bound, "hidden")
+        _close(r.weight, want.weight, want.weight_bound, "weight")
+
+
+def test_layouts():
+    hidden, weight, targets, a, _ = _inputs(60, 64, 500, torch.bfloat16, 9)
+    want = asi.linear_logprobs_grad(hidden, weight, targets, a)
+    assert torch.equal(asi.linear_logprobs_grad(hidden.view(3, 20, 64), weight, targets.view(3, 20), a.view(3, 20)).hidden, want.hidden.view(3, 20, 64))
+    across = hidden.t().contiguous().t()                                  # a row's entries are not next to each other
+    assert torch.equal(asi.linear_logprobs_grad(across, weight, targets, a).weight, want.weight)
+    apart = torch.empty(3, 25, 64, device="cuda", dtype=torch.bfloat16)
+    apart[:, :20] = hidden.view(3, 20, 64)
+    r = asi.linear_logprobs_grad(apart[:, :20], weight, targets.view(3, 20), a.view(3, 20))
+    assert torch.equal(r.hidden.reshape(60, 64), want.hidden) and torch.equal(r.weight, want.weight)
+    one = hidden[:1].expand(60, 64)                                       # rows at distance 0
+    assert torch.equal(asi.linear_logprobs(one, weight, targets).logprob, asi.linear_logprobs(one.contiguous(), weight, targets).logprob)
+    for n in (0,):
+        none = asi.linear_logprobs_grad(hidden[:n], weight, targets[:n], a[:n])
+        assert none.hidden.shape == (0, 64) and none.logprob.shape == (0,) and none.weight.shape == weight.shape and not none.weight.any()
+        assert asi.linear_logprobs(hidden[:n], weight, targets[:n]).entropy.shape == (0,)
+
+
+def test_another_stream_and_a_graph_with_eager_work_between_replays():
+    hidden, weight, targets, a, _ = _inputs(300, 128, 2000, torch.bfloat16, 10)
+    few = hidden[:4].clone()
+    want = asi.linear_logprobs_grad(hidden, weight, targets, a)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        r = asi.linear_logprobs_grad(hidden, weight, targets, a)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(x, y) for x, y in zip(r, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = asi.linear_logprobs_grad(hidden, weight, targets, a)
+        values = asi.linear_logprobs(few, weight, targets[:4])
+    for seed in range(4):
+        h, _, t, _, _ = _inputs(300, 128, 2000, torch.bfloat16, 20 + seed, ignored=0.2 * seed)      # other rows are left out
+        hidden.copy_(h)
+        targets.copy_(t)
+        few.copy_(h[:4])
+        graph.replay()
+        eager = asi.linear_logprobs_grad(h, weight, t, a)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(captured, eager))
+        assert torch.equal(values.logprob, asi.linear_logprobs(h[:4], weight, t[:4]).logprob)
+
+
+def test_backward_into_a_graph():
+    hidden, weight, targets, a, _ = _inputs(64, 64, 300, torch.float32, 13)
+    want = asi.linear_logprobs_grad(hidden, weight, targets, a)
+    h, w = hidden.clone().requires_grad_(), weight.clone().requires_grad_()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = torch.autograd.grad(asi.linear_logprobs(h, w, targets).logprob, (h, w), a)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want.hidden) and torch.equal(got[1], want.weight)
+
+
+@pytest.mark.skip(reason="torch's engine joins the captured stream with that of the leaves' living eager graph, which ends the capture and the "
+                         "process; no operator can see it beforehand")
+def test_backward_into_a_graph_while_an_eager_graph_of_the_same_leaves_lives():
+    hidden, weight, targets, _, _ = _inputs(64, 64, 300, torch.float32, 13)
+    h, w = hidden.clone().requires_grad_(), weight.clone().requires_grad_()
+    lives = asi.linear_logprobs(h, w, targets).logprob.sum()
+    want = torch.autograd.grad(asi.linear_logprobs(h, w, targets).logprob.sum(), (h, w))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = torch.autograd.grad(asi.linear_logprobs(h, w, targets).logprob.sum(), (h, w))
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+    lives.backward()
+    assert torch.equal(h.grad, want[0]) and torch.equal(w.grad, want[1])
+
+
+def test_memory_stays_below_the_logits():
+    rows, dim, vocab = 4096, 256, 64000
+    hidden, weight, targets, a, _ = _inputs(rows, dim, vocab, torch.bfloat16, 14)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    r = asi.linear_logprobs_grad(hidden, weight, targets, a)
+    used = torch.cuda.max_memory_allocated() - before - sum(t.numel() * t.element_size() for t in r)
+    assert used < rows * vocab * 2 / 3                                    # the logits in bf16 are 524 MB
+    assert math.isfinite(float(r.logprob.sum()))
+
+
+def test_refusals():
+    hidden, weight, targets, a, b = _inputs(6, 64, 100, torch.float32, 15)
+    f, g = asi.linear_logprobs, asi.linear_logprobs_grad
+    for bad in (lambda: f(hidden, weight[:, :32], targets), lambda: f(hidden, weight.bfloat16(), targets), lambda: f(hidden, weight[0], targets),
+                lambda: f(hidden, weight, targets[:5]), lambda: f(hidden, weight.t().contiguous().t(), targets), lambda: f(hidden.cpu(), weight, targets),
+                lambda: f(hidden, weight, targets.cpu()), lambda: g(hidden, weight, None, a), lambda: g(hidden, weight, targets, a[:3]),
+                lambda: g(hidden, weight, targets, a.double()), lambda: f(hidden, weight[:0], targets)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: f(hidden.half(), weight.half(), targets), lambda: f(hidden, weight, targets.int())):
+        with pytest.raises(TypeError):
+            bad()
+    for scale in (0.0, -1.0, NAN, INF, 1e30):
+        with pytest.raises(asi.AsiError):
+            f(hidden, weight, targets, scale=scale)
+    with forward_ad.dual_level(), pytest.raises(NotImplementedError):
+        f(forward_ad.make_dual(hidden, hidden), weight, targets)
