@@ -13,13 +13,13 @@
 namespace asi {
 namespace {
 
-constexpr int kMostBlocks = 512;                   // workgroups of the backward pass
+constexpr int kGradThreads = 512, kMostBlocks = 256;      // of the backward pass: a workgroup a CU
 constexpr int kSumColumns = 64, kSumShares = 16;
 
 struct Args {
     const void *x, *y, *post, *gate, *pre, *ds, *dout;
     void *stream, *out, *dx, *dy;
-    float *part, *unit_part, *dgate;               // sums of a workgroup: [workgroup][pre, post, gate][dim]; of a unit: [unit][dim]
+    float *part, *unit_part, *dgate;               // sums of a workgroup: [workgroup][2][dim]; of a unit: [unit][dim]
     long long rows, dim, x_stride, y_stride, gate_rows, rows_a_gate, first;      // first: row with which the launch begins
     long long units;                               // of rows that share a gate row and a lane's sums: gate_rows * parts; 0: no such units
     int parts;
@@ -39,10 +39,25 @@ __device__ __forceinline__ void gain8(const Args& a, const void* p, long long at
     }
 }
 
-// Sums of N numbers over the LANES lanes of a row, in all of them.  `lds` has N floats for each wave of the workgroup.
+// Sums of N numbers over the LANES lanes of a row (16, a wave or several), in all of them and always in the same order: turns within 16
+// lanes, then the 16s of a wave, then the waves through LDS, which has N floats for each wave of the workgroup.
+template <int CTRL> __device__ __forceinline__ float turned(float x) { return __uint_as_float(moved<CTRL>(__float_as_uint(x))); }
 template <int LANES, int N> __device__ __forceinline__ void row_sums(float* v, float* lds) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = lanes_sum<(LANES < 64 ? LANES : 64)>(v[i]);
+    for (int i = 0; i < N; ++i) v[i] += turned<0x128>(v[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += turned<0x124>(v[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += turned<0x122>(v[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += turned<0x121>(v[i]);
+    if constexpr (LANES == 16) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int x = __float_as_int(v[i]);
+        v[i] = (__int_as_float(__builtin_amdgcn_readlane(x, 0)) + __int_as_float(__builtin_amdgcn_readlane(x, 16))) +
+               (__int_as_float(__builtin_amdgcn_readlane(x, 32)) + __int_as_float(__builtin_amdgcn_readlane(x, 48)));
+    }
     if constexpr (LANES > 64) {
         constexpr int waves = LANES / 64;
         const int wave = threadIdx.x >> 6, first = wave / waves * waves;
@@ -65,7 +80,7 @@ template <int LANES> constexpr int threads_of() { return LANES > 256 ? LANES : 2
 
 template <int K> __device__ __forceinline__ int count_at(const Args& a, int col) { return a.dim - col >= 8 ? 8 : a.dim > col ? (int)(a.dim - col) : 0; }
 
-template <typename S, typename T, int LANES, int K> __global__ __launch_bounds__(threads_of<LANES>()) void k_residual(const Args a) {
+template <typename S, typename T, int LANES, int K, bool DROP> __global__ __launch_bounds__(threads_of<LANES>()) void k_residual(const Args a) {
     __shared__ float lds[threads_of<LANES>() / 64];
     constexpr int kRows = threads_of<LANES>() / LANES;
     const int lane = threadIdx.x % LANES;
@@ -83,7 +98,7 @@ template <typename S, typename T, int LANES, int K> __global__ __launch_bounds__
         load8(static_cast<const S*>(a.x) + row * a.x_stride + col, count[k], x[k]);
     }
     if (a.y) {
-        if (a.drop) read_seed(&keep);
+        if constexpr (DROP) read_seed(&keep);
         float r = 1.f;
         if (a.post_norm) {
 #pragma unroll
@@ -101,10 +116,10 @@ template <typename S, typename T, int LANES, int K> __global__ __launch_bounds__
             gain8(a, a.post, col, count[k], post);
             gain8(a, a.gate, gate_row * a.dim + col, count[k], gate);
             uint32_t w[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
-            if (a.drop) drawn_from(keep, (unsigned long long)(row * a.dim + col), w);
+            if (DROP) drawn_from(keep, (unsigned long long)(row * a.dim + col), w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float n = y[k][e] * r * post[e], d = a.drop ? (kept(keep, w, e) ? n * keep.factor : 0.f) : n;
+                const float n = y[k][e] * r * post[e], d = DROP ? (kept(keep, w, e) ? n * keep.factor : 0.f) : n;
                 x[k][e] = to_f32(from_f32<S>(fmaf(d * gate[e], a.scale, x[k][e])));
             }
             store8(static_cast<S*>(a.stream) + row * a.dim + col, count[k], x[k]);
@@ -130,189 +145,288 @@ template <typename S, typename T, int LANES, int K> __global__ __launch_bounds__
     }
 }
 
-// The sums of a lane's columns over the rows that it has been through.
-template <int K> struct Sums {
-    float pre[K][8], post[K][8], gate[K][8];
+// Eight entries of a row as they were loaded, at half the registers where they are bf16.
+template <typename T> struct Row8 {
+    uint32_t w[2 * sizeof(T)];
+    __device__ __forceinline__ void load(const T* p, int count) {
+        if (count >= 8) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+                const loose4 v = *reinterpret_cast<const loose4*>(p + i * 16 / sizeof(T));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[4 * i + e] = v[e];
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * (int)sizeof(T); ++i) w[i] = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < count) {
+                if constexpr (sizeof(T) == 2) w[e >> 1] |= (uint32_t)p[e].bits << (16 * (e & 1));
+                else w[e] = __float_as_uint(p[e]);
+            }
+    }
+    __device__ __forceinline__ float get(int e) const {
+        if constexpr (sizeof(T) == 2) return __uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+        else return __uint_as_float(w[e]);
+    }
+};
+template <typename S, typename T, int K> struct GradRow {
+    Row8<S> ds[K], s[K];
+    Row8<T> dout[K], y[K];
 };
 
-// One row of the backward pass.
-template <typename S, typename T, int LANES, int K> __device__ __forceinline__ void grad_row(const Args& a, const Keep& keep, long long row, bool there, Sums<K>& sums, float* lds) {
-    const int lane = threadIdx.x % LANES;
-    float s[K][8], go[K][8], ds[K][8], y[K][8];
-    int count[K];
-    float v[3] = {0.f, 0.f, 0.f};
+// Eight gains, as they were loaded
+struct Gain8 {
+    uint32_t w[8];
+    __device__ __forceinline__ void load(const Args& a, const void* p, long long at, int count) {
+        if (!p) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int col = (k * LANES + lane) * 8;
-        count[k] = there ? count_at<K>(a, col) : 0;
-        load8(static_cast<const S*>(a.ds) + row * a.dim + col, a.ds ? count[k] : 0, ds[k]);
-        load8(static_cast<const T*>(a.dout) + row * a.dim + col, a.dout ? count[k] : 0, go[k]);
-        load8(static_cast<const S*>(a.x) + row * a.x_stride + col, a.dout ? count[k] : 0, s[k]);
-        load8(static_cast<const T*>(a.y) + row * a.y_stride + col, a.y ? count[k] : 0, y[k]);
-    }
+            for (int i = 0; i < 8; ++i) w[i] = 0x3f800000u;
+        } else if (a.gain_bf16) {
+            Row8<bf16_t> r;
+            r.load(static_cast<const bf16_t*>(p) + at, count);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        float pre[8];
-        gain8(a, a.pre, (k * LANES + lane) * 8, count[k], pre);
+            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(r.get(i));
+        } else {
+            Row8<float> r;
+            r.load(static_cast<const float*>(p) + at, count);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v[0] = fmaf(s[k][e], s[k][e], v[0]);
-            v[1] = fmaf(go[k][e] * pre[e], s[k][e], v[1]);
-            v[2] = fmaf(y[k][e], y[k][e], v[2]);
+            for (int i = 0; i < 8; ++i) w[i] = r.w[i];
         }
     }
-    row_sums<LANES, 3>(v, lds);
-    const float rs = a.dout ? rsqrtf(v[0] * a.inv_dim + a.eps) : 0.f, ry = a.post_norm ? rsqrtf(v[2] * a.inv_dim + a.eps) : 1.f;
-    const float along = v[1] * a.inv_dim * rs * rs;
-    const long long gate_row = a.gate ? row / a.rows_a_gate : 0;
-    float dot = 0.f;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int col = (k * LANES + lane) * 8;
-        if (a.dout) {
-            float pre[8];
-            gain8(a, a.pre, col, count[k], pre);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                ds[k][e] = fmaf(rs, fmaf(go[k][e], pre[e], -s[k][e] * along), ds[k][e]);
-                sums.pre[k][e] = fmaf(go[k][e], s[k][e] * rs, sums.pre[k][e]);
-            }
-        }
-        if (a.dx) store8(static_cast<S*>(a.dx) + row * a.dim + col, count[k], ds[k]);
-        if (a.y) {
-            float post[8], gate[8];
-            gain8(a, a.post, col, count[k], post);
-            gain8(a, a.gate, gate_row * a.dim + col, count[k], gate);
-            uint32_t w[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
-            if (a.drop) drawn_from(keep, (unsigned long long)(row * a.dim + col), w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const bool keeps = !a.drop || kept(keep, w, e);
-                const float t = ds[k][e] * a.scale * (a.drop ? keep.factor : 1.f), u = y[k][e] * ry;
-                if (e < count[k] && keeps) sums.gate[k][e] = fmaf(t, u * post[e], sums.gate[k][e]);
-                const float d = keeps ? t * gate[e] : 0.f;
-                if (e < count[k]) sums.post[k][e] = fmaf(d, u, sums.post[k][e]);
-                ds[k][e] = d * post[e];
-                y[k][e] = u;
-                if (e < count[k]) dot = fmaf(ds[k][e], u, dot);
-            }
-        }
-    }
-    if (!a.y) return;
-    if (a.post_norm) {
-        row_sums<LANES, 1>(&dot, lds);
-        dot *= a.inv_dim;
-    }
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int col = (k * LANES + lane) * 8;
-        if (a.post_norm) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) ds[k][e] = ry * fmaf(-y[k][e], dot, ds[k][e]);
-        }
-        store8(static_cast<T*>(a.dy) + row * a.dim + col, count[k], ds[k]);
-    }
-}
+    __device__ __forceinline__ float get(int e) const { return __uint_as_float(w[e]); }
+};
 
-template <typename S, typename T, int LANES, int K> __global__ __launch_bounds__(threads_of<LANES>()) void k_residual_grad(const Args a) {
-    constexpr int kThreads = threads_of<LANES>(), kRows = kThreads / LANES;
-    __shared__ float lds[kThreads * 8];
-    const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
+// The rows that the lanes of a row go through: all of them in turns, or those of their units of rows with a gate row in common.
+struct Walk {
+    long long row, apart, unit, end;               // end: the unit's last row and one; without units, all rows'
+    int at, most;
+    __device__ __forceinline__ void enter(const Args& a) {
+        const long long gate_row = unit / a.parts, part = unit - gate_row * a.parts, first = part * a.rows_a_gate / a.parts;
+        row = gate_row * a.rows_a_gate + first;
+        end = unit < a.units ? gate_row * a.rows_a_gate + (part + 1) * a.rows_a_gate / a.parts : row;
+    }
+    __device__ __forceinline__ void start(const Args& a, long long slot, long long slots) {
+        apart = slots;
+        at = 0;
+        most = 1;
+        row = unit = slot;
+        end = a.rows;
+        if (a.units) {
+            most = (int)((a.rows_a_gate + a.parts - 1) / a.parts);
+            enter(a);
+        }
+    }
+    __device__ __forceinline__ bool there() const { return row < end; }
+    __device__ __forceinline__ void next(const Args& a) {
+        if (!a.units) { row += apart; return; }
+        ++row;
+        if (++at == most) { at = 0; unit += apart; enter(a); }
+    }
+};
+
+// What bounds the backward pass besides memory is the chain load, sum, sum, store of a row: the next row's loads are on their way
+// meanwhile (K = 1), and the gains stay in registers (K = 1, all but the gate of a unit).  Between gate and post gain one sum serves both:
+// with q = sum over rows of t dropout' u it is post_gain q that is the gate's gradient and gate q the post gain's.
+template <typename S, typename T, int LANES, int K, bool DROP> __global__ __launch_bounds__(kGradThreads, 2) void k_residual_grad(const Args a) {
+    constexpr int kRows = kGradThreads / LANES;
+    __shared__ float lds[kGradThreads * 8];
+    const int lane = threadIdx.x % LANES;
     Keep keep = a.keep;
-    if (a.drop) read_seed(&keep);
-    Sums<K> sums;
+    if constexpr (DROP) read_seed(&keep);
+    int col[K], count[K];
+    float sum_pre[K][8], sum_q[K][8], sum_post[K][8];
+    Gain8 pre, post, gate;
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+    for (int k = 0; k < K; ++k) {
+        col[k] = (k * LANES + lane) * 8;
+        count[k] = count_at<K>(a, col[k]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sums.pre[k][e] = sums.post[k][e] = sums.gate[k][e] = 0.f;
-    if (!a.units) {
-        for (long long at = (long long)blockIdx.x * kRows; at < a.rows; at += (long long)gridDim.x * kRows)
-            grad_row<S, T, LANES, K>(a, keep, at + slot, at + slot < a.rows, sums, lds);
-    } else {
-        // rows [part * rows_a_gate / parts, (part + 1) * rows_a_gate / parts) of a gate row, by the lanes of one row; the workgroup's
-        // others go on with it, so that all of it comes to its barriers
-        const long long most = (a.rows_a_gate + a.parts - 1) / a.parts;
-        for (long long at = (long long)blockIdx.x * kRows; at < a.units; at += (long long)gridDim.x * kRows) {
-            const long long unit = at + slot, gate_row = unit / a.parts, part = unit - gate_row * a.parts;
-            const long long from = part * a.rows_a_gate / a.parts, to = (part + 1) * a.rows_a_gate / a.parts;
-            const bool mine = unit < a.units;
-            for (long long i = 0; i < most; ++i) grad_row<S, T, LANES, K>(a, keep, gate_row * a.rows_a_gate + from + i, mine && from + i < to, sums, lds);
-            float* sum = a.parts > 1 ? a.unit_part : a.dgate;
+        for (int e = 0; e < 8; ++e) sum_pre[k][e] = sum_q[k][e] = sum_post[k][e] = 0.f;
+    }
+    if constexpr (K == 1) {
+        pre.load(a, a.pre, col[0], count[0]);
+        post.load(a, a.post, col[0], count[0]);
+        gate.load(a, a.units ? nullptr : a.gate, col[0], count[0]);
+    }
+    auto load = [&](const Walk& at, bool go, GradRow<S, T, K>& r) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int n = go && at.there() ? count[k] : 0;
+            r.s[k].load(static_cast<const S*>(a.x) + at.row * a.x_stride + col[k], a.dout ? n : 0);
+            r.dout[k].load(static_cast<const T*>(a.dout) + at.row * a.dim + col[k], a.dout ? n : 0);
+            r.y[k].load(static_cast<const T*>(a.y) + at.row * a.y_stride + col[k], a.y ? n : 0);
+            r.ds[k].load(static_cast<const S*>(a.ds) + at.row * a.dim + col[k], a.ds ? n : 0);
+        }
+    };
+    const long long slots = (long long)gridDim.x * kRows;
+    Walk walk;
+    walk.start(a, (long long)blockIdx.x * kRows + threadIdx.x / LANES, slots);
+    const long long turns = ((a.units ? a.units : a.rows) + slots - 1) / slots * walk.most;
+    GradRow<S, T, K> r;
+    load(walk, true, r);
+    for (long long turn = 0; turn < turns; ++turn) {
+        const long long row = walk.row, unit = walk.unit;
+        const bool there = walk.there(), ends = a.units && walk.at + 1 == walk.most;
+        const bool mine = unit < a.units;
+        const long long gate_at = mine ? unit / a.parts * a.dim : 0;
+        if (K == 1 && a.units && walk.at == 0) gate.load(a, a.gate, gate_at + col[0], mine ? count[0] : 0);
+        walk.next(a);
+        GradRow<S, T, K> ahead;
+        if constexpr (K == 1) load(walk, turn + 1 < turns, ahead);
+        float v[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if constexpr (K > 1) pre.load(a, a.pre, col[k], count[k]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float s = r.s[k].get(e), y = r.y[k].get(e);
+                v[0] = fmaf(s, s, v[0]);
+                v[1] = fmaf(r.dout[k].get(e) * pre.get(e), s, v[1]);
+                v[2] = fmaf(y, y, v[2]);
+            }
+        }
+        row_sums<LANES, 3>(v, lds);
+        const float rs = a.dout ? rsqrtf(v[0] * a.inv_dim + a.eps) : 0.f, ry = a.post_norm ? rsqrtf(v[2] * a.inv_dim + a.eps) : 1.f;
+        const float along = v[1] * a.inv_dim * rs * rs;
+        float w[K][8], dot = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int n = there ? count[k] : 0;
+            if constexpr (K > 1) pre.load(a, a.pre, col[k], count[k]);
+            float dx[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float s = r.s[k].get(e), go = r.dout[k].get(e);
+                // where there is no row, or no norm behind the edge, s and go are 0; rs may be infinite where there is no row
+                dx[e] = e < n ? fmaf(rs, fmaf(go, pre.get(e), -s * along), r.ds[k].get(e)) : 0.f;
+                if (e < n) sum_pre[k][e] = fmaf(go, s * rs, sum_pre[k][e]);
+            }
+            if (a.dx) store8(static_cast<S*>(a.dx) + row * a.dim + col[k], n, dx);
+            if (!a.y) continue;
+            if constexpr (K > 1) {
+                post.load(a, a.post, col[k], count[k]);
+                gate.load(a, a.gate, gate_at + col[k], count[k]);
+            }
+            uint32_t bits[4];
+            if constexpr (DROP) drawn_from(keep, (unsigned long long)(row * a.dim + col[k]), bits);
+            const float size = DROP ? a.scale * keep.factor : a.scale;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                w[k][e] = 0.f;
+                if (e < n && (!DROP || kept(keep, bits, e))) {
+                    const float t = dx[e] * size, u = r.y[k].get(e) * ry;
+                    sum_q[k][e] = fmaf(t, u, sum_q[k][e]);
+                    w[k][e] = t * gate.get(e) * post.get(e);
+                    dot = fmaf(w[k][e], u, dot);
+                }
+            }
+        }
+        if (a.y) {
+            if (a.post_norm) {
+                row_sums<LANES, 1>(&dot, lds);
+                dot *= a.inv_dim * ry;
+            }
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const int col = (k * LANES + lane) * 8;
-                if (sum) store8(sum + unit * a.dim + col, mine ? count_at<K>(a, col) : 0, sums.gate[k]);
+                if (a.post_norm) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sums.gate[k][e] = 0.f;
+                    for (int e = 0; e < 8; ++e) w[k][e] = ry * fmaf(-r.y[k].get(e), dot, w[k][e]);
+                }
+                store8(static_cast<T*>(a.dy) + row * a.dim + col[k], there ? count[k] : 0, w[k]);
+            }
+            if (ends) {
+                // a unit's rows are through: its gate row's gradient, and its share of the post gain's
+                float* sum = a.parts > 1 ? a.unit_part : a.dgate;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    if constexpr (K > 1) {
+                        post.load(a, a.post, col[k], count[k]);
+                        gate.load(a, a.gate, gate_at + col[k], count[k]);
+                    }
+                    float d[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (mine && e < count[k]) sum_post[k][e] = fmaf(gate.get(e), sum_q[k][e], sum_post[k][e]);
+                        d[e] = post.get(e) * sum_q[k][e];
+                        sum_q[k][e] = 0.f;
+                    }
+                    if (sum) store8(sum + unit * a.dim + col[k], mine ? count[k] : 0, d);
+                }
             }
         }
+        if constexpr (K == 1) r = ahead;
+        else load(walk, turn + 1 < turns, r);
     }
     if (!a.part) return;
+    // two sums of a workgroup: those of the pre gain, and q or, where gate rows differ, the post gain's
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        for (int which = 0; which < 3; ++which) {
-            if ((which == 0 && !a.dout) || (which > 0 && !a.y) || (which == 2 && a.units)) continue;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            if (which == 0 ? !a.dout : !a.y) continue;
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) lds[threadIdx.x * 8 + e] = which == 0 ? sums.pre[k][e] : which == 1 ? sums.post[k][e] : sums.gate[k][e];
+            for (int e = 0; e < 8; ++e) lds[threadIdx.x * 8 + e] = which == 0 ? sum_pre[k][e] : a.units ? sum_post[k][e] : sum_q[k][e];
             __syncthreads();
-            for (int c = threadIdx.x; c < LANES * 8; c += kThreads) {
+            for (int c = threadIdx.x; c < LANES * 8; c += kGradThreads) {
                 float t = 0.f;
 #pragma unroll
-                for (int r = 0; r < kRows; ++r) t += lds[r * LANES * 8 + c];
-                const long long col = (long long)k * LANES * 8 + c;
-                if (col < a.dim) a.part[((long long)blockIdx.x * 3 + which) * a.dim + col] = t;
+                for (int slot = 0; slot < kRows; ++slot) t += lds[slot * LANES * 8 + c];
+                const long long at = (long long)k * LANES * 8 + c;
+                if (at < a.dim) a.part[((long long)blockIdx.x * 2 + which) * a.dim + at] = t;
             }
         }
 }
 
-// Columns' sums over the workgroups, in their order: `count` rows for gains, and for gate row g the `parts` rows of its units.
+// Columns' sums over the workgroups, in their order: job 0 the pre gain's, job 1 what post gain and gate have in common, job 2 + g gate
+// row g's from the `parts` rows of its units.  16 threads share a column, each with eight loads on their way.
 struct SumArgs {
     const float *part, *unit_part;
-    float *pre, *post, *gate;
+    const void *post_gain, *gate_row;              // job 1: factors of the gate's and the post gain's gradients; nullable
+    bool gain_bf16;
+    float *pre, *post, *one_gate, *gate;           // one_gate: the gradient of a gate of one row; gate: of the jobs from 2 on
     long long dim, first_gate;
-    int blocks, parts;
-    bool units;
+    int pre_blocks, blocks, parts;
 };
 __global__ __launch_bounds__(kSumColumns * kSumShares) void k_residual_sums(const SumArgs a) {
     __shared__ float lds[kSumShares][kSumColumns];
     const int c = threadIdx.x % kSumColumns, share = threadIdx.x / kSumColumns;
-    const long long col = (long long)blockIdx.x * kSumColumns + c;
-    const int job = (int)blockIdx.y;
-    const float* in;
-    float* out;
-    long long apart;
-    int n;
-    if (job < 2 || !a.units) {
-        in = a.part + job * a.dim; apart = 3 * a.dim; n = a.blocks;
-        out = job == 0 ? a.pre : job == 1 ? a.post : a.gate;
-    } else {
-        const long long g = a.first_gate + job - 2;
-        in = a.unit_part + g * a.parts * a.dim; apart = a.dim; n = a.parts;
-        out = a.gate + g * a.dim;
-    }
-    if (!out) return;
+    const long long col = (long long)blockIdx.x * kSumColumns + c, g = a.first_gate + (int)blockIdx.y - 2;
+    const int job = (int)blockIdx.y, n = job == 0 ? a.pre_blocks : job == 1 ? a.blocks : a.parts;
+    if (job == 0 ? !a.pre : job == 1 ? !a.post && !a.one_gate : !a.gate) return;
+    const float* in = (job < 2 ? a.part + job * a.dim : a.unit_part + g * a.parts * a.dim) + col;
+    const long long apart = job < 2 ? 2 * a.dim : a.dim;
     float t = 0.f;
-    if (col < a.dim)
-        for (int i = share; i < n; i += kSumShares) t += in[i * apart + col];
+    if (col < a.dim) {
+        constexpr int kAhead = 8;
+        for (int i = share; i < n; i += kSumShares * kAhead) {
+            float f[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) f[u] = i + u * kSumShares < n ? in[(i + u * kSumShares) * apart] : 0.f;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) t += f[u];
+        }
+    }
     lds[share][c] = t;
     __syncthreads();
-    if (share == 0 && col < a.dim) {
-        for (int i = 1; i < kSumShares; ++i) t += lds[i][c];
-        out[col] = t;
-    }
+    if (share || col >= a.dim) return;
+    for (int i = 1; i < kSumShares; ++i) t += lds[i][c];
+    auto factor = [&](const void* p) { return !p ? 1.f : a.gain_bf16 ? to_f32(static_cast<const bf16_t*>(p)[col]) : static_cast<const float*>(p)[col]; };
+    if (job == 0) a.pre[col] = t;
+    else if (job == 1) {
+        if (a.post) a.post[col] = t * factor(a.gate_row);
+        if (a.one_gate) a.one_gate[col] = t * factor(a.post_gain);
+    } else a.gate[g * a.dim + col] = t;
 }
 
 // ---- host ----
 int lanes_for(long long dim) {
-    int lanes = 8;
-    while (lanes < 512 && lanes * 8 < dim) lanes *= 2;
-    return lanes;
+    return dim <= 128 ? 16 : dim <= 512 ? 64 : dim <= 1024 ? 128 : dim <= 2048 ? 256 : 512;
 }
-int rows_a_block(long long dim) {
-    const int lanes = lanes_for(dim);
-    return lanes >= 256 ? 1 : 256 / lanes;
-}
+int rows_a_block(long long dim) { return kGradThreads / lanes_for(dim); }      // of the backward pass
 
 asi_status check(const asi_residual_desc* d) {
     if (!d || d->rows < 0 || d->dim < 1 || d->x_stride < d->dim || d->y_stride < d->dim || d->gate_rows < 0 || d->gate_rows > d->rows ||
@@ -351,35 +465,37 @@ Plan plan(const asi_residual_desc* d) {
     }
     const long long blocks = (items + slots - 1) / slots;
     p.blocks = (int)(blocks < kMostBlocks ? blocks : kMostBlocks);
-    p.part_floats = (size_t)p.blocks * 3 * d->dim;
+    p.part_floats = (size_t)p.blocks * 2 * d->dim;
     return p;
 }
 
-template <typename S, typename T, int LANES, int K> void launch(const Args& a, bool back, int blocks, hipStream_t st) {
+template <typename S, typename T, int LANES, int K, bool DROP> void launch(const Args& a, bool back, int blocks, hipStream_t st) {
     if (back) {
-        hipLaunchKernelGGL((k_residual_grad<S, T, LANES, K>), dim3(blocks), threads_of<LANES>(), 0, st, a);
+        hipLaunchKernelGGL((k_residual_grad<S, T, LANES, K, DROP>), dim3(blocks), kGradThreads, 0, st, a);
         return;
     }
     constexpr long long rows = threads_of<LANES>() / LANES, most = most_workgroups(threads_of<LANES>()) * rows;
     Args b = a;
     for (b.first = 0; b.first < a.rows; b.first += most) {
         const long long left = a.rows - b.first < most ? a.rows - b.first : most;
-        hipLaunchKernelGGL((k_residual<S, T, LANES, K>), dim3((unsigned)((left + rows - 1) / rows)), threads_of<LANES>(), 0, st, b);
+        hipLaunchKernelGGL((k_residual<S, T, LANES, K, DROP>), dim3((unsigned)((left + rows - 1) / rows)), threads_of<LANES>(), 0, st, b);
+    }
+}
+template <typename S, typename T, bool DROP> void go(const Args& a, bool back, int blocks, hipStream_t st) {
+    switch (lanes_for(a.dim)) {
+        case 16: return launch<S, T, 16, 1, DROP>(a, back, blocks, st);
+        case 64: return launch<S, T, 64, 1, DROP>(a, back, blocks, st);
+        case 128: return launch<S, T, 128, 1, DROP>(a, back, blocks, st);
+        case 256: return launch<S, T, 256, 1, DROP>(a, back, blocks, st);
+        default:
+            if (a.dim <= 4096) return launch<S, T, 512, 1, DROP>(a, back, blocks, st);
+            if (a.dim <= 8192) return launch<S, T, 512, 2, DROP>(a, back, blocks, st);
+            return launch<S, T, 512, 4, DROP>(a, back, blocks, st);
     }
 }
 template <typename S, typename T> void go(const Args& a, bool back, int blocks, hipStream_t st) {
-    switch (lanes_for(a.dim)) {
-        case 8: return launch<S, T, 8, 1>(a, back, blocks, st);
-        case 16: return launch<S, T, 16, 1>(a, back, blocks, st);
-        case 32: return launch<S, T, 32, 1>(a, back, blocks, st);
-        case 64: return launch<S, T, 64, 1>(a, back, blocks, st);
-        case 128: return launch<S, T, 128, 1>(a, back, blocks, st);
-        case 256: return launch<S, T, 256, 1>(a, back, blocks, st);
-        default:
-            if (a.dim <= 4096) return launch<S, T, 512, 1>(a, back, blocks, st);
-            if (a.dim <= 8192) return launch<S, T, 512, 2>(a, back, blocks, st);
-            return launch<S, T, 512, 4>(a, back, blocks, st);
-    }
+    if (a.drop) go<S, T, true>(a, back, blocks, st);
+    else go<S, T, false>(a, back, blocks, st);
 }
 void go(const asi_residual_desc* d, const Args& a, bool back, int blocks, hipStream_t st) {
     if (d->dtype == ASI_F32) go<float, float>(a, back, blocks, st);
@@ -429,7 +545,6 @@ asi_status asi_residual_norm_grad(const asi_residual_desc* desc, const void* gra
     hipStream_t st = static_cast<hipStream_t>(stream);
     SumArgs sums{};
     sums.dim = desc->dim;
-    sums.pre = dpre_gain; sums.post = dpost_gain; sums.gate = dgate;
     Plan p{};
     if (desc->rows) {
         if ((!grad_stream && !grad_out) || (grad_out && !s) || (!y) != (!dy) || (desc->gate_rows != 0) != (gate != nullptr) || (!y && gate) || (dgate && !gate)) return ASI_ERR_INVALID_ARG;
@@ -449,28 +564,21 @@ asi_status asi_residual_norm_grad(const asi_residual_desc* desc, const void* gra
         if (!gains) return launched();
         sums.part = a.part; sums.unit_part = a.unit_part;
     }
-    // what has no summands (no rows, no block, no norm behind the edge) is zero
-    const dim3 grid_x((unsigned)((desc->dim + kSumColumns - 1) / kSumColumns));
+    // what has no summands (no rows, no block, no norm behind the edge) is zero; one gate row's gradient is made with the post gain's
+    const unsigned columns = (unsigned)((desc->dim + kSumColumns - 1) / kSumColumns);
     sums.parts = p.parts;
-    auto go_sums = [&](float* pre, float* post, float* gate, int blocks, bool units, unsigned jobs, long long first) {
-        SumArgs b = sums;
-        b.pre = pre; b.post = post; b.gate = gate; b.blocks = blocks; b.units = units; b.first_gate = first;
-        hipLaunchKernelGGL(k_residual_sums, dim3(grid_x.x, jobs), kSumColumns * kSumShares, 0, st, b);
-    };
-    const int pre_blocks = grad_out ? p.blocks : 0, post_blocks = y ? p.blocks : 0;
-    const bool by_unit = p.units != 0;
-    float* gate_sum = desc->gate_rows == 1 ? dgate : nullptr;
-    if (pre_blocks == post_blocks) {
-        go_sums(dpre_gain, dpost_gain, gate_sum, pre_blocks, false, 3, 0);
-    } else {
-        if (dpre_gain) go_sums(dpre_gain, nullptr, nullptr, pre_blocks, false, 3, 0);
-        if (dpost_gain || gate_sum) go_sums(nullptr, dpost_gain, gate_sum, post_blocks, false, 3, 0);
-    }
-    if (dgate && by_unit && p.parts > 1) {
+    sums.pre_blocks = grad_out ? p.blocks : 0;
+    sums.blocks = y ? p.blocks : 0;
+    sums.pre = dpre_gain; sums.post = dpost_gain; sums.one_gate = desc->gate_rows == 1 ? dgate : nullptr;
+    sums.post_gain = post_gain; sums.gate_row = p.units ? nullptr : gate; sums.gain_bf16 = desc->gain_dtype == ASI_BF16;
+    if (dpre_gain || dpost_gain || sums.one_gate) hipLaunchKernelGGL(k_residual_sums, dim3(columns, 2), kSumColumns * kSumShares, 0, st, sums);
+    if (dgate && p.units && p.parts > 1) {
         constexpr long long most = 65000;
-        for (long long g = 0; g < desc->gate_rows; g += most) {
-            const long long n = desc->gate_rows - g < most ? desc->gate_rows - g : most;
-            go_sums(nullptr, nullptr, dgate, 0, true, (unsigned)(n + 2), g);
+        sums.pre = sums.post = nullptr;
+        sums.gate = dgate;
+        for (sums.first_gate = 0; sums.first_gate < desc->gate_rows; sums.first_gate += most) {
+            const long long n = desc->gate_rows - sums.first_gate < most ? desc->gate_rows - sums.first_gate : most;
+            hipLaunchKernelGGL(k_residual_sums, dim3(columns, (unsigned)(n + 2)), kSumColumns * kSumShares, 0, st, sums);
         }
     }
     return launched();
