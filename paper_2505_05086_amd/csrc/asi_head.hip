@@ -9,7 +9,7 @@
 //                 each token, d = x - x_max, e = exp(scale d), and the target's logit.  Gradient: dz, rounded to bf16
 //   k_few         the same values for up to 16 rows, the weights from memory straight into the matrix instructions
 //   k_join        joins the tiles' values
-//   k_dhidden, k_dweight  the products of dz with weights and hidden states, read across as they lie (asi_tiles.h)
+//   k_products    the products of dz with weights (dH) and hidden states (dW), read across as they lie (asi_tiles.h)
 //   k_hidden      the sums of dH, in fp32 over the pieces of the vocabulary and the parts of a piece, to their rows
 //
 // What bounds it: the matrix products, 2 rows dim vocab for the values and 8 with the gradients (6 if the logits were kept); the
@@ -24,8 +24,9 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLow = -1e30f;                       // stands for -infinity where that is multiplied by 0
+constexpr int kTileThreads = 256;                    // of k_logits and k_logits_grad
 constexpr int kFew = 16;                             // rows of k_few
-constexpr size_t kPieceBytes = size_t(64) << 20;     // dz of a piece, in bf16
+constexpr size_t kPieceBytes = size_t(96) << 20;     // dz of a piece, in bf16
 
 // What the gradient needs of a row: p = exp2(scale' (x - top) - log2sum); dz = [target] a - p (a + b (log p + entropy))
 struct RowInfo {
@@ -94,7 +95,7 @@ struct PackArgs {
     const int *count, *live;                         // nullable: all rows
     int dim, pieces;                                 // pieces of 8 of a packed row
     uint16_t* out;
-    long long plane;
+    long long ld, plane;
     bool whole;                                      // rows are whole vectors
 };
 template <typename T> __global__ __launch_bounds__(256) void k_pack(const PackArgs a) {
@@ -118,7 +119,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_pack(const PackAr
         uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = h[2 * e][p] | ((uint32_t)h[2 * e + 1][p] << 16);
-        store_words(a.out + p * a.plane + row * a.pieces * 8 + col, make_uint4(w[0], w[1], w[2], w[3]));
+        store_words(a.out + p * a.plane + row * a.ld + col, make_uint4(w[0], w[1], w[2], w[3]));
     }
 }
 
@@ -138,7 +139,7 @@ __device__ __forceinline__ bool my_tile(long long id, long long m_tiles, long lo
 struct LogitArgs {
     Operand w, h;                                    // the piece's weights; the live rows' hidden states
     const int* count;
-    int pairs, k_steps;
+    int k_steps;
     long long vocab, first;                          // of the piece; its first token
     float scale;
     // values: [tile][top, sum, along][rows], the targets' logits [rows]
@@ -152,6 +153,7 @@ struct LogitArgs {
     long long dz_stride, dz_plane;
 };
 
+constexpr int pairs_of(int planes) { return planes == 1 ? 1 : kPairs; }
 template <int BM, int BN> using LogitTile = Tile<BM, BN, false, false>;
 
 struct Joined {
@@ -166,7 +168,7 @@ __device__ __forceinline__ Joined join(Joined a, Joined b, float c) {
     return Joined{top, a.sum * ea + b.sum * eb, ea * fmaf(a.sum, da, a.along) + eb * fmaf(b.sum, db, b.along)};
 }
 
-template <int BM, int BN> __global__ __launch_bounds__(kTileThreads, BM * BN > 128 * 128 ? 1 : 2) void k_logits(const LogitArgs a) {
+template <int BM, int BN, int PLANES> __global__ __launch_bounds__(kTileThreads, BM * BN > 128 * 128 ? 1 : 2) void k_logits(const LogitArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     using Tl = LogitTile<BM, BN>;
     const long long rows = *a.count;
@@ -176,7 +178,7 @@ template <int BM, int BN> __global__ __launch_bounds__(kTileThreads, BM * BN > 1
     t.clear();
     Operand h = a.h;
     h.rows = rows;
-    t.run(a.w, h, tm * BM, tn * BN, 0, a.k_steps, a.pairs, lds);
+    t.template run<pairs_of(PLANES)>(a.w, h, tm * BM, tn * BN, 0, a.k_steps, lds);
     __syncthreads();
     const float c = a.scale * kLog2e;
     const int lane = threadIdx.x & 63;
@@ -214,7 +216,7 @@ template <int BM, int BN> __global__ __launch_bounds__(kTileThreads, BM * BN > 1
             }
         sum += __shfl_xor(sum, 32);
         along += __shfl_xor(along, 32);
-        if (lane < 32) shared[(threadIdx.x >> 7) * BN + col] = Joined{top, sum, along};
+        if (lane < 32) shared[Tl::wave_m() * BN + col] = Joined{top, sum, along};
         if (a.targets) {
             const long long target = row < rows ? a.targets[a.live[row]] - a.first - v0 : -1;
             if (__any(target >= 0 && target < BM / 2)) {
@@ -258,12 +260,12 @@ template <typename Tl, int BM, int BN, typename F> __device__ __forceinline__ vo
     constexpr int pieces = BM / 8;
     if (whole) {
 #pragma unroll 4
-        for (int at = threadIdx.x; at < BN * pieces; at += kTileThreads) {
+        for (int at = threadIdx.x; at < BN * pieces; at += Tl::kThreads) {
             const int n = at / pieces, piece = at % pieces;
             if (n < n_left && piece * 8 < m_left) store_words(out + n * stride + piece * 8, load_words4(lds + n * pitch + piece * 16));
         }
     } else {
-        for (int at = threadIdx.x; at < BN * BM; at += kTileThreads) {
+        for (int at = threadIdx.x; at < BN * BM; at += Tl::kThreads) {
             const int n = at / BM, m = at % BM;
             if (n < n_left && m < m_left) out[n * stride + m] = *reinterpret_cast<const uint16_t*>(lds + n * pitch + m * 2);
         }
@@ -280,34 +282,51 @@ template <int BM, int BN, int PLANES> __global__ __launch_bounds__(kTileThreads,
     t.clear();
     Operand h = a.h;
     h.rows = rows;
-    t.run(a.w, h, tm * BM, tn * BN, 0, a.k_steps, a.pairs, lds);
+    t.template run<pairs_of(PLANES)>(a.w, h, tm * BM, tn * BN, 0, a.k_steps, lds);
     const float c = a.scale * kLog2e;
     const int lane = threadIdx.x & 63;
     const long long v0 = tm * BM + Tl::at_m();
-    const bool over = v0 + BM / 2 > a.vocab;
 #pragma unroll
     for (int j = 0; j < Tl::kN; ++j) {
         const long long row = tn * BN + Tl::at_n() + 32 * j + (lane & 31);
         RowInfo f{0.f, INFINITY, 0.f, 0.f, 0.f, -1, {0, 0}};
         if (row < rows) f = a.info[row];
-        const int target = f.target >= 0 ? (int)(f.target - a.first - v0) : -1;
-        const bool here = __any(target >= 0 && target < BM / 2);
-        const bool entropy = __any(f.b != 0.f);      // NaN too
+        const long long target = f.target >= 0 ? f.target - a.first - v0 : -1;
+        if (__any(f.b != 0.f)) {                     // NaN too
+#pragma unroll
+            for (int i = 0; i < Tl::kM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float x = fmaf(t.acc[i][j][r] - f.top, c, -f.log2sum), p = __builtin_amdgcn_exp2f(x);
+                    t.acc[i][j][r] = -p * fmaf(f.b, fmaf(max_nan(x, kLow), 1.f / kLog2e, f.entropy), f.a);
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < Tl::kM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) t.acc[i][j][r] = -f.a * __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][r] - f.top, c, -f.log2sum));
+        }
+        if (__any(target >= 0 && target < BM / 2)) {
+#pragma unroll
+            for (int i = 0; i < Tl::kM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (target == 32 * i + Tl::row_of(r)) t.acc[i][j][r] += f.a;
+        }
+    }
+    if (v0 + BM / 2 > a.vocab) {                     // behind the vocabulary's end
 #pragma unroll
         for (int i = 0; i < Tl::kM; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float x = fmaf(t.acc[i][j][r] - f.top, c, -f.log2sum), p = __builtin_amdgcn_exp2f(x);
-                float d = -f.a * p;
-                if (entropy) d = -p * fmaf(f.b, fmaf(max_nan(x, kLow), 1.f / kLog2e, f.entropy), f.a);
-                if (here && target == 32 * i + Tl::row_of(r)) d += f.a;
-                if (over && v0 + 32 * i + Tl::row_of(r) >= a.vocab) d = 0.f;
-                t.acc[i][j][r] = d;
-            }
+            for (int r = 0; r < 16; ++r)
+                if (v0 + 32 * i + Tl::row_of(r) >= a.vocab) {
+#pragma unroll
+                    for (int j = 0; j < Tl::kN; ++j) t.acc[i][j][r] = 0.f;
+                }
     }
 #pragma unroll
     for (int p = 0; p < PLANES; ++p)
-        store_across<Tl, BM, BN>(lds, a.dz + p * a.dz_plane + tn * BN * a.dz_stride + tm * BM, a.dz_stride, rows - tn * BN, a.dz_stride - tm * BM, true,
+        store_across<Tl, BM, BN>(lds, a.dz + p * a.dz_plane + tn * BN * a.dz_stride + tm * BM, a.dz_stride, rows - tn * BN, BM, true,
                                  [&](int i, int j, int r) -> uint32_t {
                                      const uint32_t bits = to_bf16(t.acc[i][j][r]).bits;
                                      if (p + 1 < PLANES) t.acc[i][j][r] -= __uint_as_float(bits << 16);
@@ -504,28 +523,26 @@ __global__ __launch_bounds__(256) void k_info(const InfoArgs a) {
 
 // ---- the gradients' products ----------------------------------------------------------------------------------
 struct ProductArgs {
-    Operand dz, x;                                   // dz of a piece; the weights of the piece (k_dhidden), the hidden states (k_dweight)
+    Operand dz, weights, hidden;                     // dz and weights of a piece, hidden states
     const int* count;
-    int pairs;
     long long vocab, dim;                            // of the piece
-    // k_dhidden: sums in fp32, [split][row][dim]
+    long long hidden_tiles;                          // tiles of dH; those of dW follow
+    // dH: sums in fp32, [split][row][dim]
     float* sums;
     long long sums_plane;
     int splits;
     bool add;
-    // k_dweight: rows of the piece
+    // dW: rows of the piece
     void* dw;
     bool whole;
 };
 
 // dH: rows along m, dim along n, the piece's vocabulary along k in `splits` parts
-template <int BM, int BN> __global__ __launch_bounds__(kTileThreads, BM * BN > 128 * 128 ? 1 : 2) void k_dhidden(const ProductArgs a) {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    using Tl = Tile<BM, BN, false, true>;
-    const long long rows = *a.count;
+template <int BM, int BN, int WN, int PLANES> __device__ __forceinline__ void dhidden_tile(const ProductArgs& a, long long id, long long rows, char* lds) {
+    using Tl = Tile<BM, BN, false, true, WN>;
     const long long n_tiles = (a.dim + BN - 1) / BN;
     long long tm, tn;
-    if (!my_tile(blockIdx.x, (rows + BM - 1) / BM, n_tiles * a.splits, 1024 / BM, &tm, &tn)) return;
+    if (!my_tile(id, (rows + BM - 1) / BM, n_tiles * a.splits, 1024 / BM, &tm, &tn)) return;
     const int split = (int)(tn / n_tiles);
     tn -= split * n_tiles;
     const int steps = (int)((a.vocab + kStep - 1) / kStep), from = (int)((long long)steps * split / a.splits), to = (int)((long long)steps * (split + 1) / a.splits);
@@ -533,7 +550,7 @@ template <int BM, int BN> __global__ __launch_bounds__(kTileThreads, BM * BN > 1
     t.clear();
     Operand dz = a.dz;
     dz.rows = rows;
-    if (to > from) t.run(dz, a.x, tm * BM, tn * BN, from, to - from, a.pairs, lds);
+    if (to > from) t.template run<pairs_of(PLANES)>(dz, a.weights, tm * BM, tn * BN, from, to - from, lds);
     float* out = a.sums + split * a.sums_plane;
     const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -554,19 +571,18 @@ template <int BM, int BN> __global__ __launch_bounds__(kTileThreads, BM * BN > 1
 }
 
 // dW: the rows are k.  bf16: dim along m, so that a lane has neighbours of a row of dW; fp32: dim along n, a line of a row a store
-template <int BM, int BN, typename T> __global__ __launch_bounds__(kTileThreads, BM * BN > 128 * 128 ? 1 : 2) void k_dweight(const ProductArgs a) {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    using Tl = Tile<BM, BN, true, true>;
+template <int BM, int BN, int WN, typename T> __device__ __forceinline__ void dweight_tile(const ProductArgs& a, long long id, long long rows, char* lds) {
+    using Tl = Tile<BM, BN, true, true, WN>;
     constexpr bool kDimFirst = sizeof(T) == 2;
-    const long long rows = *a.count, m_size = kDimFirst ? a.dim : a.vocab, n_size = kDimFirst ? a.vocab : a.dim;
+    const long long m_size = kDimFirst ? a.dim : a.vocab, n_size = kDimFirst ? a.vocab : a.dim;
     long long tm, tn;
-    if (!my_tile(blockIdx.x, (m_size + BM - 1) / BM, (n_size + BN - 1) / BN, 1024 / BM, &tm, &tn)) return;
+    if (!my_tile(id, (m_size + BM - 1) / BM, (n_size + BN - 1) / BN, 1024 / BM, &tm, &tn)) return;
     Tl t;
     t.clear();
-    Operand dz = a.dz, x = a.x;
+    Operand dz = a.dz, x = a.hidden;
     dz.rows = x.rows = rows;
     const int steps = (int)((rows + kStep - 1) / kStep);
-    if (steps) t.run(kDimFirst ? x : dz, kDimFirst ? dz : x, tm * BM, tn * BN, 0, steps, a.pairs, lds);
+    if (steps) t.template run<kDimFirst ? 1 : kPairs>(kDimFirst ? x : dz, kDimFirst ? dz : x, tm * BM, tn * BN, 0, steps, lds);
     if constexpr (kDimFirst) {
         store_across<Tl, BM, BN>(lds, static_cast<uint16_t*>(a.dw) + tn * BN * a.dim + tm * BM, a.dim, a.vocab - tn * BN, a.dim - tm * BM, a.whole,
                                  [&](int i, int j, int r) -> uint32_t { return to_bf16(t.acc[i][j][r]).bits; });
@@ -588,6 +604,14 @@ template <int BM, int BN, typename T> __global__ __launch_bounds__(kTileThreads,
     }
 }
 
+// Both in one launch, dH's longer tiles first, so that neither waits for the other's last ones.
+template <int BM, int BN, int WN, typename T> __global__ __launch_bounds__(128 * WN, 2) void k_products(const ProductArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const long long rows = *a.count, id = blockIdx.x;
+    if (id < a.hidden_tiles) dhidden_tile<BM, BN, WN, sizeof(T) == 4 ? kPlanes : 1>(a, id, rows, lds);
+    else dweight_tile<BM, BN, WN, T>(a, id - a.hidden_tiles, rows, lds);
+}
+
 // dH's rows from their sums; zeros for rows that are left out
 template <typename T> __global__ __launch_bounds__(256) void k_hidden(const float* sums, long long plane, int splits, const int* place, long long rows, long long dim, T* out) {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -604,7 +628,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_hidden(const floa
 // ---- host ----
 struct Plan {
     bool f32, few, staged;                           // fp32; rows for k_few; weights are packed by pieces
-    int pairs, planes, k_steps;
+    int planes, k_steps;
     long long rows, dim, vocab, packed_dim;
     int tile;                                        // 128 or 256
     long long parts;                                 // of the values
@@ -626,7 +650,6 @@ asi_status check(const asi_linear_logprob_desc* d) {
 Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     Plan p{};
     p.f32 = d->dtype == ASI_F32;
-    p.pairs = p.f32 ? kPairs : 1;
     p.planes = p.f32 ? kPlanes : 1;
     p.rows = d->rows; p.dim = d->dim; p.vocab = d->vocab;
     p.packed_dim = up(d->dim, kStep);
@@ -638,7 +661,9 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     p.piece = (long long)(kPieceBytes / 2 / (size_t)rows_up) / 256 * 256;
     if (p.piece < 256) p.piece = 256;
     if (p.piece > up(d->vocab, 256)) p.piece = up(d->vocab, 256);
-    if (p.staged && p.piece > 16384) p.piece = 16384;
+    // packed weights of a piece are no more than that either, but where 4096 of them are
+    const long long most_packed = (long long)(kPieceBytes / (size_t)(p.planes * p.packed_dim * 2)) / 256 * 256;
+    if (p.staged && p.piece > most_packed) p.piece = most_packed > 4096 ? most_packed : p.piece < 4096 ? p.piece : 4096;
     p.parts = p.few ? (d->vocab + 16 * kFewWaves - 1) / (16 * kFewWaves) : (d->vocab + p.tile - 1) / p.tile;
     // enough parts of k for two workgroups a CU, none shorter than 8 steps
     const long long tiles = (rows_up / p.tile) * (up(d->dim, p.tile) / p.tile), most = p.piece / kStep / 8;
@@ -689,7 +714,7 @@ struct Call {
     }
     void pack(const void* x, long long stride, long long rows, const int* count, const int* live, uint16_t* out, long long plane) {
         const size_t es = p.f32 ? 4 : 2;
-        const PackArgs a{x, stride, rows, count, live, (int)p.dim, (int)(p.packed_dim / 8), out, plane, aligned(x, 16) && stride * es % 16 == 0};
+        const PackArgs a{x, stride, rows, count, live, (int)p.dim, (int)(p.packed_dim / 8), out, p.packed_dim, plane, aligned(x, 16) && stride * es % 16 == 0};
         const dim3 grid((unsigned)((rows * a.pieces + 255) / 256));
         if (p.f32) hipLaunchKernelGGL(k_pack<float>, grid, 256, 0, st, a);
         else hipLaunchKernelGGL(k_pack<bf16_t>, grid, 256, 0, st, a);
@@ -702,14 +727,14 @@ struct Call {
         pack(from, d->weight_stride, n, nullptr, nullptr, out, p.piece * p.packed_dim);
         return Operand{out, p.packed_dim, p.piece * p.packed_dim, n, p.packed_dim};
     }
-    template <typename K, typename A> void tiles(K kernel, size_t lds, LdsAllowed& allowed, long long count, const A& a) {
+    template <typename K, typename A> void tiles(K kernel, size_t lds, LdsAllowed& allowed, long long count, const A& a, int threads = kTileThreads) {
         if (status != ASI_OK) return;
         if (allow_lds(reinterpret_cast<const void*>(kernel), lds, allowed) != hipSuccess) { status = ASI_ERR_HIP; return; }
-        hipLaunchKernelGGL(kernel, dim3((unsigned)count), kTileThreads, lds, st, a);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)count), threads, lds, st, a);
     }
     LogitArgs logit_args(const Operand& w, long long first, long long n) const {
         LogitArgs a{};
-        a.w = w; a.h = packed_hidden(); a.count = at<int>(p.count); a.pairs = p.pairs; a.k_steps = p.k_steps;
+        a.w = w; a.h = packed_hidden(); a.count = at<int>(p.count); a.k_steps = p.k_steps;
         a.vocab = n; a.first = first; a.scale = d->scale;
         return a;
     }
@@ -730,8 +755,9 @@ struct Call {
                 LogitArgs a = logit_args(weights(first, n), first, n);
                 a.live = at<int>(p.live); a.targets = targets; a.part = at<float>(p.part); a.target_logit = at<float>(p.target);
                 a.part_rows = p.rows; a.first_part = first / p.tile;
-                static LdsAllowed allowed;
-                tiles(k_logits<128, 128>, LogitTile<128, 128>::kLds, allowed, up(n, 128) / 128 * (up(p.rows, 128) / 128), a);
+                static LdsAllowed one, three;
+                if (p.f32) tiles(k_logits<128, 128, kPlanes>, LogitTile<128, 128>::kLds, three, up(n, 128) / 128 * (up(p.rows, 128) / 128), a);
+                else tiles(k_logits<128, 128, 1>, LogitTile<128, 128>::kLds, one, up(n, 128) / 128 * (up(p.rows, 128) / 128), a);
             }
             j.count = at<int>(p.count);
             j.live = at<int>(p.live);
@@ -751,25 +777,22 @@ struct Call {
             a.info = at<RowInfo>(p.info); a.dz = at<uint16_t>(p.dz); a.dz_stride = p.piece; a.dz_plane = p.rows * p.piece;
             constexpr size_t lds = LogitTile<128, 128>::kLds > 128 * (256 + 16) ? LogitTile<128, 128>::kLds : 128 * (256 + 16);
             const long long row_tiles = up(p.rows, 128) / 128, vocab_tiles = up(n, 128) / 128, dim_tiles = up(p.dim, 128) / 128;
-            static LdsAllowed one, three, hid, w16, w32;
+            static LdsAllowed one, three, w16, w32;
             if (p.f32) tiles(k_logits_grad<128, 128, kPlanes>, lds, three, vocab_tiles * row_tiles, a);
             else tiles(k_logits_grad<128, 128, 1>, lds, one, vocab_tiles * row_tiles, a);
             ProductArgs b{};
             b.dz = Operand{a.dz, p.piece, a.dz_plane, p.rows, p.piece};
-            b.count = a.count; b.pairs = p.pairs; b.vocab = n; b.dim = p.dim;
-            if (dhidden) {
-                b.x = w;
-                b.sums = at<float>(p.sums); b.sums_plane = p.rows * p.dim; b.splits = p.splits; b.add = first > 0;
-                tiles(k_dhidden<128, 128>, Tile<128, 128, false, true>::kLds, hid, row_tiles * dim_tiles * p.splits, b);
-            }
-            if (dweight) {
-                b.x = packed_hidden();
-                b.dw = static_cast<char*>(dweight) + first * p.dim * es;
-                b.whole = p.dim % 8 == 0 && aligned(dweight, 16);
-                constexpr size_t lds_w = Tile<128, 128, true, true>::kLds > 128 * (256 + 16) ? Tile<128, 128, true, true>::kLds : 128 * (256 + 16);
-                if (p.f32) tiles(k_dweight<128, 128, float>, lds_w, w32, vocab_tiles * dim_tiles, b);
-                else tiles(k_dweight<128, 128, bf16_t>, lds_w, w16, vocab_tiles * dim_tiles, b);
-            }
+            b.count = a.count; b.vocab = n; b.dim = p.dim;
+            b.weights = w;
+            b.hidden = packed_hidden();
+            b.sums = at<float>(p.sums); b.sums_plane = p.rows * p.dim; b.splits = p.splits; b.add = first > 0;
+            b.dw = static_cast<char*>(dweight) + first * p.dim * es;
+            b.whole = p.dim % 8 == 0 && aligned(dweight, 16);
+            b.hidden_tiles = dhidden ? up(row_tiles * dim_tiles * p.splits, 8) : 0;
+            constexpr size_t lds_p = Tile<128, 128, true, true>::kLds > 128 * (256 + 16) ? Tile<128, 128, true, true>::kLds : 128 * (256 + 16);
+            const long long all = b.hidden_tiles + (dweight ? vocab_tiles * dim_tiles : 0);
+            if (all && p.f32) tiles(k_products<128, 128, 2, float>, lds_p, w32, all, b);
+            else if (all) tiles(k_products<128, 128, 2, bf16_t>, lds_p, w16, all, b);
         }
         if (dhidden) {
             const dim3 grid((unsigned)((p.rows * p.dim + 255) / 256));
