@@ -24,9 +24,16 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLow = -1e30f;                       // stands for -infinity where that is multiplied by 0
-constexpr int kTileThreads = 256;                    // of k_logits and k_logits_grad
 constexpr int kFew = 16;                             // rows of k_few
 constexpr size_t kPieceBytes = size_t(96) << 20;     // dz of a piece, in bf16
+
+// Tiles of 256 x 256 by 8 waves where they fill the chip (8190 x 2048 logits of 100003: 2.76 ms, with tiles of 128 3.26), of 128 x 128 by
+// 4 waves, two workgroups a CU, where they would not.
+template <int B> struct Shape {
+    static constexpr int WN = B == 256 ? 4 : 2, kThreads = 128 * WN, kSlots = B == 256 ? 256 : 512;
+    template <bool A, bool X> using Of = Tile<B, B, A, X, WN>;
+    static constexpr size_t kLds = 4 * B * kStep * 2 > B * (2 * B + 16) ? 4 * B * kStep * 2 : B * (2 * B + 16);      // two buffers, or a tile in bf16
+};
 
 // What the gradient needs of a row: p = exp2(scale' (x - top) - log2sum); dz = [target] a - p (a + b (log p + entropy))
 struct RowInfo {
@@ -35,11 +42,58 @@ struct RowInfo {
 };
 
 // ---- rows ---------------------------------------------------------------------------------------------------
+// What follows from the number of live rows, which the GPU alone knows.
+struct Split {
+    int rows, piece, splits, pad;                    // live rows; tokens of a piece; parts that the vocabulary of a piece is cut in for dH
+};
+struct SplitArgs {
+    long long vocab, dim, elements, piece, most_sums, most_splits;      // elements of dz and rows of sums that there is memory for
+    int tile, pairs;
+    bool grad, flexible, dhidden, dweight;           // flexible: pieces may be larger than `piece` where rows are fewer
+};
+// The number of parts that ends a launch of dH's tiles, then dW's, soonest, `slots` workgroups at a time: lengths in steps of 64 k, to which
+// writing a tile adds about 6.  A lane of the wave for each number of parts.  (2731 x 2048 x 32000: 1434 us with two parts, 1508 with one.)
+__device__ int best_splits(const SplitArgs& a, long long rows, long long piece) {
+    const int s = (int)(threadIdx.x & 63) + 1;
+    const float slots = a.tile == 256 ? 256.f : 512.f, row_tiles = (float)((rows + a.tile - 1) / a.tile), dim_tiles = (float)((a.dim + a.tile - 1) / a.tile);
+    const long long v = a.vocab < piece ? a.vocab : piece;
+    const float steps = (float)((v + kStep - 1) / kStep), w_units = a.dweight ? (float)((v + a.tile - 1) / a.tile) * dim_tiles : 0.f;
+    const float w = (float)((rows + kStep - 1) / kStep) * a.pairs + 6.f, h = ceilf(steps / s) * a.pairs + 6.f;
+    const float units = row_tiles * dim_tiles * s, whole = floorf(units / slots), late = units - whole * slots, start = whole * h;
+    float end = fmaxf(start + (late > 0.f ? h : 0.f), (units * h + w_units * w) / slots);
+    for (int i = 0; i < 64; ++i) {                   // until the slots that are free after `whole` tiles of dH and after one more can take dW's
+        const float room = (slots - late) * floorf((end - start) / w) + late * floorf(fmaxf(end - start - h, 0.f) / w);
+        if (room >= w_units) break;
+        end += 0.125f * w;
+    }
+    const bool may = s <= a.most_splits && s * rows <= a.most_sums && (s == 1 || steps >= 8.f * s);
+    // positive numbers order as their bits do; the lane in the last bits, so that of equal ends the fewest parts are taken
+    uint32_t key = may ? (__float_as_uint(end) & ~63u) | (uint32_t)(s - 1) : 0xffffffffu;
+    return (int)((~wave_max(~key)) & 63u) + 1;
+}
+// By a whole wave.
+__device__ void split_rows(const SplitArgs& a, long long rows, Split* to) {
+    Split p{(int)rows, (int)a.piece, 1, 0};
+    if (a.grad && rows > 0) {
+        if (a.flexible) {
+            const long long up = (rows + a.tile - 1) / a.tile * a.tile, all = (a.vocab + 255) / 256 * 256;
+            long long size = a.elements / up / 256 * 256;
+            if (size > 2 * a.piece) size = 2 * a.piece;
+            if (size > all) size = all;
+            const long long pieces = (a.vocab + size - 1) / size;
+            p.piece = (int)((a.vocab + pieces * 256 - 1) / (pieces * 256) * 256);
+        }
+        p.splits = best_splits(a, rows, p.piece);
+    }
+    if ((threadIdx.x & 63) == 0) *to = p;
+}
 struct LiveArgs {
     const int64_t* targets;
     long long rows, ignore;
-    int *count, *live, *place;                       // place[row]: its place among the live ones, -1 if it is left out
+    Split* split;
+    int *live, *place;                               // place[row]: its place among the live ones, -1 if it is left out
     float *logprob, *entropy, *stats;                // 0 for a row that is left out; nullable
+    SplitArgs how;
 };
 __global__ __launch_bounds__(1024) void k_live(const LiveArgs a) {
     __shared__ int waves[16];
@@ -70,12 +124,12 @@ __global__ __launch_bounds__(1024) void k_live(const LiveArgs a) {
             if (a.stats) a.stats[2 * r] = a.stats[2 * r + 1] = 0.f;
         }
     }
-    if (threadIdx.x == 0) *a.count = all;
+    if (threadIdx.x < 64) split_rows(a.how, all, a.split);
 }
-__global__ __launch_bounds__(256) void k_all_live(long long rows, int* count, int* live, int* place) {
+__global__ __launch_bounds__(256) void k_all_live(const LiveArgs a) {
     const long long r = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (r < rows) live[r] = place[r] = (int)r;
-    if (r == 0) *count = (int)rows;
+    if (r < a.rows) a.live[r] = a.place[r] = (int)r;
+    if (r < 64) split_rows(a.how, a.rows, a.split);
 }
 
 // ---- operands -----------------------------------------------------------------------------------------------
@@ -92,7 +146,8 @@ template <typename T> __device__ __forceinline__ void planes_of(float x, uint16_
 struct PackArgs {
     const void* x;
     long long stride, rows;                          // rows are at least those that are packed
-    const int *count, *live;                         // nullable: all rows
+    const Split* split;                              // nullable, with live: all rows
+    const int* live;
     int dim, pieces;                                 // pieces of 8 of a packed row
     uint16_t* out;
     long long ld, plane;
@@ -101,7 +156,7 @@ struct PackArgs {
 template <typename T> __global__ __launch_bounds__(256) void k_pack(const PackArgs a) {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / a.pieces;
     const int col = (int)(at - row * a.pieces) * 8;
-    if (row >= (a.count ? *a.count : a.rows)) return;
+    if (row >= (a.split ? a.split->rows : a.rows)) return;
     const T* x = static_cast<const T*>(a.x) + (a.live ? a.live[row] : row) * a.stride + col;
     float f[8];
     if (a.whole && col + 8 <= a.dim) {
@@ -137,10 +192,12 @@ __device__ __forceinline__ bool my_tile(long long id, long long m_tiles, long lo
 }
 
 struct LogitArgs {
-    Operand w, h;                                    // the piece's weights; the live rows' hidden states
-    const int* count;
+    Operand w, h;                                    // weights, of the whole vocabulary or of a packed piece; the live rows' hidden states
+    const Split* split;
     int k_steps;
-    long long vocab, first;                          // of the piece; its first token
+    long long vocab, first;                          // tokens of the piece; its first one
+    long long all;                                   // tokens of the vocabulary where the GPU decides on the pieces; 0: it does not
+    int number;                                      // the piece's
     float scale;
     // values: [tile][top, sum, along][rows], the targets' logits [rows]
     const int *live;
@@ -154,7 +211,16 @@ struct LogitArgs {
 };
 
 constexpr int pairs_of(int planes) { return planes == 1 ? 1 : kPairs; }
-template <int BM, int BN> using LogitTile = Tile<BM, BN, false, false>;
+// The piece that is asked for, as decided on the GPU; `w`: the weights, moved on to it.  False: there is no such piece.
+__device__ __forceinline__ bool my_piece(const Split& s, long long all, int number, long long* first, long long* n, Operand* w) {
+    if (!all) return true;
+    *first = (long long)number * s.piece;
+    *n = all - *first < s.piece ? all - *first : s.piece;
+    if (*n <= 0) return false;
+    w->p += *first * w->ld;
+    w->rows = *n;
+    return true;
+}
 
 struct Joined {
     float top, sum, along;
@@ -168,10 +234,11 @@ __device__ __forceinline__ Joined join(Joined a, Joined b, float c) {
     return Joined{top, a.sum * ea + b.sum * eb, ea * fmaf(a.sum, da, a.along) + eb * fmaf(b.sum, db, b.along)};
 }
 
-template <int BM, int BN, int PLANES> __global__ __launch_bounds__(kTileThreads, BM * BN > 128 * 128 ? 1 : 2) void k_logits(const LogitArgs a) {
+template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2) void k_logits(const LogitArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    using Tl = LogitTile<BM, BN>;
-    const long long rows = *a.count;
+    constexpr int BM = B, BN = B;
+    using Tl = typename Shape<B>::template Of<false, false>;
+    const long long rows = a.split->rows;
     long long tm, tn;
     if (!my_tile(blockIdx.x, (a.vocab + BM - 1) / BM, (rows + BN - 1) / BN, 1024 / BM, &tm, &tn)) return;
     Tl t;
@@ -272,10 +339,15 @@ template <typename Tl, int BM, int BN, typename F> __device__ __forceinline__ vo
     }
 }
 
-template <int BM, int BN, int PLANES> __global__ __launch_bounds__(kTileThreads, BM * BN > 128 * 128 ? 1 : 2) void k_logits_grad(const LogitArgs a) {
+template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2) void k_logits_grad(const LogitArgs given) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    using Tl = LogitTile<BM, BN>;
-    const long long rows = *a.count;
+    constexpr int BM = B, BN = B;
+    using Tl = typename Shape<B>::template Of<false, false>;
+    LogitArgs a = given;
+    const Split split = *a.split;
+    const long long rows = split.rows;
+    if (!my_piece(split, a.all, a.number, &a.first, &a.vocab, &a.w)) return;
+    a.dz_stride = split.piece;
     long long tm, tn;
     if (!my_tile(blockIdx.x, (a.vocab + BM - 1) / BM, (rows + BN - 1) / BN, 1024 / BM, &tm, &tn)) return;
     Tl t;
@@ -441,7 +513,8 @@ template <typename T> __global__ __launch_bounds__(64 * kFewWaves) void k_few(co
 struct JoinArgs {
     const float *part, *target_logit;
     long long part_rows, parts, vocab, ignore;
-    const int *count, *live;                         // live nullable: all `rows` rows as they are
+    const Split* split;                              // nullable, with live: all `rows` rows as they are
+    const int* live;
     long long rows;
     const int64_t* targets;
     float scale;
@@ -461,7 +534,7 @@ template <int ROWS> __global__ __launch_bounds__(256) void k_join(const JoinArgs
     constexpr int kShares = 256 / ROWS;
     __shared__ Joined shared[kShares][ROWS];
     const int in = threadIdx.x % ROWS, share = threadIdx.x / ROWS;
-    const long long rows = a.count ? *a.count : a.rows, at = (long long)blockIdx.x * ROWS + in;
+    const long long rows = a.split ? a.split->rows : a.rows, at = (long long)blockIdx.x * ROWS + in;
     if ((long long)blockIdx.x * ROWS >= rows) return;
     const float c = a.scale * kLog2e;
     float top = -INFINITY;
@@ -506,7 +579,8 @@ template <int ROWS> __global__ __launch_bounds__(256) void k_join(const JoinArgs
 }
 
 struct InfoArgs {
-    const int *count, *live;
+    const Split* split;
+    const int* live;
     const int64_t* targets;
     const float *stats, *entropy, *a, *b;
     float scale;
@@ -515,7 +589,7 @@ struct InfoArgs {
 };
 __global__ __launch_bounds__(256) void k_info(const InfoArgs a) {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (at >= *a.count) return;
+    if (at >= a.split->rows) return;
     const long long row = a.live[at];
     write_info(a.info + at, a.stats[2 * row], a.stats[2 * row + 1], a.b ? a.entropy[row] : 0.f, a.a ? a.a[row] : 0.f, a.b ? a.b[row] : 0.f, a.scale,
                a.targets ? a.targets[row] : 0, a.vocab, a.targets != nullptr);
@@ -523,35 +597,34 @@ __global__ __launch_bounds__(256) void k_info(const InfoArgs a) {
 
 // ---- the gradients' products ----------------------------------------------------------------------------------
 struct ProductArgs {
-    Operand dz, weights, hidden;                     // dz and weights of a piece, hidden states
-    const int* count;
-    long long vocab, dim;                            // of the piece
-    long long hidden_tiles;                          // tiles of dH; those of dW follow
-    // dH: sums in fp32, [split][row][dim]
+    Operand dz, weights, hidden;                     // dz of the piece, weights as k_logits has them, hidden states
+    const Split* split;
+    long long vocab, first, all, dim;                // as k_logits has them
+    int number;
+    bool dhidden, dweight;
+    // dH: sums in fp32, [part][live row][dim]
     float* sums;
-    long long sums_plane;
-    int splits;
     bool add;
-    // dW: rows of the piece
-    void* dw;
+    void* dw;                                        // all rows of dW
     bool whole;
 };
 
 // dH: rows along m, dim along n, the piece's vocabulary along k in `splits` parts
-template <int BM, int BN, int WN, int PLANES> __device__ __forceinline__ void dhidden_tile(const ProductArgs& a, long long id, long long rows, char* lds) {
-    using Tl = Tile<BM, BN, false, true, WN>;
+template <int B, int PLANES> __device__ __forceinline__ void dhidden_tile(const ProductArgs& a, long long id, long long rows, int splits, char* lds) {
+    constexpr int BM = B, BN = B;
+    using Tl = typename Shape<B>::template Of<false, true>;
     const long long n_tiles = (a.dim + BN - 1) / BN;
     long long tm, tn;
-    if (!my_tile(id, (rows + BM - 1) / BM, n_tiles * a.splits, 1024 / BM, &tm, &tn)) return;
+    if (!my_tile(id, (rows + BM - 1) / BM, n_tiles * splits, 1024 / BM, &tm, &tn)) return;
     const int split = (int)(tn / n_tiles);
     tn -= split * n_tiles;
-    const int steps = (int)((a.vocab + kStep - 1) / kStep), from = (int)((long long)steps * split / a.splits), to = (int)((long long)steps * (split + 1) / a.splits);
+    const int steps = (int)((a.vocab + kStep - 1) / kStep), from = (int)((long long)steps * split / splits), to = (int)((long long)steps * (split + 1) / splits);
     Tl t;
     t.clear();
     Operand dz = a.dz;
     dz.rows = rows;
     if (to > from) t.template run<pairs_of(PLANES)>(dz, a.weights, tm * BM, tn * BN, from, to - from, lds);
-    float* out = a.sums + split * a.sums_plane;
+    float* out = a.sums + split * rows * a.dim;
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int i = 0; i < Tl::kM; ++i)
@@ -571,8 +644,9 @@ template <int BM, int BN, int WN, int PLANES> __device__ __forceinline__ void dh
 }
 
 // dW: the rows are k.  bf16: dim along m, so that a lane has neighbours of a row of dW; fp32: dim along n, a line of a row a store
-template <int BM, int BN, int WN, typename T> __device__ __forceinline__ void dweight_tile(const ProductArgs& a, long long id, long long rows, char* lds) {
-    using Tl = Tile<BM, BN, true, true, WN>;
+template <int B, typename T> __device__ __forceinline__ void dweight_tile(const ProductArgs& a, long long id, long long rows, char* lds) {
+    constexpr int BM = B, BN = B;
+    using Tl = typename Shape<B>::template Of<true, true>;
     constexpr bool kDimFirst = sizeof(T) == 2;
     const long long m_size = kDimFirst ? a.dim : a.vocab, n_size = kDimFirst ? a.vocab : a.dim;
     long long tm, tn;
@@ -584,10 +658,10 @@ template <int BM, int BN, int WN, typename T> __device__ __forceinline__ void dw
     const int steps = (int)((rows + kStep - 1) / kStep);
     if (steps) t.template run<kDimFirst ? 1 : kPairs>(kDimFirst ? x : dz, kDimFirst ? dz : x, tm * BM, tn * BN, 0, steps, lds);
     if constexpr (kDimFirst) {
-        store_across<Tl, BM, BN>(lds, static_cast<uint16_t*>(a.dw) + tn * BN * a.dim + tm * BM, a.dim, a.vocab - tn * BN, a.dim - tm * BM, a.whole,
+        store_across<Tl, BM, BN>(lds, static_cast<uint16_t*>(a.dw) + (a.first + tn * BN) * a.dim + tm * BM, a.dim, a.vocab - tn * BN, a.dim - tm * BM, a.whole,
                                  [&](int i, int j, int r) -> uint32_t { return to_bf16(t.acc[i][j][r]).bits; });
     } else {
-        float* out = static_cast<float*>(a.dw);
+        float* out = static_cast<float*>(a.dw) + a.first * a.dim;
         const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int i = 0; i < Tl::kM; ++i)
@@ -605,22 +679,27 @@ template <int BM, int BN, int WN, typename T> __device__ __forceinline__ void dw
 }
 
 // Both in one launch, dH's longer tiles first, so that neither waits for the other's last ones.
-template <int BM, int BN, int WN, typename T> __global__ __launch_bounds__(128 * WN, 2) void k_products(const ProductArgs a) {
+template <int B, typename T> __global__ __launch_bounds__(Shape<B>::kThreads, 2) void k_products(const ProductArgs given) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const long long rows = *a.count, id = blockIdx.x;
-    if (id < a.hidden_tiles) dhidden_tile<BM, BN, WN, sizeof(T) == 4 ? kPlanes : 1>(a, id, rows, lds);
-    else dweight_tile<BM, BN, WN, T>(a, id - a.hidden_tiles, rows, lds);
+    ProductArgs a = given;
+    const Split split = *a.split;
+    const long long rows = split.rows, id = blockIdx.x;
+    if (!my_piece(split, a.all, a.number, &a.first, &a.vocab, &a.weights)) return;
+    a.dz.ld = a.dz.cols = split.piece;
+    const long long tiles = (rows + B - 1) / B * ((a.dim + B - 1) / B) * split.splits, first = a.dhidden ? (tiles + 7) / 8 * 8 : 0;
+    if (id < first) dhidden_tile<B, sizeof(T) == 4 ? kPlanes : 1>(a, id, rows, split.splits, lds);
+    else if (a.dweight) dweight_tile<B, T>(a, id - first, rows, lds);
 }
 
 // dH's rows from their sums; zeros for rows that are left out
-template <typename T> __global__ __launch_bounds__(256) void k_hidden(const float* sums, long long plane, int splits, const int* place, long long rows, long long dim, T* out) {
+template <typename T> __global__ __launch_bounds__(256) void k_hidden(const float* sums, const Split* split, const int* place, long long rows, long long dim, T* out) {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
     if (at >= rows * dim) return;
     const long long row = at / dim, from = place[row];
     float t = 0.f;
     if (from >= 0) {
         const float* p = sums + from * dim + (at - row * dim);
-        for (int s = 0; s < splits; ++s) t += p[s * plane];
+        for (int s = 0; s < split->splits; ++s) t += p[s * (split->rows * dim)];
     }
     out[at] = from_f32<T>(t);
 }
@@ -631,10 +710,11 @@ struct Plan {
     int planes, k_steps;
     long long rows, dim, vocab, packed_dim;
     int tile;                                        // 128 or 256
+    bool flexible;
     long long parts;                                 // of the values
     long long piece;                                 // tokens of a piece of the gradient, and of packed weights
-    int splits;
-    size_t count, live, place, hidden, weights, part, target, info, dz, sums, bytes;      // offsets
+    long long most_sums, most_splits;
+    size_t split, live, place, hidden, weights, part, target, info, dz, sums, bytes;      // offsets
 };
 long long up(long long x, long long to) { return (x + to - 1) / to * to; }
 
@@ -644,6 +724,7 @@ asi_status check(const asi_linear_logprob_desc* d) {
     if (!dtype_ok(d->dtype) || d->scale < 1e-20f || d->scale > 1e20f) return ASI_ERR_UNSUPPORTED;
     if (d->rows >= (1 << 24) || d->dim >= (1 << 18) || d->vocab >= (1 << 28)) return ASI_ERR_UNSUPPORTED;
     if (up(d->rows, 128) / 128 * (up(d->vocab, 128) / 128) > (1 << 23)) return ASI_ERR_UNSUPPORTED;      // tiles of a launch
+    if (up(d->dim, 128) / 128 * (up(d->vocab, 128) / 128) > (1 << 23)) return ASI_ERR_UNSUPPORTED;
     if (d->rows * up(d->dim, kStep) / 8 > most_workgroups(256) * 256) return ASI_ERR_UNSUPPORTED;          // threads of k_pack
     return ASI_OK;
 }
@@ -656,7 +737,7 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     p.k_steps = (int)(p.packed_dim / kStep);
     p.few = !grad && d->rows <= kFew;
     p.staged = !p.few && (p.f32 || d->dim % kStep || d->weight_stride % 8 || d->weight_stride >= (1 << 21) || d->any_address);
-    p.tile = 128;
+    p.tile = up(d->rows, 256) / 256 * (up(d->vocab, 256) / 256) >= 256 ? 256 : 128;
     const long long rows_up = up(d->rows, p.tile);
     p.piece = (long long)(kPieceBytes / 2 / (size_t)rows_up) / 256 * 256;
     if (p.piece < 256) p.piece = 256;
@@ -664,18 +745,22 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     // packed weights of a piece are no more than that either, but where 4096 of them are
     const long long most_packed = (long long)(kPieceBytes / (size_t)(p.planes * p.packed_dim * 2)) / 256 * 256;
     if (p.staged && p.piece > most_packed) p.piece = most_packed > 4096 ? most_packed : p.piece < 4096 ? p.piece : 4096;
+    p.flexible = !p.staged;
     p.parts = p.few ? (d->vocab + 16 * kFewWaves - 1) / (16 * kFewWaves) : (d->vocab + p.tile - 1) / p.tile;
-    // enough parts of k for two workgroups a CU, none shorter than 8 steps
-    const long long tiles = (rows_up / p.tile) * (up(d->dim, p.tile) / p.tile), most = p.piece / kStep / 8;
-    long long splits = 512 / tiles;
-    if (splits > most) splits = most;
-    if (splits < 1) splits = 1;
-    p.splits = (int)splits;
+    // parts that the vocabulary of a piece may be cut in for dH, and the memory for their sums: twice what fills the chip, but no more than
+    // half a piece's or twice dH's size in fp32
+    const long long tiles = (rows_up / p.tile) * (up(d->dim, p.tile) / p.tile), slots = p.tile == 256 ? 256 : 512;
+    const long long memory = (long long)(kPieceBytes / 2 / 4) / (d->rows * d->dim > 0 ? d->rows * d->dim : 1);
+    p.most_splits = (2 * slots + tiles - 1) / (tiles > 0 ? tiles : 1);
+    if (p.most_splits > (memory > 2 ? memory : 2)) p.most_splits = memory > 2 ? memory : 2;
+    if (p.most_splits > 32) p.most_splits = 32;
+    if (p.most_splits < 2) p.most_splits = 2;
+    p.most_sums = d->rows * p.most_splits;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += round256(bytes); return here; };
     const size_t rows = (size_t)d->rows;
     if (!p.few) {
-        p.count = take(4);
+        p.split = take(sizeof(Split));
         p.live = take(rows * 4);
         p.place = take(rows * 4);
         p.hidden = take((size_t)p.planes * rows * p.packed_dim * 2);
@@ -685,8 +770,8 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     p.target = take(rows * 4);
     if (grad) {
         p.info = take(rows * sizeof(RowInfo));
-        p.dz = take((size_t)p.planes * rows * p.piece * 2);
-        p.sums = take((size_t)p.splits * rows * d->dim * 4);
+        p.dz = take((size_t)p.planes * (size_t)rows_up * p.piece * 2);
+        p.sums = take((size_t)p.most_sums * d->dim * 4);
     }
     p.bytes = at;
     return p;
@@ -704,17 +789,16 @@ struct Call {
     template <typename T> T* at(size_t offset) const { return reinterpret_cast<T*>(ws + offset); }
     Operand packed_hidden() const { return Operand{at<uint16_t>(p.hidden), p.packed_dim, p.rows * p.packed_dim, p.rows, p.packed_dim}; }
 
-    void rows_of(float* logprob, float* entropy, float* stats) {
-        if (targets) {
-            hipLaunchKernelGGL(k_live, 1, 1024, 0, st, LiveArgs{targets, p.rows, d->ignore_index, at<int>(p.count), at<int>(p.live), at<int>(p.place), logprob, entropy, stats});
-        } else {
-            hipLaunchKernelGGL(k_all_live, dim3((unsigned)((p.rows + 255) / 256)), 256, 0, st, p.rows, at<int>(p.count), at<int>(p.live), at<int>(p.place));
-        }
-        pack(hidden, d->hidden_stride, p.rows, at<int>(p.count), at<int>(p.live), at<uint16_t>(p.hidden), p.rows * p.packed_dim);
+    void rows_of(float* logprob, float* entropy, float* stats, bool grad, bool dhidden, bool dweight) {
+        const SplitArgs how{p.vocab, p.dim, up(p.rows, p.tile) * p.piece, p.piece, p.most_sums, p.most_splits, p.tile, p.f32 ? kPairs : 1, grad, p.flexible, dhidden, dweight};
+        const LiveArgs a{targets, p.rows, d->ignore_index, at<Split>(p.split), at<int>(p.live), at<int>(p.place), logprob, entropy, stats, how};
+        if (targets) hipLaunchKernelGGL(k_live, 1, 1024, 0, st, a);
+        else hipLaunchKernelGGL(k_all_live, dim3((unsigned)((p.rows + 255) / 256)), 256, 0, st, a);
+        pack(hidden, d->hidden_stride, p.rows, a.split, a.live, at<uint16_t>(p.hidden), p.rows * p.packed_dim);
     }
-    void pack(const void* x, long long stride, long long rows, const int* count, const int* live, uint16_t* out, long long plane) {
+    void pack(const void* x, long long stride, long long rows, const Split* split, const int* live, uint16_t* out, long long plane) {
         const size_t es = p.f32 ? 4 : 2;
-        const PackArgs a{x, stride, rows, count, live, (int)p.dim, (int)(p.packed_dim / 8), out, p.packed_dim, plane, aligned(x, 16) && stride * es % 16 == 0};
+        const PackArgs a{x, stride, rows, split, live, (int)p.dim, (int)(p.packed_dim / 8), out, p.packed_dim, plane, aligned(x, 16) && stride * es % 16 == 0};
         const dim3 grid((unsigned)((rows * a.pieces + 255) / 256));
         if (p.f32) hipLaunchKernelGGL(k_pack<float>, grid, 256, 0, st, a);
         else hipLaunchKernelGGL(k_pack<bf16_t>, grid, 256, 0, st, a);
@@ -727,16 +811,35 @@ struct Call {
         pack(from, d->weight_stride, n, nullptr, nullptr, out, p.piece * p.packed_dim);
         return Operand{out, p.packed_dim, p.piece * p.packed_dim, n, p.packed_dim};
     }
-    template <typename K, typename A> void tiles(K kernel, size_t lds, LdsAllowed& allowed, long long count, const A& a, int threads = kTileThreads) {
+    template <int B, typename K, typename A> void tiles(K kernel, LdsAllowed& allowed, long long count, const A& a) {
         if (status != ASI_OK) return;
-        if (allow_lds(reinterpret_cast<const void*>(kernel), lds, allowed) != hipSuccess) { status = ASI_ERR_HIP; return; }
-        hipLaunchKernelGGL(kernel, dim3((unsigned)count), threads, lds, st, a);
+        if (allow_lds(reinterpret_cast<const void*>(kernel), Shape<B>::kLds, allowed) != hipSuccess) { status = ASI_ERR_HIP; return; }
+        hipLaunchKernelGGL(kernel, dim3((unsigned)count), Shape<B>::kThreads, Shape<B>::kLds, st, a);
     }
     LogitArgs logit_args(const Operand& w, long long first, long long n) const {
         LogitArgs a{};
-        a.w = w; a.h = packed_hidden(); a.count = at<int>(p.count); a.k_steps = p.k_steps;
+        a.w = w; a.h = packed_hidden(); a.split = at<Split>(p.split); a.k_steps = p.k_steps;
         a.vocab = n; a.first = first; a.scale = d->scale;
         return a;
+    }
+    template <int B> void logits(const LogitArgs& a) {
+        static LdsAllowed one, three;
+        const long long count = up(a.vocab, B) / B * (up(p.rows, B) / B);
+        if (p.f32) tiles<B>(k_logits<B, kPlanes>, three, count, a);
+        else tiles<B>(k_logits<B, 1>, one, count, a);
+    }
+    template <int B> void products(const LogitArgs& a, const ProductArgs& b) {
+        static LdsAllowed grad1, grad3, products2, products4;
+        const long long row_tiles = up(p.rows, B) / B, dim_tiles = up(p.dim, B) / B;
+        // no more tiles of logits in a piece than its memory holds, however it is cut
+        const long long logit_tiles = up(p.piece, B) / B * row_tiles;
+        if (p.f32) tiles<B>(k_logits_grad<B, kPlanes>, grad3, logit_tiles, a);
+        else tiles<B>(k_logits_grad<B, 1>, grad1, logit_tiles, a);
+        const long long hidden_tiles = b.dhidden ? up((up(p.most_sums, B) / B + p.most_splits) * dim_tiles, 8) : 0;
+        const long long tokens = !b.all ? b.vocab : b.all < 2 * p.piece ? b.all : 2 * p.piece;
+        const long long weight_tiles = b.dweight ? up(tokens, B) / B * dim_tiles : 0;
+        if (p.f32) tiles<B>(k_products<B, float>, products4, hidden_tiles + weight_tiles, b);
+        else tiles<B>(k_products<B, bf16_t>, products2, hidden_tiles + weight_tiles, b);
     }
     void values(float* logprob, float* entropy, float* stats, RowInfo* info, const float* wa, const float* wb) {
         JoinArgs j{};
@@ -755,11 +858,10 @@ struct Call {
                 LogitArgs a = logit_args(weights(first, n), first, n);
                 a.live = at<int>(p.live); a.targets = targets; a.part = at<float>(p.part); a.target_logit = at<float>(p.target);
                 a.part_rows = p.rows; a.first_part = first / p.tile;
-                static LdsAllowed one, three;
-                if (p.f32) tiles(k_logits<128, 128, kPlanes>, LogitTile<128, 128>::kLds, three, up(n, 128) / 128 * (up(p.rows, 128) / 128), a);
-                else tiles(k_logits<128, 128, 1>, LogitTile<128, 128>::kLds, one, up(n, 128) / 128 * (up(p.rows, 128) / 128), a);
+                if (p.tile == 256) logits<256>(a);
+                else logits<128>(a);
             }
-            j.count = at<int>(p.count);
+            j.split = at<Split>(p.split);
             j.live = at<int>(p.live);
         }
         j.part = at<float>(p.part); j.target_logit = at<float>(p.target); j.part_rows = p.rows; j.parts = p.parts; j.vocab = p.vocab;
@@ -769,35 +871,27 @@ struct Call {
         else hipLaunchKernelGGL(k_join<1>, dim3((unsigned)p.rows), 256, 0, st, j);
     }
     void gradients(void* dhidden, void* dweight) {
-        const size_t es = p.f32 ? 4 : 2;
-        for (long long first = 0; first < p.vocab; first += p.piece) {
+        int number = 0;
+        for (long long first = 0; first < p.vocab && (dhidden || dweight); first += p.piece, ++number) {
             const long long n = p.vocab - first < p.piece ? p.vocab - first : p.piece;
-            const Operand w = weights(first, n);
-            LogitArgs a = logit_args(w, first, n);
-            a.info = at<RowInfo>(p.info); a.dz = at<uint16_t>(p.dz); a.dz_stride = p.piece; a.dz_plane = p.rows * p.piece;
-            constexpr size_t lds = LogitTile<128, 128>::kLds > 128 * (256 + 16) ? LogitTile<128, 128>::kLds : 128 * (256 + 16);
-            const long long row_tiles = up(p.rows, 128) / 128, vocab_tiles = up(n, 128) / 128, dim_tiles = up(p.dim, 128) / 128;
-            static LdsAllowed one, three, w16, w32;
-            if (p.f32) tiles(k_logits_grad<128, 128, kPlanes>, lds, three, vocab_tiles * row_tiles, a);
-            else tiles(k_logits_grad<128, 128, 1>, lds, one, vocab_tiles * row_tiles, a);
+            LogitArgs a = p.flexible ? logit_args(weights(0, p.vocab), 0, p.vocab) : logit_args(weights(first, n), first, n);
+            a.all = p.flexible ? p.vocab : 0;
+            a.number = number;
+            a.info = at<RowInfo>(p.info); a.dz = at<uint16_t>(p.dz); a.dz_plane = p.rows * p.piece;
             ProductArgs b{};
             b.dz = Operand{a.dz, p.piece, a.dz_plane, p.rows, p.piece};
-            b.count = a.count; b.vocab = n; b.dim = p.dim;
-            b.weights = w;
-            b.hidden = packed_hidden();
-            b.sums = at<float>(p.sums); b.sums_plane = p.rows * p.dim; b.splits = p.splits; b.add = first > 0;
-            b.dw = static_cast<char*>(dweight) + first * p.dim * es;
+            b.weights = a.w; b.hidden = a.h; b.split = a.split; b.vocab = a.vocab; b.first = a.first; b.all = a.all; b.number = number; b.dim = p.dim;
+            b.dhidden = dhidden; b.dweight = dweight;
+            b.sums = at<float>(p.sums); b.add = first > 0;
+            b.dw = dweight;
             b.whole = p.dim % 8 == 0 && aligned(dweight, 16);
-            b.hidden_tiles = dhidden ? up(row_tiles * dim_tiles * p.splits, 8) : 0;
-            constexpr size_t lds_p = Tile<128, 128, true, true>::kLds > 128 * (256 + 16) ? Tile<128, 128, true, true>::kLds : 128 * (256 + 16);
-            const long long all = b.hidden_tiles + (dweight ? vocab_tiles * dim_tiles : 0);
-            if (all && p.f32) tiles(k_products<128, 128, 2, float>, lds_p, w32, all, b);
-            else if (all) tiles(k_products<128, 128, 2, bf16_t>, lds_p, w16, all, b);
+            if (p.tile == 256) products<256>(a, b);
+            else products<128>(a, b);
         }
         if (dhidden) {
             const dim3 grid((unsigned)((p.rows * p.dim + 255) / 256));
-            if (p.f32) hipLaunchKernelGGL(k_hidden<float>, grid, 256, 0, st, at<float>(p.sums), p.rows * p.dim, p.splits, at<int>(p.place), p.rows, p.dim, static_cast<float*>(dhidden));
-            else hipLaunchKernelGGL(k_hidden<bf16_t>, grid, 256, 0, st, at<float>(p.sums), p.rows * p.dim, p.splits, at<int>(p.place), p.rows, p.dim, static_cast<bf16_t*>(dhidden));
+            if (p.f32) hipLaunchKernelGGL(k_hidden<float>, grid, 256, 0, st, at<float>(p.sums), at<Split>(p.split), at<int>(p.place), p.rows, p.dim, static_cast<float*>(dhidden));
+            else hipLaunchKernelGGL(k_hidden<bf16_t>, grid, 256, 0, st, at<float>(p.sums), at<Split>(p.split), at<int>(p.place), p.rows, p.dim, static_cast<bf16_t*>(dhidden));
         }
     }
 };
@@ -829,7 +923,7 @@ asi_status asi_linear_logprobs(const asi_linear_logprob_desc* desc, const void* 
     if (!hidden || !weight || (logprob && !targets)) return ASI_ERR_INVALID_ARG;
     if (!ws || !aligned(ws, 256) || ws_bytes < asi_linear_logprobs_workspace_bytes(desc)) return ASI_ERR_WORKSPACE;
     Call c{desc, plan(desc, false), static_cast<char*>(ws), hidden, weight, targets, static_cast<hipStream_t>(stream)};
-    if (!c.p.few) c.rows_of(logprob, entropy, stats);
+    if (!c.p.few) c.rows_of(logprob, entropy, stats, false, false, false);
     c.values(logprob, entropy, stats, nullptr, nullptr, nullptr);
     return c.status != ASI_OK ? c.status : launched();
 }
@@ -862,10 +956,10 @@ asi_status asi_linear_logprobs_grad(const asi_linear_logprob_desc* desc, int giv
     if (!ws || !aligned(ws, 256) || ws_bytes < asi_linear_logprobs_grad_workspace_bytes(desc)) return ASI_ERR_WORKSPACE;
     Call c{desc, plan(desc, true), static_cast<char*>(ws), hidden, weight, targets, st};
     RowInfo* info = c.at<RowInfo>(c.p.info);
-    c.rows_of(given ? nullptr : logprob, given ? nullptr : entropy, nullptr);
+    c.rows_of(given ? nullptr : logprob, given ? nullptr : entropy, nullptr, true, dhidden, dweight);
     if (given) {
         hipLaunchKernelGGL(k_info, dim3((unsigned)((desc->rows + 255) / 256)), 256, 0, st,
-                           InfoArgs{c.at<int>(c.p.count), c.at<int>(c.p.live), targets, stats, entropy, grad_logprob, grad_entropy, desc->scale, desc->vocab, info});
+                           InfoArgs{c.at<Split>(c.p.split), c.at<int>(c.p.live), targets, stats, entropy, grad_logprob, grad_entropy, desc->scale, desc->vocab, info});
     } else {
         c.values(logprob, entropy, nullptr, info, grad_logprob, grad_entropy);
     }
