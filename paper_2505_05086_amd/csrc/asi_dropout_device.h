@@ -45,41 +45,6 @@ __device__ __forceinline__ bool kept(const Keep& k, const uint32_t w[4], int e) 
     return ((e & 1) ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu) >= k.below;
 }
 
-// Eight neighbouring values, of which the first `count` exist, at an address that is a multiple of the element's size only: the
-// hardware takes whole vectors at such addresses, and at multiples of 16 in no more time than otherwise.
-typedef uint32_t loose4 __attribute__((ext_vector_type(4), aligned(2), may_alias));
-template <typename T> __device__ __forceinline__ void load8(const T* p, int count, float* f) {
-    if (count >= 8) {
-        const loose4 a = *reinterpret_cast<const loose4*>(p);
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float((i & 1) ? a[i >> 1] & 0xffff0000u : a[i >> 1] << 16);
-        } else {
-            const loose4 b = *reinterpret_cast<const loose4*>(p + 4);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(i < 4 ? a[i] : b[i - 4]);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = i < count ? to_f32(p[i]) : 0.f;
-}
-template <typename T> __device__ __forceinline__ void store8(T* p, int count, const float* f) {
-    if (count >= 8) {
-        if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<loose4*>(p) = loose4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; i += 4)
-                *reinterpret_cast<loose4*>(p + i) = loose4{__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3])};
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < count) p[i] = from_f32<T>(f[i]);
-}
-
 // ---- host ----
 // Fills what the device reads from p, seed and offset; false if p is none that is taken.
 inline bool fill_keep(double p, int64_t seed, int64_t offset, const int64_t* on_device, Keep* k) {

@@ -7,7 +7,7 @@
 //   k_logits      a tile of logits, vocabulary along the registers of a lane and tokens along the lanes, so that a token's maximum
 //                 and sums over 128 (64) of the vocabulary stay in a lane but for one exchange.  Values: (x_max, sum e, sum e d) of
 //                 each token, d = x - x_max, e = exp(scale d), and the target's logit.  Gradient: dz, rounded to bf16
-//   k_few         the same values for up to 16 rows, the weights from memory straight into the matrix instructions
+//   k_few         the same values for few rows, the weights from memory straight into the matrix instructions; k_few_grad their gradients
 //   k_join        joins the tiles' values
 //   k_products    the products of dz with weights (dH) and hidden states (dW), read across as they lie (asi_tiles.h)
 //   k_hidden      the sums of dH, in fp32 over the pieces of the vocabulary and the parts of a piece, to their rows
@@ -24,7 +24,12 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLow = -1e30f;                       // stands for -infinity where that is multiplied by 0
-constexpr int kFew = 16;                             // rows of k_few
+// Rows that k_few and its gradients take; more are faster as a part of a tile.
+// (32000 x 2048, us: fp32 values of 128 rows 340 so and 598 in tiles, with gradients 1110 and 1496; bf16 values of 16 rows 36 and 38, of 32
+// rows 51 and 40, of 64 rows and 50001 x 1000, which tiles cannot take as it lies, 54 and 77; bf16 gradients of 8 rows 112 and 121, of 12
+// rows 218 and 123.)
+constexpr int kFewF32 = 128, kFewBf16 = 16, kFewBf16Packed = 64, kFewGradBf16 = 8, kFewGradVector = 8, kFewAtOnce = 64;
+constexpr int kLeftOut = -2;                         // a RowInfo's target: the row is left out
 constexpr size_t kPieceBytes = size_t(96) << 20;     // dz of a piece, in bf16
 
 // Tiles of 256 x 256 by 8 waves where they fill the chip (8190 x 2048 logits of 100003: 2.76 ms, with tiles of 128 3.26), of 128 x 128 by
@@ -407,17 +412,16 @@ template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2)
 }
 
 // ---- few rows -----------------------------------------------------------------------------------------------
-// Logits of up to 16 rows: a wave takes 16 of the vocabulary and all k, both operands from memory straight into the registers of the
+// Logits of up to 64 rows: a wave takes 16 of the vocabulary and all k, both operands from memory straight into the registers of the
 // matrix instruction, a token along four lanes.  What bounds it: the weights' memory.
 struct FewArgs {
     const void *h, *w;
-    long long h_stride, w_stride, vocab, rows, first_row;
+    long long h_stride, w_stride, vocab, rows;
     int dim;
-    bool whole;
     float scale;
     const int64_t* targets;
-    long long ignore;
-    float *part, *target_logit;
+    float *part, *target_logit;                      // nullable, both
+    float* logits;                                   // [16 rows][token][16], for the gradients; nullable
     long long part_rows;
 };
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -433,76 +437,89 @@ __device__ __forceinline__ v4f few_product(const Vec16<float>& w, const Vec16<fl
     for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(w.get(i), h.get(i), c, 0, 0, 0);
     return c;
 }
-template <typename T> __device__ __forceinline__ Vec16<T> few_load(const T* p, int k, int dim, bool there, bool whole) {
-    Vec16<T> v;
-    v.raw = make_uint4(0, 0, 0, 0);
-    if (there && k < dim) {
-        if (whole && k + Vec16<T>::N <= dim) {
-            v.load(p + k);
-        } else {
-            float f[Vec16<T>::N];
-#pragma unroll
-            for (int e = 0; e < Vec16<T>::N; ++e) f[e] = k + e < dim ? to_f32(p[k + e]) : 0.f;
-            v.set(f);
-        }
-    }
-    return v;
+template <typename T> __device__ __forceinline__ Vec16<T> few_load(const T* p, int count) {
+    Loose<T, Vec16<T>::N> v;
+    v.load(p, count);
+    return Vec16<T>{make_uint4(v.w[0], v.w[1], v.w[2], v.w[3])};
 }
-template <typename T> __global__ __launch_bounds__(64 * kFewWaves) void k_few(const FewArgs a) {
-    __shared__ Joined shared[kFewWaves][16];
+// NB: 16s of rows
+template <typename T, int NB> __global__ __launch_bounds__(64 * kFewWaves) void k_few(const FewArgs a) {
+    __shared__ Joined shared[kFewWaves][16 * NB];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15;
-    const long long v0 = ((long long)blockIdx.x * kFewWaves + wave) * 16, row = a.first_row + col;
-    const bool w_there = v0 + col < a.vocab, h_there = row < a.rows;
-    const T* w = static_cast<const T*>(a.w) + (v0 + col) * a.w_stride;
-    const T* h = static_cast<const T*>(a.h) + row * a.h_stride;
-    constexpr int step = FewStep<T>::k;
-    v4f acc = {0.f, 0.f, 0.f, 0.f};
-    int k = (lane >> 4) * Vec16<T>::N;
-    for (int at = 0; at < a.dim; at += step * kFewAhead) {
-        Vec16<T> wv[kFewAhead], hv[kFewAhead];
+    const long long v0 = ((long long)blockIdx.x * kFewWaves + wave) * 16;
+    // behind the end of either the first row is read, and what comes of it left alone
+    const T* w = static_cast<const T*>(a.w) + (v0 + col < a.vocab ? v0 + col : 0) * a.w_stride;
+    const T* h[NB];
 #pragma unroll
-        for (int u = 0; u < kFewAhead; ++u) wv[u] = few_load(w, at + u * step + k, a.dim, w_there, a.whole);
+    for (int b = 0; b < NB; ++b) h[b] = static_cast<const T*>(a.h) + (16 * b + col < a.rows ? 16 * b + col : 0) * a.h_stride;
+    constexpr int step = FewStep<T>::k, ahead = NB > 2 ? kFewAhead / 2 : kFewAhead, all = Vec16<T>::N;
+    v4f acc[NB];
 #pragma unroll
-        for (int u = 0; u < kFewAhead; ++u) hv[u] = few_load(h, at + u * step + k, a.dim, h_there, a.whole);
+    for (int b = 0; b < NB; ++b) acc[b] = v4f{0.f, 0.f, 0.f, 0.f};
+    const int k = (lane >> 4) * all;
+    int at = 0;
+    for (; at + step * ahead <= a.dim; at += step * ahead) {
+        Vec16<T> wv[ahead], hv[NB][ahead];
 #pragma unroll
-        for (int u = 0; u < kFewAhead; ++u) acc = few_product(wv[u], hv[u], acc);
+        for (int u = 0; u < ahead; ++u) wv[u] = few_load(w + at + u * step + k, all);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int u = 0; u < ahead; ++u) hv[b][u] = few_load(h[b] + at + u * step + k, all);
+#pragma unroll
+        for (int u = 0; u < ahead; ++u)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) acc[b] = few_product(wv[u], hv[b][u], acc[b]);
     }
-    // a lane has tokens v0 + 4 (lane / 16) + r of row `col`
+    for (; at < a.dim; at += step) {
+        const int count = at + k < a.dim ? a.dim - at - k : 0;
+        const Vec16<T> wv = few_load(w + at + k, count);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[b] = few_product(wv, few_load(h[b] + at + k, count), acc[b]);
+    }
+    // a lane has tokens v0 + 4 (lane / 16) + r of rows 16 b + col
     const float c = a.scale * kLog2e;
     const long long first = v0 + 4 * (lane >> 4);
-    float top = -INFINITY;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        if (first + r >= a.vocab) acc[r] = -INFINITY;
-        top = fmaxf(top, acc[r]);
-    }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, along = 0.f;
+    for (int b = 0; b < NB; ++b) {
+        float top = -INFINITY;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float d = max_nan(acc[r] - base, kLow), e = __builtin_amdgcn_exp2f(d * c);
-        sum += e;
-        along = fmaf(e, d, along);
-    }
-    sum += __shfl_xor(sum, 16);
-    along += __shfl_xor(along, 16);
-    sum += __shfl_xor(sum, 32);
-    along += __shfl_xor(along, 32);
-    if (lane < 16) shared[wave][lane] = Joined{top, sum, along};
-    if (a.targets && h_there) {
-        const long long target = a.targets[row] - first;
+        for (int r = 0; r < 4; ++r) {
+            if (first + r >= a.vocab) acc[b][r] = -INFINITY;
+            else if (a.logits) a.logits[((long long)b * a.vocab + first + r) * 16 + col] = acc[b][r];
+            top = fmaxf(top, acc[b][r]);
+        }
+        if (!a.part) continue;
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float base = top == -INFINITY ? 0.f : top;
+        float sum = 0.f, along = 0.f;
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (target == r && first + r < a.vocab) a.target_logit[row] = acc[r];
+        for (int r = 0; r < 4; ++r) {
+            const float d = max_nan(acc[b][r] - base, kLow), e = __builtin_amdgcn_exp2f(d * c);
+            sum += e;
+            along = fmaf(e, d, along);
+        }
+        sum += __shfl_xor(sum, 16);
+        along += __shfl_xor(along, 16);
+        sum += __shfl_xor(sum, 32);
+        along += __shfl_xor(along, 32);
+        if (lane < 16) shared[wave][16 * b + lane] = Joined{top, sum, along};
+        const long long row = 16 * b + col;
+        if (a.targets && row < a.rows) {
+            const long long target = a.targets[row] - first;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (target == r && first + r < a.vocab) a.target_logit[row] = acc[b][r];
+        }
     }
+    if (!a.part) return;
     __syncthreads();
-    if (threadIdx.x < 16 && h_there) {
+    if (threadIdx.x < 16 * NB && (int)threadIdx.x < a.rows) {
         Joined x = shared[0][threadIdx.x];
 #pragma unroll
         for (int i = 1; i < kFewWaves; ++i) x = join(x, shared[i][threadIdx.x], c);
-        float* to = a.part + (long long)blockIdx.x * 3 * a.part_rows + row;
+        float* to = a.part + (long long)blockIdx.x * 3 * a.part_rows + threadIdx.x;
         to[0] = x.top;
         to[a.part_rows] = x.sum;
         to[2 * a.part_rows] = x.along;
@@ -522,11 +539,13 @@ struct JoinArgs {
     RowInfo* info;                                   // nullable; with it the weights
     const float *a, *b;
 };
-__device__ __forceinline__ void write_info(RowInfo* to, float top, float logsum, float entropy, float a, float b, float scale, int64_t target, long long vocab, bool given) {
+__device__ __forceinline__ void write_info(RowInfo* to, float top, float logsum, float entropy, float a, float b, float scale, int64_t target, long long vocab, bool given, bool left_out) {
     RowInfo f{top, logsum * kLog2e, a * scale, b * scale, entropy, (int)target, {0, 0}};
     if (top == -INFINITY) f = RowInfo{0.f, INFINITY, 0.f, 0.f, 0.f, -1, {0, 0}};      // nothing but -infinity: no gradient
-    if (given && (target < 0 || target >= vocab)) { f.target = -1; f.log2sum = NAN; }
+    if (left_out) f = RowInfo{0.f, INFINITY, 0.f, 0.f, 0.f, kLeftOut, {0, 0}};
+    else if (given && (target < 0 || target >= vocab)) { f.target = -1; f.log2sum = NAN; }
     if (!given) f.target = -1;
+    if (left_out) f.target = kLeftOut;
     *to = f;
 }
 // ROWS rows a workgroup, the parts of each shared out to 256 / ROWS threads
@@ -575,12 +594,13 @@ template <int ROWS> __global__ __launch_bounds__(256) void k_join(const JoinArgs
         a.stats[2 * row] = left_out ? 0.f : x.top;
         a.stats[2 * row + 1] = left_out ? 0.f : logsum;
     }
-    if (a.info) write_info(a.info + at, x.top, logsum, entropy, a.a ? a.a[row] : 0.f, a.b ? a.b[row] : 0.f, a.scale, target, a.vocab, a.targets != nullptr);
+    if (a.info) write_info(a.info + at, x.top, logsum, entropy, a.a ? a.a[row] : 0.f, a.b ? a.b[row] : 0.f, a.scale, target, a.vocab, a.targets != nullptr, left_out);
 }
 
 struct InfoArgs {
-    const Split* split;
+    const Split* split;                              // nullable, with live: all `rows` rows as they are
     const int* live;
+    long long rows, ignore;
     const int64_t* targets;
     const float *stats, *entropy, *a, *b;
     float scale;
@@ -589,10 +609,231 @@ struct InfoArgs {
 };
 __global__ __launch_bounds__(256) void k_info(const InfoArgs a) {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (at >= a.split->rows) return;
-    const long long row = a.live[at];
+    if (at >= (a.split ? a.split->rows : a.rows)) return;
+    const long long row = a.live ? a.live[at] : at;
     write_info(a.info + at, a.stats[2 * row], a.stats[2 * row + 1], a.b ? a.entropy[row] : 0.f, a.a ? a.a[row] : 0.f, a.b ? a.b[row] : 0.f, a.scale,
-               a.targets ? a.targets[row] : 0, a.vocab, a.targets != nullptr);
+               a.targets ? a.targets[row] : 0, a.vocab, a.targets != nullptr, a.targets && a.targets[row] == a.ignore);
+}
+
+// ---- few rows' gradients ------------------------------------------------------------------------------------
+// dz of 64 tokens is made in LDS from their logits; then every token's row of the weights is read once, for dH, and its row of dW written
+// once, by lanes of COLS neighbouring columns that hold ROWS rows' hidden states and sums of dH in registers.  Where a row needs fewer
+// lanes than the workgroup has, tokens go round groups of lanes.  What bounds it: memory, from 12 rows on its 2 rows vocab dim products.
+struct FewGradArgs {
+    const void *h, *w;
+    long long h_stride, w_stride, vocab, dim;
+    int rows, all_rows, lanes, blocks;               // rows of this launch and of the call; lanes of a row (a power of two, up to 256); blocks of the vocabulary
+    bool add;                                        // to what the launch before has written into dw
+    float scale;
+    const float* logits;                             // [16 rows][token][16]
+    const RowInfo* info;
+    float* sums;                                     // [block][row][dim], nullable
+    void* dw;                                        // nullable
+};
+constexpr int kFewTokens = 64;
+template <typename T, int ROWS, int COLS> __global__ __launch_bounds__(256) void k_few_grad(const FewGradArgs a) {
+    __shared__ __attribute__((aligned(16))) float dz[kFewTokens][ROWS];
+    __shared__ float share[256 * COLS];
+    __shared__ RowInfo info[ROWS];
+    if (threadIdx.x < ROWS) info[threadIdx.x] = (int)threadIdx.x < a.rows ? a.info[threadIdx.x] : RowInfo{0.f, INFINITY, 0.f, 0.f, 0.f, kLeftOut, {0, 0}};
+    const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = 256 / a.lanes;
+    const long long col = ((long long)blockIdx.x * a.lanes + lane) * COLS;
+    const int count = a.dim - col >= COLS ? COLS : a.dim > col ? (int)(a.dim - col) : 0;
+    __syncthreads();
+    float h[ROWS][COLS], sum[ROWS][COLS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        // a row that is left out is not read
+        load_some<COLS>(static_cast<const T*>(a.h) + r * a.h_stride + col, info[r].target != kLeftOut ? count : 0, h[r]);
+#pragma unroll
+        for (int e = 0; e < COLS; ++e) sum[r][e] = 0.f;
+    }
+    const float c = a.scale * kLog2e;
+    const long long steps = (a.vocab + kFewTokens - 1) / kFewTokens, from = steps * blockIdx.y / a.blocks, to = steps * (blockIdx.y + 1) / a.blocks;
+    for (long long step = from; step < to; ++step) {
+        const long long v0 = step * kFewTokens;
+        const int tokens = a.vocab - v0 < kFewTokens ? (int)(a.vocab - v0) : kFewTokens;
+        for (int i = threadIdx.x; i < kFewTokens * ROWS; i += 256) {
+            const int v = i / ROWS, r = i % ROWS;
+            const RowInfo f = info[r];
+            float d = 0.f;
+            if (v < tokens && f.target != kLeftOut) {
+                const float x = fmaf(a.logits[((long long)(r / 16) * a.vocab + v0 + v) * 16 + r % 16] - f.top, c, -f.log2sum), p = __builtin_amdgcn_exp2f(x);
+                d = f.b != 0.f ? -p * fmaf(f.b, fmaf(max_nan(x, kLow), 1.f / kLog2e, f.entropy), f.a) : -f.a * p;
+                if (f.target == v0 + v) d += f.a;
+            }
+            dz[v][r] = d;
+        }
+        __syncthreads();
+        constexpr int ahead = 4;
+        for (int v = group; v < tokens; v += groups * ahead) {
+            Loose<T, COLS> w[ahead];
+            if (a.sums) {
+#pragma unroll
+                for (int u = 0; u < ahead; ++u)
+                    w[u].load(static_cast<const T*>(a.w) + (v0 + v + u * groups) * a.w_stride + col, v + u * groups < tokens ? count : 0);
+            }
+#pragma unroll
+            for (int u = 0; u < ahead; ++u) {
+                const int at = v + u * groups;
+                if (at >= tokens) break;
+                float out[COLS];
+#pragma unroll
+                for (int e = 0; e < COLS; ++e) out[e] = 0.f;
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    const float d = dz[at][r];
+#pragma unroll
+                    for (int e = 0; e < COLS; ++e) {
+                        out[e] = fmaf(d, h[r][e], out[e]);
+                        if (a.sums) sum[r][e] = fmaf(d, w[u].get(e), sum[r][e]);
+                    }
+                }
+                if (a.dw) store_some<COLS>(static_cast<T*>(a.dw) + (v0 + at) * a.dim + col, count, out);
+            }
+        }
+        __syncthreads();
+    }
+    if (!a.sums) return;
+    // the groups' sums in their order
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        if (groups > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < COLS; ++e) share[threadIdx.x * COLS + e] = sum[r][e];
+            __syncthreads();
+            if (group == 0) {
+                for (int g = 1; g < groups; ++g)
+#pragma unroll
+                    for (int e = 0; e < COLS; ++e) sum[r][e] += share[(g * a.lanes + lane) * COLS + e];
+            }
+        }
+        if (group == 0 && r < a.rows) store_some<COLS>(a.sums + ((long long)blockIdx.y * a.all_rows + r) * a.dim + col, count, sum[r]);
+    }
+}
+// The same for 9 to 64 rows of fp32 by matrix instructions (16 x 16 x 4, fp32 throughout), where 2 rows vocab dim multiply-adds a side on
+// the vector units would take longer than the memory.  A wave has 64 columns, lane l the four from 4 (l % 16) on, so that 16 lanes read a
+// row of W, or write one of dW, side by side: column 4 n + e is column n of block e of a matrix instruction.  TB: 16s of rows.
+template <int TB> __global__ __launch_bounds__(256) void k_few_grad_f32(const FewGradArgs a) {
+    __shared__ float dz[2][16 * TB][17];             // two turns of 16 tokens
+    __shared__ RowInfo info[16 * TB];
+    if (threadIdx.x < 16 * TB) info[threadIdx.x] = (int)threadIdx.x < a.rows ? a.info[threadIdx.x] : RowInfo{0.f, INFINITY, 0.f, 0.f, 0.f, kLeftOut, {0, 0}};
+    const int lane = threadIdx.x & 63, n = lane & 15, k = lane >> 4;
+    const long long col = ((long long)blockIdx.x * 4 + (threadIdx.x >> 6)) * 64 + 4 * n;
+    const int count = a.dim - col >= 4 ? 4 : a.dim > col ? (int)(a.dim - col) : 0;
+    __syncthreads();
+    const float *hidden = static_cast<const float*>(a.h), *weights = static_cast<const float*>(a.w);
+    float h[4 * TB][4];                              // rows 4 j + k
+    v4f sum[TB][4];
+#pragma unroll
+    for (int j = 0; j < 4 * TB; ++j) load_some<4>(hidden + (4 * j + k) * a.h_stride + col, info[4 * j + k].target != kLeftOut ? count : 0, h[j]);
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[t][e] = v4f{0.f, 0.f, 0.f, 0.f};
+    const float c = a.scale * kLog2e;
+    const long long turns = (a.vocab + 15) / 16, from = turns * blockIdx.y / a.blocks, to = turns * (blockIdx.y + 1) / a.blocks;
+    auto load = [&](long long turn, Loose<float, 4>* w) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const long long v = turn * 16 + 4 * i + k;
+            w[i].load(weights + v * a.w_stride + col, a.sums && turn < to && v < a.vocab ? count : 0);
+        }
+    };
+    auto gradients = [&](long long turn) {           // of 16 tokens' logits, a thread for a token and every 16th row
+        const int v = threadIdx.x & 15;
+#pragma unroll
+        for (int i = 0; i < TB; ++i) {
+            const int r = 16 * i + (threadIdx.x >> 4);
+            const RowInfo f = info[r];
+            float d = 0.f;
+            if (turn < to && turn * 16 + v < a.vocab && f.target != kLeftOut) {
+                const float x = fmaf(a.logits[((long long)i * a.vocab + turn * 16 + v) * 16 + r % 16] - f.top, c, -f.log2sum), p = __builtin_amdgcn_exp2f(x);
+                d = f.b != 0.f ? -p * fmaf(f.b, fmaf(max_nan(x, kLow), 1.f / kLog2e, f.entropy), f.a) : -f.a * p;
+                if (f.target == turn * 16 + v) d += f.a;
+            }
+            dz[turn & 1][r][v] = d;
+        }
+    };
+    Loose<float, 4> w[4];
+    load(from, w);
+    gradients(from);
+    __syncthreads();
+    for (long long turn = from; turn < to; ++turn) {
+        Loose<float, 4> ahead[4];
+        load(turn + 1, ahead);
+        gradients(turn + 1);
+        const float(*d)[17] = dz[turn & 1];
+        if (a.sums) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int t = 0; t < TB; ++t) {
+                    const float x = d[16 * t + n][4 * i + k];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, w[i].get(e), sum[t][e], 0, 0, 0);
+                }
+        }
+        if (a.dw) {
+            v4f out[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 4 * TB; ++j) {
+                const float x = d[4 * j + k][n];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, h[j][e], out[e], 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float f[4] = {out[0][r], out[1][r], out[2][r], out[3][r]};
+                const long long v = turn * 16 + 4 * k + r;
+                float* to = static_cast<float*>(a.dw) + v * a.dim + col;
+                if (a.add) {
+                    float before[4];
+                    load_some<4>(to, v < a.vocab ? count : 0, before);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f[e] += before[e];
+                }
+                store_some<4>(to, v < a.vocab ? count : 0, f);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = ahead[i];
+    }
+    if (!a.sums) return;
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = 16 * t + 4 * k + r;
+            const float f[4] = {sum[t][0][r], sum[t][1][r], sum[t][2][r], sum[t][3][r]};
+            store_some<4>(a.sums + ((long long)blockIdx.y * a.all_rows + row) * a.dim + col, row < a.rows ? count : 0, f);
+        }
+}
+// dH's rows from the blocks' sums, in their order: 8 threads share a column
+template <typename T> __global__ __launch_bounds__(256) void k_few_hidden(const float* sums, int blocks, long long rows, long long dim, T* out) {
+    __shared__ float lds[8][32];
+    const int in = threadIdx.x % 32, share = threadIdx.x / 32;
+    const long long at = (long long)blockIdx.x * 32 + in, n = rows * dim;
+    float t = 0.f;
+    if (at < n) {
+        constexpr int ahead = 8;
+        for (int b = share; b < blocks; b += 8 * ahead) {
+            float f[ahead];
+#pragma unroll
+            for (int u = 0; u < ahead; ++u) f[u] = b + 8 * u < blocks ? sums[(b + 8 * u) * n + at] : 0.f;
+#pragma unroll
+            for (int u = 0; u < ahead; ++u) t += f[u];
+        }
+    }
+    lds[share][in] = t;
+    __syncthreads();
+    if (share || at >= n) return;
+    for (int i = 1; i < 8; ++i) t += lds[i][in];
+    out[at] = from_f32<T>(t);
 }
 
 // ---- the gradients' products ----------------------------------------------------------------------------------
@@ -691,17 +932,24 @@ template <int B, typename T> __global__ __launch_bounds__(Shape<B>::kThreads, 2)
     else if (a.dweight) dweight_tile<B, T>(a, id - first, rows, lds);
 }
 
-// dH's rows from their sums; zeros for rows that are left out
-template <typename T> __global__ __launch_bounds__(256) void k_hidden(const float* sums, const Split* split, const int* place, long long rows, long long dim, T* out) {
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (at >= rows * dim) return;
-    const long long row = at / dim, from = place[row];
-    float t = 0.f;
+// dH's rows from their sums, four entries a thread; zeros for rows that are left out
+template <typename T> __global__ __launch_bounds__(256) void k_hidden(const float* sums, const Split* split, const int* place, long long rows, int dim, T* out) {
+    const int pieces = (dim + 3) / 4;
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / pieces;
+    if (row >= rows) return;
+    const int col = (int)(at - row * pieces) * 4, count = dim - col, splits = split->splits;
+    const long long from = place[row], plane = (long long)split->rows * dim;
+    float t[4] = {0.f, 0.f, 0.f, 0.f};
     if (from >= 0) {
-        const float* p = sums + from * dim + (at - row * dim);
-        for (int s = 0; s < split->splits; ++s) t += p[s * (split->rows * dim)];
+        const float* p = sums + from * dim + col;
+        for (int s = 0; s < splits; ++s) {
+            float f[4];
+            load_some<4>(p + s * plane, count, f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] += f[e];
+        }
     }
-    out[at] = from_f32<T>(t);
+    store_some<4>(out + row * dim + col, count, t);
 }
 
 // ---- host ----
@@ -714,7 +962,8 @@ struct Plan {
     long long parts;                                 // of the values
     long long piece;                                 // tokens of a piece of the gradient, and of packed weights
     long long most_sums, most_splits;
-    size_t split, live, place, hidden, weights, part, target, info, dz, sums, bytes;      // offsets
+    int few_blocks;                                  // of the vocabulary for few rows
+    size_t logits, split, live, place, hidden, weights, part, target, info, dz, sums, bytes;      // offsets
 };
 long long up(long long x, long long to) { return (x + to - 1) / to * to; }
 
@@ -735,8 +984,9 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     p.rows = d->rows; p.dim = d->dim; p.vocab = d->vocab;
     p.packed_dim = up(d->dim, kStep);
     p.k_steps = (int)(p.packed_dim / kStep);
-    p.few = !grad && d->rows <= kFew;
-    p.staged = !p.few && (p.f32 || d->dim % kStep || d->weight_stride % 8 || d->weight_stride >= (1 << 21) || d->any_address);
+    const bool as_it_lies = !p.f32 && d->dim % kStep == 0 && d->weight_stride % 8 == 0 && d->weight_stride < (1 << 21) && !d->any_address;
+    p.few = d->rows <= (p.f32 ? kFewF32 : grad ? kFewGradBf16 : as_it_lies ? kFewBf16 : kFewBf16Packed);
+    p.staged = !p.few && !as_it_lies;
     p.tile = up(d->rows, 256) / 256 * (up(d->vocab, 256) / 256) >= 256 ? 256 : 128;
     const long long rows_up = up(d->rows, p.tile);
     p.piece = (long long)(kPieceBytes / 2 / (size_t)rows_up) / 256 * 256;
@@ -756,6 +1006,10 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     if (p.most_splits > 32) p.most_splits = 32;
     if (p.most_splits < 2) p.most_splits = 2;
     p.most_sums = d->rows * p.most_splits;
+    // blocks of the vocabulary for few rows' gradients: workgroups for the chip, two to four a CU, each with 64 tokens at least
+    const long long few_columns = d->rows <= 4 ? 2048 : d->rows <= kFewGradVector ? 1024 : 256, few_want = 1024 / ((d->dim + few_columns - 1) / few_columns);
+    const long long few_most = (d->vocab + kFewTokens - 1) / kFewTokens, few_cap = few_want < 1 ? 1 : few_want > 512 ? 512 : few_want;
+    p.few_blocks = (int)(few_cap < few_most ? few_cap : few_most);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += round256(bytes); return here; };
     const size_t rows = (size_t)d->rows;
@@ -770,6 +1024,12 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     p.target = take(rows * 4);
     if (grad) {
         p.info = take(rows * sizeof(RowInfo));
+        if (p.few) {
+            p.logits = take((rows + 15) / 16 * 16 * (size_t)d->vocab * 4);
+            p.sums = take((size_t)p.few_blocks * rows * d->dim * 4);
+            p.bytes = at;
+            return p;
+        }
         p.dz = take((size_t)p.planes * (size_t)rows_up * p.piece * 2);
         p.sums = take((size_t)p.most_sums * d->dim * 4);
     }
@@ -822,6 +1082,55 @@ struct Call {
         a.vocab = n; a.first = first; a.scale = d->scale;
         return a;
     }
+    template <typename T> void few_logits(bool values, bool keep) {
+        for (long long base = 0; base < p.rows; base += kFewAtOnce) {
+            const long long rows = p.rows - base < kFewAtOnce ? p.rows - base : kFewAtOnce;
+            const T* h = static_cast<const T*>(hidden) + base * d->hidden_stride;
+            const FewArgs a{h, weight, d->hidden_stride, d->weight_stride, p.vocab, rows, (int)p.dim, d->scale,
+                            targets ? targets + base : nullptr, values ? at<float>(p.part) + base : nullptr, at<float>(p.target) + base,
+                            keep ? at<float>(p.logits) + base * p.vocab : nullptr, p.rows};
+            const dim3 grid((unsigned)p.parts);
+            if (rows <= 16) hipLaunchKernelGGL((k_few<T, 1>), grid, 64 * kFewWaves, 0, st, a);
+            else if (rows <= 32) hipLaunchKernelGGL((k_few<T, 2>), grid, 64 * kFewWaves, 0, st, a);
+            else hipLaunchKernelGGL((k_few<T, 4>), grid, 64 * kFewWaves, 0, st, a);
+        }
+    }
+    void few_logits(bool values, bool keep) {
+        if (p.f32) few_logits<float>(values, keep);
+        else few_logits<bf16_t>(values, keep);
+    }
+    FewGradArgs few_args(void* dhidden, void* dweight, int lanes) const {
+        return FewGradArgs{hidden, weight, d->hidden_stride, d->weight_stride, p.vocab, p.dim, (int)p.rows, (int)p.rows, lanes, p.few_blocks, false, d->scale,
+                           at<float>(p.logits), at<RowInfo>(p.info), dhidden ? at<float>(p.sums) : nullptr, dweight};
+    }
+    void few_grad_f32(void* dhidden, void* dweight) {
+        for (long long base = 0; base < p.rows; base += kFewAtOnce) {
+            FewGradArgs a = few_args(dhidden, dweight, 64);
+            a.rows = (int)(p.rows - base < kFewAtOnce ? p.rows - base : kFewAtOnce);
+            a.h = static_cast<const float*>(hidden) + base * d->hidden_stride;
+            a.logits += base * p.vocab;
+            a.info += base;
+            if (a.sums) a.sums += base * p.dim;
+            a.add = base > 0;
+            const dim3 grid((unsigned)((p.dim + 255) / 256), (unsigned)p.few_blocks);
+            if (a.rows <= 16) hipLaunchKernelGGL(k_few_grad_f32<1>, grid, 256, 0, st, a);
+            else if (a.rows <= 32) hipLaunchKernelGGL(k_few_grad_f32<2>, grid, 256, 0, st, a);
+            else hipLaunchKernelGGL(k_few_grad_f32<4>, grid, 256, 0, st, a);
+        }
+    }
+    template <typename T, int ROWS, int COLS> void few_grad(void* dhidden, void* dweight) {
+        int lanes = 8;
+        while (lanes < 256 && lanes * COLS < p.dim) lanes *= 2;
+        const FewGradArgs a = few_args(dhidden, dweight, lanes);
+        hipLaunchKernelGGL((k_few_grad<T, ROWS, COLS>), dim3((unsigned)((p.dim + lanes * COLS - 1) / (lanes * COLS)), (unsigned)p.few_blocks), 256, 0, st, a);
+    }
+    template <typename T> void few_gradients(void* dhidden, void* dweight) {
+        if (!dhidden && !dweight) return;
+        if (p.rows <= 4) few_grad<T, 4, 8>(dhidden, dweight);
+        else if (p.rows <= kFewGradVector) few_grad<T, 8, 4>(dhidden, dweight);
+        else few_grad_f32(dhidden, dweight);
+        if (dhidden) hipLaunchKernelGGL(k_few_hidden<T>, dim3((unsigned)((p.rows * p.dim + 31) / 32)), 256, 0, st, at<float>(p.sums), p.few_blocks, p.rows, p.dim, static_cast<T*>(dhidden));
+    }
     template <int B> void logits(const LogitArgs& a) {
         static LdsAllowed one, three;
         const long long count = up(a.vocab, B) / B * (up(p.rows, B) / B);
@@ -844,13 +1153,7 @@ struct Call {
     void values(float* logprob, float* entropy, float* stats, RowInfo* info, const float* wa, const float* wb) {
         JoinArgs j{};
         if (p.few) {
-            FewArgs a{hidden, weight, d->hidden_stride, d->weight_stride, p.vocab, p.rows, 0, (int)p.dim, false, d->scale, targets, d->ignore_index,
-                      at<float>(p.part), at<float>(p.target), p.rows};
-            const size_t es = p.f32 ? 4 : 2;
-            a.whole = aligned(hidden, 16) && aligned(weight, 16) && d->hidden_stride * es % 16 == 0 && d->weight_stride * es % 16 == 0;
-            const dim3 grid((unsigned)p.parts);
-            if (p.f32) hipLaunchKernelGGL(k_few<float>, grid, 64 * kFewWaves, 0, st, a);
-            else hipLaunchKernelGGL(k_few<bf16_t>, grid, 64 * kFewWaves, 0, st, a);
+            few_logits(true, info != nullptr);
         } else {
             const long long each = p.staged ? p.piece : p.vocab;
             for (long long first = 0; first < p.vocab; first += each) {
@@ -889,9 +1192,9 @@ struct Call {
             else products<128>(a, b);
         }
         if (dhidden) {
-            const dim3 grid((unsigned)((p.rows * p.dim + 255) / 256));
-            if (p.f32) hipLaunchKernelGGL(k_hidden<float>, grid, 256, 0, st, at<float>(p.sums), at<Split>(p.split), at<int>(p.place), p.rows, p.dim, static_cast<float*>(dhidden));
-            else hipLaunchKernelGGL(k_hidden<bf16_t>, grid, 256, 0, st, at<float>(p.sums), at<Split>(p.split), at<int>(p.place), p.rows, p.dim, static_cast<bf16_t*>(dhidden));
+            const dim3 grid((unsigned)((p.rows * ((p.dim + 3) / 4) + 255) / 256));
+            if (p.f32) hipLaunchKernelGGL(k_hidden<float>, grid, 256, 0, st, at<float>(p.sums), at<Split>(p.split), at<int>(p.place), p.rows, (int)p.dim, static_cast<float*>(dhidden));
+            else hipLaunchKernelGGL(k_hidden<bf16_t>, grid, 256, 0, st, at<float>(p.sums), at<Split>(p.split), at<int>(p.place), p.rows, (int)p.dim, static_cast<bf16_t*>(dhidden));
         }
     }
 };
@@ -956,14 +1259,17 @@ asi_status asi_linear_logprobs_grad(const asi_linear_logprob_desc* desc, int giv
     if (!ws || !aligned(ws, 256) || ws_bytes < asi_linear_logprobs_grad_workspace_bytes(desc)) return ASI_ERR_WORKSPACE;
     Call c{desc, plan(desc, true), static_cast<char*>(ws), hidden, weight, targets, st};
     RowInfo* info = c.at<RowInfo>(c.p.info);
-    c.rows_of(given ? nullptr : logprob, given ? nullptr : entropy, nullptr, true, dhidden, dweight);
+    if (!c.p.few) c.rows_of(given ? nullptr : logprob, given ? nullptr : entropy, nullptr, true, dhidden, dweight);
     if (given) {
+        if (c.p.few) c.few_logits(false, true);
         hipLaunchKernelGGL(k_info, dim3((unsigned)((desc->rows + 255) / 256)), 256, 0, st,
-                           InfoArgs{c.at<Split>(c.p.split), c.at<int>(c.p.live), targets, stats, entropy, grad_logprob, grad_entropy, desc->scale, desc->vocab, info});
+                           InfoArgs{c.p.few ? nullptr : c.at<Split>(c.p.split), c.p.few ? nullptr : c.at<int>(c.p.live), desc->rows, desc->ignore_index, targets, stats, entropy, grad_logprob, grad_entropy, desc->scale, desc->vocab, info});
     } else {
         c.values(logprob, entropy, nullptr, info, grad_logprob, grad_entropy);
     }
-    c.gradients(dhidden, dweight);
+    if (!c.p.few) c.gradients(dhidden, dweight);
+    else if (c.p.f32) c.few_gradients<float>(dhidden, dweight);
+    else c.few_gradients<bf16_t>(dhidden, dweight);
     return c.status != ASI_OK ? c.status : launched();
 }
 

@@ -170,6 +170,84 @@ template <int N> __device__ __forceinline__ void store_values_past(bf16_t* p, co
     }
 }
 
+// N neighbouring values (2, 4 or 8), of which the first `count` exist, at an address that is a multiple of the element's size only: the
+// hardware takes whole vectors at such addresses, and at multiples of 16 in no more time than otherwise.
+typedef uint32_t loose4 __attribute__((ext_vector_type(4), aligned(2), may_alias));
+typedef uint32_t loose2 __attribute__((ext_vector_type(2), aligned(2), may_alias));
+typedef uint32_t loose1 __attribute__((aligned(2), may_alias));
+template <int WORDS> __device__ __forceinline__ void load_loose(const void* p, uint32_t* w) {
+    if constexpr (WORDS >= 4) {
+#pragma unroll
+        for (int i = 0; i < WORDS; i += 4) {
+            const loose4 v = *reinterpret_cast<const loose4*>(static_cast<const char*>(p) + 4 * i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[i + e] = v[e];
+        }
+    } else if constexpr (WORDS == 2) {
+        const loose2 v = *static_cast<const loose2*>(p);
+        w[0] = v.x; w[1] = v.y;
+    } else {
+        w[0] = *static_cast<const loose1*>(p);
+    }
+}
+template <int WORDS> __device__ __forceinline__ void store_loose(void* p, const uint32_t* w) {
+    if constexpr (WORDS >= 4) {
+#pragma unroll
+        for (int i = 0; i < WORDS; i += 4) *reinterpret_cast<loose4*>(static_cast<char*>(p) + 4 * i) = loose4{w[i], w[i + 1], w[i + 2], w[i + 3]};
+    } else if constexpr (WORDS == 2) {
+        *static_cast<loose2*>(p) = loose2{w[0], w[1]};
+    } else {
+        *static_cast<loose1*>(p) = w[0];
+    }
+}
+// as they were loaded, at half the registers where they are bf16
+template <typename T, int N = 8> struct Loose {
+    static constexpr int kWords = N * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* p, int count) {
+        if (count >= N) {
+            load_loose<kWords>(p, w);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < count) {
+                if constexpr (sizeof(T) == 2) w[e >> 1] |= (uint32_t)p[e].bits << (16 * (e & 1));
+                else w[e] = __float_as_uint(p[e]);
+            }
+    }
+    __device__ __forceinline__ float get(int e) const {
+        if constexpr (sizeof(T) == 2) return __uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+        else return __uint_as_float(w[e]);
+    }
+};
+template <int N, typename T> __device__ __forceinline__ void load_some(const T* p, int count, float* f) {
+    Loose<T, N> r;
+    r.load(p, count);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = r.get(i);
+}
+template <int N, typename T> __device__ __forceinline__ void store_some(T* p, int count, const float* f) {
+    if (count >= N) {
+        constexpr int words = N * (int)sizeof(T) / 4;
+        uint32_t w[words];
+#pragma unroll
+        for (int i = 0; i < words; ++i) {
+            if constexpr (sizeof(T) == 2) w[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
+            else w[i] = __float_as_uint(f[i]);
+        }
+        store_loose<words>(p, w);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < count) p[i] = from_f32<T>(f[i]);
+}
+template <typename T> __device__ __forceinline__ void load8(const T* p, int count, float* f) { load_some<8>(p, count, f); }
+template <typename T> __device__ __forceinline__ void store8(T* p, int count, const float* f) { store_some<8>(p, count, f); }
+
 // Reductions over `width` neighbouring lanes (a power of two); every lane gets the result, always in the same order.
 template <int WIDTH = kWave> __device__ __forceinline__ float lanes_sum(float x) {
 #pragma unroll

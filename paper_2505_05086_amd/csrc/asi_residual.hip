@@ -145,36 +145,9 @@ template <typename S, typename T, int LANES, int K, bool DROP> __global__ __laun
     }
 }
 
-// Eight entries of a row as they were loaded, at half the registers where they are bf16.
-template <typename T> struct Row8 {
-    uint32_t w[2 * sizeof(T)];
-    __device__ __forceinline__ void load(const T* p, int count) {
-        if (count >= 8) {
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-                const loose4 v = *reinterpret_cast<const loose4*>(p + i * 16 / sizeof(T));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[4 * i + e] = v[e];
-            }
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < 2 * (int)sizeof(T); ++i) w[i] = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < count) {
-                if constexpr (sizeof(T) == 2) w[e >> 1] |= (uint32_t)p[e].bits << (16 * (e & 1));
-                else w[e] = __float_as_uint(p[e]);
-            }
-    }
-    __device__ __forceinline__ float get(int e) const {
-        if constexpr (sizeof(T) == 2) return __uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
-        else return __uint_as_float(w[e]);
-    }
-};
 template <typename S, typename T, int K> struct GradRow {
-    Row8<S> ds[K], s[K];
-    Row8<T> dout[K], y[K];
+    Loose<S> ds[K], s[K];
+    Loose<T> dout[K], y[K];
 };
 
 // Eight gains, as they were loaded
@@ -185,12 +158,12 @@ struct Gain8 {
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = 0x3f800000u;
         } else if (a.gain_bf16) {
-            Row8<bf16_t> r;
+            Loose<bf16_t> r;
             r.load(static_cast<const bf16_t*>(p) + at, count);
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(r.get(i));
         } else {
-            Row8<float> r;
+            Loose<float> r;
             r.load(static_cast<const float*>(p) + at, count);
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = r.w[i];
