@@ -13,7 +13,6 @@
 namespace asi {
 namespace {
 
-constexpr int kGradThreads = 512, kMostBlocks = 256;      // of the backward pass: a workgroup a CU
 constexpr int kSumColumns = 64, kSumShares = 16;
 
 struct Args {
@@ -76,13 +75,13 @@ template <int LANES, int N> __device__ __forceinline__ void row_sums(float* v, f
     }
 }
 
-template <int LANES> constexpr int threads_of() { return LANES > 256 ? LANES : 256; }
+constexpr int threads_of(int lanes) { return lanes > 256 ? lanes : 256; }
 
 template <int K> __device__ __forceinline__ int count_at(const Args& a, int col) { return a.dim - col >= 8 ? 8 : a.dim > col ? (int)(a.dim - col) : 0; }
 
-template <typename S, typename T, int LANES, int K, bool DROP> __global__ __launch_bounds__(threads_of<LANES>()) void k_residual(const Args a) {
-    __shared__ float lds[threads_of<LANES>() / 64];
-    constexpr int kRows = threads_of<LANES>() / LANES;
+template <typename S, typename T, int LANES, int K, bool DROP> __global__ __launch_bounds__(threads_of(LANES)) void k_residual(const Args a) {
+    __shared__ float lds[threads_of(LANES) / 64];
+    constexpr int kRows = threads_of(LANES) / LANES;
     const int lane = threadIdx.x % LANES;
     const long long row = a.first + (long long)blockIdx.x * kRows + threadIdx.x / LANES;
     const bool there = row < a.rows;
@@ -203,9 +202,9 @@ struct Walk {
 // What bounds the backward pass besides memory is the chain load, sum, sum, store of a row: the next row's loads are on their way
 // meanwhile (K = 1), and the gains stay in registers (K = 1, all but the gate of a unit).  Between gate and post gain one sum serves both:
 // with q = sum over rows of t dropout' u it is post_gain q that is the gate's gradient and gate q the post gain's.
-template <typename S, typename T, int LANES, int K, bool DROP> __global__ __launch_bounds__(kGradThreads, 2) void k_residual_grad(const Args a) {
-    constexpr int kRows = kGradThreads / LANES;
-    __shared__ float lds[kGradThreads * 8];
+template <typename S, typename T, int LANES, int K, bool DROP> __global__ __launch_bounds__(threads_of(LANES), 2) void k_residual_grad(const Args a) {
+    constexpr int kThreads = threads_of(LANES), kRows = kThreads / LANES;
+    __shared__ float lds[kThreads * 8];
     const int lane = threadIdx.x % LANES;
     Keep keep = a.keep;
     if constexpr (DROP) read_seed(&keep);
@@ -344,7 +343,7 @@ template <typename S, typename T, int LANES, int K, bool DROP> __global__ __laun
 #pragma unroll
             for (int e = 0; e < 8; ++e) lds[threadIdx.x * 8 + e] = which == 0 ? sum_pre[k][e] : a.units ? sum_post[k][e] : sum_q[k][e];
             __syncthreads();
-            for (int c = threadIdx.x; c < LANES * 8; c += kGradThreads) {
+            for (int c = threadIdx.x; c < LANES * 8; c += kThreads) {
                 float t = 0.f;
 #pragma unroll
                 for (int slot = 0; slot < kRows; ++slot) t += lds[slot * LANES * 8 + c];
@@ -399,7 +398,11 @@ __global__ __launch_bounds__(kSumColumns * kSumShares) void k_residual_sums(cons
 int lanes_for(long long dim) {
     return dim <= 128 ? 16 : dim <= 512 ? 64 : dim <= 1024 ? 128 : dim <= 2048 ? 256 : 512;
 }
-int rows_a_block(long long dim) { return kGradThreads / lanes_for(dim); }      // of the backward pass
+int rows_a_block(long long dim) { return threads_of(lanes_for(dim)) / lanes_for(dim); }
+
+// Workgroups of the backward pass: as many as are resident, three a CU of 256 threads, one of 512 (32768 x 1024 bf16 with dropout, us: two a CU
+// 115, three 101, four 118; 8192 x 4096 with a stream in fp32: one a CU 176, one and a half 226, two 185).
+int most_blocks(long long dim) { return threads_of(lanes_for(dim)) == 256 ? 768 : 256; }
 
 asi_status check(const asi_residual_desc* d) {
     if (!d || d->rows < 0 || d->dim < 1 || d->x_stride < d->dim || d->y_stride < d->dim || d->gate_rows < 0 || d->gate_rows > d->rows ||
@@ -431,27 +434,27 @@ Plan plan(const asi_residual_desc* d) {
     p.parts = 1;
     long long items = d->rows;
     if (d->gate_rows > 1) {
-        const long long each = d->rows / d->gate_rows, want = (long long)kMostBlocks * slots / d->gate_rows;
+        const long long each = d->rows / d->gate_rows, want = (long long)most_blocks(d->dim) * slots / d->gate_rows;
         p.parts = (int)(want < 1 ? 1 : want > each ? each : want);
         items = p.units = d->gate_rows * p.parts;
         if (p.parts > 1) p.unit_floats = (size_t)p.units * d->dim;
     }
     const long long blocks = (items + slots - 1) / slots;
-    p.blocks = (int)(blocks < kMostBlocks ? blocks : kMostBlocks);
+    p.blocks = (int)(blocks < most_blocks(d->dim) ? blocks : most_blocks(d->dim));
     p.part_floats = (size_t)p.blocks * 2 * d->dim;
     return p;
 }
 
 template <typename S, typename T, int LANES, int K, bool DROP> void launch(const Args& a, bool back, int blocks, hipStream_t st) {
     if (back) {
-        hipLaunchKernelGGL((k_residual_grad<S, T, LANES, K, DROP>), dim3(blocks), kGradThreads, 0, st, a);
+        hipLaunchKernelGGL((k_residual_grad<S, T, LANES, K, DROP>), dim3(blocks), threads_of(LANES), 0, st, a);
         return;
     }
-    constexpr long long rows = threads_of<LANES>() / LANES, most = most_workgroups(threads_of<LANES>()) * rows;
+    constexpr long long rows = threads_of(LANES) / LANES, most = most_workgroups(threads_of(LANES)) * rows;
     Args b = a;
     for (b.first = 0; b.first < a.rows; b.first += most) {
         const long long left = a.rows - b.first < most ? a.rows - b.first : most;
-        hipLaunchKernelGGL((k_residual<S, T, LANES, K, DROP>), dim3((unsigned)((left + rows - 1) / rows)), threads_of<LANES>(), 0, st, b);
+        hipLaunchKernelGGL((k_residual<S, T, LANES, K, DROP>), dim3((unsigned)((left + rows - 1) / rows)), threads_of(LANES), 0, st, b);
     }
 }
 template <typename S, typename T, bool DROP> void go(const Args& a, bool back, int blocks, hipStream_t st) {
