@@ -3,11 +3,12 @@ paper_2505_05086_amd.lm.
 
     embedding          token lookup with scaling; its gradient by sorted tokens
     qk_norm_rotate     norms of queries and keys for each head with the position rotation
-    token_logprobs_grad  the loss and its gradient in the logits in one pass, the gradient in the logits' place
+    residual_norm      what lies between two blocks: dropout of a block's output, its sum with the stream, the next block's norm
+    linear_logprobs    the loss from the hidden states and the table, without the logits
     AdamW              one launch for all tensors, states in 8 bits, the gradients' norm clipped on the way
     token_logprobs     at the end, the next token and its alternatives, one token at a time over a cache of keys and values
 
-    python examples/finetune_lm.py [--steps 150] [--state-bits 8]
+    python examples/finetune_lm.py [--steps 150] [--state-bits 8] [--dropout 0.0]
 
 The data is synthetic: every token is followed by the one that a fixed permutation gives.
 """
@@ -37,8 +38,8 @@ class Block(nn.Module):
         self.down = asi.AsiLinear(ff, dim, bias=False, ranks=ranks, seed=4)
         self.q_gain, self.k_gain = nn.Parameter(torch.ones(self.head_dim)), nn.Parameter(torch.ones(self.head_dim))
 
-    def forward(self, x, cos, sin, positions, cache=None):
-        q, k, v = self.qkv(self.norm1(x)).split([n * self.head_dim for n in (self.heads, self.k_heads, self.k_heads)], -1)
+    def attend(self, x, cos, sin, positions, cache=None):
+        q, k, v = self.qkv(x).split([n * self.head_dim for n in (self.heads, self.k_heads, self.k_heads)], -1)
         heads = lambda t: t.unflatten(-1, (-1, self.head_dim))  # noqa: E731
         q, k = asi.qk_norm_rotate(heads(q), heads(k), self.q_gain, self.k_gain, cos, sin, positions, heads_first=True)
         v = heads(v).transpose(1, 2)
@@ -48,46 +49,58 @@ class Block(nn.Module):
             cache[:] = k, v
         each = self.heads // self.k_heads
         y = F.scaled_dot_product_attention(q, k.repeat_interleave(each, 1), v.repeat_interleave(each, 1), is_causal=q.shape[2] > 1)
-        x = x + self.out(y.transpose(1, 2).flatten(2))
-        gate, up = self.up(self.norm2(x)).chunk(2, -1)
-        return x + self.down(F.silu(gate) * up)
+        return self.out(y.transpose(1, 2).flatten(2))
+
+    def feed(self, x):
+        gate, up = self.up(x).chunk(2, -1)
+        return self.down(F.silu(gate) * up)
 
 
 class Decoder(nn.Module):
-    """The output layer shares the embedding's table."""
+    """The output layer shares the embedding's table.  `seed` is on the GPU; a step that draws other numbers moves it on."""
 
     def __init__(self, vocab: int, dim: int = 128, layers: int = 2, heads: int = 4, k_heads: int = 2, ff: int = 256, length: int = 512,
-                 ranks=(8, 16, 32)):
+                 ranks=(8, 16, 32), dropout: float = 0.0):
         super().__init__()
+        self.dropout = dropout
         self.table = nn.Parameter(torch.randn(vocab, dim) * dim ** -0.5)
         self.blocks = nn.ModuleList(Block(dim, heads, k_heads, ff, ranks) for _ in range(layers))
         self.norm = nn.RMSNorm(dim)
         cos, sin = asi.rotary_table(length, dim // heads, device="cpu")
         self.register_buffer("cos", cos)
         self.register_buffer("sin", sin)
+        self.register_buffer("seed", torch.zeros(1, dtype=torch.int64))
+
+    def hidden(self, tokens, start: int = 0, caches=None):
+        """The output layer's input."""
+        positions = torch.arange(start, start + tokens.shape[1], device=tokens.device)
+        p = self.dropout if self.training else 0.0
+        eps = torch.finfo(torch.float32).eps
+        x = asi.embedding(tokens, self.table, scale=math.sqrt(self.table.shape[1]))
+        if p:
+            x = asi.dropout(x, p, self.seed, 2 * len(self.blocks))
+        x, h = asi.residual_norm(x, pre_gain=self.blocks[0].norm1.weight, eps=eps)
+        for n, block in enumerate(self.blocks):
+            y = block.attend(h, self.cos, self.sin, positions, None if caches is None else caches[n])
+            x, h = asi.residual_norm(x, y, pre_gain=block.norm2.weight, post_norm=False, eps=eps, p=p, seed=self.seed, offset=2 * n)
+            norm = self.blocks[n + 1].norm1 if n + 1 < len(self.blocks) else self.norm
+            x, h = asi.residual_norm(x, block.feed(h), pre_gain=norm.weight, post_norm=False, eps=eps, p=p, seed=self.seed, offset=2 * n + 1)
+        return h
 
     def forward(self, tokens, start: int = 0, caches=None):
-        positions = torch.arange(start, start + tokens.shape[1], device=tokens.device)
-        x = asi.embedding(tokens, self.table, scale=math.sqrt(self.table.shape[1]))
-        for n, block in enumerate(self.blocks):
-            x = block(x, self.cos, self.sin, positions, None if caches is None else caches[n])
-        return self.norm(x) @ self.table.t()
+        return self.hidden(tokens, start, caches) @ self.table.t()
 
 
 def train_step(model, optimizer, tokens, clip: float = 1.0) -> torch.Tensor:
     """One step on (batch, length) tokens, each position's target the next token.  Nothing waits for the GPU."""
-    logits = model(tokens)
     targets = torch.cat((tokens[:, 1:], torch.full_like(tokens[:, :1], asi.lm.IGNORE_INDEX)), 1)
-    weights = torch.full(targets.shape, -1.0 / targets[:, 1:].numel(), device=tokens.device)
-    with torch.no_grad():
-        r = asi.token_logprobs_grad(logits, targets, weights, out=logits)
-        loss = (r.logprob * weights).sum()
+    loss = asi.linear_logprobs(model.hidden(tokens), model.table, targets).logprob.sum() * (-1.0 / targets[:, 1:].numel())
     optimizer.zero_grad(set_to_none=True)
-    # the products behind the logits need the table and their inputs, not the logits: their gradient may take their place
-    logits.backward(r.grad)
+    loss.backward()
+    model.seed.add_(1)
     norm = torch.linalg.vector_norm(torch.stack([p.grad.norm() for p in model.parameters()]))
     optimizer.step(grad_scale=(clip / norm).clamp(max=1.0).reshape(1))
-    return loss
+    return loss.detach()
 
 
 @torch.no_grad()
@@ -104,10 +117,11 @@ def generate(model, tokens, count: int, top: int = 3):
     return torch.cat(found, 1), torch.stack(scores, 1)
 
 
-def main(steps: int = 150, state_bits: int = 8, vocab: int = 997, batch: int = 8, length: int = 64, device: str = "cuda", quiet: bool = False):
+def main(steps: int = 150, state_bits: int = 8, vocab: int = 997, batch: int = 8, length: int = 64, device: str = "cuda", quiet: bool = False,
+         dropout: float = 0.0):
     torch.manual_seed(0)
     follows = torch.randperm(vocab, device=device)
-    model = Decoder(vocab).to(device)
+    model = Decoder(vocab, dropout=dropout).to(device)
     decayed = [p for p in model.parameters() if p.dim() > 1]
     optimizer = asi.AdamW([{"params": decayed}, {"params": [p for p in model.parameters() if p.dim() < 2], "weight_decay": 0.0}], lr=3e-3,
                           weight_decay=0.01, state_bits=state_bits)
@@ -135,5 +149,6 @@ if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--steps", type=int, default=150)
     ap.add_argument("--state-bits", type=int, default=8, choices=(8, 32))
+    ap.add_argument("--dropout", type=float, default=0.0)
     a = ap.parse_args()
-    main(a.steps, a.state_bits)
+    main(a.steps, a.state_bits, dropout=a.dropout)
