@@ -40,7 +40,8 @@ template <int B> struct Shape {
     static constexpr size_t kLds = 4 * B * kStep * 2 > B * (2 * B + 16) ? 4 * B * kStep * 2 : B * (2 * B + 16);      // two buffers, or a tile in bf16
 };
 
-// What the gradient needs of a row: p = exp2(scale' (x - top) - log2sum); dz = [target] a - p (a + b (log p + entropy))
+// What the gradient needs of a row: p = exp2(scale' (x - top) - log2sum); dz = [target] a - p (a + b (log p + entropy)).  Of the target
+// a (1 - p) is -a expm1(log p), which keeps its bits where p is nearly 1.
 struct RowInfo {
     float top, log2sum, a, b, entropy;
     int target, pad[2];
@@ -204,7 +205,7 @@ struct LogitArgs {
     long long all;                                   // tokens of the vocabulary where the GPU decides on the pieces; 0: it does not
     int number;                                      // the piece's
     float scale;
-    // values: [tile][top, sum, along][rows], the targets' logits [rows]
+    // values: [tile][top, ones, rest, along][rows], the targets' logits [rows]
     const int *live;
     const int64_t* targets;
     float *part, *target_logit;
@@ -227,16 +228,43 @@ __device__ __forceinline__ bool my_piece(const Split& s, long long all, int numb
     return true;
 }
 
+// Of a set of logits: the largest, how many are as large, the sum of exp(scale d) over the others (d = x - top), and sum exp(scale d) d.
+// The ones are counted apart: where one token is nearly sure, the others' sum is all that its log probability is made of, and added to
+// 1 it would lose its last bits.
 struct Joined {
-    float top, sum, along;
+    float top, ones, rest, along;
+    __device__ __forceinline__ float all() const { return ones + rest; }
 };
-// of two sets of logits: the largest, sum exp(scale d) and sum exp(scale d) d with d = x - top
 __device__ __forceinline__ Joined join(Joined a, Joined b, float c) {
     const float top = fmaxf(a.top, b.top), base = top == -INFINITY ? 0.f : top;
     const float da = fmaxf(a.top - base, kLow), db = fmaxf(b.top - base, kLow);
-    const float ea = __builtin_amdgcn_exp2f(da * c), eb = __builtin_amdgcn_exp2f(db * c);
+    const float ea = __builtin_amdgcn_exp2f(da * c), eb = __builtin_amdgcn_exp2f(db * c), sa = a.all(), sb = b.all();
+    const bool as = a.top == top, bs = b.top == top;
     // sums that are NaN stay NaN: they are multiplied, not compared
-    return Joined{top, a.sum * ea + b.sum * eb, ea * fmaf(a.sum, da, a.along) + eb * fmaf(b.sum, db, b.along)};
+    return Joined{top, (as ? a.ones : 0.f) + (bs ? b.ones : 0.f), (as ? a.rest : sa * ea) + (bs ? b.rest : sb * eb),
+                  ea * fmaf(sa, da, a.along) + eb * fmaf(sb, db, b.along)};
+}
+// The sums over logits of a lane, base being the largest (0 if that is -infinity).  exp2 of 0 is 1 exactly, and its fraction 0.
+struct Summed {
+    float all = 0.f, rest = 0.f, along = 0.f;
+    __device__ __forceinline__ void add(float x, float base, float c) {
+        const float d = max_nan(x - base, kLow), e = __builtin_amdgcn_exp2f(d * c);
+        all += e;
+        rest += __builtin_amdgcn_fractf(e);
+        along = fmaf(e, d, along);
+    }
+    __device__ __forceinline__ void across(int lanes) {
+        all += __shfl_xor(all, lanes);
+        rest += __shfl_xor(rest, lanes);
+        along += __shfl_xor(along, lanes);
+    }
+    __device__ __forceinline__ Joined joined(float top) const { return Joined{top, rintf(all - rest), rest, along}; }
+};
+__device__ __forceinline__ void store_joined(float* to, long long apart, const Joined& x) {
+    to[0] = x.top;
+    to[apart] = x.ones;
+    to[2 * apart] = x.rest;
+    to[3 * apart] = x.along;
 }
 
 template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2) void k_logits(const LogitArgs a) {
@@ -277,18 +305,13 @@ template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2)
             for (int r = 0; r < 16; ++r) top = fmaxf(top, t.acc[i][j][r]);
         top = fmaxf(top, __shfl_xor(top, 32));
         const float base = top == -INFINITY ? 0.f : top;
-        float sum = 0.f, along = 0.f;
+        Summed sum;
 #pragma unroll
         for (int i = 0; i < Tl::kM; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float d = max_nan(t.acc[i][j][r] - base, kLow), e = __builtin_amdgcn_exp2f(d * c);
-                sum += e;
-                along = fmaf(e, d, along);
-            }
-        sum += __shfl_xor(sum, 32);
-        along += __shfl_xor(along, 32);
-        if (lane < 32) shared[Tl::wave_m() * BN + col] = Joined{top, sum, along};
+            for (int r = 0; r < 16; ++r) sum.add(t.acc[i][j][r], base, c);
+        sum.across(32);
+        if (lane < 32) shared[Tl::wave_m() * BN + col] = sum.joined(top);
         if (a.targets) {
             const long long target = row < rows ? a.targets[a.live[row]] - a.first - v0 : -1;
             if (__any(target >= 0 && target < BM / 2)) {
@@ -305,10 +328,7 @@ template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2)
         const long long row = tn * BN + threadIdx.x;
         if (row < rows) {
             const Joined x = join(shared[threadIdx.x], shared[BN + threadIdx.x], c);
-            float* to = a.part + (a.first_part + tm) * 3 * a.part_rows + row;
-            to[0] = x.top;
-            to[a.part_rows] = x.sum;
-            to[2 * a.part_rows] = x.along;
+            store_joined(a.part + (a.first_part + tm) * 4 * a.part_rows + row, a.part_rows, x);
         }
     }
 }
@@ -344,6 +364,17 @@ template <typename Tl, int BM, int BN, typename F> __device__ __forceinline__ vo
     }
 }
 
+// dz of a logit that is not the target's, and of the target's
+__device__ __forceinline__ float of_logit(float z, const RowInfo& f, float c) {
+    const float x = fmaf(z - f.top, c, -f.log2sum), p = __builtin_amdgcn_exp2f(x);
+    return -p * (f.b != 0.f ? fmaf(f.b, fmaf(max_nan(x, kLow), 1.f / kLog2e, f.entropy), f.a) : f.a);
+}
+__device__ __forceinline__ float of_target(float z, const RowInfo& f, float c) {
+    const float logp = max_nan(fmaf(z - f.top, c, -f.log2sum), kLow) * (1.f / kLog2e);
+    const float d = -f.a * expm1f(logp);
+    return f.b != 0.f ? fmaf(-expf(logp) * f.b, logp + f.entropy, d) : d;
+}
+
 template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2) void k_logits_grad(const LogitArgs given) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     constexpr int BM = B, BN = B;
@@ -369,26 +400,32 @@ template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2)
         RowInfo f{0.f, INFINITY, 0.f, 0.f, 0.f, -1, {0, 0}};
         if (row < rows) f = a.info[row];
         const long long target = f.target >= 0 ? f.target - a.first - v0 : -1;
+        const bool here = __any(target >= 0 && target < BM / 2);
+        float hit = 0.f;                             // the target's logit
+        if (here) {
+#pragma unroll
+            for (int i = 0; i < Tl::kM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) hit = target == 32 * i + Tl::row_of(r) ? t.acc[i][j][r] : hit;
+        }
         if (__any(f.b != 0.f)) {                     // NaN too
 #pragma unroll
             for (int i = 0; i < Tl::kM; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float x = fmaf(t.acc[i][j][r] - f.top, c, -f.log2sum), p = __builtin_amdgcn_exp2f(x);
-                    t.acc[i][j][r] = -p * fmaf(f.b, fmaf(max_nan(x, kLow), 1.f / kLog2e, f.entropy), f.a);
-                }
+                for (int r = 0; r < 16; ++r) t.acc[i][j][r] = of_logit(t.acc[i][j][r], f, c);
         } else {
 #pragma unroll
             for (int i = 0; i < Tl::kM; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) t.acc[i][j][r] = -f.a * __builtin_amdgcn_exp2f(fmaf(t.acc[i][j][r] - f.top, c, -f.log2sum));
         }
-        if (__any(target >= 0 && target < BM / 2)) {
+        if (here) {
+            const float of = of_target(hit, f, c);
 #pragma unroll
             for (int i = 0; i < Tl::kM; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (target == 32 * i + Tl::row_of(r)) t.acc[i][j][r] += f.a;
+                    if (target == 32 * i + Tl::row_of(r)) t.acc[i][j][r] = of;
         }
     }
     if (v0 + BM / 2 > a.vocab) {                     // behind the vocabulary's end
@@ -429,13 +466,14 @@ constexpr int kFewWaves = 4, kFewAhead = 8;
 template <typename T> struct FewStep;               // the k of a wave's load of 16 bytes a lane
 template <> struct FewStep<bf16_t> { static constexpr int k = 32; };
 template <> struct FewStep<float> { static constexpr int k = 16; };
-__device__ __forceinline__ v4f few_product(const Vec16<bf16_t>& w, const Vec16<bf16_t>& h, v4f c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, w.raw), __builtin_bit_cast(v8bf, h.raw), c, 0, 0, 0);
+// Products of load number u, added to one of several sums: short chains are faster, and their roundings fewer: one chain over 3875 entries in
+// fp32 left 1.3e-5 of a log probability near 0, eight 8e-6.
+__device__ __forceinline__ void few_product(const Vec16<bf16_t>& w, const Vec16<bf16_t>& h, int u, v4f* sums, int count) {
+    sums[u % count] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, w.raw), __builtin_bit_cast(v8bf, h.raw), sums[u % count], 0, 0, 0);
 }
-__device__ __forceinline__ v4f few_product(const Vec16<float>& w, const Vec16<float>& h, v4f c) {
+__device__ __forceinline__ void few_product(const Vec16<float>& w, const Vec16<float>& h, int u, v4f* sums, int count) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(w.get(i), h.get(i), c, 0, 0, 0);
-    return c;
+    for (int i = 0; i < 4; ++i) sums[(4 * u + i) % count] = __builtin_amdgcn_mfma_f32_16x16x4f32(w.get(i), h.get(i), sums[(4 * u + i) % count], 0, 0, 0);
 }
 template <typename T> __device__ __forceinline__ Vec16<T> few_load(const T* p, int count) {
     Loose<T, Vec16<T>::N> v;
@@ -453,9 +491,12 @@ template <typename T, int NB> __global__ __launch_bounds__(64 * kFewWaves) void 
 #pragma unroll
     for (int b = 0; b < NB; ++b) h[b] = static_cast<const T*>(a.h) + (16 * b + col < a.rows ? 16 * b + col : 0) * a.h_stride;
     constexpr int step = FewStep<T>::k, ahead = NB > 2 ? kFewAhead / 2 : kFewAhead, all = Vec16<T>::N;
-    v4f acc[NB];
+    constexpr int sums = NB == 1 ? 8 : 4;
+    v4f part[NB][sums], acc[NB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) acc[b] = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < sums; ++i) part[b][i] = v4f{0.f, 0.f, 0.f, 0.f};
     const int k = (lane >> 4) * all;
     int at = 0;
     for (; at + step * ahead <= a.dim; at += step * ahead) {
@@ -469,13 +510,21 @@ template <typename T, int NB> __global__ __launch_bounds__(64 * kFewWaves) void 
 #pragma unroll
         for (int u = 0; u < ahead; ++u)
 #pragma unroll
-            for (int b = 0; b < NB; ++b) acc[b] = few_product(wv[u], hv[b][u], acc[b]);
+            for (int b = 0; b < NB; ++b) few_product(wv[u], hv[b][u], u, part[b], sums);
     }
     for (; at < a.dim; at += step) {
         const int count = at + k < a.dim ? a.dim - at - k : 0;
         const Vec16<T> wv = few_load(w + at + k, count);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) acc[b] = few_product(wv, few_load(h[b] + at + k, count), acc[b]);
+        for (int b = 0; b < NB; ++b) few_product(wv, few_load(h[b] + at + k, count), 0, part[b], sums);
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+        for (int n = sums / 2; n; n >>= 1)
+#pragma unroll
+            for (int i = 0; i < n; ++i) part[b][i] += part[b][i + n];
+        acc[b] = part[b][0];
     }
     // a lane has tokens v0 + 4 (lane / 16) + r of rows 16 b + col
     const float c = a.scale * kLog2e;
@@ -493,18 +542,12 @@ template <typename T, int NB> __global__ __launch_bounds__(64 * kFewWaves) void 
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const float base = top == -INFINITY ? 0.f : top;
-        float sum = 0.f, along = 0.f;
+        Summed sum;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float d = max_nan(acc[b][r] - base, kLow), e = __builtin_amdgcn_exp2f(d * c);
-            sum += e;
-            along = fmaf(e, d, along);
-        }
-        sum += __shfl_xor(sum, 16);
-        along += __shfl_xor(along, 16);
-        sum += __shfl_xor(sum, 32);
-        along += __shfl_xor(along, 32);
-        if (lane < 16) shared[wave][16 * b + lane] = Joined{top, sum, along};
+        for (int r = 0; r < 4; ++r) sum.add(acc[b][r], base, c);
+        sum.across(16);
+        sum.across(32);
+        if (lane < 16) shared[wave][16 * b + lane] = sum.joined(top);
         const long long row = 16 * b + col;
         if (a.targets && row < a.rows) {
             const long long target = a.targets[row] - first;
@@ -519,10 +562,7 @@ template <typename T, int NB> __global__ __launch_bounds__(64 * kFewWaves) void 
         Joined x = shared[0][threadIdx.x];
 #pragma unroll
         for (int i = 1; i < kFewWaves; ++i) x = join(x, shared[i][threadIdx.x], c);
-        float* to = a.part + (long long)blockIdx.x * 3 * a.part_rows + threadIdx.x;
-        to[0] = x.top;
-        to[a.part_rows] = x.sum;
-        to[2 * a.part_rows] = x.along;
+        store_joined(a.part + (long long)blockIdx.x * 4 * a.part_rows + threadIdx.x, a.part_rows, x);
     }
 }
 
@@ -559,18 +599,20 @@ template <int ROWS> __global__ __launch_bounds__(256) void k_join(const JoinArgs
     float top = -INFINITY;
     const float* p = a.part + at;
     if (at < rows)
-        for (long long i = share; i < a.parts; i += kShares) top = fmaxf(top, p[i * 3 * a.part_rows]);
+        for (long long i = share; i < a.parts; i += kShares) top = fmaxf(top, p[i * 4 * a.part_rows]);
     const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, along = 0.f;
+    Joined sum{top, 0.f, 0.f, 0.f};
     if (at < rows)
 #pragma unroll 4
         for (long long i = share; i < a.parts; i += kShares) {
-            const float* q = p + i * 3 * a.part_rows;
-            const float d = fmaxf(q[0] - base, kLow), e = __builtin_amdgcn_exp2f(d * c), s = q[a.part_rows];
-            sum = fmaf(s, e, sum);
-            along = fmaf(fmaf(s, d, q[2 * a.part_rows]), e, along);
+            const float* q = p + i * 4 * a.part_rows;
+            const float own = q[0], ones = q[a.part_rows], rest = q[2 * a.part_rows];
+            const float d = fmaxf(own - base, kLow), e = __builtin_amdgcn_exp2f(d * c);
+            sum.ones += own == top ? ones : 0.f;
+            sum.rest += own == top ? rest : (ones + rest) * e;
+            sum.along = fmaf(fmaf(ones + rest, d, q[3 * a.part_rows]), e, sum.along);
         }
-    shared[share][in] = Joined{top, sum, along};
+    shared[share][in] = sum;
     __syncthreads();
     for (int n = kShares / 2; n; n >>= 1) {
         if (share < n) shared[share][in] = join(shared[share][in], shared[share + n][in], c);
@@ -579,14 +621,16 @@ template <int ROWS> __global__ __launch_bounds__(256) void k_join(const JoinArgs
     if (share || at >= rows) return;
     const Joined x = shared[0][in];
     const long long row = a.live ? a.live[at] : at;
-    const bool empty = x.top == -INFINITY && !(x.sum != x.sum);
-    const float logsum = empty ? 0.f : logf(x.sum), entropy = empty ? 0.f : fmaxf(logsum - a.scale * (x.along / x.sum), 0.f) + (x.sum - x.sum);
+    const float all = x.all();
+    const bool nan = all != all, empty = x.top == -INFINITY && !nan;
+    const float logsum = empty ? 0.f : nan ? NAN : logf(x.ones) + log1pf(x.rest / x.ones);
+    const float entropy = empty ? 0.f : nan ? NAN : fmaxf(logsum - a.scale * (x.along / all), 0.f);
     const int64_t target = a.targets ? a.targets[row] : 0;
     const bool left_out = a.targets && target == a.ignore;      // where the rows have not been sorted out
     if (a.logprob) {
         float v = NAN;
         if (target >= 0 && target < a.vocab) v = empty ? -INFINITY : fmaf(a.scale, a.target_logit[at] - x.top, -logsum);
-        if (x.sum != x.sum) v = NAN;
+        if (nan) v = NAN;
         a.logprob[row] = left_out ? 0.f : v;
     }
     if (a.entropy) a.entropy[row] = left_out ? 0.f : entropy;
@@ -658,9 +702,8 @@ template <typename T, int ROWS, int COLS> __global__ __launch_bounds__(256) void
             const RowInfo f = info[r];
             float d = 0.f;
             if (v < tokens && f.target != kLeftOut) {
-                const float x = fmaf(a.logits[((long long)(r / 16) * a.vocab + v0 + v) * 16 + r % 16] - f.top, c, -f.log2sum), p = __builtin_amdgcn_exp2f(x);
-                d = f.b != 0.f ? -p * fmaf(f.b, fmaf(max_nan(x, kLow), 1.f / kLog2e, f.entropy), f.a) : -f.a * p;
-                if (f.target == v0 + v) d += f.a;
+                const float z = a.logits[((long long)(r / 16) * a.vocab + v0 + v) * 16 + r % 16];
+                d = f.target == v0 + v ? of_target(z, f, c) : of_logit(z, f, c);
             }
             dz[v][r] = d;
         }
@@ -749,9 +792,8 @@ template <int TB> __global__ __launch_bounds__(256) void k_few_grad_f32(const Fe
             const RowInfo f = info[r];
             float d = 0.f;
             if (turn < to && turn * 16 + v < a.vocab && f.target != kLeftOut) {
-                const float x = fmaf(a.logits[((long long)i * a.vocab + turn * 16 + v) * 16 + r % 16] - f.top, c, -f.log2sum), p = __builtin_amdgcn_exp2f(x);
-                d = f.b != 0.f ? -p * fmaf(f.b, fmaf(max_nan(x, kLow), 1.f / kLog2e, f.entropy), f.a) : -f.a * p;
-                if (f.target == turn * 16 + v) d += f.a;
+                const float z = a.logits[((long long)i * a.vocab + turn * 16 + v) * 16 + r % 16];
+                d = f.target == turn * 16 + v ? of_target(z, f, c) : of_logit(z, f, c);
             }
             dz[turn & 1][r][v] = d;
         }
@@ -1020,7 +1062,7 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
         p.hidden = take((size_t)p.planes * rows * p.packed_dim * 2);
         if (p.staged) p.weights = take((size_t)p.planes * p.piece * p.packed_dim * 2);
     }
-    p.part = take((size_t)p.parts * 3 * rows * 4);
+    p.part = take((size_t)p.parts * 4 * rows * 4);
     p.target = take(rows * 4);
     if (grad) {
         p.info = take(rows * sizeof(RowInfo));

@@ -261,6 +261,38 @@ def test_large_logits_and_scales(dtype):
         _close(r.weight, want.weight, want.weight_bound, "weight")
 
 
+@pytest.mark.parametrize("rows", [1, 5, 30, 300])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_nearly_sure_tokens(rows, dtype):
+    """Log probabilities of targets with p near 1, and their gradients, are good to a share of themselves, not of 1: what is left is
+    the others' sum, each of whose terms is off by twice the logits' error and a few roundings."""
+    dim, vocab = 64, 700
+    hidden, weight, targets, a, _ = _inputs(rows, dim, vocab, DTYPES[dtype], 16, ignored=0.0, spread=0.8)
+    # the target's logit is about 24 * 64 * 0.01 = 15, the others' have a deviation of about 2: 700 of them sum up to 700 e^2 e^-15 = 2^-9 of it
+    hidden = (hidden.float() + 24.0 * weight[targets].float()).to(hidden.dtype)
+    z = hidden.double() @ weight.double().t().contiguous()
+    e = (6 * dim + 16) * U * (hidden.double().abs() @ weight.double().abs().t().contiguous()).amax(-1)
+    at = targets[:, None]
+    others = (z - z.gather(1, at)).scatter(1, at, -INF).exp().sum(-1)
+    assert float(others.min()) < 2.0 ** -8
+    want = -torch.log1p(others)
+    share = 2 * e + 256 * U
+    for r in (asi.linear_logprobs(hidden, weight, targets), asi.linear_logprobs_grad(hidden, weight, targets, a)):
+        _close(r.logprob, want, share * want.abs(), "logprob")
+    # rows of which the target's own part of dz, a (1 - p), is all that W's row of it meets: the sum over the vocabulary cancels for
+    # weights that are all the same, so dz is looked at through weights that are zero but for one token
+    one = torch.zeros_like(weight)
+    token = int(targets[0])
+    one[token] = weight[token]
+    r = asi.linear_logprobs_grad(hidden[:1], one, targets[:1], a[:1])
+    z0 = (hidden[:1].double() @ one[token].double())[0]
+    rest = (vocab - 1) * (-z0).exp()
+    dz = float(a[0]) * float(rest / (1 + rest))
+    want = dz * one[token].double()[None]
+    bound = ((2 * e[0] + 256 * U + 2 * _round(weight.dtype)) * want.abs())
+    _close(r.hidden, want, bound, "hidden")
+
+
 def test_layouts():
     hidden, weight, targets, a, _ = _inputs(60, 64, 500, torch.bfloat16, 9)
     want = asi.linear_logprobs_grad(hidden, weight, targets, a)
