@@ -29,6 +29,10 @@ constexpr float kLow = -1e30f;                       // stands for -infinity whe
 // rows 51 and 40, of 64 rows and 50001 x 1000, which tiles cannot take as it lies, 54 and 77; bf16 gradients of 8 rows 112 and 121, of 12
 // rows 218 and 123.)
 constexpr int kFewF32 = 128, kFewBf16 = 16, kFewBf16Packed = 64, kFewGradBf16 = 8, kFewGradVector = 8, kFewAtOnce = 64;
+// Up to this many rows of bf16, dz is held in two parts of bf16: rounded to one, its error adds as much as the results' own rounding does where
+// many rows' errors meet, but more than that where a few rows make up the gradient.  (256 rows x 2048 x 32000: 268 us, with one part 205;
+// 128 rows: 200 and 162.)
+constexpr int kFineRows = 256;
 constexpr int kLeftOut = -2;                         // a RowInfo's target: the row is left out
 constexpr size_t kPieceBytes = size_t(96) << 20;     // dz of a piece, in bf16
 
@@ -216,7 +220,6 @@ struct LogitArgs {
     long long dz_stride, dz_plane;
 };
 
-constexpr int pairs_of(int planes) { return planes == 1 ? 1 : kPairs; }
 // The piece that is asked for, as decided on the GPU; `w`: the weights, moved on to it.  False: there is no such piece.
 __device__ __forceinline__ bool my_piece(const Split& s, long long all, int number, long long* first, long long* n, Operand* w) {
     if (!all) return true;
@@ -278,7 +281,7 @@ template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2)
     t.clear();
     Operand h = a.h;
     h.rows = rows;
-    t.template run<pairs_of(PLANES)>(a.w, h, tm * BM, tn * BN, 0, a.k_steps, lds);
+    t.template run<PLANES == 1 ? kOne : kSix>(a.w, h, tm * BM, tn * BN, 0, a.k_steps, lds);
     __syncthreads();
     const float c = a.scale * kLog2e;
     const int lane = threadIdx.x & 63;
@@ -375,7 +378,8 @@ __device__ __forceinline__ float of_target(float z, const RowInfo& f, float c) {
     return f.b != 0.f ? fmaf(-expf(logp) * f.b, logp + f.entropy, d) : d;
 }
 
-template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2) void k_logits_grad(const LogitArgs given) {
+// PLANES: of the inputs; DZ: of dz
+template <int B, int PLANES, int DZ> __global__ __launch_bounds__(Shape<B>::kThreads, 2) void k_logits_grad(const LogitArgs given) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     constexpr int BM = B, BN = B;
     using Tl = typename Shape<B>::template Of<false, false>;
@@ -390,7 +394,7 @@ template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2)
     t.clear();
     Operand h = a.h;
     h.rows = rows;
-    t.template run<pairs_of(PLANES)>(a.w, h, tm * BM, tn * BN, 0, a.k_steps, lds);
+    t.template run<PLANES == 1 ? kOne : kSix>(a.w, h, tm * BM, tn * BN, 0, a.k_steps, lds);
     const float c = a.scale * kLog2e;
     const int lane = threadIdx.x & 63;
     const long long v0 = tm * BM + Tl::at_m();
@@ -439,11 +443,11 @@ template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2)
                 }
     }
 #pragma unroll
-    for (int p = 0; p < PLANES; ++p)
+    for (int p = 0; p < DZ; ++p)
         store_across<Tl, BM, BN>(lds, a.dz + p * a.dz_plane + tn * BN * a.dz_stride + tm * BM, a.dz_stride, rows - tn * BN, BM, true,
                                  [&](int i, int j, int r) -> uint32_t {
                                      const uint32_t bits = to_bf16(t.acc[i][j][r]).bits;
-                                     if (p + 1 < PLANES) t.acc[i][j][r] -= __uint_as_float(bits << 16);
+                                     if (p + 1 < DZ) t.acc[i][j][r] -= __uint_as_float(bits << 16);
                                      return bits;
                                  });
 }
@@ -893,7 +897,7 @@ struct ProductArgs {
 };
 
 // dH: rows along m, dim along n, the piece's vocabulary along k in `splits` parts
-template <int B, int PLANES> __device__ __forceinline__ void dhidden_tile(const ProductArgs& a, long long id, long long rows, int splits, char* lds) {
+template <int B, int DZ> __device__ __forceinline__ void dhidden_tile(const ProductArgs& a, long long id, long long rows, int splits, char* lds) {
     constexpr int BM = B, BN = B;
     using Tl = typename Shape<B>::template Of<false, true>;
     const long long n_tiles = (a.dim + BN - 1) / BN;
@@ -906,7 +910,7 @@ template <int B, int PLANES> __device__ __forceinline__ void dhidden_tile(const 
     t.clear();
     Operand dz = a.dz;
     dz.rows = rows;
-    if (to > from) t.template run<pairs_of(PLANES)>(dz, a.weights, tm * BM, tn * BN, from, to - from, lds);
+    if (to > from) t.template run<DZ == 1 ? kOne : DZ == 2 ? kTwoA : kSix>(dz, a.weights, tm * BM, tn * BN, from, to - from, lds);
     float* out = a.sums + split * rows * a.dim;
     const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -927,7 +931,7 @@ template <int B, int PLANES> __device__ __forceinline__ void dhidden_tile(const 
 }
 
 // dW: the rows are k.  bf16: dim along m, so that a lane has neighbours of a row of dW; fp32: dim along n, a line of a row a store
-template <int B, typename T> __device__ __forceinline__ void dweight_tile(const ProductArgs& a, long long id, long long rows, char* lds) {
+template <int B, typename T, int DZ> __device__ __forceinline__ void dweight_tile(const ProductArgs& a, long long id, long long rows, char* lds) {
     constexpr int BM = B, BN = B;
     using Tl = typename Shape<B>::template Of<true, true>;
     constexpr bool kDimFirst = sizeof(T) == 2;
@@ -939,7 +943,7 @@ template <int B, typename T> __device__ __forceinline__ void dweight_tile(const 
     Operand dz = a.dz, x = a.hidden;
     dz.rows = x.rows = rows;
     const int steps = (int)((rows + kStep - 1) / kStep);
-    if (steps) t.template run<kDimFirst ? 1 : kPairs>(kDimFirst ? x : dz, kDimFirst ? dz : x, tm * BM, tn * BN, 0, steps, lds);
+    if (steps) t.template run<DZ == 1 ? kOne : DZ == 2 ? kTwoB : kSix>(kDimFirst ? x : dz, kDimFirst ? dz : x, tm * BM, tn * BN, 0, steps, lds);
     if constexpr (kDimFirst) {
         store_across<Tl, BM, BN>(lds, static_cast<uint16_t*>(a.dw) + (a.first + tn * BN) * a.dim + tm * BM, a.dim, a.vocab - tn * BN, a.dim - tm * BM, a.whole,
                                  [&](int i, int j, int r) -> uint32_t { return to_bf16(t.acc[i][j][r]).bits; });
@@ -962,7 +966,7 @@ template <int B, typename T> __device__ __forceinline__ void dweight_tile(const 
 }
 
 // Both in one launch, dH's longer tiles first, so that neither waits for the other's last ones.
-template <int B, typename T> __global__ __launch_bounds__(Shape<B>::kThreads, 2) void k_products(const ProductArgs given) {
+template <int B, typename T, int DZ> __global__ __launch_bounds__(Shape<B>::kThreads, 2) void k_products(const ProductArgs given) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     ProductArgs a = given;
     const Split split = *a.split;
@@ -970,8 +974,8 @@ template <int B, typename T> __global__ __launch_bounds__(Shape<B>::kThreads, 2)
     if (!my_piece(split, a.all, a.number, &a.first, &a.vocab, &a.weights)) return;
     a.dz.ld = a.dz.cols = split.piece;
     const long long tiles = (rows + B - 1) / B * ((a.dim + B - 1) / B) * split.splits, first = a.dhidden ? (tiles + 7) / 8 * 8 : 0;
-    if (id < first) dhidden_tile<B, sizeof(T) == 4 ? kPlanes : 1>(a, id, rows, split.splits, lds);
-    else if (a.dweight) dweight_tile<B, T>(a, id - first, rows, lds);
+    if (id < first) dhidden_tile<B, DZ>(a, id, rows, split.splits, lds);
+    else if (a.dweight) dweight_tile<B, T, DZ>(a, id - first, rows, lds);
 }
 
 // dH's rows from their sums, four entries a thread; zeros for rows that are left out
@@ -997,7 +1001,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_hidden(const floa
 // ---- host ----
 struct Plan {
     bool f32, few, staged;                           // fp32; rows for k_few; weights are packed by pieces
-    int planes, k_steps;
+    int planes, dz_planes, k_steps;                  // of the inputs, and of dz
     long long rows, dim, vocab, packed_dim;
     int tile;                                        // 128 or 256
     bool flexible;
@@ -1023,6 +1027,7 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     Plan p{};
     p.f32 = d->dtype == ASI_F32;
     p.planes = p.f32 ? kPlanes : 1;
+    p.dz_planes = p.f32 ? kPlanes : d->rows <= kFineRows ? 2 : 1;
     p.rows = d->rows; p.dim = d->dim; p.vocab = d->vocab;
     p.packed_dim = up(d->dim, kStep);
     p.k_steps = (int)(p.packed_dim / kStep);
@@ -1072,7 +1077,7 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
             p.bytes = at;
             return p;
         }
-        p.dz = take((size_t)p.planes * (size_t)rows_up * p.piece * 2);
+        p.dz = take((size_t)p.dz_planes * (size_t)rows_up * p.piece * 2);
         p.sums = take((size_t)p.most_sums * d->dim * 4);
     }
     p.bytes = at;
@@ -1092,7 +1097,7 @@ struct Call {
     Operand packed_hidden() const { return Operand{at<uint16_t>(p.hidden), p.packed_dim, p.rows * p.packed_dim, p.rows, p.packed_dim}; }
 
     void rows_of(float* logprob, float* entropy, float* stats, bool grad, bool dhidden, bool dweight) {
-        const SplitArgs how{p.vocab, p.dim, up(p.rows, p.tile) * p.piece, p.piece, p.most_sums, p.most_splits, p.tile, p.f32 ? kPairs : 1, grad, p.flexible, dhidden, dweight};
+        const SplitArgs how{p.vocab, p.dim, up(p.rows, p.tile) * p.piece, p.piece, p.most_sums, p.most_splits, p.tile, p.f32 ? kPairs : p.dz_planes, grad, p.flexible, dhidden, dweight};
         const LiveArgs a{targets, p.rows, d->ignore_index, at<Split>(p.split), at<int>(p.live), at<int>(p.place), logprob, entropy, stats, how};
         if (targets) hipLaunchKernelGGL(k_live, 1, 1024, 0, st, a);
         else hipLaunchKernelGGL(k_all_live, dim3((unsigned)((p.rows + 255) / 256)), 256, 0, st, a);
@@ -1180,17 +1185,19 @@ struct Call {
         else tiles<B>(k_logits<B, 1>, one, count, a);
     }
     template <int B> void products(const LogitArgs& a, const ProductArgs& b) {
-        static LdsAllowed grad1, grad3, products2, products4;
+        static LdsAllowed grad1, grad2, grad3, products1, products2, products3;
         const long long row_tiles = up(p.rows, B) / B, dim_tiles = up(p.dim, B) / B;
         // no more tiles of logits in a piece than its memory holds, however it is cut
         const long long logit_tiles = up(p.piece, B) / B * row_tiles;
-        if (p.f32) tiles<B>(k_logits_grad<B, kPlanes>, grad3, logit_tiles, a);
-        else tiles<B>(k_logits_grad<B, 1>, grad1, logit_tiles, a);
+        if (p.f32) tiles<B>(k_logits_grad<B, kPlanes, kPlanes>, grad3, logit_tiles, a);
+        else if (p.dz_planes == 2) tiles<B>(k_logits_grad<B, 1, 2>, grad2, logit_tiles, a);
+        else tiles<B>(k_logits_grad<B, 1, 1>, grad1, logit_tiles, a);
         const long long hidden_tiles = b.dhidden ? up((up(p.most_sums, B) / B + p.most_splits) * dim_tiles, 8) : 0;
         const long long tokens = !b.all ? b.vocab : b.all < 2 * p.piece ? b.all : 2 * p.piece;
         const long long weight_tiles = b.dweight ? up(tokens, B) / B * dim_tiles : 0;
-        if (p.f32) tiles<B>(k_products<B, float>, products4, hidden_tiles + weight_tiles, b);
-        else tiles<B>(k_products<B, bf16_t>, products2, hidden_tiles + weight_tiles, b);
+        if (p.f32) tiles<B>(k_products<B, float, kPlanes>, products3, hidden_tiles + weight_tiles, b);
+        else if (p.dz_planes == 2) tiles<B>(k_products<B, bf16_t, 2>, products2, hidden_tiles + weight_tiles, b);
+        else tiles<B>(k_products<B, bf16_t, 1>, products1, hidden_tiles + weight_tiles, b);
     }
     void values(float* logprob, float* entropy, float* stats, RowInfo* info, const float* wa, const float* wb) {
         JoinArgs j{};
@@ -1222,7 +1229,7 @@ struct Call {
             LogitArgs a = p.flexible ? logit_args(weights(0, p.vocab), 0, p.vocab) : logit_args(weights(first, n), first, n);
             a.all = p.flexible ? p.vocab : 0;
             a.number = number;
-            a.info = at<RowInfo>(p.info); a.dz = at<uint16_t>(p.dz); a.dz_plane = p.rows * p.piece;
+            a.info = at<RowInfo>(p.info); a.dz = at<uint16_t>(p.dz); a.dz_plane = up(p.rows, p.tile) * p.piece;
             ProductArgs b{};
             b.dz = Operand{a.dz, p.piece, a.dz_plane, p.rows, p.piece};
             b.weights = a.w; b.hidden = a.h; b.split = a.split; b.vocab = a.vocab; b.first = a.first; b.all = a.all; b.number = number; b.dim = p.dim;

@@ -30,9 +30,12 @@ struct Operand {
     long long rows, cols;
 };
 
-// Pair number i of the six: which plane of either side.
-__device__ __forceinline__ int plane_a(int i) { return (0x001012 >> (4 * i)) & 15; }
-__device__ __forceinline__ int plane_b(int i) { return (0x010210 >> (4 * i)) & 15; }
+// What a product of planes consists of: one pair; A (or B) in two planes, the smaller first; or the six pairs of three planes a side.
+enum Pairs { kOne, kTwoA, kTwoB, kSix };
+constexpr int pairs_of(int pairs) { return pairs == kOne ? 1 : pairs == kSix ? kPairs : 2; }
+// Pair number i: which plane of either side.
+template <int PAIRS> __device__ __forceinline__ int plane_a(int i) { return PAIRS == kSix ? (0x001012 >> (4 * i)) & 15 : PAIRS == kTwoA ? 1 - i : 0; }
+template <int PAIRS> __device__ __forceinline__ int plane_b(int i) { return PAIRS == kSix ? (0x010210 >> (4 * i)) & 15 : PAIRS == kTwoB ? 1 - i : 0; }
 
 // copy16_to_lds (asi_device.h) in a form whose end the compiler does not track: it takes any transposing LDS read for one of what the
 // newest copies write, and would wait for them at once.  Here it is run() that waits, before the barrier that makes a buffer readable.
@@ -164,33 +167,33 @@ template <int BM, int BN, bool A_ACROSS, bool B_ACROSS, int WN = 2> struct Tile 
                 for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
     }
 
-    // Adds the products of PAIRS pairs of planes (1, or kPairs) over k_steps steps, one at least, from k = 64 first on.  The whole workgroup
+    // Adds the products of PAIRS' pairs of planes over k_steps steps, one at least, from k = 64 first on.  The whole workgroup
     // calls it.
     template <int PAIRS> __device__ __forceinline__ void run(const Operand& a, const Operand& b, long long m, long long n, int first, int k_steps, char* lds) {
         HalfA ha;
         HalfB hb;
         ha.lanes(a, wave_m());
         hb.lanes(b, wave_n());
-        const int total = k_steps * PAIRS;
+        const int total = k_steps * pairs_of(PAIRS);
         ha.start(a, m, first);
         hb.start(b, n, first);
         int at_pair = 0, at_step = 0;            // of the step that is copied next
         // without a branch: a step of the loop below is one block, or its last LDS reads would be moved behind its end
         auto moved_on = [&] {
-            if constexpr (PAIRS == 1) {
+            if constexpr (PAIRS == kOne) {
                 ha.move(false, 0, 0);
                 hb.move(false, 0, 0);
             } else {
                 const bool last = ++at_step == k_steps;
-                const int next = at_pair + 1 < PAIRS ? at_pair + 1 : at_pair;
-                ha.move(last, plane_a(next) - plane_a(at_pair), k_steps);
-                hb.move(last, plane_b(next) - plane_b(at_pair), k_steps);
+                const int next = at_pair + 1 < pairs_of(PAIRS) ? at_pair + 1 : at_pair;
+                ha.move(last, plane_a<PAIRS>(next) - plane_a<PAIRS>(at_pair), k_steps);
+                hb.move(last, plane_b<PAIRS>(next) - plane_b<PAIRS>(at_pair), k_steps);
                 at_step = last ? 0 : at_step;
                 at_pair = last ? next : at_pair;
             }
         };
-        ha.enter(PAIRS == 1 ? 0 : plane_a(0));
-        hb.enter(PAIRS == 1 ? 0 : plane_b(0));
+        ha.enter(plane_a<PAIRS>(0));
+        hb.enter(plane_b<PAIRS>(0));
 #pragma unroll
         for (int q = 0; q < HalfA::kCopies; ++q) ha.copy(lds, q);
 #pragma unroll
