@@ -1219,7 +1219,10 @@ struct Call {
         j.part = at<float>(p.part); j.target_logit = at<float>(p.target); j.part_rows = p.rows; j.parts = p.parts; j.vocab = p.vocab;
         j.ignore = d->ignore_index; j.rows = p.rows; j.targets = targets; j.scale = d->scale;
         j.logprob = logprob; j.entropy = entropy; j.stats = stats; j.info = info; j.a = wa; j.b = wb;
-        if (p.rows > 512) hipLaunchKernelGGL(k_join<32>, dim3((unsigned)((p.rows + 31) / 32)), 256, 0, st, j);
+        // rows of a workgroup: more share their loads' lines, fewer leave more workgroups (8190 rows of 391 parts, us: 32 62, 16 38, 8 44; 2731
+        // rows of 125: 32 25, 8 12)
+        if (p.rows > 4096) hipLaunchKernelGGL(k_join<16>, dim3((unsigned)((p.rows + 15) / 16)), 256, 0, st, j);
+        else if (p.rows > 512) hipLaunchKernelGGL(k_join<8>, dim3((unsigned)((p.rows + 7) / 8)), 256, 0, st, j);
         else hipLaunchKernelGGL(k_join<1>, dim3((unsigned)p.rows), 256, 0, st, j);
     }
     void gradients(void* dhidden, void* dweight) {
