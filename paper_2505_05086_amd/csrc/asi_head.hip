@@ -25,10 +25,10 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLow = -1e30f;                       // stands for -infinity where that is multiplied by 0
 // Rows that k_few and its gradients take; more are faster as a part of a tile.
-// (32000 x 2048, us: fp32 values of 128 rows 340 so and 598 in tiles, with gradients 1110 and 1496; bf16 values of 16 rows 36 and 38, of 32
-// rows 51 and 40, of 64 rows and 50001 x 1000, which tiles cannot take as it lies, 54 and 77; bf16 gradients of 8 rows 112 and 121, of 12
-// rows 218 and 123.)
-constexpr int kFewF32 = 128, kFewBf16 = 16, kFewBf16Packed = 64, kFewGradBf16 = 8, kFewGradVector = 8, kFewAtOnce = 64;
+// (2048 x 32000, us: fp32 values of 128 rows 324 so and 598 in tiles, with gradients 1240 and 1496; bf16 values of 16 rows 36 and 38, of 32
+// rows 51 and 40, gradients of 16 rows 112 and 146.  1000 x 50001, which tiles cannot take as it lies, bf16: values of 64 rows 61 and 77,
+// gradients of 32 rows 161 and 230, of 64 rows 341 and 244.  Gradients of 8 rows 108 by matrix instructions, 114 without.)
+constexpr int kFewF32 = 128, kFewBf16 = 16, kFewBf16Packed = 64, kFewGradPacked = 32, kFewGradVector = 4, kFewAtOnce = 64;
 // Up to this many rows of bf16, dz is held in two parts of bf16: rounded to one, its error adds as much as the results' own rounding does where
 // many rows' errors meet, but more than that where a few rows make up the gradient.  (256 rows x 2048 x 32000: 268 us, with one part 205;
 // 128 rows: 200 and 162.)
@@ -666,7 +666,7 @@ __global__ __launch_bounds__(256) void k_info(const InfoArgs a) {
 // ---- few rows' gradients ------------------------------------------------------------------------------------
 // dz of 64 tokens is made in LDS from their logits; then every token's row of the weights is read once, for dH, and its row of dW written
 // once, by lanes of COLS neighbouring columns that hold ROWS rows' hidden states and sums of dH in registers.  Where a row needs fewer
-// lanes than the workgroup has, tokens go round groups of lanes.  What bounds it: memory, from 12 rows on its 2 rows vocab dim products.
+// lanes than the workgroup has, tokens go round groups of lanes.  What bounds it: memory.
 struct FewGradArgs {
     const void *h, *w;
     long long h_stride, w_stride, vocab, dim;
@@ -759,10 +759,10 @@ template <typename T, int ROWS, int COLS> __global__ __launch_bounds__(256) void
         if (group == 0 && r < a.rows) store_some<COLS>(a.sums + ((long long)blockIdx.y * a.all_rows + r) * a.dim + col, count, sum[r]);
     }
 }
-// The same for 9 to 64 rows of fp32 by matrix instructions (16 x 16 x 4, fp32 throughout), where 2 rows vocab dim multiply-adds a side on
+// The same for 9 to 64 rows by matrix instructions (16 x 16 x 4, fp32 throughout), where 2 rows vocab dim multiply-adds a side on
 // the vector units would take longer than the memory.  A wave has 64 columns, lane l the four from 4 (l % 16) on, so that 16 lanes read a
 // row of W, or write one of dW, side by side: column 4 n + e is column n of block e of a matrix instruction.  TB: 16s of rows.
-template <int TB> __global__ __launch_bounds__(256) void k_few_grad_f32(const FewGradArgs a) {
+template <typename T, int TB> __global__ __launch_bounds__(256) void k_few_grad_tiles(const FewGradArgs a) {
     __shared__ float dz[2][16 * TB][17];             // two turns of 16 tokens
     __shared__ RowInfo info[16 * TB];
     if (threadIdx.x < 16 * TB) info[threadIdx.x] = (int)threadIdx.x < a.rows ? a.info[threadIdx.x] : RowInfo{0.f, INFINITY, 0.f, 0.f, 0.f, kLeftOut, {0, 0}};
@@ -770,7 +770,7 @@ template <int TB> __global__ __launch_bounds__(256) void k_few_grad_f32(const Fe
     const long long col = ((long long)blockIdx.x * 4 + (threadIdx.x >> 6)) * 64 + 4 * n;
     const int count = a.dim - col >= 4 ? 4 : a.dim > col ? (int)(a.dim - col) : 0;
     __syncthreads();
-    const float *hidden = static_cast<const float*>(a.h), *weights = static_cast<const float*>(a.w);
+    const T *hidden = static_cast<const T*>(a.h), *weights = static_cast<const T*>(a.w);
     float h[4 * TB][4];                              // rows 4 j + k
     v4f sum[TB][4];
 #pragma unroll
@@ -781,7 +781,7 @@ template <int TB> __global__ __launch_bounds__(256) void k_few_grad_f32(const Fe
         for (int e = 0; e < 4; ++e) sum[t][e] = v4f{0.f, 0.f, 0.f, 0.f};
     const float c = a.scale * kLog2e;
     const long long turns = (a.vocab + 15) / 16, from = turns * blockIdx.y / a.blocks, to = turns * (blockIdx.y + 1) / a.blocks;
-    auto load = [&](long long turn, Loose<float, 4>* w) {
+    auto load = [&](long long turn, Loose<T, 4>* w) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const long long v = turn * 16 + 4 * i + k;
@@ -802,12 +802,12 @@ template <int TB> __global__ __launch_bounds__(256) void k_few_grad_f32(const Fe
             dz[turn & 1][r][v] = d;
         }
     };
-    Loose<float, 4> w[4];
+    Loose<T, 4> w[4];
     load(from, w);
     gradients(from);
     __syncthreads();
     for (long long turn = from; turn < to; ++turn) {
-        Loose<float, 4> ahead[4];
+        Loose<T, 4> ahead[4];
         load(turn + 1, ahead);
         gradients(turn + 1);
         const float(*d)[17] = dz[turn & 1];
@@ -835,7 +835,7 @@ template <int TB> __global__ __launch_bounds__(256) void k_few_grad_f32(const Fe
             for (int r = 0; r < 4; ++r) {
                 float f[4] = {out[0][r], out[1][r], out[2][r], out[3][r]};
                 const long long v = turn * 16 + 4 * k + r;
-                float* to = static_cast<float*>(a.dw) + v * a.dim + col;
+                T* to = static_cast<T*>(a.dw) + v * a.dim + col;
                 if (a.add) {
                     float before[4];
                     load_some<4>(to, v < a.vocab ? count : 0, before);
@@ -1023,6 +1023,9 @@ asi_status check(const asi_linear_logprob_desc* d) {
     if (d->rows * up(d->dim, kStep) / 8 > most_workgroups(256) * 256) return ASI_ERR_UNSUPPORTED;          // threads of k_pack
     return ASI_OK;
 }
+// Tiles of a packed piece of n tokens: where they are too few to fill half the chip, small ones, which are through sooner (849 tokens of 1023
+// rows x 1000 fp32: 68 us, 118 in large ones).
+int piece_tile(const Plan& p, long long n) { return p.tile == 256 && p.staged && up(p.rows, 256) / 256 * (up(n, 256) / 256) < 128 ? 128 : p.tile; }
 Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     Plan p{};
     p.f32 = d->dtype == ASI_F32;
@@ -1032,7 +1035,7 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     p.packed_dim = up(d->dim, kStep);
     p.k_steps = (int)(p.packed_dim / kStep);
     const bool as_it_lies = !p.f32 && d->dim % kStep == 0 && d->weight_stride % 8 == 0 && d->weight_stride < (1 << 21) && !d->any_address;
-    p.few = d->rows <= (p.f32 ? kFewF32 : grad ? kFewGradBf16 : as_it_lies ? kFewBf16 : kFewBf16Packed);
+    p.few = d->rows <= (p.f32 ? kFewF32 : as_it_lies ? kFewBf16 : grad ? kFewGradPacked : kFewBf16Packed);
     p.staged = !p.few && !as_it_lies;
     p.tile = up(d->rows, 256) / 256 * (up(d->vocab, 256) / 256) >= 256 ? 256 : 128;
     const long long rows_up = up(d->rows, p.tile);
@@ -1044,6 +1047,10 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     if (p.staged && p.piece > most_packed) p.piece = most_packed > 4096 ? most_packed : p.piece < 4096 ? p.piece : 4096;
     p.flexible = !p.staged;
     p.parts = p.few ? (d->vocab + 16 * kFewWaves - 1) / (16 * kFewWaves) : (d->vocab + p.tile - 1) / p.tile;
+    if (p.staged) {
+        const long long last = d->vocab % p.piece;
+        p.parts = d->vocab / p.piece * (p.piece / p.tile) + (last ? (last + piece_tile(p, last) - 1) / piece_tile(p, last) : 0);
+    }
     // parts that the vocabulary of a piece may be cut in for dH, and the memory for their sums: twice what fills the chip, but no more than
     // half a piece's or twice dH's size in fp32
     const long long tiles = (rows_up / p.tile) * (up(d->dim, p.tile) / p.tile), slots = p.tile == 256 ? 256 : 512;
@@ -1054,7 +1061,7 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     if (p.most_splits < 2) p.most_splits = 2;
     p.most_sums = d->rows * p.most_splits;
     // blocks of the vocabulary for few rows' gradients: workgroups for the chip, two to four a CU, each with 64 tokens at least
-    const long long few_columns = d->rows <= 4 ? 2048 : d->rows <= kFewGradVector ? 1024 : 256, few_want = 1024 / ((d->dim + few_columns - 1) / few_columns);
+    const long long few_columns = d->rows <= kFewGradVector ? 2048 : 256, few_want = 1024 / ((d->dim + few_columns - 1) / few_columns);
     const long long few_most = (d->vocab + kFewTokens - 1) / kFewTokens, few_cap = few_want < 1 ? 1 : few_want > 512 ? 512 : few_want;
     p.few_blocks = (int)(few_cap < few_most ? few_cap : few_most);
     size_t at = 0;
@@ -1150,19 +1157,19 @@ struct Call {
         return FewGradArgs{hidden, weight, d->hidden_stride, d->weight_stride, p.vocab, p.dim, (int)p.rows, (int)p.rows, lanes, p.few_blocks, false, d->scale,
                            at<float>(p.logits), at<RowInfo>(p.info), dhidden ? at<float>(p.sums) : nullptr, dweight};
     }
-    void few_grad_f32(void* dhidden, void* dweight) {
+    template <typename T> void few_grad_tiles(void* dhidden, void* dweight) {
         for (long long base = 0; base < p.rows; base += kFewAtOnce) {
             FewGradArgs a = few_args(dhidden, dweight, 64);
             a.rows = (int)(p.rows - base < kFewAtOnce ? p.rows - base : kFewAtOnce);
-            a.h = static_cast<const float*>(hidden) + base * d->hidden_stride;
+            a.h = static_cast<const T*>(hidden) + base * d->hidden_stride;
             a.logits += base * p.vocab;
             a.info += base;
             if (a.sums) a.sums += base * p.dim;
             a.add = base > 0;
             const dim3 grid((unsigned)((p.dim + 255) / 256), (unsigned)p.few_blocks);
-            if (a.rows <= 16) hipLaunchKernelGGL(k_few_grad_f32<1>, grid, 256, 0, st, a);
-            else if (a.rows <= 32) hipLaunchKernelGGL(k_few_grad_f32<2>, grid, 256, 0, st, a);
-            else hipLaunchKernelGGL(k_few_grad_f32<4>, grid, 256, 0, st, a);
+            if (a.rows <= 16) hipLaunchKernelGGL((k_few_grad_tiles<T, 1>), grid, 256, 0, st, a);
+            else if (a.rows <= 32) hipLaunchKernelGGL((k_few_grad_tiles<T, 2>), grid, 256, 0, st, a);
+            else hipLaunchKernelGGL((k_few_grad_tiles<T, 4>), grid, 256, 0, st, a);
         }
     }
     template <typename T, int ROWS, int COLS> void few_grad(void* dhidden, void* dweight) {
@@ -1173,9 +1180,8 @@ struct Call {
     }
     template <typename T> void few_gradients(void* dhidden, void* dweight) {
         if (!dhidden && !dweight) return;
-        if (p.rows <= 4) few_grad<T, 4, 8>(dhidden, dweight);
-        else if (p.rows <= kFewGradVector) few_grad<T, 8, 4>(dhidden, dweight);
-        else few_grad_f32(dhidden, dweight);
+        if (p.rows <= kFewGradVector) few_grad<T, 4, 8>(dhidden, dweight);
+        else few_grad_tiles<T>(dhidden, dweight);
         if (dhidden) hipLaunchKernelGGL(k_few_hidden<T>, dim3((unsigned)((p.rows * p.dim + 31) / 32)), 256, 0, st, at<float>(p.sums), p.few_blocks, p.rows, p.dim, static_cast<T*>(dhidden));
     }
     template <int B> void logits(const LogitArgs& a) {
@@ -1210,7 +1216,7 @@ struct Call {
                 LogitArgs a = logit_args(weights(first, n), first, n);
                 a.live = at<int>(p.live); a.targets = targets; a.part = at<float>(p.part); a.target_logit = at<float>(p.target);
                 a.part_rows = p.rows; a.first_part = first / p.tile;
-                if (p.tile == 256) logits<256>(a);
+                if (piece_tile(p, n) == 256) logits<256>(a);
                 else logits<128>(a);
             }
             j.split = at<Split>(p.split);
@@ -1240,7 +1246,7 @@ struct Call {
             b.sums = at<float>(p.sums); b.add = first > 0;
             b.dw = dweight;
             b.whole = p.dim % 8 == 0 && aligned(dweight, 16);
-            if (p.tile == 256) products<256>(a, b);
+            if (piece_tile(p, n) == 256) products<256>(a, b);
             else products<128>(a, b);
         }
         if (dhidden) {

@@ -138,7 +138,7 @@ def test_gradients(size, dtype):
 
 
 @pytest.mark.parametrize("rows,dim,vocab,dtype", [(2100, 64, 20000, "bf16"), (2100, 65, 17000, "f32"), (20, 64, 40000, "f32"), (5000, 128, 7001, "bf16"),
-                                                  (600, 1024, 2500, "bf16"), (9, 2048, 70001, "bf16")])
+                                                  (600, 1024, 2500, "bf16"), (9, 2048, 70001, "bf16"), (1100, 64, 39700, "f32"), (200, 72, 160000, "bf16")])
 def test_several_pieces_of_the_vocabulary(rows, dim, vocab, dtype):
     hidden, weight, targets, a, b = _inputs(rows, dim, vocab, DTYPES[dtype], rows)
     want = _Definition(hidden, weight, targets, 1.0, a, b)
