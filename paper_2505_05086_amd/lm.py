@@ -5,6 +5,9 @@ position rotation, dropout without a stored mask, the edge between two blocks, A
 Thin layer over the C ABI of include/asi_lm.h: it checks and marshals arguments, allocates results and scratch from
 torch's allocator on the current stream, and wires the calls into autograd where an input requires a gradient.  All
 arithmetic runs in the HIP kernels; there is no CPU fallback.
+
+Calls and their gradient functions can be captured into a graph.  A backward pass by torch's engine can be, with leaves that no living eager
+graph holds: the engine would join the captured stream with theirs, which ends the process.
 """
 from __future__ import annotations
 
