@@ -531,7 +531,7 @@ template <typename T, int NB> __global__ __launch_bounds__(64 * kFewWaves) void 
             for (int i = 0; i < n; ++i) part[b][i] += part[b][i + n];
         acc[b] = part[b][0];
     }
-    // a lane has tokens v0 + 4 (lane / 16) + r of rows 16 b + col
+    // a lane has tokens v0 + 4 (lane / 16) + r of rows 16 b + col; logits have room for the groups of 16 that have a row, and no others
     const float c = a.scale * kLog2e;
     const long long first = v0 + 4 * (lane >> 4);
 #pragma unroll
@@ -540,7 +540,7 @@ template <typename T, int NB> __global__ __launch_bounds__(64 * kFewWaves) void 
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             if (first + r >= a.vocab) acc[b][r] = -INFINITY;
-            else if (a.logits) a.logits[((long long)b * a.vocab + first + r) * 16 + col] = acc[b][r];
+            else if (a.logits && 16 * b < a.rows) a.logits[((long long)b * a.vocab + first + r) * 16 + col] = acc[b][r];
             top = fmaxf(top, acc[b][r]);
         }
         if (!a.part) continue;

@@ -11,6 +11,8 @@ import torch
 from torch.autograd import forward_ad
 
 import paper_2505_05086_amd as asi
+from paper_2505_05086_amd import binding as B
+from paper_2505_05086_amd.lm import _DTYPE, LinearLogprobs
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -402,3 +404,32 @@ def test_refusals():
             f(hidden, weight, targets, scale=scale)
     with forward_ad.dual_level(), pytest.raises(NotImplementedError):
         f(forward_ad.make_dual(hidden, hidden), weight, targets)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows", [1, 5, 16, 17, 33, 40, 48, 49, 65, 97, 100, 112, 113, 128, 129, 300])
+def test_nothing_is_written_behind_the_workspace(rows, dtype):
+    """A workspace of the stated size, full of NaN; what lies behind it stays as it is.  A narrow head over a large vocabulary has little
+    behind its logits that a store too many could fall on."""
+    dim, vocab = 8, 9001
+    hidden, weight, targets, a, b = _inputs(rows, dim, vocab, DTYPES[dtype], 40 + rows)
+    want = _Definition(hidden, weight, targets, 1.0, a, b)
+    desc = B.LinearLogprobDesc(rows, dim, vocab, hidden.stride(0), weight.stride(0), IGNORE, _DTYPE[hidden.dtype], 1.0, 0, 0)
+    L = B.lib()
+    for f in (L.asi_linear_logprobs_workspace_bytes, L.asi_linear_logprobs_grad_workspace_bytes):
+        size = f(desc)
+        ws = torch.full((size + (1 << 22),), 255, dtype=torch.uint8, device="cuda")
+        logprob, entropy = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        st = torch.cuda.current_stream().cuda_stream
+        if f is L.asi_linear_logprobs_workspace_bytes:
+            status = L.asi_linear_logprobs(desc, hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), logprob.data_ptr(), entropy.data_ptr(),
+                                           None, ws.data_ptr(), size, st)
+        else:
+            dh, dw = torch.empty_like(hidden), torch.empty_like(weight)
+            status = L.asi_linear_logprobs_grad(desc, 0, hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), None, logprob.data_ptr(),
+                                                entropy.data_ptr(), a.data_ptr(), b.data_ptr(), dh.data_ptr(), dw.data_ptr(), ws.data_ptr(), size, st)
+            _close(dh, want.hidden, want.hidden_bound, "hidden")
+            _close(dw, want.weight, want.weight_bound, "weight")
+        assert status == 0
+        _check_values(LinearLogprobs(logprob, entropy), want, targets)
+        assert bool((ws[size:] == 255).all())
