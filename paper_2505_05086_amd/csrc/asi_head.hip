@@ -5,9 +5,11 @@
 //   k_pack        their hidden states next to each other, k filled up with zeros to whole steps; fp32 as three planes of bf16.  The
 //                 same for a piece of the weights where they cannot be read as they lie (fp32, rows that are no whole vectors)
 //   k_logits      a tile of logits, vocabulary along the registers of a lane and tokens along the lanes, so that a token's maximum
-//                 and sums over 128 (64) of the vocabulary stay in a lane but for one exchange.  Values: (x_max, sum e, sum e d) of
-//                 each token, d = x - x_max, e = exp(scale d), and the target's logit.  Gradient: dz, rounded to bf16
-//   k_few         the same values for few rows, the weights from memory straight into the matrix instructions; k_few_grad their gradients
+//                 and sums over 128 (64) of the vocabulary stay in a lane but for one exchange.  Values: x_max, how many logits are
+//                 as large, sum e over the others and sum e d of each token, d = x - x_max, e = exp(scale d), and the target's logit
+//   k_logits_grad the same tiles as dz, rounded to bf16 in one, two or three parts
+//   k_few         the values for few rows, the weights from memory straight into the matrix instructions; k_few_grad and
+//                 k_few_grad_tiles their gradients from the logits that it leaves, 16 rows a column
 //   k_join        joins the tiles' values
 //   k_products    the products of dz with weights (dH) and hidden states (dW), read across as they lie (asi_tiles.h)
 //   k_hidden      the sums of dH, in fp32 over the pieces of the vocabulary and the parts of a piece, to their rows
@@ -34,13 +36,15 @@ constexpr int kFewF32 = 128, kFewBf16 = 16, kFewBf16Packed = 64, kFewGradPacked 
 // many rows' errors meet, but more than that where a few rows make up the gradient.  (256 rows x 2048 x 32000: 268 us, with one part 205;
 // 128 rows: 200 and 162.)
 constexpr int kFineRows = 256;
+typedef float v4f __attribute__((ext_vector_type(4)));
 constexpr int kLeftOut = -2;                         // a RowInfo's target: the row is left out
+constexpr int kKeepSteps = 8;
 constexpr size_t kPieceBytes = size_t(96) << 20;     // dz of a piece, in bf16
 
 // Tiles of 256 x 256 by 8 waves where they fill the chip (8190 x 2048 logits of 100003: 2.76 ms, with tiles of 128 3.26), of 128 x 128 by
 // 4 waves, two workgroups a CU, where they would not.
 template <int B> struct Shape {
-    static constexpr int WN = B == 256 ? 4 : 2, kThreads = 128 * WN, kSlots = B == 256 ? 256 : 512;
+    static constexpr int WN = B == 256 ? 4 : 2, kThreads = 128 * WN;
     template <bool A, bool X> using Of = Tile<B, B, A, X, WN>;
     static constexpr size_t kLds = 4 * B * kStep * 2 > B * (2 * B + 16) ? 4 * B * kStep * 2 : B * (2 * B + 16);      // two buffers, or a tile in bf16
 };
@@ -215,6 +219,7 @@ struct LogitArgs {
     const int64_t* targets;
     float *part, *target_logit;
     long long part_rows, first_part;
+    float* kept;                                     // the tiles' logits as lanes hold them, from the values to the gradient
     // gradient
     const RowInfo* info;
     uint16_t* dz;                                    // [row][dz_stride], planes apart
@@ -271,7 +276,19 @@ __device__ __forceinline__ void store_joined(float* to, long long apart, const J
     to[3 * apart] = x.along;
 }
 
-template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2) void k_logits(const LogitArgs a) {
+// A lane's logits of its workgroup's tile, four at a time, the lanes' next to each other.  Values and gradient have the same tiles in the same
+// order, so each lane finds its own again.
+template <typename Tl, typename F> __device__ __forceinline__ void each_kept(float* kept, F f) {
+    v4f* at = reinterpret_cast<v4f*>(kept) + (long long)blockIdx.x * (Tl::kM * Tl::kN * 4 * Tl::kThreads) + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < Tl::kM; ++i)
+#pragma unroll
+        for (int j = 0; j < Tl::kN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) f(at[((i * Tl::kN + j) * 4 + q) * Tl::kThreads], i, j, 4 * q);
+}
+
+template <int B, int PLANES, bool KEEP> __global__ __launch_bounds__(Shape<B>::kThreads, 2) void k_logits(const LogitArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     constexpr int BM = B, BN = B;
     using Tl = typename Shape<B>::template Of<false, false>;
@@ -283,6 +300,8 @@ template <int B, int PLANES> __global__ __launch_bounds__(Shape<B>::kThreads, 2)
     Operand h = a.h;
     h.rows = rows;
     t.template run<PLANES == 1 ? kOne : kSix>(a.w, h, tm * BM, tn * BN, 0, a.k_steps, lds);
+    if constexpr (KEEP)
+        each_kept<Tl>(a.kept, [&](v4f& at, int i, int j, int r) { at = v4f{t.acc[i][j][r], t.acc[i][j][r + 1], t.acc[i][j][r + 2], t.acc[i][j][r + 3]}; });
     __syncthreads();
     const float c = a.scale * kLog2e;
     const int lane = threadIdx.x & 63;
@@ -379,7 +398,7 @@ __device__ __forceinline__ float of_target(float z, const RowInfo& f, float c) {
     return f.b != 0.f ? fmaf(-expf(logp) * f.b, logp + f.entropy, d) : d;
 }
 
-// PLANES: of the inputs; DZ: of dz
+// PLANES: of the inputs, 0 where the logits were kept; DZ: of dz
 template <int B, int PLANES, int DZ> __global__ __launch_bounds__(Shape<B>::kThreads, 2) void k_logits_grad(const LogitArgs given) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     constexpr int BM = B, BN = B;
@@ -392,10 +411,17 @@ template <int B, int PLANES, int DZ> __global__ __launch_bounds__(Shape<B>::kThr
     long long tm, tn;
     if (!my_tile(blockIdx.x, (a.vocab + BM - 1) / BM, (rows + BN - 1) / BN, 1024 / BM, &tm, &tn)) return;
     Tl t;
-    t.clear();
-    Operand h = a.h;
-    h.rows = rows;
-    t.template run<PLANES == 1 ? kOne : kSix>(a.w, h, tm * BM, tn * BN, 0, a.k_steps, lds);
+    if constexpr (PLANES == 0) {
+        each_kept<Tl>(a.kept, [&](const v4f& at, int i, int j, int r) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t.acc[i][j][r + e] = at[e];
+        });
+    } else {
+        t.clear();
+        Operand h = a.h;
+        h.rows = rows;
+        t.template run<PLANES == 1 ? kOne : kSix>(a.w, h, tm * BM, tn * BN, 0, a.k_steps, lds);
+    }
     const float c = a.scale * kLog2e;
     const int lane = threadIdx.x & 63;
     const long long v0 = tm * BM + Tl::at_m();
@@ -466,7 +492,6 @@ struct FewArgs {
     float* logits;                                   // [16 rows][token][16], for the gradients; nullable
     long long part_rows;
 };
-typedef float v4f __attribute__((ext_vector_type(4)));
 constexpr int kFewWaves = 4, kFewAhead = 8;
 template <typename T> struct FewStep;               // the k of a wave's load of 16 bytes a lane
 template <> struct FewStep<bf16_t> { static constexpr int k = 32; };
@@ -1006,11 +1031,12 @@ struct Plan {
     long long rows, dim, vocab, packed_dim;
     int tile;                                        // 128 or 256
     bool flexible;
+    bool keep;                                       // logits are kept from the values to the gradient
     long long parts;                                 // of the values
     long long piece;                                 // tokens of a piece of the gradient, and of packed weights
     long long most_sums, most_splits;
     int few_blocks;                                  // of the vocabulary for few rows
-    size_t logits, split, live, place, hidden, weights, part, target, info, dz, sums, bytes;      // offsets
+    size_t logits, kept, split, live, place, hidden, weights, part, target, info, dz, sums, bytes;      // offsets
 };
 long long up(long long x, long long to) { return (x + to - 1) / to * to; }
 
@@ -1066,6 +1092,9 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     const long long few_columns = d->rows <= kFewGradVector ? 2048 : 256, few_want = 1024 / ((d->dim + few_columns - 1) / few_columns);
     const long long few_most = (d->vocab + kFewTokens - 1) / kFewTokens, few_cap = few_want < 1 ? 1 : few_want > 512 ? 512 : few_want;
     p.few_blocks = (int)(few_cap < few_most ? few_cap : few_most);
+    // The logits of a vocabulary that is one piece, in fp32, where they are no larger than dz may be and dearer to compute again than to read
+    const long long kept = 4 * rows_up * up(d->vocab, p.tile);
+    p.keep = grad && !p.few && p.piece >= d->vocab && kept <= (long long)(kPieceBytes / 2) && p.k_steps * (p.f32 ? kPairs : 1) >= kKeepSteps;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += round256(bytes); return here; };
     const size_t rows = (size_t)d->rows;
@@ -1086,6 +1115,7 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
             p.bytes = at;
             return p;
         }
+        if (p.keep) p.kept = take((size_t)kept);
         p.dz = take((size_t)p.dz_planes * (size_t)rows_up * p.piece * 2);
         p.sums = take((size_t)p.most_sums * d->dim * 4);
     }
@@ -1119,12 +1149,12 @@ struct Call {
         if (p.f32) hipLaunchKernelGGL(k_pack<float>, grid, 256, 0, st, a);
         else hipLaunchKernelGGL(k_pack<bf16_t>, grid, 256, 0, st, a);
     }
-    // the weights of tokens first .. first + n - 1 as an operand
-    Operand weights(long long first, long long n) {
+    // the weights of tokens first .. first + n - 1 as an operand; `packed`: the call before has packed the same
+    Operand weights(long long first, long long n, bool packed = false) {
         const char* from = static_cast<const char*>(weight) + first * d->weight_stride * (p.f32 ? 4 : 2);
         if (!p.staged) return Operand{reinterpret_cast<const uint16_t*>(from), d->weight_stride, 0, n, p.dim};
         uint16_t* out = at<uint16_t>(p.weights);
-        pack(from, d->weight_stride, n, nullptr, nullptr, out, p.piece * p.packed_dim);
+        if (!packed) pack(from, d->weight_stride, n, nullptr, nullptr, out, p.piece * p.packed_dim);
         return Operand{out, p.packed_dim, p.piece * p.packed_dim, n, p.packed_dim};
     }
     template <int B, typename K, typename A> void tiles(K kernel, LdsAllowed& allowed, long long count, const A& a) {
@@ -1187,17 +1217,22 @@ struct Call {
         if (dhidden) hipLaunchKernelGGL(k_few_hidden<T>, dim3((unsigned)((p.rows * p.dim + 31) / 32)), 256, 0, st, at<float>(p.sums), p.few_blocks, p.rows, p.dim, static_cast<T*>(dhidden));
     }
     template <int B> void logits(const LogitArgs& a) {
-        static LdsAllowed one, three;
+        static LdsAllowed one, three, kept1, kept3;
         const long long count = up(a.vocab, B) / B * (up(p.rows, B) / B);
-        if (p.f32) tiles<B>(k_logits<B, kPlanes>, three, count, a);
-        else tiles<B>(k_logits<B, 1>, one, count, a);
+        if (a.kept && p.f32) tiles<B>(k_logits<B, kPlanes, true>, kept3, count, a);
+        else if (a.kept) tiles<B>(k_logits<B, 1, true>, kept1, count, a);
+        else if (p.f32) tiles<B>(k_logits<B, kPlanes, false>, three, count, a);
+        else tiles<B>(k_logits<B, 1, false>, one, count, a);
     }
     template <int B> void products(const LogitArgs& a, const ProductArgs& b) {
-        static LdsAllowed grad1, grad2, grad3, products1, products2, products3;
+        static LdsAllowed grad1, grad2, grad3, kept1, kept2, kept3, products1, products2, products3;
         const long long row_tiles = up(p.rows, B) / B, dim_tiles = up(p.dim, B) / B;
         // no more tiles of logits in a piece than its memory holds, however it is cut
         const long long logit_tiles = up(p.piece, B) / B * row_tiles;
-        if (p.f32) tiles<B>(k_logits_grad<B, kPlanes, kPlanes>, grad3, logit_tiles, a);
+        if (a.kept && p.f32) tiles<B>(k_logits_grad<B, 0, kPlanes>, kept3, logit_tiles, a);
+        else if (a.kept && p.dz_planes == 2) tiles<B>(k_logits_grad<B, 0, 2>, kept2, logit_tiles, a);
+        else if (a.kept) tiles<B>(k_logits_grad<B, 0, 1>, kept1, logit_tiles, a);
+        else if (p.f32) tiles<B>(k_logits_grad<B, kPlanes, kPlanes>, grad3, logit_tiles, a);
         else if (p.dz_planes == 2) tiles<B>(k_logits_grad<B, 1, 2>, grad2, logit_tiles, a);
         else tiles<B>(k_logits_grad<B, 1, 1>, grad1, logit_tiles, a);
         const long long hidden_tiles = b.dhidden ? up((up(p.most_sums, B) / B + p.most_splits) * dim_tiles, 8) : 0;
@@ -1218,6 +1253,7 @@ struct Call {
                 LogitArgs a = logit_args(weights(first, n), first, n);
                 a.live = at<int>(p.live); a.targets = targets; a.part = at<float>(p.part); a.target_logit = at<float>(p.target);
                 a.part_rows = p.rows; a.first_part = first / p.tile;
+                if (p.keep && info) a.kept = at<float>(p.kept);
                 if (piece_tile(p, n) == 256) logits<256>(a);
                 else logits<128>(a);
             }
@@ -1233,13 +1269,15 @@ struct Call {
         else if (p.rows > 512) hipLaunchKernelGGL(k_join<8>, dim3((unsigned)((p.rows + 7) / 8)), 256, 0, st, j);
         else hipLaunchKernelGGL(k_join<1>, dim3((unsigned)p.rows), 256, 0, st, j);
     }
-    void gradients(void* dhidden, void* dweight) {
+    // `after_values`: values() of the same call has run
+    void gradients(void* dhidden, void* dweight, bool after_values) {
         int number = 0;
         for (long long first = 0; first < p.vocab && (dhidden || dweight); first += p.piece, ++number) {
             const long long n = p.vocab - first < p.piece ? p.vocab - first : p.piece;
-            LogitArgs a = p.flexible ? logit_args(weights(0, p.vocab), 0, p.vocab) : logit_args(weights(first, n), first, n);
+            LogitArgs a = p.flexible ? logit_args(weights(0, p.vocab), 0, p.vocab) : logit_args(weights(first, n, after_values && p.piece >= p.vocab), first, n);
             a.all = p.flexible ? p.vocab : 0;
             a.number = number;
+            if (p.keep && after_values) a.kept = at<float>(p.kept);
             a.info = at<RowInfo>(p.info); a.dz = at<uint16_t>(p.dz); a.dz_plane = up(p.rows, p.tile) * p.piece;
             ProductArgs b{};
             b.dz = Operand{a.dz, p.piece, a.dz_plane, p.rows, p.piece};
@@ -1327,7 +1365,7 @@ asi_status asi_linear_logprobs_grad(const asi_linear_logprob_desc* desc, int giv
     } else {
         c.values(logprob, entropy, nullptr, info, grad_logprob, grad_entropy);
     }
-    if (!c.p.few) c.gradients(dhidden, dweight);
+    if (!c.p.few) c.gradients(dhidden, dweight, !given);
     else if (c.p.f32) c.few_gradients<float>(dhidden, dweight);
     else c.few_gradients<bf16_t>(dhidden, dweight);
     return c.status != ASI_OK ? c.status : launched();

@@ -138,7 +138,6 @@ template <int BM, int BN, bool A_ACROSS, bool B_ACROSS, int WN = 2> struct Tile 
     using HalfA = Half<BM, A_ACROSS, 2 * WN, 2>;
     using HalfB = Half<BN, B_ACROSS, 2 * WN, WN>;
     static constexpr int kBuffer = HalfA::kBytes + HalfB::kBytes;
-    static constexpr int kLds = 2 * kBuffer;
     v16f acc[kM][kN];
 
     __device__ __forceinline__ static int wave_m() { return threadIdx.x / (64 * WN); }
