@@ -27,11 +27,13 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLow = -1e30f;                       // stands for -infinity where that is multiplied by 0
-// Rows that k_few and its gradients take; more are faster as a part of a tile.
-// (2048 x 32000, us: fp32 values of 128 rows 324 so and 598 in tiles, with gradients 1240 and 1496; bf16 values of 16 rows 36 and 38, of 32
-// rows 51 and 40, gradients of 16 rows 112 and 146.  1000 x 50001, which tiles cannot take as it lies, bf16: values of 64 rows 61 and 77,
-// gradients of 32 rows 161 and 230, of 64 rows 341 and 244.  Gradients of 8 rows 108 by matrix instructions, 114 without.)
-constexpr int kFewF32 = 128, kFewBf16 = 16, kFewBf16Packed = 64, kFewGradPacked = 32, kFewGradVector = 4, kFewAtOnce = 64;
+// Rows that k_few and its gradients take; more are faster as a part of a tile.  (us so, and in tiles.  fp32 2048 x 32000: values of 64 rows 176
+// and 301, of 100 325 and 308, with gradients of 64 541 and 568, of 100 1183 and 622.  bf16 as it lies, 2048 x 32000: values of 16 rows 36 and
+// 38, of 32 rows 51 and 40, gradients of 16 rows 112 and 146.  bf16 that tiles cannot take as it lies: values of 64 rows 1000 x 50001 62 and 62,
+// 200 x 50001 28 and 36; where rows are no whole vectors, 1001 x 50001, of 32 rows 101 and 91, of 64 165 and 91, 1001 x 3000 of 32 31 and 31;
+// gradients of 32 rows 1000 x 50001 163 and 144, 200 x 50001 61 and 92, 1000 x 3000 38 and 58, of 48 rows 317, 110, 52 and 148, 94, 60.
+// Gradients of 8 rows 108 by matrix instructions, 114 without.)
+constexpr int kFewF32 = 64, kFewBf16 = 16, kFewBf16Whole = 64, kFewBf16Packed = 32, kFewGradVector = 4;
 // Up to this many rows of bf16, dz is held in two parts of bf16: rounded to one, its error adds as much as the results' own rounding does where
 // many rows' errors meet, but more than that where a few rows make up the gradient.  (256 rows x 2048 x 32000: 268 us, with one part 205;
 // 128 rows: 200 and 162.)
@@ -40,6 +42,10 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 constexpr int kLeftOut = -2;                         // a RowInfo's target: the row is left out
 constexpr int kKeepSteps = 8;
 constexpr size_t kPieceBytes = size_t(96) << 20;     // dz of a piece, in bf16
+// Packed weights of a piece.  They are larger than that of a few rows' dz, so that a piece has tiles for the whole chip: fp32 with gradients,
+// 150 rows x 2048 x 60000, us: 3054 with 96 MiB, 2396 with 192, 1962 with 384, 1398 with 768; 700 x 1000 x 32000 1212, 997 with 192 and more;
+// of values alone, 150 x 2048 x 60000, 1168, 816, 610, 628; 1023 x 1000 x 50001 637, 676, 638, 636.
+constexpr size_t kPackedBytes = size_t(768) << 20;
 
 // Tiles of 256 x 256 by 8 waves where they fill the chip (8190 x 2048 logits of 100003: 2.76 ms, with tiles of 128 3.26), of 128 x 128 by
 // 4 waves, two workgroups a CU, where they would not.
@@ -490,7 +496,6 @@ struct FewArgs {
     const int64_t* targets;
     float *part, *target_logit;                      // nullable, both
     float* logits;                                   // [16 rows][token][16], for the gradients; nullable
-    long long part_rows;
 };
 constexpr int kFewWaves = 4, kFewAhead = 8;
 template <typename T> struct FewStep;               // the k of a wave's load of 16 bytes a lane
@@ -592,7 +597,7 @@ template <typename T, int NB> __global__ __launch_bounds__(64 * kFewWaves) void 
         Joined x = shared[0][threadIdx.x];
 #pragma unroll
         for (int i = 1; i < kFewWaves; ++i) x = join(x, shared[i][threadIdx.x], c);
-        store_joined(a.part + (long long)blockIdx.x * 4 * a.part_rows + threadIdx.x, a.part_rows, x);
+        store_joined(a.part + (long long)blockIdx.x * 4 * a.rows + threadIdx.x, a.rows, x);
     }
 }
 
@@ -696,8 +701,7 @@ __global__ __launch_bounds__(256) void k_info(const InfoArgs a) {
 struct FewGradArgs {
     const void *h, *w;
     long long h_stride, w_stride, vocab, dim;
-    int rows, all_rows, lanes, blocks;               // rows of this launch and of the call; lanes of a row (a power of two, up to 256); blocks of the vocabulary
-    bool add;                                        // to what the launch before has written into dw
+    int rows, lanes, blocks;                         // lanes of a row (a power of two, up to 256); blocks of the vocabulary
     float scale;
     const float* logits;                             // [16 rows][token][16]
     const RowInfo* info;
@@ -782,7 +786,7 @@ template <typename T, int ROWS, int COLS> __global__ __launch_bounds__(256) void
                     for (int e = 0; e < COLS; ++e) sum[r][e] += share[(g * a.lanes + lane) * COLS + e];
             }
         }
-        if (group == 0 && r < a.rows) store_some<COLS>(a.sums + ((long long)blockIdx.y * a.all_rows + r) * a.dim + col, count, sum[r]);
+        if (group == 0 && r < a.rows) store_some<COLS>(a.sums + ((long long)blockIdx.y * a.rows + r) * a.dim + col, count, sum[r]);
     }
 }
 // The same for 9 to 64 rows by matrix instructions (16 x 16 x 4, fp32 throughout), where 2 rows vocab dim multiply-adds a side on
@@ -859,15 +863,9 @@ template <typename T, int TB> __global__ __launch_bounds__(256) void k_few_grad_
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                float f[4] = {out[0][r], out[1][r], out[2][r], out[3][r]};
+                const float f[4] = {out[0][r], out[1][r], out[2][r], out[3][r]};
                 const long long v = turn * 16 + 4 * k + r;
                 T* to = static_cast<T*>(a.dw) + v * a.dim + col;
-                if (a.add) {
-                    float before[4];
-                    load_some<4>(to, v < a.vocab ? count : 0, before);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) f[e] += before[e];
-                }
                 store_some<4>(to, v < a.vocab ? count : 0, f);
             }
         }
@@ -882,7 +880,7 @@ template <typename T, int TB> __global__ __launch_bounds__(256) void k_few_grad_
         for (int r = 0; r < 4; ++r) {
             const int row = 16 * t + 4 * k + r;
             const float f[4] = {sum[t][0][r], sum[t][1][r], sum[t][2][r], sum[t][3][r]};
-            store_some<4>(a.sums + ((long long)blockIdx.y * a.all_rows + row) * a.dim + col, row < a.rows ? count : 0, f);
+            store_some<4>(a.sums + ((long long)blockIdx.y * a.rows + row) * a.dim + col, row < a.rows ? count : 0, f);
         }
 }
 // dH's rows from the blocks' sums, in their order: 8 threads share a column
@@ -1061,8 +1059,8 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     p.rows = d->rows; p.dim = d->dim; p.vocab = d->vocab;
     p.packed_dim = up(d->dim, kStep);
     p.k_steps = (int)(p.packed_dim / kStep);
-    const bool as_it_lies = !p.f32 && d->dim % kStep == 0 && d->weight_stride % 8 == 0 && d->weight_stride < (1 << 21) && !d->any_address;
-    p.few = d->rows <= (p.f32 ? kFewF32 : as_it_lies ? kFewBf16 : grad ? kFewGradPacked : kFewBf16Packed);
+    const bool whole = d->weight_stride % 8 == 0 && !d->any_address, as_it_lies = !p.f32 && whole && d->dim % kStep == 0 && d->weight_stride < (1 << 21);
+    p.few = d->rows <= (p.f32 ? kFewF32 : as_it_lies ? kFewBf16 : !grad && whole ? kFewBf16Whole : kFewBf16Packed);
     p.staged = !p.few && !as_it_lies;
     // (92000 tokens x 256 bf16 with gradients of 32 rows, us: 117 in tiles of 128, 185 of 256)
     p.tile = d->rows > 128 && up(d->rows, 256) / 256 * (up(d->vocab, 256) / 256) >= 256 ? 256 : 128;
@@ -1070,8 +1068,8 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     p.piece = (long long)(kPieceBytes / 2 / (size_t)rows_up) / 256 * 256;
     if (p.piece < 256) p.piece = 256;
     if (p.piece > up(d->vocab, 256)) p.piece = up(d->vocab, 256);
-    // packed weights of a piece are no more than that either, but where 4096 of them are
-    const long long most_packed = (long long)(kPieceBytes / (size_t)(p.planes * p.packed_dim * 2)) / 256 * 256;
+    // packed weights have a limit of their own, but 4096 of them are taken whatever they need
+    const long long most_packed = (long long)(kPackedBytes / (size_t)(p.planes * p.packed_dim * 2)) / 256 * 256;
     if (p.staged && p.piece > most_packed) p.piece = most_packed > 4096 ? most_packed : p.piece < 4096 ? p.piece : 4096;
     p.flexible = !p.staged;
     p.parts = p.few ? (d->vocab + 16 * kFewWaves - 1) / (16 * kFewWaves) : (d->vocab + p.tile - 1) / p.tile;
@@ -1092,9 +1090,11 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     const long long few_columns = d->rows <= kFewGradVector ? 2048 : 256, few_want = 1024 / ((d->dim + few_columns - 1) / few_columns);
     const long long few_most = (d->vocab + kFewTokens - 1) / kFewTokens, few_cap = few_want < 1 ? 1 : few_want > 512 ? 512 : few_want;
     p.few_blocks = (int)(few_cap < few_most ? few_cap : few_most);
-    // The logits of a vocabulary that is one piece, in fp32, where they are no larger than dz may be and dearer to compute again than to read
+    // The logits of a vocabulary that is one piece, in fp32, where they are dearer to compute again than to read (3000 rows x 4000 bf16 with
+    // gradients, us: dim 256 83 either way, 512 99 either way, 1024 130 and 143 without, 2048 201 and 239; 700 x 2048 x 32000 370 and 402;
+    // fp32 3000 x 256 x 4000 284 and 310, 3000 x 2048 x 4000 953 and 1243)
     const long long kept = 4 * rows_up * up(d->vocab, p.tile);
-    p.keep = grad && !p.few && p.piece >= d->vocab && kept <= (long long)(kPieceBytes / 2) && p.k_steps * (p.f32 ? kPairs : 1) >= kKeepSteps;
+    p.keep = grad && !p.few && p.piece >= d->vocab && kept <= (long long)kPieceBytes && p.k_steps * (p.f32 ? kPairs : 1) >= kKeepSteps;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += round256(bytes); return here; };
     const size_t rows = (size_t)d->rows;
@@ -1169,40 +1169,27 @@ struct Call {
         return a;
     }
     template <typename T> void few_logits(bool values, bool keep) {
-        for (long long base = 0; base < p.rows; base += kFewAtOnce) {
-            const long long rows = p.rows - base < kFewAtOnce ? p.rows - base : kFewAtOnce;
-            const T* h = static_cast<const T*>(hidden) + base * d->hidden_stride;
-            const FewArgs a{h, weight, d->hidden_stride, d->weight_stride, p.vocab, rows, (int)p.dim, d->scale,
-                            targets ? targets + base : nullptr, values ? at<float>(p.part) + base : nullptr, at<float>(p.target) + base,
-                            keep ? at<float>(p.logits) + base * p.vocab : nullptr, p.rows};
-            const dim3 grid((unsigned)p.parts);
-            if (rows <= 16) hipLaunchKernelGGL((k_few<T, 1>), grid, 64 * kFewWaves, 0, st, a);
-            else if (rows <= 32) hipLaunchKernelGGL((k_few<T, 2>), grid, 64 * kFewWaves, 0, st, a);
-            else hipLaunchKernelGGL((k_few<T, 4>), grid, 64 * kFewWaves, 0, st, a);
-        }
+        const FewArgs a{hidden, weight, d->hidden_stride, d->weight_stride, p.vocab, p.rows, (int)p.dim, d->scale,
+                        targets, values ? at<float>(p.part) : nullptr, at<float>(p.target), keep ? at<float>(p.logits) : nullptr};
+        const dim3 grid((unsigned)p.parts);
+        if (p.rows <= 16) hipLaunchKernelGGL((k_few<T, 1>), grid, 64 * kFewWaves, 0, st, a);
+        else if (p.rows <= 32) hipLaunchKernelGGL((k_few<T, 2>), grid, 64 * kFewWaves, 0, st, a);
+        else hipLaunchKernelGGL((k_few<T, 4>), grid, 64 * kFewWaves, 0, st, a);
     }
     void few_logits(bool values, bool keep) {
         if (p.f32) few_logits<float>(values, keep);
         else few_logits<bf16_t>(values, keep);
     }
     FewGradArgs few_args(void* dhidden, void* dweight, int lanes) const {
-        return FewGradArgs{hidden, weight, d->hidden_stride, d->weight_stride, p.vocab, p.dim, (int)p.rows, (int)p.rows, lanes, p.few_blocks, false, d->scale,
+        return FewGradArgs{hidden, weight, d->hidden_stride, d->weight_stride, p.vocab, p.dim, (int)p.rows, lanes, p.few_blocks, d->scale,
                            at<float>(p.logits), at<RowInfo>(p.info), dhidden ? at<float>(p.sums) : nullptr, dweight};
     }
     template <typename T> void few_grad_tiles(void* dhidden, void* dweight) {
-        for (long long base = 0; base < p.rows; base += kFewAtOnce) {
-            FewGradArgs a = few_args(dhidden, dweight, 64);
-            a.rows = (int)(p.rows - base < kFewAtOnce ? p.rows - base : kFewAtOnce);
-            a.h = static_cast<const T*>(hidden) + base * d->hidden_stride;
-            a.logits += base * p.vocab;
-            a.info += base;
-            if (a.sums) a.sums += base * p.dim;
-            a.add = base > 0;
-            const dim3 grid((unsigned)((p.dim + 255) / 256), (unsigned)p.few_blocks);
-            if (a.rows <= 16) hipLaunchKernelGGL((k_few_grad_tiles<T, 1>), grid, 256, 0, st, a);
-            else if (a.rows <= 32) hipLaunchKernelGGL((k_few_grad_tiles<T, 2>), grid, 256, 0, st, a);
-            else hipLaunchKernelGGL((k_few_grad_tiles<T, 4>), grid, 256, 0, st, a);
-        }
+        const FewGradArgs a = few_args(dhidden, dweight, 64);
+        const dim3 grid((unsigned)((p.dim + 255) / 256), (unsigned)p.few_blocks);
+        if (p.rows <= 16) hipLaunchKernelGGL((k_few_grad_tiles<T, 1>), grid, 256, 0, st, a);
+        else if (p.rows <= 32) hipLaunchKernelGGL((k_few_grad_tiles<T, 2>), grid, 256, 0, st, a);
+        else hipLaunchKernelGGL((k_few_grad_tiles<T, 4>), grid, 256, 0, st, a);
     }
     template <typename T, int ROWS, int COLS> void few_grad(void* dhidden, void* dweight) {
         int lanes = 8;

@@ -407,11 +407,11 @@ def test_refusals():
 
 
 @pytest.mark.parametrize("dtype", list(DTYPES))
-@pytest.mark.parametrize("rows", [1, 5, 16, 17, 33, 40, 48, 49, 65, 97, 100, 112, 113, 128, 129, 300])
-def test_nothing_is_written_behind_the_workspace(rows, dtype):
+@pytest.mark.parametrize("rows,dim,vocab", [(rows, 8, 9001) for rows in (1, 5, 16, 17, 33, 40, 48, 49, 65, 97, 100, 112, 113, 128, 129, 300)] +
+                         [(rows, 600, 1100) for rows in (17, 65, 129, 300)])
+def test_nothing_is_written_behind_the_workspace(rows, dim, vocab, dtype):
     """A workspace of the stated size, full of NaN; what lies behind it stays as it is.  A narrow head over a large vocabulary has little
     behind its logits that a store too many could fall on."""
-    dim, vocab = 8, 9001
     hidden, weight, targets, a, b = _inputs(rows, dim, vocab, DTYPES[dtype], 40 + rows)
     want = _Definition(hidden, weight, targets, 1.0, a, b)
     desc = B.LinearLogprobDesc(rows, dim, vocab, hidden.stride(0), weight.stride(0), IGNORE, _DTYPE[hidden.dtype], 1.0, 0, 0)
@@ -433,3 +433,37 @@ def test_nothing_is_written_behind_the_workspace(rows, dtype):
         assert status == 0
         _check_values(LinearLogprobs(logprob, entropy), want, targets)
         assert bool((ws[size:] == 255).all())
+
+
+@pytest.mark.parametrize("rows,dim,vocab,dtype", [(40, 640, 3000, "bf16"), (100, 1024, 777, "bf16"), (300, 513, 1300, "bf16"), (1400, 512, 12000, "bf16"),
+                                                  (70, 100, 4000, "f32"), (300, 129, 1111, "f32"), (1400, 128, 12000, "f32")])
+def test_logits_that_are_kept_and_computed_again(rows, dim, vocab, dtype):
+    """A call of both keeps the logits of these sizes, a backward pass behind a forward one computes them again: the same bits."""
+    hidden, weight, targets, a, b = _inputs(rows, dim, vocab, DTYPES[dtype], 50 + rows)
+    want = _Definition(hidden, weight, targets, 0.9, a, b)
+    r = asi.linear_logprobs_grad(hidden, weight, targets, a, b, scale=0.9)
+    _check_values(r, want, targets)
+    _close(r.hidden, want.hidden, want.hidden_bound, "hidden")
+    _close(r.weight, want.weight, want.weight_bound, "weight")
+    h, w = hidden.clone().requires_grad_(), weight.clone().requires_grad_()
+    again = asi.linear_logprobs(h, w, targets, scale=0.9)
+    dh, dw = torch.autograd.grad((again.logprob, again.entropy), (h, w), (a, b))
+    assert torch.equal(dh, r.hidden) and torch.equal(dw, r.weight)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_kept_logits_in_a_graph_whose_rows_change(dtype):
+    hidden, weight, targets, a, _ = _inputs(300, 576, 2000, DTYPES[dtype], 60, ignored=0.0)
+    asi.linear_logprobs_grad(hidden, weight, targets, a)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = asi.linear_logprobs_grad(hidden, weight, targets, a)
+    for seed in range(4):
+        h, _, t, _, _ = _inputs(300, 576, 2000, DTYPES[dtype], 61 + seed, ignored=0.33 * seed)
+        hidden.copy_(h)
+        targets.copy_(t)
+        graph.replay()
+        eager = asi.linear_logprobs_grad(h, weight, t, a)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(captured, eager))
