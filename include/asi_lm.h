@@ -168,7 +168,7 @@ asi_status asi_adamw(int32_t count, const asi_adamw_tensor* tensors, int32_t sta
  * weights of the output layer (vocab, dim), and the gradients of sum_t a_t logprob_t + b_t entropy_t:
  *     dz = scale ( a (delta_target - p) - b p (log p + entropy) )       dH = dz W        dW = dz^T H
  * The logits are made in tiles and used up there; for the gradients they are made a second time, in pieces of
- * the vocabulary.  Kept between the two calls are two numbers a row: the largest logit x_max (before the scale) and
+ * the vocabulary, or kept in the workspace where the whole vocabulary is one piece and `given` is 0.  Kept between the two calls are two numbers a row: the largest logit x_max (before the scale) and
  * log sum_i exp(scale (x_i - x_max)).
  * A row whose target is ignore_index is left out: it is not read, has logprob, entropy and gradient 0 and adds nothing
  * to dW.  A target out of range otherwise gives NaN, as a row does that holds NaN or +infinity among its logits.

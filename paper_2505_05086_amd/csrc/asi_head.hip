@@ -14,7 +14,7 @@
 //   k_products    the products of dz with weights (dH) and hidden states (dW), read across as they lie (asi_tiles.h)
 //   k_hidden      the sums of dH, in fp32 over the pieces of the vocabulary and the parts of a piece, to their rows
 //
-// What bounds it: the matrix products, 2 rows dim vocab for the values and 8 with the gradients (6 if the logits were kept): 2731 rows x 2048 x
+// What bounds it: the matrix products, 2 rows dim vocab for the values and 8 with the gradients (6 where the logits are kept): 2731 rows x 2048 x
 // 32000 bf16 335 us of values (1.07 PFLOP/s), 1.30 ms with gradients (1.10); 8190 x 2048 x 100003 2.73 ms (1.23), 11.4 ms (1.18).  The weights'
 // memory for few rows: 8 x 2048 x 32000 28.6 us, 4.6 TB/s.
 #include <math.h>
