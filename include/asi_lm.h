@@ -173,8 +173,8 @@ asi_status asi_adamw(int32_t count, const asi_adamw_tensor* tensors, int32_t sta
  * A row whose target is ignore_index is left out: it is not read, has logprob, entropy and gradient 0 and adds nothing
  * to dW.  A target out of range otherwise gives NaN, as a row does that holds NaN or +infinity among its logits.
  * Products of fp32 inputs are exact to about the rounding of fp32 (each side as three bf16 numbers, six products of
- * them, sums in fp32).  For bf16 inputs dz is rounded to bf16 before it is multiplied (to two
- * parts of bf16 for up to 256 rows, not at all for up to 16), and dH and dW once at the end. */
+ * them, sums in fp32).  For bf16 inputs dz is held to 2^-16 of itself (as two parts of bf16; in
+ * fp32 for few rows) when it is multiplied, and dH and dW are rounded once at the end. */
 typedef struct {
     int64_t rows, dim, vocab;  /* rows < 2^24, dim < 2^18, vocab < 2^28 */
     int64_t hidden_stride;     /* of H, >= dim */

@@ -7,7 +7,7 @@
 //   k_logits      a tile of logits, vocabulary along the registers of a lane and tokens along the lanes, so that a token's maximum
 //                 and sums over 128 (64) of the vocabulary stay in a lane but for one exchange.  Values: x_max, how many logits are
 //                 as large, sum e over the others and sum e d of each token, d = x - x_max, e = exp(scale d), and the target's logit
-//   k_logits_grad the same tiles as dz, rounded to bf16 in one, two or three parts
+//   k_logits_grad the same tiles as dz, in two parts of bf16 for bf16 inputs and three for fp32
 //   k_few         the values for few rows, the weights from memory straight into the matrix instructions; k_few_grad and
 //                 k_few_grad_tiles their gradients from the logits that it leaves, 16 rows a column
 //   k_join        joins the tiles' values
@@ -34,14 +34,19 @@ constexpr float kLow = -1e30f;                       // stands for -infinity whe
 // gradients of 32 rows 1000 x 50001 163 and 144, 200 x 50001 61 and 92, 1000 x 3000 38 and 58, of 48 rows 317, 110, 52 and 148, 94, 60.
 // Gradients of 8 rows 108 by matrix instructions, 114 without.)
 constexpr int kFewF32 = 64, kFewBf16 = 16, kFewBf16Whole = 64, kFewBf16Packed = 32, kFewGradVector = 4;
-// Up to this many rows of bf16, dz is held in two parts of bf16: rounded to one, its error adds as much as the results' own rounding does where
-// many rows' errors meet, but more than that where a few rows make up the gradient.  (256 rows x 2048 x 32000: 268 us, with one part 205;
-// 128 rows: 200 and 162.)
-constexpr int kFineRows = 256;
+// For bf16 inputs dz is held in two parts of bf16, 2^-16 of itself: rounded to one, it would add as much error as the results' own rounding, and
+// where summands cancel, more than is left of them.
+constexpr int kFineParts = 2;
 typedef float v4f __attribute__((ext_vector_type(4)));
 constexpr int kLeftOut = -2;                         // a RowInfo's target: the row is left out
 constexpr int kKeepSteps = 8;
-constexpr size_t kPieceBytes = size_t(96) << 20;     // dz of a piece, in bf16
+constexpr size_t kPieceBytes = size_t(96) << 20;     // dz of a piece in fp32, each of its three parts; logits that are kept
+// dz of a piece in bf16, both parts: a sixteenth of the logits in fp32 between these bounds.  With gradients, us, 96 MiB, 116, 128, 144 and 192:
+// 2731 of 4096 rows x 2048 x 32000 2154, 1990, 1978, 1979, 2032; 2000 x 2048 x 32000 1536, 1525, 1394, 1394, 1414; 8190 x 2048 x 100003
+// 22129, with 128 19512, 192 18578.
+constexpr size_t kFineBytes = size_t(128) << 20, kMostFineBytes = size_t(192) << 20;
+// Sums of dH for bf16 (with dz 164 MiB), and for fp32 (1500 x 512 x 100000 bf16 with gradients, us: 20 MiB 1383, 36 1268, 48 1281; 700 x 1000 x 32000 382, 353, 354)
+constexpr size_t kFineSums = size_t(36) << 20, kSums = size_t(48) << 20;
 // Packed weights of a piece.  They are larger than that of a few rows' dz, so that a piece has tiles for the whole chip: fp32 with gradients,
 // 150 rows x 2048 x 60000, us: 3054 with 96 MiB, 2396 with 192, 1962 with 384, 1398 with 768; 700 x 1000 x 32000 1212, 997 with 192 and more;
 // of values alone, 150 x 2048 x 60000, 1168, 816, 610, 628; 1023 x 1000 x 50001 637, 676, 638, 636.
@@ -934,7 +939,7 @@ template <int B, int DZ> __device__ __forceinline__ void dhidden_tile(const Prod
     t.clear();
     Operand dz = a.dz;
     dz.rows = rows;
-    if (to > from) t.template run<DZ == 1 ? kOne : DZ == 2 ? kTwoA : kSix>(dz, a.weights, tm * BM, tn * BN, from, to - from, lds);
+    if (to > from) t.template run<DZ == 2 ? kTwoA : kSix>(dz, a.weights, tm * BM, tn * BN, from, to - from, lds);
     float* out = a.sums + split * rows * a.dim;
     const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -967,7 +972,7 @@ template <int B, typename T, int DZ> __device__ __forceinline__ void dweight_til
     Operand dz = a.dz, x = a.hidden;
     dz.rows = x.rows = rows;
     const int steps = (int)((rows + kStep - 1) / kStep);
-    if (steps) t.template run<DZ == 1 ? kOne : DZ == 2 ? kTwoB : kSix>(kDimFirst ? x : dz, kDimFirst ? dz : x, tm * BM, tn * BN, 0, steps, lds);
+    if (steps) t.template run<DZ == 2 ? kTwoB : kSix>(kDimFirst ? x : dz, kDimFirst ? dz : x, tm * BM, tn * BN, 0, steps, lds);
     if constexpr (kDimFirst) {
         store_across<Tl, BM, BN>(lds, static_cast<uint16_t*>(a.dw) + (a.first + tn * BN) * a.dim + tm * BM, a.dim, a.vocab - tn * BN, a.dim - tm * BM, a.whole,
                                  [&](int i, int j, int r) -> uint32_t { return to_bf16(t.acc[i][j][r]).bits; });
@@ -1055,7 +1060,7 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     Plan p{};
     p.f32 = d->dtype == ASI_F32;
     p.planes = p.f32 ? kPlanes : 1;
-    p.dz_planes = p.f32 ? kPlanes : d->rows <= kFineRows ? 2 : 1;
+    p.dz_planes = p.f32 ? kPlanes : kFineParts;
     p.rows = d->rows; p.dim = d->dim; p.vocab = d->vocab;
     p.packed_dim = up(d->dim, kStep);
     p.k_steps = (int)(p.packed_dim / kStep);
@@ -1065,7 +1070,12 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     // (92000 tokens x 256 bf16 with gradients of 32 rows, us: 117 in tiles of 128, 185 of 256)
     p.tile = d->rows > 128 && up(d->rows, 256) / 256 * (up(d->vocab, 256) / 256) >= 256 ? 256 : 128;
     const long long rows_up = up(d->rows, p.tile);
-    p.piece = (long long)(kPieceBytes / 2 / (size_t)rows_up) / 256 * 256;
+    size_t dz_bytes = kPieceBytes;
+    if (!p.f32) {
+        const size_t share = (size_t)rows_up * (size_t)d->vocab * 4 / 16;
+        dz_bytes = (share < kFineBytes ? kFineBytes : share < kMostFineBytes ? share : kMostFineBytes) / kFineParts;
+    }
+    p.piece = (long long)(dz_bytes / 2 / (size_t)rows_up) / 256 * 256;
     if (p.piece < 256) p.piece = 256;
     if (p.piece > up(d->vocab, 256)) p.piece = up(d->vocab, 256);
     // packed weights have a limit of their own, but 4096 of them are taken whatever they need
@@ -1078,9 +1088,9 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
         p.parts = d->vocab / p.piece * (p.piece / p.tile) + (last ? (last + piece_tile(p, last) - 1) / piece_tile(p, last) : 0);
     }
     // parts that the vocabulary of a piece may be cut in for dH, and the memory for their sums: twice what fills the chip, but no more than
-    // half a piece's or twice dH's size in fp32
+    // that or twice dH's size in fp32
     const long long tiles = (rows_up / p.tile) * (up(d->dim, p.tile) / p.tile), slots = p.tile == 256 ? 256 : 512;
-    const long long memory = (long long)(kPieceBytes / 2 / 4) / (d->rows * d->dim > 0 ? d->rows * d->dim : 1);
+    const long long memory = (long long)((p.f32 ? kSums : kFineSums) / 4) / (d->rows * d->dim > 0 ? d->rows * d->dim : 1);
     p.most_splits = (2 * slots + tiles - 1) / (tiles > 0 ? tiles : 1);
     if (p.most_splits > (memory > 2 ? memory : 2)) p.most_splits = memory > 2 ? memory : 2;
     if (p.most_splits > 32) p.most_splits = 32;
@@ -1105,18 +1115,18 @@ Plan plan(const asi_linear_logprob_desc* d, bool grad) {
         p.hidden = take((size_t)p.planes * rows * p.packed_dim * 2);
         if (p.staged) p.weights = take((size_t)p.planes * p.piece * p.packed_dim * 2);
     }
-    p.part = take((size_t)p.parts * 4 * rows * 4);
     p.target = take(rows * 4);
-    if (grad) {
-        p.info = take(rows * sizeof(RowInfo));
-        if (p.few) {
-            p.logits = take((rows + 15) / 16 * 16 * (size_t)d->vocab * 4);
-            p.sums = take((size_t)p.few_blocks * rows * d->dim * 4);
-            p.bytes = at;
-            return p;
-        }
+    if (grad) p.info = take(rows * sizeof(RowInfo));
+    p.part = take((size_t)p.parts * 4 * rows * 4);
+    if (grad && p.few) {
+        p.logits = take((rows + 15) / 16 * 16 * (size_t)d->vocab * 4);
+        p.sums = take((size_t)p.few_blocks * rows * d->dim * 4);
+    } else if (grad) {
+        // dz lies where the tiles' values were, which are joined by then
+        p.dz = p.part;
+        const size_t end = p.dz + round256((size_t)p.dz_planes * (size_t)rows_up * p.piece * 2);
+        if (at < end) at = end;
         if (p.keep) p.kept = take((size_t)kept);
-        p.dz = take((size_t)p.dz_planes * (size_t)rows_up * p.piece * 2);
         p.sums = take((size_t)p.most_sums * d->dim * 4);
     }
     p.bytes = at;
@@ -1212,22 +1222,19 @@ struct Call {
         else tiles<B>(k_logits<B, 1, false>, one, count, a);
     }
     template <int B> void products(const LogitArgs& a, const ProductArgs& b) {
-        static LdsAllowed grad1, grad2, grad3, kept1, kept2, kept3, products1, products2, products3;
+        static LdsAllowed grad2, grad3, kept2, kept3, products2, products3;
         const long long row_tiles = up(p.rows, B) / B, dim_tiles = up(p.dim, B) / B;
         // no more tiles of logits in a piece than its memory holds, however it is cut
         const long long logit_tiles = up(p.piece, B) / B * row_tiles;
         if (a.kept && p.f32) tiles<B>(k_logits_grad<B, 0, kPlanes>, kept3, logit_tiles, a);
-        else if (a.kept && p.dz_planes == 2) tiles<B>(k_logits_grad<B, 0, 2>, kept2, logit_tiles, a);
-        else if (a.kept) tiles<B>(k_logits_grad<B, 0, 1>, kept1, logit_tiles, a);
+        else if (a.kept) tiles<B>(k_logits_grad<B, 0, kFineParts>, kept2, logit_tiles, a);
         else if (p.f32) tiles<B>(k_logits_grad<B, kPlanes, kPlanes>, grad3, logit_tiles, a);
-        else if (p.dz_planes == 2) tiles<B>(k_logits_grad<B, 1, 2>, grad2, logit_tiles, a);
-        else tiles<B>(k_logits_grad<B, 1, 1>, grad1, logit_tiles, a);
+        else tiles<B>(k_logits_grad<B, 1, kFineParts>, grad2, logit_tiles, a);
         const long long hidden_tiles = b.dhidden ? up((up(p.most_sums, B) / B + p.most_splits) * dim_tiles, 8) : 0;
         const long long tokens = !b.all ? b.vocab : b.all < 2 * p.piece ? b.all : 2 * p.piece;
         const long long weight_tiles = b.dweight ? up(tokens, B) / B * dim_tiles : 0;
         if (p.f32) tiles<B>(k_products<B, float, kPlanes>, products3, hidden_tiles + weight_tiles, b);
-        else if (p.dz_planes == 2) tiles<B>(k_products<B, bf16_t, 2>, products2, hidden_tiles + weight_tiles, b);
-        else tiles<B>(k_products<B, bf16_t, 1>, products1, hidden_tiles + weight_tiles, b);
+        else tiles<B>(k_products<B, bf16_t, kFineParts>, products2, hidden_tiles + weight_tiles, b);
     }
     void values(float* logprob, float* entropy, float* stats, RowInfo* info, const float* wa, const float* wb) {
         JoinArgs j{};

@@ -467,3 +467,34 @@ def test_kept_logits_in_a_graph_whose_rows_change(dtype):
         eager = asi.linear_logprobs_grad(h, weight, t, a)
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(captured, eager))
+
+
+@pytest.mark.parametrize("rows,dim,ignored", [(40, 64, False), (256, 128, False), (258, 192, False), (700, 384, False), (700, 193, True), (2000, 512, True)])
+def test_the_gradient_of_logits_is_not_rounded_to_bf16(rows, dim, ignored):
+    """bf16 results are rounded once, however many rows there are, with or without a target.  All tokens have the same weights w, so p is
+    1 / vocab; rows come in pairs with hidden states 1 and -1 in a column of their own, one target, and factors a and a (1 + 2^-9): what is
+    left of dW in that column is 2^-9 of either summand, and nothing of dH, whose row sums dz to 0 times w."""
+    vocab, g = 500, _gen(70 + rows)
+    live = torch.arange(rows, device="cuda") // 2 % 2 == 0 if ignored else torch.ones(rows, dtype=torch.bool, device="cuda")
+    row = torch.arange(int(live.sum()), device="cuda")
+    hidden = torch.randn(rows, dim, generator=g, device="cuda")
+    small = torch.zeros(len(row), dim, device="cuda")
+    small[row, row // 2] = 1.0 - 2.0 * (row % 2)
+    hidden[live] = small
+    hidden = hidden.bfloat16()
+    w = torch.randn(dim, generator=g, device="cuda").bfloat16()
+    targets = torch.full((rows,), IGNORE, device="cuda")
+    targets[live] = torch.randint(0, vocab, (len(row) // 2,), generator=g, device="cuda").repeat_interleave(2)
+    a = torch.zeros(rows, device="cuda")
+    a[live] = (1.0 + torch.rand(len(row) // 2, generator=g, device="cuda")).repeat_interleave(2) * (1.0 + 2.0 ** -9 * (row % 2))
+    r = asi.linear_logprobs_grad(hidden, w.expand(vocab, dim).contiguous(), targets, a)
+    size, at = a[live].double(), targets[live]
+    p = 1.0 / vocab
+    dz = torch.full((len(row), vocab), -p, dtype=torch.float64, device="cuda").scatter_(1, at[:, None], 1.0 - p) * size[:, None]
+    # the logarithm of 500, 6.2, is off by 2 roundings of itself and of its product with log2 e: p by 30 U of itself, with the exponential's
+    # and the products' roundings 40 U; two parts of bf16 hold 2^-16.  Sums over the rows of products of which two are not 0, over the
+    # vocabulary of 500; the result's rounding
+    off = 2.0 ** -16 + 40 * U
+    want = dz.t().contiguous() @ small.double()
+    _close(r.weight, want, off * (dz.abs().t().contiguous() @ small.double().abs()) * (1 + U) + 2.0 ** -8 * want.abs() + 4 * U * want.abs(), "weight")
+    _close(r.hidden[live], torch.zeros(len(row), dim, device="cuda"), (off + (vocab + 64) * U) * dz.abs().sum(-1, keepdim=True) * w.double().abs(), "hidden")
