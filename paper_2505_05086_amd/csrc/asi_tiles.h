@@ -12,6 +12,7 @@
 // An fp32 operand comes as three planes of bf16 whose sum it is (8 + 8 + 8 bits); the products of planes that matter to 2^-24 are
 // six, the smallest first, and run through the same loop as a sixfold k.
 #pragma once
+#include "asi_head_plan.h"
 #include "asi_lm_device.h"
 
 namespace asi {
@@ -19,9 +20,6 @@ namespace asi {
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef short v4h __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
-
-constexpr int kStep = 64;                        // k of a step
-constexpr int kPlanes = 3, kPairs = 6;           // of an fp32 operand: its planes, and the products of planes
 
 // `rows` rows of `ld` elements, of which the first `cols` may be read; planes `plane` elements apart
 struct Operand {

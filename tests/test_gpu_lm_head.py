@@ -498,3 +498,70 @@ def test_the_gradient_of_logits_is_not_rounded_to_bf16(rows, dim, ignored):
     want = dz.t().contiguous() @ small.double()
     _close(r.weight, want, off * (dz.abs().t().contiguous() @ small.double().abs()) * (1 + U) + 2.0 ** -8 * want.abs() + 4 * U * want.abs(), "weight")
     _close(r.hidden[live], torch.zeros(len(row), dim, device="cuda"), (off + (vocab + 64) * U) * dz.abs().sum(-1, keepdim=True) * w.double().abs(), "hidden")
+
+
+def _shares(hidden, weight, targets, a):
+    """_Definition's values and gradients and their bounds where a row of W is too long and there are too many of them for all of that in 64 bits
+    at once: in pieces of the vocabulary, by the one identity log p = z - log sum exp z."""
+    rows, dim, vocab = len(hidden), weight.shape[1], weight.shape[0]
+    r = _round(hidden.dtype)
+    live = targets != IGNORE
+    h = torch.where(live[:, None], hidden.double(), 0.0)
+    pieces = [slice(i, min(vocab, i + 4096)) for i in range(0, vocab, 4096)]
+    z, size = torch.empty(rows, vocab, dtype=torch.float64, device="cuda"), torch.zeros(rows, dtype=torch.float64, device="cuda")
+    for s in pieces:
+        w = weight[s].double()
+        z[:, s] = h @ w.t().contiguous()
+        size = torch.maximum(size, (h.abs() @ w.abs().t().contiguous()).amax(-1))
+    logp = z - torch.logsumexp(z, -1, keepdim=True)
+    p = logp.exp()
+    entropy = torch.special.entr(p).sum(-1)
+    times = 6 if hidden.dtype == torch.float32 else 1                     # products of bf16 numbers are exact
+    values = 2 * (times * dim + 16) * U * size + U * (8 * z.abs().amax(-1) + 256)
+    hot = torch.zeros_like(z).scatter_(1, torch.where(live, targets, 0)[:, None], 1.0)
+    a = torch.where(live, a.double(), 0.0)[:, None]
+    dz = a * (hot - p)
+    off = a.abs() * (hot + p) * (4 * values[:, None] + 32 * U) + (2.0 ** -16 + U) * dz.abs()
+    dh, dh_bound, near = (torch.zeros(rows, dim, dtype=torch.float64, device="cuda") for _ in range(3))
+    for s in pieces:
+        w = weight[s].double()
+        dh += dz[:, s] @ w
+        dh_bound += off[:, s] @ w.abs()
+        near += dz[:, s].abs() @ w.abs()
+    dh_bound += (6 * vocab + 64) * U * near + r * dh.abs()
+    some = torch.cat([torch.arange(i, min(vocab, i + 97), device="cuda") for i in range(0, vocab, 4096 - 97)])      # of dW: rows of every piece
+    part = dz[:, some].t().contiguous()
+    dw = part @ h
+    dw_bound = off[:, some].t().contiguous() @ h.abs() + (6 * rows + 16) * U * (part.abs() @ h.abs()) + r * dw.abs()
+    return (torch.where(live, logp.gather(1, torch.where(live, targets, 0)[:, None])[:, 0], 0.0), torch.where(live, entropy, 0.0),
+            torch.where(live, values, 0.0), torch.where(live, values * (2 + entropy), 0.0), dh, dh_bound, some, dw, dw_bound)
+
+
+@pytest.mark.parametrize("rows,dim,vocab,dtype", [(200, 5120, 70000, "f32"), (200, 5120, 78336, "f32"), (256, 8192, 65536, "f32"), (512, 8320, 70000, "f32"),
+                                                  (200, 12353, 70001, "bf16")])
+def test_wide_heads_whose_pieces_take_smaller_tiles(rows, dim, vocab, dtype):
+    """Rows of W so long that a piece of packed ones has too few tiles of 256 for the chip, the vocabulary an exact number of pieces or not."""
+    # logits near 0, whose bounds are near 0.05: a part of the vocabulary that is lost moves the logarithm by more
+    hidden, weight, targets, a, _ = _inputs(rows, dim, vocab, DTYPES[dtype], 80 + rows, spread=0.25)
+    logprob, entropy, lp_bound, e_bound, dh, dh_bound, some, dw, dw_bound = _shares(hidden, weight, targets, a)
+    desc = B.LinearLogprobDesc(rows, dim, vocab, dim, dim, IGNORE, _DTYPE[hidden.dtype], 1.0, 0, 0)
+    L = B.lib()
+    st = torch.cuda.current_stream().cuda_stream
+    for f in (L.asi_linear_logprobs_workspace_bytes, L.asi_linear_logprobs_grad_workspace_bytes):
+        size = f(desc)
+        ws = torch.full((size + (1 << 24),), 255, dtype=torch.uint8, device="cuda")
+        lp, en = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        if f is L.asi_linear_logprobs_workspace_bytes:
+            assert L.asi_linear_logprobs(desc, hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), lp.data_ptr(), en.data_ptr(), None,
+                                         ws.data_ptr(), size, st) == 0
+        else:
+            got_h, got_w = torch.empty_like(hidden), torch.empty_like(weight)
+            assert L.asi_linear_logprobs_grad(desc, 0, hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), None, lp.data_ptr(), en.data_ptr(),
+                                              a.data_ptr(), None, got_h.data_ptr(), got_w.data_ptr(), ws.data_ptr(), size, st) == 0
+            _close(got_h, dh, dh_bound, "hidden")
+            _close(got_w[some], dw, dw_bound, "weight")
+        assert float(lp_bound.max()) < 0.1
+        _close(lp, logprob, lp_bound, "logprob")
+        _close(en, entropy, e_bound, "entropy")
+        assert bool((ws[size:] == 255).all())
+        del ws

@@ -1,5 +1,8 @@
 """Refusals of the operators that keep no logits, no mask and no copy of a norm's input, without a GPU: bad arguments are answered with
 a status before anything is launched."""
+import os
+import subprocess
+
 import pytest
 import torch
 
@@ -61,6 +64,102 @@ def test_head_scratch_holds_no_more_than_a_piece_of_the_logits():
     small, large = (need(_head(rows=4096, dim=1024, vocab=v, hidden_stride=1024, weight_stride=1024)) for v in (20000, 200000))
     assert large - small < 4096 * 180000 * 2 / 8                          # the values of the tiles alone grow
     assert need(_head(any_address=1)) > need(_head())
+
+
+HEAD_PLAN = """
+#include <stdio.h>
+#include <stdlib.h>
+#include "asi_head_plan.h"
+using namespace asi;
+// what a call writes in its workspace; dz may lie where the parts were
+struct Region { const char* name; size_t at, bytes; };
+int main() {
+    unsigned long long state = 1;
+    auto random = [&](long long lo, long long hi) {          // spread over the logarithm
+        state = state * 6364136223846793005ull + 1442695040888963407ull;
+        double x = (double)lo;
+        const double f = (double)(state >> 40) / (1 << 24);
+        double ratio = (double)hi / lo;
+        return (long long)(x * __builtin_pow(ratio, f) + 0.5);
+    };
+    long long several = 0, small = 0, kept = 0;
+    for (int n = 0; n < 400000; ++n) {
+        asi_linear_logprob_desc d{};
+        d.rows = random(1, n % 2 ? 1 << 23 : 2000); d.dim = random(1, (1 << 18) - 1); d.vocab = random(1, n % 2 ? (1 << 28) - 1 : 300000);
+        if (n % 3 == 0) d.dim = (d.dim + 63) / 64 * 64;
+        if (n % 5 == 0) d.vocab = (d.vocab + 255) / 256 * 256;
+        d.hidden_stride = d.dim; d.weight_stride = d.dim + random(1, 9) - 1;
+        d.dtype = n % 7 < 4 ? ASI_F32 : ASI_BF16; d.scale = 1.f; d.any_address = n % 11 == 0;
+        if (up(d.rows, 128) / 128 * (up(d.vocab, 128) / 128) > (1 << 23) || up(d.dim, 128) / 128 * (up(d.vocab, 128) / 128) > (1 << 23)) continue;
+        for (int grad = 0; grad < 2; ++grad) {
+            const Plan p = plan(&d, grad);
+            bool fine = true;
+            const int planes = d.dtype == ASI_F32 ? 3 : 1;
+            if (!p.few) {
+                long long token = 0, part = 0, pieces = 0;
+                each_piece(p, [&](long long first, long long count, int tile, long long first_part) {
+                    fine = fine && first == token && count > 0 && (count + (p.staged ? 0 : p.piece) <= p.piece || !p.staged) && first_part == part && (tile == 128 || tile == 256);
+                    token += count;
+                    part += (count + tile - 1) / tile;
+                    ++pieces;
+                    small += pieces > 1 && tile != p.tile;
+                    if (p.keep) fine = fine && pieces == 1;
+                });
+                fine = fine && token == d.vocab && part == p.parts;
+                several += pieces > 1;
+                kept += p.keep;
+            }
+            Region r[12];
+            int count = 0;
+            auto add = [&](const char* name, size_t at, long long bytes) { r[count++] = Region{name, at, (size_t)bytes}; };
+            add("target", p.target, d.rows * 4);
+            if (grad) add("info", p.info, d.rows * 32);
+            const int part = count;
+            add("part", p.part, p.parts * 16 * d.rows);
+            int dz = -1;
+            if (!p.few) {
+                const long long packed = (d.dim + 63) / 64 * 64, rows_up = up(d.rows, p.tile);
+                add("split", p.split, 16); add("live", p.live, d.rows * 4); add("place", p.place, d.rows * 4);
+                add("hidden", p.hidden, planes * d.rows * packed * 2);
+                if (p.staged) add("weights", p.weights, planes * p.piece * packed * 2);
+                if (grad) {
+                    dz = count;
+                    add("dz", p.dz, (planes == 3 ? 3 : 2) * rows_up * p.piece * 2);
+                    add("sums", p.sums, d.rows * p.most_splits * d.dim * 4);
+                    fine = fine && p.most_splits >= 1 && p.most_sums == d.rows * p.most_splits && p.piece % 256 == 0;
+                    if (p.keep) add("kept", p.kept, rows_up * up(d.vocab, p.tile) * 4);
+                }
+            } else if (grad) {
+                add("logits", p.logits, up(d.rows, 16) * d.vocab * 4);
+                add("sums", p.sums, p.few_blocks * d.rows * d.dim * 4);
+            }
+            const char* what = "";
+            for (int i = 0; i < count; ++i) {
+                if (r[i].at % 256 || r[i].at + r[i].bytes > p.bytes) { fine = false; what = r[i].name; }
+                for (int j = 0; j < i; ++j)
+                    if (r[i].at < r[j].at + r[j].bytes && r[j].at < r[i].at + r[i].bytes && !(i == dz && j == part)) { fine = false; what = r[i].name; }
+            }
+            if (!fine) {
+                printf("%lld x %lld x %lld, type %d, gradients %d: tile %d, piece %lld, parts %lld %s\\n", (long long)d.rows, (long long)d.dim, (long long)d.vocab, d.dtype, grad, p.tile, p.piece, p.parts, what);
+                return 1;
+            }
+        }
+    }
+    printf("%d %d %d\\n", several > 1000, small > 100, kept > 1000);
+    return 0;
+}
+"""
+
+
+def test_head_pieces_and_what_they_write_lie_beside_each_other(tmp_path):
+    """The parts of the pieces' tiles follow each other without a gap and end where their memory does, and no two regions of the workspace
+    overlap or reach behind its end: over random sizes of the whole range, pieces in tiles smaller than the call's among them."""
+    src, exe = tmp_path / "plan.cpp", tmp_path / "plan"
+    src.write_text(HEAD_PLAN)
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2505_05086_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-O2", "-I" + csrc, str(src), "-o", str(exe)], check=True)
+    res = subprocess.run([str(exe)], stdout=subprocess.PIPE, text=True, timeout=120)
+    assert res.returncode == 0 and res.stdout.split() == ["1", "1", "1"], res.stdout
 
 
 def _drop(**kw):
