@@ -127,14 +127,23 @@ __global__ __launch_bounds__(256) void k_all_live(const LiveArgs a) {
 }
 
 // ---- operands -----------------------------------------------------------------------------------------------
+// A number's planes.  What bf16 leaves out is exact in fp32.  A number above bf16's largest has that for its first plane, and the rest, so that it
+// stays finite.  An infinity is (1, 0, infinity) with its sign: of the six products of planes infinity then meets the other side's first plane
+// alone, which has that side's sign and is 0 only with it, and every other one is finite.  (As (infinity, 0, 0) it would meet the other
+// side's lower planes too, which may be 0 or have the other sign.)
 template <typename T> __device__ __forceinline__ void planes_of(float x, uint16_t* h) {
     h[0] = to_bf16(x).bits;
     if constexpr (sizeof(T) == 4) {
-        // what bf16 leaves out is exact in fp32; of an infinity or NaN the first plane says all
+        const uint16_t sign = (uint16_t)(__float_as_uint(x) >> 16) & 0x8000u;
+        if (fabsf(x) == INFINITY) {
+            h[0] = sign | 0x3f80u; h[1] = 0; h[2] = sign | 0x7f80u;
+            return;
+        }
+        if ((h[0] & 0x7fffu) == 0x7f80u) h[0] = sign | 0x7f7fu;
         const float r = x - to_f32(bf16_t{h[0]}), q = r - to_f32(to_bf16(r));
-        const bool fine = fabsf(to_f32(bf16_t{h[0]})) <= 3.4e38f;
-        h[1] = fine ? to_bf16(r).bits : 0;
-        h[2] = fine ? to_bf16(q).bits : 0;
+        const bool number = x == x;
+        h[1] = number ? to_bf16(r).bits : 0;
+        h[2] = number ? to_bf16(q).bits : 0;
     }
 }
 struct PackArgs {

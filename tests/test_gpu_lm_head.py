@@ -565,3 +565,49 @@ def test_wide_heads_whose_pieces_take_smaller_tiles(rows, dim, vocab, dtype):
         _close(en, entropy, e_bound, "entropy")
         assert bool((ws[size:] == 255).all())
         del ws
+
+
+@pytest.mark.parametrize("rows", [40, 65, 129, 300])
+def test_infinite_and_largest_weights_in_fp32(rows):
+    """As in bf16: tokens that -infinity in a column takes out, while what is multiplied has bits in every part of it; numbers above bf16's
+    largest are numbers; an infinite hidden state makes logits of either infinity."""
+    hidden, weight, targets, a, _ = _inputs(rows, 64, 300, torch.float32, 90, ignored=0.0)
+    a *= 2.0 ** -10
+    hidden[:, 7] = 1.0
+    hidden[1::2, 7] = 1.0 + torch.rand(len(hidden[1::2]), generator=_gen(91), device="cuda")
+    hidden[:, 9] = 2.0 ** -122
+    weight[10:20, 9] = 3.4e38 * torch.tensor([1.0, -1.0], device="cuda").repeat(5)       # products of 64
+    never = torch.arange(300, device="cuda") % 4 == 1
+    targets[never[targets]] = 0
+    kept, place = weight[~never].clone(), torch.cumsum(~never, 0) - 1
+    want = _Definition(hidden, kept, place[targets], 1.0, a)
+    weight[never, 7] = -INF
+    _check_values(asi.linear_logprobs(hidden, weight, targets), want, targets)
+    r = asi.linear_logprobs_grad(hidden, weight, targets, a)
+    _check_values(r, want, targets)
+    others = torch.arange(64, device="cuda") != 7
+    # the logits are up to 64 apart and more, so that p goes below 2^-126, the least normal number, where fp32 may hold 0: that is another 2^-126
+    # that a dz or one of its three parts may be off by, and with it their products, six of which make one, may be as well (hidden states of 2^-122)
+    least = 2.0 ** -126
+    hidden_bound = want.hidden_bound + least * (3 * kept.double().abs().sum(0) + 6 * len(kept) + 1)
+    weight_bound = want.weight_bound + least * (3 * hidden.double().abs().sum(0) + 6 * rows + 1)
+    _close(r.hidden[:, others], want.hidden[:, others], hidden_bound[:, others], "hidden")
+    assert torch.isnan(r.hidden[:, 7]).all()                              # 0 times infinity, as in dz @ W
+    _close(r.weight[~never], want.weight, weight_bound, "weight")
+    assert not r.weight[never].any()
+    h, w = hidden.clone().requires_grad_(), weight.clone().requires_grad_()
+    dh, dw = torch.autograd.grad(asi.linear_logprobs(h, w, targets).logprob, (h, w), a)
+    assert torch.equal(dh[:, others], r.hidden[:, others]) and torch.equal(dw, r.weight)
+    weight[:, 7] = -INF
+    r = asi.linear_logprobs(hidden, weight, targets)
+    assert (r.logprob == -INF).all() and not r.entropy.any()
+    hidden[2, 7] = -1.5                                                   # and now +infinity
+    r = asi.linear_logprobs(hidden, weight, targets)
+    assert torch.isnan(r.logprob[2]) and (r.logprob[torch.arange(rows, device="cuda") != 2] == -INF).all()
+    hidden[2, 7] = INF                                                    # infinity on both sides
+    assert (asi.linear_logprobs(hidden, weight, targets).logprob == -INF).all()
+    weight[:, 7] = 1.0
+    r = asi.linear_logprobs(hidden, weight, targets)
+    assert torch.isnan(r.logprob[2]) and torch.isfinite(r.logprob[3:]).all()
+    hidden[2, 7] = -INF
+    assert asi.linear_logprobs(hidden, weight, targets).logprob[2] == -INF
