@@ -457,13 +457,16 @@ template <int B, int PLANES, int DZ> __global__ __launch_bounds__(Shape<B>::kThr
                     for (int j = 0; j < Tl::kN; ++j) t.acc[i][j][r] = 0.f;
                 }
     }
-#pragma unroll
+    // a turn for each part, and no more than that in registers
+#pragma unroll 1
     for (int p = 0; p < DZ; ++p)
         store_across<Tl, BM, BN>(lds, a.dz + p * a.dz_plane + tn * BN * a.dz_stride + tm * BM, a.dz_stride, rows - tn * BN, BM, true,
                                  [&](int i, int j, int r) -> uint32_t {
+                                     // an infinity, of a row's factor that is one, is 1 and infinity in the last part, as in planes_of
                                      const uint32_t bits = to_bf16(t.acc[i][j][r]).bits;
-                                     if (p + 1 < DZ) t.acc[i][j][r] -= __uint_as_float(bits << 16);
-                                     return bits;
+                                     const bool number = (bits & 0x7fffu) != 0x7f80u;
+                                     if (number) t.acc[i][j][r] -= __uint_as_float(bits << 16);
+                                     return number || p + 1 == DZ ? bits : p == 0 ? (bits & 0x8000u) | 0x3f80u : 0u;
                                  });
 }
 

@@ -611,3 +611,17 @@ def test_infinite_and_largest_weights_in_fp32(rows):
     assert torch.isnan(r.logprob[2]) and torch.isfinite(r.logprob[3:]).all()
     hidden[2, 7] = -INF
     assert asi.linear_logprobs(hidden, weight, targets).logprob[2] == -INF
+
+
+@pytest.mark.parametrize("rows", [3, 40, 100, 300])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_an_infinite_share_gives_infinite_gradients(rows, dtype):
+    """A row's factor of infinity, an overflow say, is one in dW, with the sign of its terms, and no NaN beside what it does not cancel with."""
+    hidden, weight, targets, a, _ = _inputs(rows, 64, 300, DTYPES[dtype], 95, ignored=0.0)
+    hidden[0] = torch.where(hidden[0] >= 0, 1.0, -0.5).to(hidden.dtype)  # parts of it are 0
+    a[0] = INF
+    r = asi.linear_logprobs_grad(hidden, weight, targets, a)
+    hot = torch.nn.functional.one_hot(targets[0], 300) * 2 - 1
+    assert torch.equal(r.weight, (hot[:, None] * hidden[0][None].sign() * INF).to(weight.dtype))
+    want = _Definition(hidden[1:], weight, targets[1:], 1.0, a[1:])
+    _close(r.hidden[1:], want.hidden, want.hidden_bound, "hidden")
