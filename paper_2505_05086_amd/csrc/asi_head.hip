@@ -756,9 +756,13 @@ template <typename T, int ROWS, int COLS> __global__ __launch_bounds__(256) void
         __syncthreads();
     }
     if (!a.sums) return;
-    // the groups' sums in their order
+    // the groups' sums in their order; 0 of a row that is left out, whatever the weights that its dz of 0 has met
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
+        if (info[r].target == kLeftOut) {
+#pragma unroll
+            for (int e = 0; e < COLS; ++e) sum[r][e] = 0.f;
+        }
         if (groups > 1) {
             __syncthreads();
 #pragma unroll
@@ -863,7 +867,8 @@ template <typename T, int TB> __global__ __launch_bounds__(256) void k_few_grad_
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int row = 16 * t + 4 * k + r;
-            const float f[4] = {sum[t][0][r], sum[t][1][r], sum[t][2][r], sum[t][3][r]};
+            const bool out = info[row].target == kLeftOut;      // 0, whatever the weights that its dz of 0 has met
+            const float f[4] = {out ? 0.f : sum[t][0][r], out ? 0.f : sum[t][1][r], out ? 0.f : sum[t][2][r], out ? 0.f : sum[t][3][r]};
             store_some<4>(a.sums + ((long long)blockIdx.y * a.rows + row) * a.dim + col, row < a.rows ? count : 0, f);
         }
 }

@@ -625,3 +625,18 @@ def test_an_infinite_share_gives_infinite_gradients(rows, dtype):
     assert torch.equal(r.weight, (hot[:, None] * hidden[0][None].sign() * INF).to(weight.dtype))
     want = _Definition(hidden[1:], weight, targets[1:], 1.0, a[1:])
     _close(r.hidden[1:], want.hidden, want.hidden_bound, "hidden")
+
+
+@pytest.mark.parametrize("rows", [3, 12, 40, 150])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_a_left_out_rows_gradient_is_zero_beside_infinite_weights(rows, dtype):
+    hidden, weight, targets, a, _ = _inputs(rows, 64, 300, DTYPES[dtype], 97, ignored=0.0)
+    targets[1::2] = IGNORE
+    weight[:, 7] = INF
+    weight[5, 9] = NAN
+    r = asi.linear_logprobs_grad(hidden, weight, targets, a)
+    assert not r.hidden[1::2].any() and not r.logprob[1::2].any() and not r.entropy[1::2].any()
+    assert torch.isnan(r.hidden[::2]).all()
+    h = hidden.clone().requires_grad_()
+    dh, = torch.autograd.grad(asi.linear_logprobs(h, weight, targets).logprob, h, a)
+    assert not dh[1::2].any()
