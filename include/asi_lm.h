@@ -198,7 +198,7 @@ asi_status asi_linear_logprobs(const asi_linear_logprob_desc* desc, const void* 
 size_t asi_linear_logprobs_grad_workspace_bytes(const asi_linear_logprob_desc* desc);
 
 /*   given    0: the values are computed first, and written where logprob and entropy are not NULL; stats is not used
- *            1: stats and entropy are those of asi_linear_logprobs; entropy is read only if grad_entropy is given
+ *            1: stats and entropy are those of asi_linear_logprobs for the same descriptor; entropy is read only if grad_entropy is given
  *   targets       in  nullable if grad_logprob is
  *   grad_logprob  in  device fp32 (rows): a, nullable (all zero)
  *   grad_entropy  in  device fp32 (rows): b, nullable (all zero)

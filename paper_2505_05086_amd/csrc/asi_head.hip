@@ -1238,6 +1238,10 @@ asi_status asi_linear_logprobs_grad(const asi_linear_logprob_desc* desc, int giv
     if (!ws || !aligned(ws, 256) || ws_bytes < asi_linear_logprobs_grad_workspace_bytes(desc)) return ASI_ERR_WORKSPACE;
     Call c{desc, plan(desc, true), static_cast<char*>(ws), hidden, weight, targets, st};
     RowInfo* info = c.at<RowInfo>(c.p.info);
+    // Logits that are summed in another order than those that the statistics are of are off from them by their roundings, and where p is nearly
+    // 1 that is more than 1 - p.  33 to 64 rows of bf16 may take k_few for their values and tiles here: these make their own statistics, of
+    // logits that the gradient would need all the same.
+    if (given && plan(desc, false).few != c.p.few) given = 0, logprob = entropy = nullptr;
     if (!c.p.few) c.rows_of(given ? nullptr : logprob, given ? nullptr : entropy, nullptr, true, dhidden, dweight);
     if (given) {
         if (c.p.few) c.few_logits(false, true);

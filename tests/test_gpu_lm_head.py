@@ -640,3 +640,16 @@ def test_a_left_out_rows_gradient_is_zero_beside_infinite_weights(rows, dtype):
     h = hidden.clone().requires_grad_()
     dh, = torch.autograd.grad(asi.linear_logprobs(h, weight, targets).logprob, h, a)
     assert not dh[1::2].any()
+
+
+@pytest.mark.parametrize("rows,dim,vocab,dtype", [(33, 72, 700, "bf16"), (40, 1000, 3000, "bf16"), (64, 200, 3000, "bf16"), (20, 1000, 3000, "bf16"),
+                                                  (40, 128, 3000, "bf16"), (40, 72, 700, "f32"), (64, 1000, 2000, "f32"), (12, 128, 3000, "bf16"), (65, 72, 700, "f32")])
+def test_nearly_sure_tokens_through_autograd(rows, dim, vocab, dtype):
+    """The backward pass makes the logits in the order in which the forward pass made those that its statistics are of: the same bits as one call
+    gives, and a (1 - p) to a share of itself where p is nearly 1."""
+    hidden, weight, targets, a, _ = _inputs(rows, dim, vocab, DTYPES[dtype], 98, ignored=0.0, spread=0.8)
+    hidden = (hidden.float() + 24.0 * weight[targets].float()).to(hidden.dtype)      # a target's logit is about 15, the others' are below 5
+    h, w = hidden.clone().requires_grad_(), weight.clone().requires_grad_()
+    dh, dw = torch.autograd.grad(asi.linear_logprobs(h, w, targets).logprob, (h, w), a)
+    r = asi.linear_logprobs_grad(hidden, weight, targets, a)
+    assert torch.equal(dh, r.hidden) and torch.equal(dw, r.weight)
