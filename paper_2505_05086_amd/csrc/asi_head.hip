@@ -649,7 +649,11 @@ template <int ROWS> __global__ __launch_bounds__(256) void k_join(const JoinArgs
     const bool left_out = a.targets && target == a.ignore;      // where the rows have not been sorted out
     if (a.logprob) {
         float v = NAN;
-        if (target >= 0 && target < a.vocab) v = empty ? -INFINITY : fmaf(a.scale, a.target_logit[at] - x.top, -logsum);
+        if (target >= 0 && target < a.vocab) {
+            const float z = a.target_logit[at], d = z - x.top;
+            // finite logits farther apart than fp32 reaches: both scaled first
+            v = empty || z == -INFINITY ? -INFINITY : d == -INFINITY ? fmaf(z, a.scale, -x.top * a.scale) - logsum : fmaf(a.scale, d, -logsum);
+        }
         if (nan) v = NAN;
         a.logprob[row] = left_out ? 0.f : v;
     }

@@ -469,8 +469,10 @@ def test_kept_logits_in_a_graph_whose_rows_change(dtype):
         assert all(torch.equal(x, y) for x, y in zip(captured, eager))
 
 
-@pytest.mark.parametrize("rows,dim,ignored", [(40, 64, False), (256, 128, False), (258, 192, False), (700, 384, False), (700, 193, True), (2000, 512, True)])
-def test_the_gradient_of_logits_is_not_rounded_to_bf16(rows, dim, ignored):
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows,dim,ignored", [(4, 64, False), (16, 64, False), (40, 64, False), (100, 64, False), (256, 128, False), (258, 192, False), (700, 384, False),
+                                              (700, 193, True), (2000, 512, True)])
+def test_the_gradient_of_logits_is_not_rounded_to_bf16(rows, dim, ignored, dtype):
     """bf16 results are rounded once, however many rows there are, with or without a target.  All tokens have the same weights w, so p is
     1 / vocab; rows come in pairs with hidden states 1 and -1 in a column of their own, one target, and factors a and a (1 + 2^-9): what is
     left of dW in that column is 2^-9 of either summand, and nothing of dH, whose row sums dz to 0 times w."""
@@ -481,8 +483,8 @@ def test_the_gradient_of_logits_is_not_rounded_to_bf16(rows, dim, ignored):
     small = torch.zeros(len(row), dim, device="cuda")
     small[row, row // 2] = 1.0 - 2.0 * (row % 2)
     hidden[live] = small
-    hidden = hidden.bfloat16()
-    w = torch.randn(dim, generator=g, device="cuda").bfloat16()
+    hidden = hidden.to(DTYPES[dtype])
+    w = torch.randn(dim, generator=g, device="cuda").to(DTYPES[dtype])
     targets = torch.full((rows,), IGNORE, device="cuda")
     targets[live] = torch.randint(0, vocab, (len(row) // 2,), generator=g, device="cuda").repeat_interleave(2)
     a = torch.zeros(rows, device="cuda")
@@ -492,12 +494,14 @@ def test_the_gradient_of_logits_is_not_rounded_to_bf16(rows, dim, ignored):
     p = 1.0 / vocab
     dz = torch.full((len(row), vocab), -p, dtype=torch.float64, device="cuda").scatter_(1, at[:, None], 1.0 - p) * size[:, None]
     # the logarithm of 500, 6.2, is off by 2 roundings of itself and of its product with log2 e: p by 30 U of itself, with the exponential's
-    # and the products' roundings 40 U; two parts of bf16 hold 2^-16.  Sums over the rows of products of which two are not 0, over the
-    # vocabulary of 500; the result's rounding
-    off = 2.0 ** -16 + 40 * U
+    # and the products' roundings 40 U; two parts of bf16 hold 2^-16, three 2^-24, and for up to 16 rows it is fp32.  Sums over the rows of
+    # products of which two are not 0, over the vocabulary of 500 (six times as many for fp32); the result's rounding
+    off = (2.0 ** -16 if dtype == "bf16" and rows > 16 else U) + 40 * U
+    times = 1 if dtype == "bf16" else 6
     want = dz.t().contiguous() @ small.double()
-    _close(r.weight, want, off * (dz.abs().t().contiguous() @ small.double().abs()) * (1 + U) + 2.0 ** -8 * want.abs() + 4 * U * want.abs(), "weight")
-    _close(r.hidden[live], torch.zeros(len(row), dim, device="cuda"), (off + (vocab + 64) * U) * dz.abs().sum(-1, keepdim=True) * w.double().abs(), "hidden")
+    each = dz.abs().t().contiguous() @ small.double().abs()
+    _close(r.weight, want, (off + 4 * times * U) * each * (1 + U) + _round(hidden.dtype) * want.abs(), "weight")
+    _close(r.hidden[live], torch.zeros(len(row), dim, device="cuda"), (off + (times * vocab + 64) * U) * dz.abs().sum(-1, keepdim=True) * w.double().abs(), "hidden")
 
 
 def _shares(hidden, weight, targets, a):
@@ -653,3 +657,25 @@ def test_nearly_sure_tokens_through_autograd(rows, dim, vocab, dtype):
     dh, dw = torch.autograd.grad(asi.linear_logprobs(h, w, targets).logprob, (h, w), a)
     r = asi.linear_logprobs_grad(hidden, weight, targets, a)
     assert torch.equal(dh, r.hidden) and torch.equal(dw, r.weight)
+
+
+@pytest.mark.parametrize("rows", [3, 100])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_logits_farther_apart_than_fp32_reaches(rows, dtype):
+    """Logits of 2^127 and -2^127 are 2^128 apart, which fp32 does not hold, and 3.4e18 at a scale of 1e-20."""
+    dim, vocab = 64, 40
+    hidden = torch.zeros(rows, dim, dtype=DTYPES[dtype], device="cuda")
+    weight = torch.zeros(vocab, dim, dtype=DTYPES[dtype], device="cuda")
+    hidden[:, 3], weight[:, 3] = 2.0 ** 63, -2.0 ** 64
+    weight[7, 3] = 2.0 ** 64
+    targets = torch.arange(rows, device="cuda") % vocab
+    scale = 1e-20
+    a = torch.ones(rows, device="cuda")
+    far = (2.0 ** 128) * float(torch.tensor(scale))
+    want = torch.where(targets == 7, 0.0, -far).double()
+    for r in (asi.linear_logprobs(hidden, weight, targets, scale=scale), asi.linear_logprobs_grad(hidden, weight, targets, a, scale=scale)):
+        _close(r.logprob, want, 4 * U * want.abs(), "logprob")
+        assert not r.entropy.any()
+    # dz is scale (1 at the target, -1 at token 7): two products of numbers with few bits, the scale's rounding, the result's
+    want = torch.where(targets == 7, 0.0, -far / 2.0 ** 63).double()
+    _close(r.hidden[:, 3], want, (4 * U + (2.0 ** -8 + 2.0 ** -15 if dtype == "bf16" else 0.0)) * want.abs(), "hidden")
