@@ -1230,11 +1230,13 @@ asi_status asi_linear_logprobs_grad(const asi_linear_logprob_desc* desc, int giv
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (desc->rows == 0) {
         if (!dweight) return ASI_OK;
-        const long long n = desc->vocab * desc->dim;
-        if (n > most_workgroups(256) * 256) return ASI_ERR_UNSUPPORTED;
-        const dim3 grid((unsigned)((n + 255) / 256));
-        if (desc->dtype == ASI_F32) hipLaunchKernelGGL(k_zeros<float>, grid, 256, 0, st, static_cast<float*>(dweight), n);
-        else hipLaunchKernelGGL(k_zeros<bf16_t>, grid, 256, 0, st, static_cast<bf16_t*>(dweight), n);
+        const long long n = desc->vocab * desc->dim, most = most_workgroups(256) * 256;
+        for (long long first = 0; first < n; first += most) {
+            const long long count = n - first < most ? n - first : most;
+            const dim3 grid((unsigned)((count + 255) / 256));
+            if (desc->dtype == ASI_F32) hipLaunchKernelGGL(k_zeros<float>, grid, 256, 0, st, static_cast<float*>(dweight) + first, count);
+            else hipLaunchKernelGGL(k_zeros<bf16_t>, grid, 256, 0, st, static_cast<bf16_t*>(dweight) + first, count);
+        }
         return launched();
     }
     if (!hidden || !weight || ((logprob || grad_logprob) && !targets) || (given && (!stats || (grad_entropy && !entropy)))) return ASI_ERR_INVALID_ARG;

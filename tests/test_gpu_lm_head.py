@@ -679,3 +679,16 @@ def test_logits_farther_apart_than_fp32_reaches(rows, dtype):
     # dz is scale (1 at the target, -1 at token 7): two products of numbers with few bits, the scale's rounding, the result's
     want = torch.where(targets == 7, 0.0, -far / 2.0 ** 63).double()
     _close(r.hidden[:, 3], want, (4 * U + (2.0 ** -8 + 2.0 ** -15 if dtype == "bf16" else 0.0)) * want.abs(), "hidden")
+
+
+def test_no_rows_beside_more_weights_than_a_launch_has_threads():
+    weight = torch.empty(1 << 20, 4104, dtype=torch.bfloat16, device="cuda")
+    hidden = torch.empty(0, 4104, dtype=torch.bfloat16, device="cuda")
+    targets = torch.empty(0, dtype=torch.int64, device="cuda")
+    L, out = B.lib(), torch.full((weight.numel() + 64,), 1.0, dtype=torch.bfloat16, device="cuda")
+    desc = B.LinearLogprobDesc(0, 4104, 1 << 20, 4104, 4104, IGNORE, _DTYPE[torch.bfloat16], 1.0, 0, 0)
+    assert L.asi_linear_logprobs_grad(desc, 0, None, weight.data_ptr(), None, None, None, None, None, None, None, out.data_ptr(), None, 0,
+                                      torch.cuda.current_stream().cuda_stream) == 0
+    assert not out[:weight.numel()].any() and bool((out[weight.numel():] == 1).all())
+    del out
+    assert not asi.linear_logprobs_grad(hidden, weight, targets, torch.empty(0, device="cuda")).weight.any()
