@@ -168,10 +168,15 @@ asi_status asi_adamw(int32_t count, const asi_adamw_tensor* tensors, int32_t sta
  * weights of the output layer (vocab, dim), and the gradients of sum_t a_t logprob_t + b_t entropy_t:
  *     dz = scale ( a (delta_target - p) - b p (log p + entropy) )       dH = dz W        dW = dz^T H
  * The logits are made in tiles and used up there; for the gradients they are made a second time, in pieces of
- * the vocabulary, or kept in the workspace where the whole vocabulary is one piece and `given` is 0.  Kept between the two calls are two numbers a row: the largest logit x_max (before the scale) and
- * log sum_i exp(scale (x_i - x_max)).
- * A row whose target is ignore_index is left out: it is not read, has logprob, entropy and gradient 0 and adds nothing
- * to dW.  A target out of range otherwise gives NaN, as a row does that holds NaN or +infinity among its logits.
+ * the vocabulary, or kept in the workspace where the whole vocabulary is one piece (for up to 64 rows always; otherwise up to 96 MiB
+ * and where `given` is 0).  Weights that cannot be multiplied as they lie (fp32; bf16 whose rows are no whole vectors or no multiple of
+ * 64 entries) are copied into the workspace by pieces of up to 768 MiB, so that it may be larger than the logits of few rows.  Kept
+ * between the two calls are two numbers a row: the largest logit x_max (before the scale) and log sum_i exp(scale (x_i - x_max)).
+ * A row whose target is ignore_index is left out: whatever it holds, it has logprob, entropy and gradient 0 and adds nothing
+ * to dW.  A target out of range otherwise gives NaN, as a row does that holds NaN or +infinity among its logits.  A logit of
+ * -infinity has probability 0; where a weight is infinite, dH has 0 times infinity, NaN, in its column.
+ * ASI_ERR_UNSUPPORTED where a launch has not enough workgroups: above 2^23 tiles of 128 x 128 logits, 2^23 of dW, or 2^32
+ * entries of H with gradients (2^35 without).
  * Products of fp32 inputs are exact to about the rounding of fp32 (each side as three bf16 numbers, six products of
  * them, sums in fp32).  For bf16 inputs dz is held to 2^-16 of itself (as two parts of bf16; in
  * fp32 for few rows) when it is multiplied, and dH and dW are rounded once at the end. */

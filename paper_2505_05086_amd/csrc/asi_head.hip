@@ -8,15 +8,16 @@
 //                 and sums over 128 (64) of the vocabulary stay in a lane but for one exchange.  Values: x_max, how many logits are
 //                 as large, sum e over the others and sum e d of each token, d = x - x_max, e = exp(scale d), and the target's logit
 //   k_logits_grad the same tiles as dz, in two parts of bf16 for bf16 inputs and three for fp32
-//   k_few         the values for few rows, the weights from memory straight into the matrix instructions; k_few_grad and
+//   k_few         the values for few rows, left out or not, the weights from memory straight into the matrix instructions; k_few_grad and
 //                 k_few_grad_tiles their gradients from the logits that it leaves, 16 rows a column
 //   k_join        joins the tiles' values
 //   k_products    the products of dz with weights (dH) and hidden states (dW), read across as they lie (asi_tiles.h)
 //   k_hidden      the sums of dH, in fp32 over the pieces of the vocabulary and the parts of a piece, to their rows
 //
-// What bounds it: the matrix products, 2 rows dim vocab for the values and 8 with the gradients (6 where the logits are kept): 2731 rows x 2048 x
-// 32000 bf16 335 us of values (1.07 PFLOP/s), 1.30 ms with gradients (1.10); 8190 x 2048 x 100003 2.73 ms (1.23), 11.4 ms (1.18).  The weights'
-// memory for few rows: 8 x 2048 x 32000 28.6 us, 4.6 TB/s.
+// What bounds it: the matrix products, 2 rows dim vocab for the values and with the gradients 12 for bf16, whose dz has two parts, or six times 8 for
+// fp32 (2 less where the logits are kept): 2731 rows x 2048 x 32000 bf16 344 us of values (1.04 PFLOP/s), 2.06 ms with gradients (1.04); 8190 x
+// 2048 x 100003 2.76 ms (1.22), 18.5 ms (1.09).  The weights' memory for few rows: 8 x 2048 x 32000 28.1 us, 4.7 TB/s.  From 17 rows on k_few is
+// bound by the caches instead: each wave reads all hidden states for its 16 tokens, 1 GB for 64 x 2048 x 32000 fp32, 177 us.
 #include <math.h>
 
 #include "asi_head_plan.h"
@@ -46,7 +47,7 @@ struct SplitArgs {
     bool grad, flexible, dhidden, dweight;           // flexible: pieces may be larger than `piece` where rows are fewer
 };
 // The number of parts that ends a launch of dH's tiles, then dW's, soonest, `slots` workgroups at a time: lengths in steps of 64 k, to which
-// writing a tile adds about 6.  A lane of the wave for each number of parts.  (2731 x 2048 x 32000: 1434 us with two parts, 1508 with one.)
+// writing a tile adds about 6.  A lane of the wave for each number of parts.  (2731 x 2048 x 32000: 2076 us so, 2310 with one.)
 __device__ int best_splits(const SplitArgs& a, long long rows, long long piece) {
     const int s = (int)(threadIdx.x & 63) + 1;
     const float slots = a.tile == 256 ? 256.f : 512.f, row_tiles = (float)((rows + a.tile - 1) / a.tile), dim_tiles = (float)((a.dim + a.tile - 1) / a.tile);
@@ -698,6 +699,7 @@ struct FewGradArgs {
     void* dw;                                        // nullable
 };
 template <typename T, int ROWS, int COLS> __global__ __launch_bounds__(256) void k_few_grad(const FewGradArgs a) {
+    static_assert(ROWS <= 16, "logits of one group of 16 rows");
     __shared__ __attribute__((aligned(16))) float dz[kFewTokens][ROWS];
     __shared__ float share[256 * COLS];
     __shared__ RowInfo info[ROWS];
@@ -724,7 +726,7 @@ template <typename T, int ROWS, int COLS> __global__ __launch_bounds__(256) void
             const RowInfo f = info[r];
             float d = 0.f;
             if (v < tokens && f.target != kLeftOut) {
-                const float z = a.logits[((long long)(r / 16) * a.vocab + v0 + v) * 16 + r % 16];
+                const float z = a.logits[(v0 + v) * 16 + r];
                 d = f.target == v0 + v ? of_target(z, f, c) : of_logit(z, f, c);
             }
             dz[v][r] = d;
@@ -781,7 +783,7 @@ template <typename T, int ROWS, int COLS> __global__ __launch_bounds__(256) void
         if (group == 0 && r < a.rows) store_some<COLS>(a.sums + ((long long)blockIdx.y * a.rows + r) * a.dim + col, count, sum[r]);
     }
 }
-// The same for 9 to 64 rows by matrix instructions (16 x 16 x 4, fp32 throughout), where 2 rows vocab dim multiply-adds a side on
+// The same for 5 to 64 rows by matrix instructions (16 x 16 x 4, fp32 throughout), where 2 rows vocab dim multiply-adds a side on
 // the vector units would take longer than the memory.  A wave has 64 columns, lane l the four from 4 (l % 16) on, so that 16 lanes read a
 // row of W, or write one of dW, side by side: column 4 n + e is column n of block e of a matrix instruction.  TB: 16s of rows.
 template <typename T, int TB> __global__ __launch_bounds__(256) void k_few_grad_tiles(const FewGradArgs a) {

@@ -30,11 +30,13 @@ constexpr size_t kPieceBytes = size_t(96) << 20;     // dz of a piece in fp32, e
 // 2731 of 4096 rows x 2048 x 32000 2154, 1990, 1978, 1979, 2032; 2000 x 2048 x 32000 1536, 1525, 1394, 1394, 1414; 8190 x 2048 x 100003
 // 22129, with 128 19512, 192 18578.
 constexpr size_t kFineBytes = size_t(128) << 20, kMostFineBytes = size_t(192) << 20;
-// Sums of dH for bf16 (with dz 164 MiB), and for fp32 (1500 x 512 x 100000 bf16 with gradients, us: 20 MiB 1383, 36 1268, 48 1281; 700 x 1000 x 32000 382, 353, 354)
+// Sums of dH for bf16 (with dz 164 MiB), and for fp32.  (1500 x 512 x 100000 bf16 with gradients, us: 20 MiB 1383, 36 1268, 48 1281; 700 x 1000
+// x 32000 382, 353, 354.)
 constexpr size_t kFineSums = size_t(36) << 20, kSums = size_t(48) << 20;
-// Packed weights of a piece.  They are larger than that of a few rows' dz, so that a piece has tiles for the whole chip: fp32 with gradients,
-// 150 rows x 2048 x 60000, us: 3054 with 96 MiB, 2396 with 192, 1962 with 384, 1398 with 768; 700 x 1000 x 32000 1212, 997 with 192 and more;
-// of values alone, 150 x 2048 x 60000, 1168, 816, 610, 628; 1023 x 1000 x 50001 637, 676, 638, 636.
+// Packed weights of a piece.  Larger than a few rows' dz would ask for, so that a piece has tiles for the whole chip, and a bound between memory
+// and time: fp32 with gradients, 150 rows x 2048 x 60000, us: 3054 with 96 MiB, 2396 with 192, 1985 with 384, 1425 with 768, 1420 with 1536; 700
+// x 1000 x 32000 1212, 997 with 192 and more; 200 x 5120 x 70000 8475 with 384, 6730, 6140; 512 x 8192 x 70000 19950, 18450, 14720; of values
+// alone, 150 x 2048 x 60000, 1168, 816, 610, 628; 1023 x 1000 x 50001 637, 676, 638, 636; 200 x 5120 x 70000 3028, 2132, 1933.
 constexpr size_t kPackedBytes = size_t(768) << 20;
 
 // What the gradient needs of a row: p = exp2(scale' (x - top) - log2sum); dz = [target] a - p (a + b (log p + entropy)).  Of the target
@@ -90,7 +92,7 @@ inline Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     const bool whole = d->weight_stride % 8 == 0 && !d->any_address, as_it_lies = !p.f32 && whole && d->dim % kStep == 0 && d->weight_stride < (1 << 21);
     p.few = d->rows <= (p.f32 ? kFewF32 : as_it_lies ? kFewBf16 : !grad && whole ? kFewBf16Whole : kFewBf16Packed);
     p.staged = !p.few && !as_it_lies;
-    // (92000 tokens x 256 bf16 with gradients of 32 rows, us: 117 in tiles of 128, 185 of 256)
+    // (92000 tokens x 256 bf16 with gradients of 32 rows, us: 124 in tiles of 128, 185 of 256)
     p.tile = d->rows > 128 && up(d->rows, 256) / 256 * (up(d->vocab, 256) / 256) >= 256 ? 256 : 128;
     const long long rows_up = up(d->rows, p.tile);
     size_t dz_bytes = kPieceBytes;
@@ -121,8 +123,8 @@ inline Plan plan(const asi_linear_logprob_desc* d, bool grad) {
     const long long few_most = (d->vocab + kFewTokens - 1) / kFewTokens, few_cap = few_want < 1 ? 1 : few_want > 512 ? 512 : few_want;
     p.few_blocks = (int)(few_cap < few_most ? few_cap : few_most);
     // The logits of a vocabulary that is one piece, in fp32, where they are dearer to compute again than to read (3000 rows x 4000 bf16 with
-    // gradients, us: dim 256 83 either way, 512 99 either way, 1024 130 and 143 without, 2048 201 and 239; 700 x 2048 x 32000 370 and 402;
-    // fp32 3000 x 256 x 4000 284 and 310, 3000 x 2048 x 4000 953 and 1243)
+    // gradients, us: dim 256 130 either way, 512 152 and 153 without, 1024 198 and 213, 2048 321 and 359; 700 x 2048 x 32000 570 and 617;
+    // fp32 3000 x 256 x 4000 303 and 328, 3000 x 2048 x 4000 986 and 1265)
     const long long kept = 4 * rows_up * up(d->vocab, p.tile);
     p.keep = grad && !p.few && p.piece >= d->vocab && kept <= (long long)kPieceBytes && p.k_steps * (p.f32 ? kPairs : 1) >= kKeepSteps;
     size_t at = 0;
