@@ -692,3 +692,15 @@ def test_no_rows_beside_more_weights_than_a_launch_has_threads():
     assert not out[:weight.numel()].any() and bool((out[weight.numel():] == 1).all())
     del out
     assert not asi.linear_logprobs_grad(hidden, weight, targets, torch.empty(0, device="cuda")).weight.any()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("size", [(3, 70001, 130), (12, 65536, 200), (40, 20000, 300), (100, 16384, 257), (300, 9001, 500), (2, 262143, 65)])
+def test_wide_heads_of_few_rows_and_tokens(size, dtype):
+    hidden, weight, targets, a, b = _inputs(*size, DTYPES[dtype], 99, spread=0.25)
+    want = _Definition(hidden, weight, targets, 1.0, a, b)
+    _check_values(asi.linear_logprobs(hidden, weight, targets), want, targets)
+    r = asi.linear_logprobs_grad(hidden, weight, targets, a, b)
+    _check_values(r, want, targets)
+    _close(r.hidden, want.hidden, want.hidden_bound, "hidden")
+    _close(r.weight, want.weight, want.weight_bound, "weight")
