@@ -168,7 +168,7 @@ asi_status asi_adamw(int32_t count, const asi_adamw_tensor* tensors, int32_t sta
  * weights of the output layer (vocab, dim), and the gradients of sum_t a_t logprob_t + b_t entropy_t:
  *     dz = scale ( a (delta_target - p) - b p (log p + entropy) )       dH = dz W        dW = dz^T H
  * The logits are made in tiles and used up there; for the gradients they are made a second time, in pieces of
- * the vocabulary, or kept in the workspace where the whole vocabulary is one piece (for up to 64 rows always; otherwise up to 96 MiB
+ * the vocabulary, or kept in the workspace where the whole vocabulary is one piece (for few rows, 64 at most, always; otherwise up to 96 MiB
  * and where `given` is 0).  Weights that cannot be multiplied as they lie (fp32; bf16 whose rows are no whole vectors or no multiple of
  * 64 entries) are copied into the workspace by pieces of up to 768 MiB, so that it may be larger than the logits of few rows.  Kept
  * between the two calls are two numbers a row: the largest logit x_max (before the scale) and log sum_i exp(scale (x_i - x_max)).

@@ -577,7 +577,7 @@ class _LinearLogprobsFn(torch.autograd.Function):
 def linear_logprobs(hidden: torch.Tensor, weight: torch.Tensor, targets: Optional[torch.Tensor] = None, *, scale: float = 1.0,
                     ignore_index: int = IGNORE_INDEX) -> LinearLogprobs:
     """Log probabilities of `targets` under softmax(scale * hidden @ weight.T) and the entropy of each row, without the logits: none
-    are in memory in the forward pass, a piece of them and of their gradient in the backward pass (all of them for up to 64 rows).  Weights
+    are in memory in the forward pass, a piece of them and of their gradient in the backward pass (all of them for few rows, 64 at most).  Weights
     that cannot be multiplied as they lie, fp32 ones above all, are copied by pieces of up to 768 MiB, which for few rows is more than
     their logits; bf16 weights whose rows are a multiple of 64 entries, at multiples of 16 bytes, are read in place.  hidden (..., dim), weight (vocab, dim), fp32
     or bf16; targets (...) int64.  A row whose target is ignore_index is left out: logprob and entropy 0, no gradient, whatever it
